@@ -293,11 +293,13 @@ def run(s):
 
 
 def _quantise(x):
-    """A row's codes in [-127, 127] and its scale: its largest magnitude over 127."""
+    """A row's codes in [-127, 127] and its scale: its largest magnitude over 127.
+    Both quotients are of two tensors: by or of a number, torch multiplies by a reciprocal."""
     x = x.float()
     most = x.abs().amax(-1, keepdim=True)
-    code = torch.round(x * (127.0 / most.clamp(min=2.0 ** -110))).to(torch.int8)
-    return code, (most / 127.0)[..., 0]
+    full = torch.full_like(most, 127.0)
+    code = torch.round(x * (full / most.clamp(min=2.0 ** -110))).to(torch.int8)
+    return code, (most / full)[..., 0]
 
 
 def _values(s, name, slot):
