@@ -21,7 +21,9 @@
  *   - a budget per layer and KV head (mmshift_select_head_budgets,
  *     mmshift_topk_head_budgets; Section 3.1's C_{l,h});
  *   - the attention-mass coverage of a kept set for given decode queries
- *     (mmshift_coverage; Section 1, Fig. 1b).
+ *     (mmshift_coverage; Section 1, Fig. 1b);
+ *   - a paged cache for the kept rows, 8-bit if wanted: filled from a
+ *     selection, appended to, read back and attended to (mmshift_cache_*).
  *
  * Conventions shared by every entry point:
  *   - All pointers except the ones marked "host" are device pointers. The
@@ -358,6 +360,101 @@ mmshift_status mmshift_coverage(const mmshift_shape* s, const void* K, const voi
                                 const void* dec_q, int32_t n_dec, float softmax_scale,
                                 const int32_t* idx, float* cov, void* workspace,
                                 size_t workspace_bytes, mmshift_stream_t stream);
+
+/* ---- The paged cache: where the kept rows live after the selection ----
+ *
+ * A selection keeps other rows for every KV head (and, with head budgets,
+ * another number of them), so every (layer, request, KV head) has a sequence
+ * of its own: positions 0 .. lens - 1, in pages of page_size rows taken from
+ * one pool. Position t of a sequence lies in row t % page_size of page
+ * page_table[l][b][h][t / page_size]. mmshift_cache_fill starts the sequences
+ * with a prompt's kept rows, mmshift_cache_append writes new tokens' rows
+ * behind them, mmshift_cache_read copies rows back out, and
+ * mmshift_cache_attention attends to them.
+ *
+ * With dtype MMSHIFT_I8 a row is held as d signed bytes and one float32 scale:
+ *   most  = max_j |x_j|,  scale = most / 127,  code_j = rint(x_j * (127 / most))
+ * in float32 (ties to even), and stands for code_j * scale. A row whose most is
+ * below 2^-110 is held as zero codes with scale most / 127; a row with a NaN or
+ * an infinity as zero codes with a NaN scale (it reads back as NaN).
+ *
+ * lens counts the rows that a call appends or queries for too: a decode step
+ * first adds each request's number of new tokens to lens, then appends and
+ * attends for every layer. lens and page_table are read on the device, so a
+ * captured step can be replayed as the sequences grow. lens outside
+ * [0, max_pages * page_size] is clamped; a position there whose table entry is
+ * outside [0, n_pages) has no page: a write to it is dropped, it reads as zeros,
+ * attention leaves its key out, and mmshift_poll_status reports it.
+ *
+ * The shape of append, read and attention lists the rows of the call, not a
+ * prompt: request b has T_b = cu_seqlens[b+1] - cu_seqlens[b] >= 0 rows
+ * (n_b below); window and budgets are not read. Pages that a call writes belong to
+ * one sequence; pages that it only reads may be shared. Workspace (and status
+ * word, zero at first): mmshift_cache_workspace_size() bytes, 256-byte aligned;
+ * what it holds besides the status word need not outlive the call. */
+enum { MMSHIFT_I8 = 2 };  /* cache type only */
+
+typedef struct {
+  int32_t dtype;            /* the shape's dtype, or MMSHIFT_I8 */
+  int32_t page_size;        /* 16, 32, 64, 128 or 256 rows */
+  int32_t n_pages;          /* pages of the pool; n_pages * page_size < 2^31 - 256 */
+  int32_t max_pages;        /* table entries of a sequence; max_pages * page_size <= 2^30 */
+  void* k_pages;            /* [n_pages, page_size, d], 16-byte aligned */
+  void* v_pages;
+  float* k_scales;          /* MMSHIFT_I8: [n_pages, page_size], else unused */
+  float* v_scales;
+  const int32_t* page_table;/* [L, batch, Hkv, max_pages] */
+  int32_t* lens;            /* [L, batch, Hkv] */
+} mmshift_cache;
+
+mmshift_status mmshift_cache_workspace_size(const mmshift_shape* s, const mmshift_cache* c,
+                                            size_t* bytes);
+
+/* Step 6 into pages: the kept rows K[cu_b + idx[c, h], h] (and V's) of a
+ * prompt become positions 0, 1, ... of their sequences, and lens their number.
+ * Shape, K, V and idx [L, R, Hkv] as in mmshift_gather; count (nullable):
+ * device [L][batch][Hkv] rows kept per head (mmshift_select_head_budgets'
+ * out_count), clamped to [0, min(C_b, T_b)], else min(C_b, T_b). An index outside
+ * [0, T_b) gives a zero row, and rows behind the sequence's table are dropped;
+ * both are reported by mmshift_poll_status. */
+mmshift_status mmshift_cache_fill(const mmshift_shape* s, const mmshift_cache* c, const void* K,
+                                  const void* V, const int32_t* idx, const int32_t* count,
+                                  void* workspace, size_t workspace_bytes,
+                                  mmshift_stream_t stream);
+
+/* New tokens' rows: K[l][cu_b + i][h] becomes position lens[l][b][h] - n_b + i
+ * (dropped where that is negative). K, V: [L][T, Hkv, d] in the shape's
+ * dtype, tokens row_stride elements apart (0 = Hkv * d), layers
+ * layer_stride_kv apart. */
+mmshift_status mmshift_cache_append(const mmshift_shape* s, const mmshift_cache* c, const void* K,
+                                    const void* V, int64_t row_stride, void* workspace,
+                                    size_t workspace_bytes, mmshift_stream_t stream);
+
+/* Rows back out, in the shape's dtype: out_K[l][cu_b + i][h] = position
+ * first[l][b][h] + i of the sequence (first nullable: 0), zeros where the
+ * sequence has no such position. out_K, out_V: [L, T, Hkv, d], dense. */
+mmshift_status mmshift_cache_read(const mmshift_shape* s, const mmshift_cache* c,
+                                  const int32_t* first, void* out_K, void* out_V, void* workspace,
+                                  size_t workspace_bytes, mmshift_stream_t stream);
+
+/* Attention of new tokens over one layer's sequences (n_layers = 1): for
+ * token i of request b and query head hq, with h = hq / r and the keys and values
+ * k_t, v_t that sequence (b, h) holds,
+ *   z_t = scale * q . k_t,  lse = ln sum_t e^(z_t),  out = sum_t e^(z_t - lse) v_t
+ * over t <= lens - n_b + i if causal (the tokens' own rows are the sequence's
+ * last n_b), over all t < lens if not. A token without any key (or only keys
+ * with z_t = -inf) gets out = 0 and lse = -inf, one with a z_t of NaN or +inf
+ * NaN in both. Keys that a token does not attend to
+ * have no part in its result whatever they hold, NaN included.
+ * Q [T, Hq, d], tokens row_stride elements apart (0 = Hq * d); out [T, Hq, d],
+ * dense; lse (nullable) [T, Hq] float32; scale 0 = 1/sqrt(d). bfloat16
+ * weights e^(z - max) are rounded to bfloat16 before the product with v, and an
+ * 8-bit row's scale is multiplied into them before that. */
+mmshift_status mmshift_cache_attention(const mmshift_shape* s, const mmshift_cache* c,
+                                       const void* Q, int64_t row_stride, int32_t causal,
+                                       float softmax_scale, void* out, float* lse,
+                                       void* workspace, size_t workspace_bytes,
+                                       mmshift_stream_t stream);
 
 /* Allocation-free variant of mmshift_scores_topk.
  *

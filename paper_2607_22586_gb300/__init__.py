@@ -7,7 +7,7 @@ synthetic workloads. Importing the package does not load the library; the first
 call does, and fails loudly if the library cannot be built or loaded.
 """
 from . import synth  # noqa: F401
-from ._lib import (MMShiftError, Params, Shape, Debug, check, default_params,  # noqa: F401
+from ._lib import (MMShiftError, Params, Shape, Debug, Cache, check, default_params,  # noqa: F401
                    load_library, make_debug, make_shape, mmshift_build_proxies, mmshift_gather,
                    mmshift_output_rows, mmshift_poll_status, mmshift_proxy_mass,
                    mmshift_scores_topk, mmshift_scores_topk_noalloc, mmshift_select, mmshift_topk,
@@ -16,4 +16,6 @@ from ._lib import (MMShiftError, Params, Shape, Debug, check, default_params,  #
                    mmshift_hidden_stats_workspace_size, mmshift_hidden_stats,
                    mmshift_hidden_proxies_workspace_size, mmshift_build_hidden_proxies,
                    mmshift_coverage_workspace_size, mmshift_coverage,
-                   mmshift_select_head_budgets, mmshift_topk_head_budgets)
+                   mmshift_select_head_budgets, mmshift_topk_head_budgets,
+                   make_cache, mmshift_cache_workspace_size, mmshift_cache_fill,
+                   mmshift_cache_append, mmshift_cache_read, mmshift_cache_attention)

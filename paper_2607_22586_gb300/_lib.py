@@ -23,6 +23,7 @@ MMSHIFT_ERR_DEVICE = 6
 
 MMSHIFT_BF16 = 0
 MMSHIFT_F32 = 1
+MMSHIFT_I8 = 2
 MMSHIFT_SCORE_VOTE = 0
 MMSHIFT_SCORE_MASS = 1
 MMSHIFT_MAX_BATCH = 64
@@ -38,6 +39,8 @@ EXPORTED = [
     "mmshift_hidden_proxies_workspace_size", "mmshift_build_hidden_proxies",
     "mmshift_coverage_workspace_size", "mmshift_coverage",
     "mmshift_select_head_budgets", "mmshift_topk_head_budgets",
+    "mmshift_cache_workspace_size", "mmshift_cache_fill", "mmshift_cache_append",
+    "mmshift_cache_read", "mmshift_cache_attention",
 ]
 MMSHIFT_NOALLOC_SCRATCH_BYTES = 8 << 20
 
@@ -76,10 +79,20 @@ class Debug(ctypes.Structure):
     ]
 
 
+class Cache(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int32), ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+        ("max_pages", ctypes.c_int32), ("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p),
+        ("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p),
+        ("page_table", ctypes.c_void_p), ("lens", ctypes.c_void_p),
+    ]
+
+
 _LIB: Optional[ctypes.CDLL] = None
 _VP = ctypes.c_void_p
 _SP = ctypes.POINTER(Shape)
 _PP = ctypes.POINTER(Params)
+_CP = ctypes.POINTER(Cache)
 
 
 def load_library(path: Optional[str] = None) -> ctypes.CDLL:
@@ -142,6 +155,17 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.mmshift_select_with_stats.argtypes = [_SP, _VP, _VP, _VP, _VP, _PP, _VP, _VP, _VP,
                                               ctypes.POINTER(Debug), _VP, ctypes.c_size_t, _VP]
     lib.mmshift_select_with_stats.restype = st
+    lib.mmshift_cache_workspace_size.argtypes = [_SP, _CP, ctypes.POINTER(ctypes.c_size_t)]
+    lib.mmshift_cache_workspace_size.restype = st
+    lib.mmshift_cache_fill.argtypes = [_SP, _CP, _VP, _VP, _VP, _VP, _VP, ctypes.c_size_t, _VP]
+    lib.mmshift_cache_fill.restype = st
+    lib.mmshift_cache_append.argtypes = [_SP, _CP, _VP, _VP, ctypes.c_int64, _VP, ctypes.c_size_t, _VP]
+    lib.mmshift_cache_append.restype = st
+    lib.mmshift_cache_read.argtypes = [_SP, _CP, _VP, _VP, _VP, _VP, ctypes.c_size_t, _VP]
+    lib.mmshift_cache_read.restype = st
+    lib.mmshift_cache_attention.argtypes = [_SP, _CP, _VP, ctypes.c_int64, ctypes.c_int32, ctypes.c_float,
+                                            _VP, _VP, _VP, ctypes.c_size_t, _VP]
+    lib.mmshift_cache_attention.restype = st
     lib.mmshift_scores_topk_noalloc.argtypes = [_SP, _PP, _VP, _VP, _VP, _VP, _VP]
     lib.mmshift_scores_topk_noalloc.restype = st
     lib.mmshift_poll_status.argtypes = [_VP, _VP]
@@ -358,6 +382,70 @@ def mmshift_topk_head_budgets(shape, scores, head_budgets, out_idx, out_count, w
     return load_library().mmshift_topk_head_budgets(
         ctypes.byref(shape), _ptr(scores), _ptr(head_budgets), _ptr(out_idx), _ptr(out_count),
         _ptr(workspace), workspace_bytes, _ptr(stream))
+
+
+def make_cache(k_pages, v_pages, page_table, lens, k_scales=None, v_scales=None) -> Cache:
+    """Cache over tensors (kept alive on the returned object): pages
+    [n_pages, page_size, d] of bfloat16, float32 or int8 (then with scales
+    [n_pages, page_size]), page_table [..., max_pages] and lens int32."""
+    import torch
+
+    dtypes = {torch.bfloat16: MMSHIFT_BF16, torch.float32: MMSHIFT_F32, torch.int8: MMSHIFT_I8}
+    tensors = [k_pages, v_pages, page_table, lens] + [x for x in (k_scales, v_scales) if x is not None]
+    if k_pages.dtype not in dtypes or k_pages.dtype != v_pages.dtype or k_pages.shape != v_pages.shape \
+            or k_pages.dim() != 3:
+        raise ValueError("pages must be two [n_pages, page_size, d] tensors of one supported dtype")
+    if page_table.dtype != torch.int32 or lens.dtype != torch.int32 \
+            or page_table.shape[:-1].numel() != lens.numel():
+        raise ValueError("page_table [..., max_pages] and lens [...] must be int32 tensors")
+    if k_pages.dtype == torch.int8:
+        for x in (k_scales, v_scales):
+            if x is None or x.dtype != torch.float32 or x.shape != k_pages.shape[:2]:
+                raise ValueError("8-bit pages need float32 scales [n_pages, page_size]")
+    elif k_scales is not None or v_scales is not None:
+        raise ValueError("scales belong to 8-bit pages")
+    if any(not x.is_contiguous() or x.device != k_pages.device for x in tensors):
+        raise ValueError("a cache's tensors must be contiguous and on one device")
+    c = Cache(dtype=dtypes[k_pages.dtype], page_size=k_pages.shape[1], n_pages=k_pages.shape[0],
+              max_pages=page_table.shape[-1], k_pages=_ptr(k_pages), v_pages=_ptr(v_pages),
+              k_scales=_ptr(k_scales), v_scales=_ptr(v_scales), page_table=_ptr(page_table),
+              lens=_ptr(lens))
+    c._keep = tensors
+    return c
+
+
+def mmshift_cache_workspace_size(shape: Shape, cache: Cache) -> int:
+    n = ctypes.c_size_t()
+    check(load_library().mmshift_cache_workspace_size(ctypes.byref(shape), ctypes.byref(cache),
+                                                      ctypes.byref(n)), "mmshift_cache_workspace_size")
+    return n.value
+
+
+def mmshift_cache_fill(shape, cache, K, V, idx, count, workspace, workspace_bytes, stream=None) -> int:
+    return load_library().mmshift_cache_fill(
+        ctypes.byref(shape), ctypes.byref(cache), _ptr(K), _ptr(V), _ptr(idx), _ptr(count),
+        _ptr(workspace), workspace_bytes, _ptr(stream))
+
+
+def mmshift_cache_append(shape, cache, K, V, row_stride, workspace, workspace_bytes,
+                         stream=None) -> int:
+    return load_library().mmshift_cache_append(
+        ctypes.byref(shape), ctypes.byref(cache), _ptr(K), _ptr(V), int(row_stride), _ptr(workspace),
+        workspace_bytes, _ptr(stream))
+
+
+def mmshift_cache_read(shape, cache, first, out_K, out_V, workspace, workspace_bytes,
+                       stream=None) -> int:
+    return load_library().mmshift_cache_read(
+        ctypes.byref(shape), ctypes.byref(cache), _ptr(first), _ptr(out_K), _ptr(out_V),
+        _ptr(workspace), workspace_bytes, _ptr(stream))
+
+
+def mmshift_cache_attention(shape, cache, Q, row_stride, causal, softmax_scale, out, lse, workspace,
+                            workspace_bytes, stream=None) -> int:
+    return load_library().mmshift_cache_attention(
+        ctypes.byref(shape), ctypes.byref(cache), _ptr(Q), int(row_stride), int(causal),
+        float(softmax_scale), _ptr(out), _ptr(lse), _ptr(workspace), workspace_bytes, _ptr(stream))
 
 
 def mmshift_poll_status(workspace, stream=None) -> int:

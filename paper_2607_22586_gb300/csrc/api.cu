@@ -293,7 +293,7 @@ static mmshift_status stats_job(const mmshift_shape* s, int64_t qfull_layer_stri
 // Whether kernels may read `p` with plain loads: device or managed memory,
 // or page-locked host memory mapped at the same address (unified
 // addressing). Pageable host memory is refused.
-static bool device_readable(const void* p) {
+bool mmshift::device_readable(const void* p) {
   cudaPointerAttributes a;
   if (cudaPointerGetAttributes(&a, p) != cudaSuccess) {
     cudaGetLastError();   // clear the sticky error of a failed query

@@ -1,0 +1,401 @@
+// The paged cache's entry points and the kernels that write and read its rows.
+//
+// A row moves once: 16 bytes a lane, the lanes of a row together, K and V of a
+// row by the same lanes. An 8-bit row's largest magnitude is a reduction over
+// those lanes (8 to 32), so quantising costs no second pass. All three kernels
+// are bound by the bytes they move, short calls by their launch.
+#include <cmath>
+#include <cstring>
+
+#include "cache.cuh"
+
+namespace mmshift {
+mmshift_status noalloc_cuda_fail(cudaError_t e);
+mmshift_status noalloc_prepare(const mmshift_shape* s, const mmshift_params* p, Problem* P);
+
+namespace {
+
+constexpr float kLeastMost = 7.703719777548943e-34f;   // 2^-110: 127 / it is finite
+
+// The codes of 16 bytes of a row (8 bfloat16 or 4 float32 values) and the row's
+// scale. LPR lanes hold a row. The product x * (127 / most) is at most 127 (1 + 2^-23),
+// which rounds to 127.
+template <typename T, int LPR>
+__device__ __forceinline__ float quantise16(const uint4& w, uint32_t (&code)[2]) {
+  constexpr int N = 16 / (int)sizeof(T);
+  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+  float x[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    if constexpr (sizeof(T) == 2) x[i] = (i & 1) ? bf16_hi(u[i / 2]) : bf16_lo(u[i / 2]);
+    else x[i] = __uint_as_float(u[i]);
+  }
+  // magnitudes as bit patterns: their order is the values', and a NaN is the largest
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);
+#pragma unroll
+  for (int s = LPR / 2; s; s >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, s));
+  const float most = __uint_as_float(m);
+  const bool fine = m < 0x7f800000u;
+  const float inv = fine && most >= kLeastMost ? __fdiv_rn(127.f, most) : 0.f;
+  code[0] = code[1] = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (inv != 0.f)
+      code[i / 4] |= (uint32_t)(uint8_t)(int8_t)__float2int_rn(__fmul_rn(x[i], inv)) << (8 * (i & 3));
+  return fine ? __fdiv_rn(most, 127.f) : __uint_as_float(0x7fffffffu);
+}
+
+// Rows into pages. FILL: the rows idx keeps of a prompt, to positions 0, 1, ...;
+// else a call's own rows, to the last positions of their sequences.
+template <typename T, int D, bool I8, bool FILL>
+__global__ void __launch_bounds__(256) cache_write_kernel(const __grid_constant__ CacheJob J,
+                                                          const uint8_t* K, const uint8_t* V,
+                                                          const int32_t* idx, const int32_t* count,
+                                                          bool vec) {
+  dependent_start();
+  constexpr int ROWB = D * (int)sizeof(T), LPR = ROWB / 16;
+  const int l = blockIdx.y;
+  const long long q = (long long)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
+  const int part = threadIdx.x % LPR;
+  const bool live = q < (long long)J.off[J.B] * J.Hkv;   // all lanes stay for the reduction
+  const int c = live ? (int)(q / J.Hkv) : 0, h = live ? (int)(q % J.Hkv) : 0;
+  const int b = cache_request(J, c), i = c - J.off[b];
+  const size_t u = ((size_t)l * J.B + b) * J.Hkv + h;
+  int pos;
+  bool there = live, bad = false;
+  size_t src;
+  if constexpr (FILL) {
+    int n = J.off[b + 1] - J.off[b];
+    if (live && count) n = min(max(count[u], 0), n);
+    if (live && part == 0 && i == 0) J.lens[u] = min(n, J.cap);
+    pos = i;
+    there = live && i < n;
+    const int t = there ? idx[(size_t)l * J.off[J.B] * J.Hkv + q] : 0;
+    bad = there && (t < 0 || t >= J.src[b + 1] - J.src[b]);
+    src = ((size_t)l * J.ls + (((size_t)J.src[b] + (bad ? 0 : t)) * J.Hkv + h) * D) * sizeof(T);
+  } else {
+    const int n = J.off[b + 1] - J.off[b];
+    pos = live ? cache_len(J, u) - n + i : 0;
+    there = live && pos >= 0;
+    src = ((size_t)l * J.ls + (size_t)c * J.stride + (size_t)h * D) * sizeof(T);
+  }
+  int64_t slot = -1;
+  if (there) slot = pos < J.cap ? cache_slot(J, u, pos) : -1;
+  uint4 k = make_uint4(0, 0, 0, 0), v = k;
+  if (slot >= 0 && !bad) {
+    k = load_plain16(K + src + part * 16, vec);
+    v = load_plain16(V + src + part * 16, vec);
+  }
+  if (there && part == 0) {
+    if (bad) set_status(J.status, kStatusBadIndex);
+    if (slot < 0) set_status(J.status, kStatusBadPage);
+  }
+  if constexpr (I8) {
+    uint32_t ck[2], cv[2];
+    const float sk = quantise16<T, LPR>(k, ck), sv = quantise16<T, LPR>(v, cv);
+    if (slot < 0) return;
+    constexpr int CB = 16 / (int)sizeof(T);   // code bytes of a lane
+    const size_t dst = (size_t)slot * D + part * CB;
+    if constexpr (CB == 8) {
+      *reinterpret_cast<uint2*>(J.kp + dst) = make_uint2(ck[0], ck[1]);
+      *reinterpret_cast<uint2*>(J.vp + dst) = make_uint2(cv[0], cv[1]);
+    } else {
+      *reinterpret_cast<uint32_t*>(J.kp + dst) = ck[0];
+      *reinterpret_cast<uint32_t*>(J.vp + dst) = cv[0];
+    }
+    if (part == 0) {
+      J.ks[slot] = sk;
+      J.vs[slot] = sv;
+    }
+  } else {
+    if (slot < 0) return;
+    const size_t dst = (size_t)slot * ROWB + part * 16;
+    *reinterpret_cast<uint4*>(J.kp + dst) = k;
+    *reinterpret_cast<uint4*>(J.vp + dst) = v;
+  }
+}
+
+// The 16 bytes of an output row that lie at `part`.
+template <typename T, int D, bool I8>
+__device__ __forceinline__ uint4 read16(const uint8_t* pages, const float* scales, int64_t slot, int part) {
+  if constexpr (!I8) {
+    return *reinterpret_cast<const uint4*>(pages + (size_t)slot * D * sizeof(T) + part * 16);
+  } else {
+    constexpr int N = 16 / (int)sizeof(T);
+    const float s = scales[slot];
+    uint32_t c[2];
+    const uint8_t* p = pages + (size_t)slot * D + part * N;
+    if constexpr (N == 8) {
+      const uint2 w = *reinterpret_cast<const uint2*>(p);
+      c[0] = w.x;
+      c[1] = w.y;
+    } else {
+      c[0] = *reinterpret_cast<const uint32_t*>(p);
+    }
+    float x[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = (float)(int8_t)(c[i / 4] >> (8 * (i & 3))) * s;
+    if constexpr (N == 8)
+      return make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]),
+                        pack_bf16(x[6], x[7]));
+    else
+      return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]),
+                        __float_as_uint(x[3]));
+  }
+}
+
+template <typename T, int D, bool I8>
+__global__ void __launch_bounds__(256) cache_read_kernel(const __grid_constant__ CacheJob J,
+                                                         const int32_t* first, uint8_t* oK,
+                                                         uint8_t* oV, bool vec) {
+  dependent_start();
+  constexpr int ROWB = D * (int)sizeof(T), LPR = ROWB / 16;
+  const int l = blockIdx.y;
+  const long long q = (long long)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
+  const int part = threadIdx.x % LPR;
+  if (q >= (long long)J.off[J.B] * J.Hkv) return;
+  const int c = (int)(q / J.Hkv), h = (int)(q % J.Hkv);
+  const int b = cache_request(J, c);
+  const size_t u = ((size_t)l * J.B + b) * J.Hkv + h;
+  const long long pos = (long long)(c - J.off[b]) + (first ? first[u] : 0);
+  uint4 k = make_uint4(0, 0, 0, 0), v = k;
+  if (pos >= 0 && pos < cache_len(J, u)) {
+    const int64_t slot = cache_slot(J, u, (int)pos);
+    if (slot >= 0) {
+      k = read16<T, D, I8>(J.kp, J.ks, slot, part);
+      v = read16<T, D, I8>(J.vp, J.vs, slot, part);
+    } else if (part == 0) {
+      set_status(J.status, kStatusBadPage);
+    }
+  }
+  const size_t dst = ((size_t)l * J.off[J.B] * J.Hkv + q) * ROWB + part * 16;
+  store_row16(oK + dst, k, vec);
+  store_row16(oV + dst, v, vec);
+}
+
+bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+mmshift_status check_cache(const mmshift_shape* s, const mmshift_cache* c) {
+  if (!c) return MMSHIFT_ERR_INVALID_ARG;
+  if (c->dtype != s->dtype && c->dtype != MMSHIFT_I8) return MMSHIFT_ERR_UNSUPPORTED;
+  if (c->page_size < 16 || c->page_size > 256 || (c->page_size & (c->page_size - 1)))
+    return MMSHIFT_ERR_UNSUPPORTED;
+  if (c->n_pages < 1 || c->max_pages < 1) return MMSHIFT_ERR_INVALID_ARG;
+  if ((int64_t)c->n_pages * c->page_size >= (int64_t)INT32_MAX - 256 ||
+      (int64_t)c->max_pages * c->page_size > (int64_t)1 << 30)
+    return MMSHIFT_ERR_UNSUPPORTED;
+  if (!c->k_pages || !c->v_pages || !c->page_table || !c->lens) return MMSHIFT_ERR_INVALID_ARG;
+  if (!aligned(c->k_pages, 16) || !aligned(c->v_pages, 16) || !aligned(c->page_table, 4) || !aligned(c->lens, 4))
+    return MMSHIFT_ERR_INVALID_ARG;
+  if (c->dtype == MMSHIFT_I8 &&
+      (!c->k_scales || !c->v_scales || !aligned(c->k_scales, 4) || !aligned(c->v_scales, 4)))
+    return MMSHIFT_ERR_INVALID_ARG;
+  return MMSHIFT_OK;
+}
+
+// The shape of a call on a cache: its rows, some requests without any.
+mmshift_status check_rows(const mmshift_shape* s) {
+  if (!s || !s->cu_seqlens) return MMSHIFT_ERR_INVALID_ARG;
+  if (s->batch < 1 || s->batch > MMSHIFT_MAX_BATCH) return MMSHIFT_ERR_INVALID_ARG;
+  if (s->n_layers < 1 || s->n_layers > MMSHIFT_MAX_LAYERS) return MMSHIFT_ERR_INVALID_ARG;
+  if (s->n_kv_heads < 1 || s->n_q_heads < s->n_kv_heads || s->n_q_heads % s->n_kv_heads)
+    return MMSHIFT_ERR_INVALID_ARG;
+  if (s->dtype != MMSHIFT_BF16 && s->dtype != MMSHIFT_F32) return MMSHIFT_ERR_UNSUPPORTED;
+  if (s->head_dim != 64 && s->head_dim != 128) return MMSHIFT_ERR_UNSUPPORTED;
+  if (s->cu_seqlens[0] != 0) return MMSHIFT_ERR_INVALID_ARG;
+  for (int b = 0; b < s->batch; ++b)
+    if (s->cu_seqlens[b + 1] < s->cu_seqlens[b]) return MMSHIFT_ERR_INVALID_ARG;
+  // rows of all heads are counted in 31 bits of blocks and of indices
+  if ((int64_t)s->cu_seqlens[s->batch] * s->n_q_heads > (int64_t)1 << 30) return MMSHIFT_ERR_UNSUPPORTED;
+  return MMSHIFT_OK;
+}
+
+void fill_job(const mmshift_shape* s, const mmshift_cache* c, void* ws, CacheJob* J) {
+  std::memset(J, 0, sizeof(*J));
+  J->B = s->batch;
+  J->L = s->n_layers;
+  J->Hq = s->n_q_heads;
+  J->Hkv = s->n_kv_heads;
+  J->r = s->n_q_heads / s->n_kv_heads;
+  J->d = s->head_dim;
+  J->bf16 = s->dtype == MMSHIFT_BF16;
+  J->i8 = c->dtype == MMSHIFT_I8;
+  while ((1 << J->page_shift) < c->page_size) ++J->page_shift;
+  J->n_pages = c->n_pages;
+  J->max_pages = c->max_pages;
+  J->cap = c->max_pages << J->page_shift;
+  J->kp = static_cast<uint8_t*>(c->k_pages);
+  J->vp = static_cast<uint8_t*>(c->v_pages);
+  J->ks = c->k_scales;
+  J->vs = c->v_scales;
+  J->table = c->page_table;
+  J->lens = c->lens;
+  J->status = static_cast<int*>(ws);
+}
+
+mmshift_status rows_job(const mmshift_shape* s, const mmshift_cache* c, void* ws, CacheJob* J) {
+  mmshift_status st = check_rows(s);
+  if (st == MMSHIFT_OK) st = check_cache(s, c);
+  if (st != MMSHIFT_OK) return st;
+  fill_job(s, c, ws, J);
+  for (int b = 0; b <= s->batch; ++b) J->off[b] = s->cu_seqlens[b];
+  return MMSHIFT_OK;
+}
+
+mmshift_status check_workspace(const CacheJob& J, const void* ws, size_t bytes) {
+  if (!ws || !aligned(ws, 256) || bytes < 256 + attend_scratch_bytes(J)) return MMSHIFT_ERR_WORKSPACE;
+  return MMSHIFT_OK;
+}
+
+template <bool FILL>
+cudaError_t launch_write(const CacheJob& J, const void* K, const void* V, const int32_t* idx,
+                         const int32_t* count, cudaStream_t st) {
+  const long long rows = (long long)J.off[J.B] * J.Hkv;
+  if (!rows) return cudaSuccess;
+  const int esz = J.bf16 ? 2 : 4, per = 256 / (J.d * esz / 16);
+  const bool vec = aligned(K, 16) && aligned(V, 16) && J.stride * esz % 16 == 0 && J.ls * esz % 16 == 0;
+  const dim3 grid((unsigned)((rows + per - 1) / per), J.L);
+  auto go = [&](auto kernel) {
+    return launch_kernel(kernel, grid, 256, 0, st, true, 0, J, (const uint8_t*)K, (const uint8_t*)V, idx,
+                         count, vec);
+  };
+  if (J.bf16) {
+    if (J.d == 128)
+      return J.i8 ? go(cache_write_kernel<__nv_bfloat16, 128, true, FILL>)
+                  : go(cache_write_kernel<__nv_bfloat16, 128, false, FILL>);
+    return J.i8 ? go(cache_write_kernel<__nv_bfloat16, 64, true, FILL>)
+                : go(cache_write_kernel<__nv_bfloat16, 64, false, FILL>);
+  }
+  if (J.d == 128)
+    return J.i8 ? go(cache_write_kernel<float, 128, true, FILL>) : go(cache_write_kernel<float, 128, false, FILL>);
+  return J.i8 ? go(cache_write_kernel<float, 64, true, FILL>) : go(cache_write_kernel<float, 64, false, FILL>);
+}
+
+cudaError_t launch_read(const CacheJob& J, const int32_t* first, void* oK, void* oV, cudaStream_t st) {
+  const long long rows = (long long)J.off[J.B] * J.Hkv;
+  if (!rows) return cudaSuccess;
+  const int esz = J.bf16 ? 2 : 4, per = 256 / (J.d * esz / 16);
+  const bool vec = aligned(oK, 16) && aligned(oV, 16);
+  const dim3 grid((unsigned)((rows + per - 1) / per), J.L);
+  auto go = [&](auto kernel) {
+    return launch_kernel(kernel, grid, 256, 0, st, true, 0, J, first, (uint8_t*)oK, (uint8_t*)oV, vec);
+  };
+  if (J.bf16) {
+    if (J.d == 128)
+      return J.i8 ? go(cache_read_kernel<__nv_bfloat16, 128, true>) : go(cache_read_kernel<__nv_bfloat16, 128, false>);
+    return J.i8 ? go(cache_read_kernel<__nv_bfloat16, 64, true>) : go(cache_read_kernel<__nv_bfloat16, 64, false>);
+  }
+  if (J.d == 128)
+    return J.i8 ? go(cache_read_kernel<float, 128, true>) : go(cache_read_kernel<float, 128, false>);
+  return J.i8 ? go(cache_read_kernel<float, 64, true>) : go(cache_read_kernel<float, 64, false>);
+}
+
+mmshift_status done(cudaError_t e) { return e == cudaSuccess ? MMSHIFT_OK : noalloc_cuda_fail(e); }
+
+}  // namespace
+}  // namespace mmshift
+
+using namespace mmshift;
+
+extern "C" {
+
+mmshift_status mmshift_cache_workspace_size(const mmshift_shape* s, const mmshift_cache* c,
+                                            size_t* bytes) {
+  CacheJob J;
+  const mmshift_status st = rows_job(s, c, nullptr, &J);
+  if (st != MMSHIFT_OK) return st;
+  if (!bytes) return MMSHIFT_ERR_INVALID_ARG;
+  *bytes = 256 + attend_scratch_bytes(J);
+  return MMSHIFT_OK;
+}
+
+mmshift_status mmshift_cache_fill(const mmshift_shape* s, const mmshift_cache* c, const void* K,
+                                  const void* V, const int32_t* idx, const int32_t* count,
+                                  void* workspace, size_t workspace_bytes,
+                                  mmshift_stream_t stream) {
+  Problem P;
+  mmshift_status st = noalloc_prepare(s, nullptr, &P);
+  if (st == MMSHIFT_OK) st = check_cache(s, c);
+  if (st != MMSHIFT_OK) return st;
+  const size_t esz = s->dtype == MMSHIFT_BF16 ? 2 : 4;
+  if (!K || !V || !idx || !aligned(K, esz) || !aligned(V, esz) || !aligned(idx, 4) || !aligned(count, 4))
+    return MMSHIFT_ERR_INVALID_ARG;
+  if ((int64_t)P.R * P.Hkv > (int64_t)1 << 30) return MMSHIFT_ERR_UNSUPPORTED;
+  CacheJob J;
+  fill_job(s, c, workspace, &J);
+  for (int b = 0; b < P.B; ++b) {
+    J.off[b] = P.req[b].out_off;
+    J.src[b + 1] = P.req[b].tok_off + P.req[b].t_len;
+  }
+  J.off[P.B] = P.R;
+  J.ls = P.ls_kv;
+  if (!workspace || !aligned(workspace, 256) || workspace_bytes < 256) return MMSHIFT_ERR_WORKSPACE;
+  if (!device_readable(K) || !device_readable(V)) return MMSHIFT_ERR_INVALID_ARG;
+  return done(launch_write<true>(J, K, V, idx, count, (cudaStream_t)stream));
+}
+
+mmshift_status mmshift_cache_append(const mmshift_shape* s, const mmshift_cache* c, const void* K,
+                                    const void* V, int64_t row_stride, void* workspace,
+                                    size_t workspace_bytes, mmshift_stream_t stream) {
+  CacheJob J;
+  mmshift_status st = rows_job(s, c, workspace, &J);
+  if (st != MMSHIFT_OK) return st;
+  const size_t esz = J.bf16 ? 2 : 4;
+  const int64_t dense = (int64_t)J.Hkv * J.d, total = J.off[J.B];
+  if (row_stride && row_stride < dense) return MMSHIFT_ERR_INVALID_ARG;
+  J.stride = row_stride ? row_stride : dense;
+  J.ls = J.L > 1 ? s->layer_stride_kv : 0;
+  if (J.L > 1 && total && J.ls < (total - 1) * J.stride + dense) return MMSHIFT_ERR_INVALID_ARG;
+  if (total && (!K || !V)) return MMSHIFT_ERR_INVALID_ARG;
+  if (!aligned(K, esz) || !aligned(V, esz)) return MMSHIFT_ERR_INVALID_ARG;
+  if ((st = check_workspace(J, workspace, workspace_bytes)) != MMSHIFT_OK) return st;
+  return done(launch_write<false>(J, K, V, nullptr, nullptr, (cudaStream_t)stream));
+}
+
+mmshift_status mmshift_cache_read(const mmshift_shape* s, const mmshift_cache* c,
+                                  const int32_t* first, void* out_K, void* out_V, void* workspace,
+                                  size_t workspace_bytes, mmshift_stream_t stream) {
+  CacheJob J;
+  mmshift_status st = rows_job(s, c, workspace, &J);
+  if (st != MMSHIFT_OK) return st;
+  const size_t esz = J.bf16 ? 2 : 4;
+  if (J.off[J.B] && (!out_K || !out_V)) return MMSHIFT_ERR_INVALID_ARG;
+  if (!aligned(out_K, esz) || !aligned(out_V, esz) || !aligned(first, 4)) return MMSHIFT_ERR_INVALID_ARG;
+  if ((st = check_workspace(J, workspace, workspace_bytes)) != MMSHIFT_OK) return st;
+  return done(launch_read(J, first, out_K, out_V, (cudaStream_t)stream));
+}
+
+mmshift_status mmshift_cache_attention(const mmshift_shape* s, const mmshift_cache* c,
+                                       const void* Q, int64_t row_stride, int32_t causal,
+                                       float softmax_scale, void* out, float* lse,
+                                       void* workspace, size_t workspace_bytes,
+                                       mmshift_stream_t stream) {
+  AttendJob A;
+  std::memset(&A, 0, sizeof(A));
+  CacheJob& J = A.c;
+  mmshift_status st = rows_job(s, c, workspace, &J);
+  if (st != MMSHIFT_OK) return st;
+  if (J.L != 1) return MMSHIFT_ERR_UNSUPPORTED;
+  const size_t esz = J.bf16 ? 2 : 4;
+  const int64_t dense = (int64_t)J.Hq * J.d;
+  if (row_stride && row_stride < dense) return MMSHIFT_ERR_INVALID_ARG;
+  if (causal != 0 && causal != 1) return MMSHIFT_ERR_INVALID_ARG;
+  if (!(softmax_scale >= 0.f) || !std::isfinite(softmax_scale)) return MMSHIFT_ERR_INVALID_ARG;
+  if (J.off[J.B] && (!Q || !out)) return MMSHIFT_ERR_INVALID_ARG;
+  if (!aligned(Q, esz) || !aligned(out, esz) || !aligned(lse, 4)) return MMSHIFT_ERR_INVALID_ARG;
+  if ((st = check_workspace(J, workspace, workspace_bytes)) != MMSHIFT_OK) return st;
+  J.stride = row_stride ? row_stride : dense;
+  A.q = static_cast<const uint8_t*>(Q);
+  A.out = static_cast<uint8_t*>(out);
+  A.lse = lse;
+  A.causal = causal;
+  A.qvec = aligned(Q, 16) && J.stride * esz % 16 == 0;
+  A.ovec = aligned(out, 16);
+  A.alpha = (softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt((float)J.d)) * kLog2e;
+  if (!J.off[J.B]) return MMSHIFT_OK;
+  return done(launch_attend(A, static_cast<char*>(workspace) + 256, (cudaStream_t)stream));
+}
+
+}  // extern "C"

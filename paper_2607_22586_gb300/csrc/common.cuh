@@ -28,6 +28,7 @@ enum : int {
   kStatusTimeout = 1,   // a bounded wait gave up
   kStatusBadIndex = 2,  // gather saw an index outside [0, T_b)
   kStatusBadBudget = 4, // a per-head budget outside [1, C_b] (clamped)
+  kStatusBadPage = 8,   // a cache position without a page
 };
 
 struct ReqInfo {
@@ -261,6 +262,9 @@ cudaError_t launch_kernel(void (*k)(KP...), dim3 grid, unsigned block, size_t sm
   cfg.numAttrs = n;
   return cudaLaunchKernelEx(&cfg, k, static_cast<KP>(args)...);
 }
+
+// Host-side checks shared by the translation units with entry points (api.cu).
+bool device_readable(const void* p);
 
 // Host-side launchers (one translation unit each).
 cudaError_t launch_prefill_stats(const StatsJob& J, const void* Q, float* part, float* stats,
