@@ -229,7 +229,7 @@ def _handles(s, case):
 
     def shape(cu, budgets, stride_kv):
         return M.make_shape(case["hq"], case["hkv"], case["d"], 2, dt, cu, budgets, n_layers=L,
-                            layer_stride_kv=stride_kv, layer_stride_q=0)
+                            layer_stride_kv=stride_kv, layer_stride_q=len(budgets) * 2 * case["hq"] * case["d"])
 
     rows = shape(s["cu_out"], [1] * (len(s["cu_out"]) - 1), s["K"].stride(0) if "K" in s else 0)
     n = M.mmshift_cache_workspace_size(rows, cache)
