@@ -390,8 +390,9 @@ mmshift_status mmshift_coverage(const mmshift_shape* s, const void* K, const voi
  * prompt: request b has T_b = cu_seqlens[b+1] - cu_seqlens[b] >= 0 rows
  * (n_b below); window and budgets are not read. Pages that a call writes belong to
  * one sequence; pages that it only reads may be shared. Workspace (and status
- * word, zero at first): mmshift_cache_workspace_size() bytes, 256-byte aligned;
- * what it holds besides the status word need not outlive the call. */
+ * word, zero at first): mmshift_cache_workspace_size() bytes for attention with
+ * that shape, 256 for the other calls, 256-byte aligned; what it holds besides
+ * the status word need not outlive the call. */
 enum { MMSHIFT_I8 = 2 };  /* cache type only */
 
 typedef struct {

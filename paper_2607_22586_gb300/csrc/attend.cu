@@ -1,6 +1,9 @@
-// Attention of new tokens over the paged cache (mmshift_cache_attention): one
-// warp a row, one key at a time.
-#include "cache.cuh"
+// Attention of new tokens over the paged cache (mmshift_cache_attention): which
+// kernel takes which requests, and the merge of partial sums.
+#include <algorithm>
+#include <cstring>
+
+#include "attend.cuh"
 
 namespace mmshift {
 namespace {
@@ -52,12 +55,174 @@ __global__ void __launch_bounds__(128) attend_row_kernel(const __grid_constant__
   if (A.lse && lane == 0) A.lse[row] = z == 0.f ? -INFINITY : (m + log2f(z)) * 0.6931471805599453f;
 }
 
+// The partial sums of units that several workers share, and zeros for units
+// without keys. A block takes RPB rows: RPB = 1 with all its warps on the parts of
+// a row (few rows, many parts), else a warp a row.
+template <typename T, int D, int RPB>
+__global__ void __launch_bounds__(256) attend_merge_kernel(const __grid_constant__ AttendJob A,
+                                                           const __grid_constant__ AttendPlan P) {
+  dependent_start();
+  constexpr int LV = D / 32;                           // values of a lane
+  const int u = blockIdx.x, w = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int64_t a = P.pre[u], b = P.pre[u + 1], W = P.pre[P.uoff[A.c.B]];
+  int n = 0, i0 = 0, i1 = -1;
+  if (a < b) {
+    n = span_workers(W, P.workers, P.least);
+    i0 = span_of(W, n, a);
+    i1 = span_of(W, n, b - 1);
+    if (i0 == i1) return;                              // one worker had it all
+  }
+  const AttendUnit U = attend_unit(A, P, u);
+  const int r = RPB == 1 ? blockIdx.y : blockIdx.y * RPB + w;
+  if (r >= U.rows) return;
+  const int parts = i1 - i0 + 1;
+  auto at = [&](int k) {
+    return (size_t)attend_slot(i0 + k, span_begin(W, n, i0 + k), a) * P.rows + r;
+  };
+  float top = -INFINITY;
+  for (int k = lane; k < parts; k += 32) top = fmaxf(top, P.pml[at(k)].x);
+#pragma unroll
+  for (int s = 16; s; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+  float z = 0.f, o[LV] = {};
+  constexpr int STEP = RPB == 1 ? 8 : 1;
+#pragma unroll 4
+  for (int k = RPB == 1 ? w : 0; k < parts; k += STEP) {
+    const size_t slot = at(k);
+    const float2 ml = P.pml[slot];
+    const float f = ml.x == -INFINITY ? 1.f : fast_exp2(ml.x - top);
+    z += ml.y * f;
+    const float* p = P.po + slot * D + lane * LV;
+    if constexpr (LV == 4) {
+      const float4 v = *reinterpret_cast<const float4*>(p);
+      o[0] += v.x * f;
+      o[1] += v.y * f;
+      o[2] += v.z * f;
+      o[3] += v.w * f;
+    } else {
+      const float2 v = *reinterpret_cast<const float2*>(p);
+      o[0] += v.x * f;
+      o[1] += v.y * f;
+    }
+  }
+  if constexpr (RPB == 1) {
+    __shared__ alignas(16) float so[8][D];
+    __shared__ float sz[8];
+#pragma unroll
+    for (int i = 0; i < LV; ++i) so[w][lane * LV + i] = o[i];
+    if (lane == 0) sz[w] = z;
+    __syncthreads();
+    if (threadIdx.x >= D / 4) return;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    z = 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float4 x = *reinterpret_cast<const float4*>(&so[k][threadIdx.x * 4]);
+      v.x += x.x;
+      v.y += x.y;
+      v.z += x.z;
+      v.w += x.w;
+      z += sz[k];
+    }
+    attend_write<T, D>(A, U.b, U.h, U.row0 + r, threadIdx.x * 4, v, top, z);
+  } else {
+    // four neighbouring values to one lane
+    float4 v;
+    if constexpr (LV == 4) {
+      v = make_float4(o[0], o[1], o[2], o[3]);
+      attend_write<T, D>(A, U.b, U.h, U.row0 + r, lane * 4, v, top, z);
+    } else {
+      const float x = __shfl_down_sync(0xffffffffu, o[0], 1), y = __shfl_down_sync(0xffffffffu, o[1], 1);
+      v = make_float4(o[0], o[1], x, y);
+      if (lane % 2 == 0) attend_write<T, D>(A, U.b, U.h, U.row0 + r, lane * 2, v, top, z);
+    }
+  }
+}
+
+template <typename T, int D>
+cudaError_t launch_merge(const AttendJob& A, const AttendPlan& P, cudaStream_t st) {
+  const unsigned units = P.uoff[A.c.B];
+  if (P.rows <= 16)
+    return launch_kernel(attend_merge_kernel<T, D, 1>, dim3(units, P.rows), 256, 0, st, true, 0, A, P);
+  return launch_kernel(attend_merge_kernel<T, D, 8>, dim3(units, (P.rows + 7) / 8), 256, 0, st, true, 0, A, P);
+}
+
+// Requests whose rows of a KV head are at most this many go to the token kernel.
+constexpr int kTokenRows = 16;
+
+int sm_count() {
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    return 0;
+  return n;
+}
+
+size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
+
+// Workers of the plans at most: the workspace is sized without asking the device.
+constexpr int kMostWorkers = 152 * 4;
+
+size_t plan_bytes(int units, int rows, int d, int workers) {
+  return align256((size_t)(units + 1) * sizeof(int64_t)) +
+         align256((size_t)2 * workers * rows * d * sizeof(float)) + align256((size_t)2 * workers * rows * sizeof(float2));
+}
+
+// The plan of the requests that `take`s, with tiles of at most `most` rows.
+template <class Take>
+AttendPlan plan_of(const CacheJob& J, int most, Take take) {
+  AttendPlan P;
+  std::memset(&P, 0, sizeof(P));
+  int widest = 0;
+  for (int b = 0; b < J.B; ++b) {
+    const int rows = (J.off[b + 1] - J.off[b]) * J.r;
+    if (rows && take(rows)) widest = std::max(widest, rows);
+  }
+  P.rows = std::min(widest, most);
+  for (int b = 0; b < J.B; ++b) {
+    const int rows = (J.off[b + 1] - J.off[b]) * J.r;
+    P.uoff[b + 1] = P.uoff[b] + (rows && take(rows) ? J.Hkv * ((rows + P.rows - 1) / P.rows) : 0);
+  }
+  return P;
+}
+
+AttendPlan token_plan(const CacheJob& J) {
+  AttendPlan P = plan_of(J, kTokenRows, [&](int rows) { return J.bf16 && rows <= kTokenRows; });
+  const int row = J.i8 ? J.d : 2 * J.d;
+  while ((row << P.step_shift) < 4096) ++P.step_shift;   // a warp's piece: 4 KB of K
+  P.least = 4;
+  return P;
+}
+
+void place(AttendPlan& P, const CacheJob& J, int workers, char*& at) {
+  P.workers = workers;
+  P.pre = reinterpret_cast<int64_t*>(at);
+  at += align256((size_t)(P.uoff[J.B] + 1) * sizeof(int64_t));
+  P.po = reinterpret_cast<float*>(at);
+  at += align256((size_t)2 * workers * P.rows * J.d * sizeof(float));
+  P.pml = reinterpret_cast<float2*>(at);
+  at += align256((size_t)2 * workers * P.rows * sizeof(float2));
+}
+
 }  // namespace
 
-size_t attend_scratch_bytes(const CacheJob&) { return 0; }
+size_t attend_scratch_bytes(const CacheJob& J) {
+  const AttendPlan t = token_plan(J);
+  return plan_bytes(t.uoff[J.B], t.rows, J.d, kMostWorkers);
+}
 
-cudaError_t launch_attend(const AttendJob& A, void*, cudaStream_t st) {
+cudaError_t launch_attend(const AttendJob& A, void* scratch, cudaStream_t st) {
   const CacheJob& J = A.c;
+  const int nsm = std::min(sm_count(), 152);
+  if (nsm <= 0) return cudaErrorInvalidDevice;
+  char* at = static_cast<char*>(scratch);
+  AttendPlan t = token_plan(J);
+  bool all = true;
+  for (int b = 0; b < J.B; ++b) all &= J.bf16 && (J.off[b + 1] - J.off[b]) * J.r <= kTokenRows;
+  if (all) {
+    place(t, J, nsm * (t.rows <= 8 ? 4 : 3), at);
+    cudaError_t e = launch_attend_token(A, t, st);
+    if (e != cudaSuccess) return e;
+    return J.d == 128 ? launch_merge<__nv_bfloat16, 128>(A, t, st) : launch_merge<__nv_bfloat16, 64>(A, t, st);
+  }
   const long long rows = (long long)J.off[J.B] * J.Hq;
   auto go = [&](auto kernel) {
     return launch_kernel(kernel, dim3((unsigned)((rows + 3) / 4)), 128, 0, st, true, 0, A);

@@ -1,0 +1,154 @@
+// Attention over the paged cache: how its work is cut and shared out.
+//
+// A unit is (request, KV head, tile of query rows); row rho of a request's
+// head is token rho / r and query head h * r + rho % r. Its keys, up to its last
+// row's, are cut into pieces of 2^step_shift, and the pieces of all units in
+// their order are shared out evenly to the workers (CTAs), however long the
+// sequences are: their lengths are read on the device, so every CTA adds up
+// the pieces itself. A worker's range covers whole units, whose results it
+// writes, and at most two pieces of units, its first and its last, whose
+// partial sums it leaves for the merge kernel.
+#pragma once
+
+#include "cache.cuh"
+
+namespace mmshift {
+
+struct AttendPlan {
+  int32_t uoff[MMSHIFT_MAX_BATCH + 1];  // units, prefix over requests
+  int32_t rows;                         // query rows of a tile
+  int32_t step_shift;
+  int32_t workers, least;               // workers at most; pieces that one has at least, if there are so many
+  int64_t* pre;                         // [units + 1] pieces before each unit (written by the first CTA)
+  float* po;                            // [2 * workers][rows][d] sums of weights times values
+  float2* pml;                          // [2 * workers][rows] their maximum (base 2) and sum of weights
+};
+
+struct AttendUnit {
+  int b, h, n;         // request, KV head, the request's tokens
+  int row0, rows;      // the tile's first row, its rows
+  int len, keys;       // rows of the sequence; keys that the tile's last row attends to
+  int pieces;
+};
+
+__device__ __forceinline__ AttendUnit attend_unit(const AttendJob& A, const AttendPlan& P, int u) {
+  const CacheJob& J = A.c;
+  AttendUnit x;
+  x.b = range_of(P.uoff, J.B, u);
+  x.n = J.off[x.b + 1] - J.off[x.b];
+  const int all = x.n * J.r, tiles = (all + P.rows - 1) / P.rows, rem = u - P.uoff[x.b];
+  x.h = rem / tiles;
+  x.row0 = (rem - x.h * tiles) * P.rows;
+  x.rows = min(P.rows, all - x.row0);
+  x.len = cache_len(J, (size_t)x.b * J.Hkv + x.h);
+  x.keys = keys_of(A.causal, x.len, x.n, (x.row0 + x.rows - 1) / J.r);
+  x.pieces = (x.keys + (1 << P.step_shift) - 1) >> P.step_shift;
+  return x;
+}
+
+// A worker's place in the work: pieces [begin, end) of all, the unit that
+// holds the first of them and the pieces before that unit.
+struct AttendSpan {
+  int64_t begin, end, before;
+  int unit;
+};
+
+template <int NT>
+struct AttendScan {
+  int64_t warp[NT / 32];
+  AttendSpan span;
+};
+
+// Called by the CTA's first NT threads together (`bar` is their barrier).
+// Every thread adds up a run of units; a scan over the threads gives the pieces
+// before each run.
+template <int NT, class Barrier>
+__device__ __forceinline__ AttendSpan attend_span(const AttendJob& A, const AttendPlan& P, AttendScan<NT>* s,
+                                                  Barrier bar) {
+  const int tid = threadIdx.x, lane = tid % 32, w = tid / 32, U = P.uoff[A.c.B];
+  const int per = (U + NT - 1) / NT, u0 = min(tid * per, U), u1 = min(u0 + per, U);
+  int64_t sum = 0;
+  for (int u = u0; u < u1; ++u) sum += attend_unit(A, P, u).pieces;
+  int64_t x = sum;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int64_t y = __shfl_up_sync(0xffffffffu, x, d);
+    if (lane >= d) x += y;
+  }
+  if (lane == 31) s->warp[w] = x;
+  bar();
+  int64_t W = 0, before = x - sum;
+#pragma unroll
+  for (int i = 0; i < NT / 32; ++i) {
+    if (i < w) before += s->warp[i];
+    W += s->warp[i];
+  }
+  const int n = span_workers(W, P.workers, P.least), i = blockIdx.x;
+  const int64_t begin = i < n ? span_begin(W, n, i) : W, end = i < n ? span_begin(W, n, i + 1) : W;
+  if (i == 0) {
+    int64_t a = before;
+    for (int u = u0; u < u1; ++u) {
+      P.pre[u] = a;
+      a += attend_unit(A, P, u).pieces;
+    }
+    if (tid == 0) P.pre[U] = W;
+  }
+  if (tid == 0) s->span = AttendSpan{begin, end, 0, 0};
+  bar();
+  if (begin < end && begin >= before && begin < before + sum) {
+    int u = u0;
+    int64_t a = before;
+    for (;;) {
+      const int p = attend_unit(A, P, u).pieces;
+      if (a + p > begin) break;
+      a += p;
+      ++u;
+    }
+    s->span.before = a;
+    s->span.unit = u;
+  }
+  bar();
+  return s->span;
+}
+
+// The partial sums' slot of a worker's piece of the unit with `before` pieces before it.
+__device__ __forceinline__ int attend_slot(int worker, int64_t begin, int64_t before) {
+  return 2 * worker + (before > begin);
+}
+
+// Four values of an output row from its sums; a row without weights is zeros.
+// `row` counts the rows of the request's KV head.
+template <typename T, int D>
+__device__ __forceinline__ void attend_write(const AttendJob& A, int b, int h, int row, int d0, float4 v, float top,
+                                             float z) {
+  const CacheJob& J = A.c;
+  const int tok = row / J.r;
+  const size_t at = (size_t)(J.off[b] + tok) * J.Hq + h * J.r + row - tok * J.r;
+  const float f = z == 0.f ? 0.f : 1.f / z;
+  T* out = reinterpret_cast<T*>(A.out) + at * D + d0;
+  if (z == 0.f) v = make_float4(0.f, 0.f, 0.f, 0.f);
+  if constexpr (sizeof(T) == 2) {
+    if (A.ovec) {
+      *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(v.x * f, v.y * f), pack_bf16(v.z * f, v.w * f));
+    } else {
+      out[0] = from_f32<T>(v.x * f);
+      out[1] = from_f32<T>(v.y * f);
+      out[2] = from_f32<T>(v.z * f);
+      out[3] = from_f32<T>(v.w * f);
+    }
+  } else {
+    if (A.ovec) {
+      *reinterpret_cast<float4*>(out) = make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
+    } else {
+      out[0] = v.x * f;
+      out[1] = v.y * f;
+      out[2] = v.z * f;
+      out[3] = v.w * f;
+    }
+  }
+  if (d0 == 0 && A.lse) A.lse[at] = z == 0.f ? -INFINITY : (top + log2f(z)) * 0.6931471805599453f;
+}
+
+cudaError_t launch_attend_token(const AttendJob& A, const AttendPlan& P, cudaStream_t st);
+
+}  // namespace mmshift

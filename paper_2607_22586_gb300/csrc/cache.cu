@@ -244,9 +244,9 @@ mmshift_status rows_job(const mmshift_shape* s, const mmshift_cache* c, void* ws
   return MMSHIFT_OK;
 }
 
-mmshift_status check_workspace(const CacheJob& J, const void* ws, size_t bytes) {
-  if (!ws || !aligned(ws, 256) || bytes < 256 + attend_scratch_bytes(J)) return MMSHIFT_ERR_WORKSPACE;
-  return MMSHIFT_OK;
+// Rows are moved with the status word alone, attention takes `scratch` bytes more.
+mmshift_status check_workspace(const void* ws, size_t bytes, size_t scratch = 0) {
+  return ws && aligned(ws, 256) && bytes >= 256 + scratch ? MMSHIFT_OK : MMSHIFT_ERR_WORKSPACE;
 }
 
 template <bool FILL>
@@ -331,7 +331,7 @@ mmshift_status mmshift_cache_fill(const mmshift_shape* s, const mmshift_cache* c
   }
   J.off[P.B] = P.R;
   J.ls = P.ls_kv;
-  if (!workspace || !aligned(workspace, 256) || workspace_bytes < 256) return MMSHIFT_ERR_WORKSPACE;
+  if ((st = check_workspace(workspace, workspace_bytes)) != MMSHIFT_OK) return st;
   if (!device_readable(K) || !device_readable(V)) return MMSHIFT_ERR_INVALID_ARG;
   return done(launch_write<true>(J, K, V, idx, count, (cudaStream_t)stream));
 }
@@ -350,7 +350,7 @@ mmshift_status mmshift_cache_append(const mmshift_shape* s, const mmshift_cache*
   if (J.L > 1 && total && J.ls < (total - 1) * J.stride + dense) return MMSHIFT_ERR_INVALID_ARG;
   if (total && (!K || !V)) return MMSHIFT_ERR_INVALID_ARG;
   if (!aligned(K, esz) || !aligned(V, esz)) return MMSHIFT_ERR_INVALID_ARG;
-  if ((st = check_workspace(J, workspace, workspace_bytes)) != MMSHIFT_OK) return st;
+  if ((st = check_workspace(workspace, workspace_bytes)) != MMSHIFT_OK) return st;
   return done(launch_write<false>(J, K, V, nullptr, nullptr, (cudaStream_t)stream));
 }
 
@@ -363,7 +363,7 @@ mmshift_status mmshift_cache_read(const mmshift_shape* s, const mmshift_cache* c
   const size_t esz = J.bf16 ? 2 : 4;
   if (J.off[J.B] && (!out_K || !out_V)) return MMSHIFT_ERR_INVALID_ARG;
   if (!aligned(out_K, esz) || !aligned(out_V, esz) || !aligned(first, 4)) return MMSHIFT_ERR_INVALID_ARG;
-  if ((st = check_workspace(J, workspace, workspace_bytes)) != MMSHIFT_OK) return st;
+  if ((st = check_workspace(workspace, workspace_bytes)) != MMSHIFT_OK) return st;
   return done(launch_read(J, first, out_K, out_V, (cudaStream_t)stream));
 }
 
@@ -385,7 +385,7 @@ mmshift_status mmshift_cache_attention(const mmshift_shape* s, const mmshift_cac
   if (!(softmax_scale >= 0.f) || !std::isfinite(softmax_scale)) return MMSHIFT_ERR_INVALID_ARG;
   if (J.off[J.B] && (!Q || !out)) return MMSHIFT_ERR_INVALID_ARG;
   if (!aligned(Q, esz) || !aligned(out, esz) || !aligned(lse, 4)) return MMSHIFT_ERR_INVALID_ARG;
-  if ((st = check_workspace(J, workspace, workspace_bytes)) != MMSHIFT_OK) return st;
+  if ((st = check_workspace(workspace, workspace_bytes, attend_scratch_bytes(J))) != MMSHIFT_OK) return st;
   J.stride = row_stride ? row_stride : dense;
   A.q = static_cast<const uint8_t*>(Q);
   A.out = static_cast<uint8_t*>(out);

@@ -80,7 +80,8 @@ def test_bad_arguments():
     n = M.mmshift_cache_workspace_size(s, c)
     assert n >= 256
     assert _calls(s, c, ws=None) == _calls(s, c, ws=FAKE + 16) == [L.MMSHIFT_ERR_WORKSPACE] * 3
-    assert _calls(s, c, n=n - 1) == [L.MMSHIFT_ERR_WORKSPACE] * 3
+    assert _calls(s, c, n=255) == [L.MMSHIFT_ERR_WORKSPACE] * 3
+    assert _calls(s, c, n=n - 1)[2] == L.MMSHIFT_ERR_WORKSPACE
     assert _calls(s, c, Q=None, K=None, out=None) == [L.MMSHIFT_ERR_INVALID_ARG] * 3
     assert _calls(s, c, Q=FAKE + 1, K=FAKE + 1, out=FAKE + 1) == [L.MMSHIFT_ERR_INVALID_ARG] * 3
     for stride in (-1, 255):                                     # rows that overlap
