@@ -139,11 +139,17 @@ __global__ void __launch_bounds__(256) attend_merge_kernel(const __grid_constant
 }
 
 template <typename T, int D>
-cudaError_t launch_merge(const AttendJob& A, const AttendPlan& P, cudaStream_t st) {
+cudaError_t launch_merge_t(const AttendJob& A, const AttendPlan& P, cudaStream_t st) {
   const unsigned units = P.uoff[A.c.B];
   if (P.rows <= 16)
     return launch_kernel(attend_merge_kernel<T, D, 1>, dim3(units, P.rows), 256, 0, st, true, 0, A, P);
   return launch_kernel(attend_merge_kernel<T, D, 8>, dim3(units, (P.rows + 7) / 8), 256, 0, st, true, 0, A, P);
+}
+
+cudaError_t launch_merge(const AttendJob& A, const AttendPlan& P, cudaStream_t st) {
+  if (A.c.bf16)
+    return A.c.d == 128 ? launch_merge_t<__nv_bfloat16, 128>(A, P, st) : launch_merge_t<__nv_bfloat16, 64>(A, P, st);
+  return A.c.d == 128 ? launch_merge_t<float, 128>(A, P, st) : launch_merge_t<float, 64>(A, P, st);
 }
 
 // Requests whose rows of a KV head are at most this many go to the token kernel.
@@ -159,7 +165,7 @@ int sm_count() {
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
 // Workers of the plans at most: the workspace is sized without asking the device.
-constexpr int kMostWorkers = 152 * 4;
+constexpr int kMostWorkers = 152 * 4, kMostChunkWorkers = 152;
 
 size_t plan_bytes(int units, int rows, int d, int workers) {
   return align256((size_t)(units + 1) * sizeof(int64_t)) +
@@ -192,6 +198,13 @@ AttendPlan token_plan(const CacheJob& J) {
   return P;
 }
 
+AttendPlan chunk_plan(const CacheJob& J) {
+  AttendPlan P = plan_of(J, 256, [&](int rows) { return J.bf16 && rows > kTokenRows; });
+  P.step_shift = 7;
+  P.least = 1;
+  return P;
+}
+
 void place(AttendPlan& P, const CacheJob& J, int workers, char*& at) {
   P.workers = workers;
   P.pre = reinterpret_cast<int64_t*>(at);
@@ -205,23 +218,33 @@ void place(AttendPlan& P, const CacheJob& J, int workers, char*& at) {
 }  // namespace
 
 size_t attend_scratch_bytes(const CacheJob& J) {
-  const AttendPlan t = token_plan(J);
-  return plan_bytes(t.uoff[J.B], t.rows, J.d, kMostWorkers);
+  const AttendPlan t = token_plan(J), c = chunk_plan(J);
+  return plan_bytes(t.uoff[J.B], t.rows, J.d, kMostWorkers) + plan_bytes(c.uoff[J.B], c.rows, J.d, kMostChunkWorkers);
 }
 
 cudaError_t launch_attend(const AttendJob& A, void* scratch, cudaStream_t st) {
   const CacheJob& J = A.c;
-  const int nsm = std::min(sm_count(), 152);
+  const int nsm = std::min(sm_count(), kMostChunkWorkers);
   if (nsm <= 0) return cudaErrorInvalidDevice;
   char* at = static_cast<char*>(scratch);
-  AttendPlan t = token_plan(J);
-  bool all = true;
-  for (int b = 0; b < J.B; ++b) all &= J.bf16 && (J.off[b + 1] - J.off[b]) * J.r <= kTokenRows;
-  if (all) {
-    place(t, J, nsm * (t.rows <= 8 ? 4 : 3), at);
-    cudaError_t e = launch_attend_token(A, t, st);
-    if (e != cudaSuccess) return e;
-    return J.d == 128 ? launch_merge<__nv_bfloat16, 128>(A, t, st) : launch_merge<__nv_bfloat16, 64>(A, t, st);
+  AttendPlan t = token_plan(J), c = chunk_plan(J);
+  place(t, J, nsm * (t.rows <= 8 ? 4 : 3), at);
+  place(c, J, nsm, at);
+  if (J.bf16 && !J.i8) {
+    cudaError_t e = cudaSuccess;
+    if (c.uoff[J.B]) {
+      e = launch_attend_chunk(A, c, st);
+      if (e == cudaSuccess) e = launch_merge(A, c, st);
+    }
+    if (e == cudaSuccess && t.uoff[J.B]) {
+      e = launch_attend_token(A, t, st);
+      if (e == cudaSuccess) e = launch_merge(A, t, st);
+    }
+    return e;
+  }
+  if (J.bf16 && !c.uoff[J.B]) {
+    const cudaError_t e = launch_attend_token(A, t, st);
+    return e == cudaSuccess ? launch_merge(A, t, st) : e;
   }
   const long long rows = (long long)J.off[J.B] * J.Hq;
   auto go = [&](auto kernel) {

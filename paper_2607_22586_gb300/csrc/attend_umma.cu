@@ -1,0 +1,580 @@
+// Attention of chunks (more than 16 query rows of a request and KV head) on the
+// 5th-generation tensor cores (tcgen05 + TMA + TMEM).
+//
+// Tiles of 256 query rows, two blocks of 128, over tiles of 128 keys:
+//   S = Q K^T   [128 x 128]  both operands in shared memory, S in tensor memory;
+//   O += P V    [128 x d]    P in tensor memory, over the columns of its S, V in
+//               shared memory as it lies in the page (keys by dimensions: the
+//               MN-major B operand), O in tensor memory for the whole run of keys.
+// Roles (384 threads, one CTA per SM):
+//   warps 0-7   softmax, one warpgroup a block, one thread a row: its maximum
+//               and sum need no reduction across threads. It reads S, writes P
+//               and, at the end of the run, O;
+//   warp 8      TMA producer: a ring of K and V tiles. A page is a box of up to
+//               128 rows, so a tile is 1 to 8 boxes and 64 columns wide halves;
+//   warp 9      MMA issuer.
+// The blocks alternate: while one block's softmax runs, the tensor cores have
+// the other block's products. A row's maximum is only raised when a logit passes it
+// by 8 (base 2); then the thread rescales its row of O itself, which is idle at
+// that point: S of a tile is complete only after the products of the tile before.
+// P is rounded to bfloat16 (the tensor cores' operand type), its sum is not.
+//
+// Tiles that hold keys which some row of the tile does not attend to (the chunk's
+// own keys under the causal mask, the last tile) are masked, and their V rows are
+// cleaned first: behind the last key a page may hold anything, and a zero weight
+// times a NaN is a NaN. Values that are not finite and that some rows do attend to
+// are set to zero for the product and added to those rows at the end.
+// Every wait is bounded; a role that gives up ends the CTA as score_umma.cu says.
+#include <cudaTypedefs.h>
+
+#include <algorithm>
+
+#include "attend.cuh"
+#include "umma.cuh"
+
+namespace mmshift {
+namespace {
+
+using namespace umma;
+
+constexpr int NT = 384;
+constexpr int BQ = 128, BK = 128;      // rows of a block, keys of a tile
+constexpr int PRODUCER = 8, ISSUER = 9;
+constexpr float kRaise = 8.f;
+
+template <int D>
+struct ChunkSmem {
+  static constexpr int HALVES = D / 64;
+  static constexpr int HALF = BK * 128;              // 64 columns of 128 rows
+  static constexpr int TILE = HALVES * HALF;         // a block of Q, a tile of K or V
+  static constexpr int STAGES = D == 128 ? 5 : 8;
+  static constexpr int BYTES = 2 * TILE + STAGES * TILE + 1024;
+  static constexpr uint32_t O_COL = 256, O_STRIDE = D;
+};
+
+__device__ __forceinline__ void mma_p(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc,
+                                      uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+
+// B operand whose rows are keys: 64 columns of 8 keys a 1024-byte swizzled atom,
+// groups of 8 keys 1024 bytes apart, the next 64 columns `half` bytes on.
+__device__ __forceinline__ uint64_t sdesc_mn_sw128(uint32_t saddr, uint32_t half) {
+  uint64_t d = 0;
+  d |= static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4);
+  d |= static_cast<uint64_t>(half >> 4) << 16;
+  d |= static_cast<uint64_t>(1024 >> 4) << 32;
+  d |= static_cast<uint64_t>(1) << 46;
+  d |= static_cast<uint64_t>(2) << 61;
+  return d;
+}
+
+// 32 columns of the warp's 32 lanes; what was read may be used after ld_wait on it.
+__device__ __forceinline__ void ld32(uint32_t taddr, float* v) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]),
+        "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]),
+        "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]),
+        "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
+      : "r"(taddr));
+}
+__device__ __forceinline__ void pin32(float* v) {
+  asm volatile("" : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]),
+                    "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]),
+                    "+f"(v[15]), "+f"(v[16]), "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]),
+                    "+f"(v[22]), "+f"(v[23]), "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]),
+                    "+f"(v[29]), "+f"(v[30]), "+f"(v[31]));
+}
+__device__ __forceinline__ void st32(uint32_t taddr, const uint32_t* v) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(taddr),
+      "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
+      "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]),
+      "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]),
+      "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31])
+      : "memory");
+}
+__device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+__device__ __forceinline__ bool not_finite2(uint32_t w) {
+  return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
+}
+__device__ __forceinline__ uint32_t finite2(uint32_t w) {
+  if ((w & 0x7f80u) == 0x7f80u) w &= 0xffff0000u;
+  if ((w & 0x7f800000u) == 0x7f800000u) w &= 0xffffu;
+  return w;
+}
+
+// A role's walk over the CTA's runs of keys.
+struct Run {
+  AttendUnit U;
+  int64_t before;
+  int unit, s0, s1;      // key tiles [s0, s1) of the unit
+  bool two;              // the second block has rows
+};
+
+__device__ __forceinline__ bool next_run(const AttendJob& A, const AttendPlan& P, const AttendSpan& sp, int64_t& at,
+                                         int& u, int64_t& before, Run& R) {
+  while (at < sp.end) {
+    R.U = attend_unit(A, P, u);
+    const int64_t last = before + R.U.pieces;
+    if (last > at) {
+      const int64_t stop = min(sp.end, last);
+      R.before = before;
+      R.unit = u;
+      R.s0 = (int)(at - before);
+      R.s1 = (int)(stop - before);
+      R.two = R.U.rows > BQ;
+      at = stop;
+      if (stop == last) {
+        before = last;
+        ++u;
+      }
+      return true;
+    }
+    before = last;
+    ++u;
+  }
+  return false;
+}
+
+// The part of a row's sums that comes from values that are not finite, of columns
+// [d0, d0 + 32): added with the row's weights, key by key. Rare, so slow.
+template <int D>
+static __device__ __noinline__ void add_not_finite(const AttendJob& A, const Run& R, int row, int lim, float m, int d0,
+                                                   float* o) {
+  const CacheJob& J = A.c;
+  const size_t seq = (size_t)R.U.b * J.Hkv + R.U.h;
+  const int tok = row / J.r, j = row - tok * J.r;
+  const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(A.q) +
+                           (size_t)(J.off[R.U.b] + tok) * J.stride + (size_t)(R.U.h * J.r + j) * D;
+  const int first = keys_of(A.causal, R.U.len, R.U.n, R.U.row0 / J.r);
+  for (int t = max(R.s0 * BK, first / BK * BK); t < min(R.s1 * BK, lim); ++t) {
+    const int64_t slot = cache_slot(J, seq, t);
+    if (slot < 0) continue;
+    const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(J.vp) + (size_t)slot * D + d0;
+    bool any = false;
+    for (int i = 0; i < 32; ++i) any |= !isfinite(to_f32(v[i]));
+    if (!any) continue;
+    const __nv_bfloat16* k = reinterpret_cast<const __nv_bfloat16*>(J.kp) + (size_t)slot * D;
+    float s = 0.f;
+    for (int i = 0; i < D; ++i) s = fmaf(to_f32(q[i]), to_f32(k[i]), s);
+    const float p = fast_exp2(fmaf(s, A.alpha, -m));
+    for (int i = 0; i < 32; ++i) {
+      const float x = to_f32(v[i]);
+      if (!isfinite(x)) o[i] += p * x;
+    }
+  }
+}
+
+template <int D>
+__global__ void __launch_bounds__(NT, 1) attend_chunk_kernel(const __grid_constant__ CUtensorMap kmap,
+                                                             const __grid_constant__ CUtensorMap vmap,
+                                                             const __grid_constant__ AttendJob A,
+                                                             const __grid_constant__ AttendPlan P) {
+  using SM = ChunkSmem<D>;
+  extern __shared__ unsigned char smraw[];
+  unsigned char* sm =
+      reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smraw) + 1023) & ~uintptr_t(1023));
+  unsigned char* ring = sm + 2 * SM::TILE;
+  __shared__ uint64_t full[SM::STAGES], empty[SM::STAGES], q_ready[2], s_ready[2], p_ready[2], o_ready[2], o_free[2];
+  __shared__ uint64_t drain;
+  __shared__ uint32_t tbase;
+  __shared__ int abort_flag, odd_flag;
+  __shared__ AttendScan<NT> scan;
+  volatile int* abort_ = &abort_flag;
+  const CacheJob& J = A.c;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+
+  if (threadIdx.x == 0) {
+    abort_flag = odd_flag = 0;
+    for (int s = 0; s < SM::STAGES; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&q_ready[i], 4);     // a warpgroup's warps
+      mbar_init(&s_ready[i], 1);
+      mbar_init(&p_ready[i], 4);
+      mbar_init(&o_ready[i], 1);
+      mbar_init(&o_free[i], 4);
+    }
+    mbar_init(&drain, 1);
+    fence_barrier_init();
+    prefetch_tmap(&kmap);
+    prefetch_tmap(&vmap);
+  }
+  if (warp == ISSUER) {
+    tmem_alloc(&tbase, 512);
+    tmem_relinquish();
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = tbase;
+  dependent_start();
+  const AttendSpan sp = attend_span<NT>(A, P, &scan, [] { __syncthreads(); });
+  int64_t at = sp.begin, before = sp.before;
+  int u = sp.unit;
+  Run R;
+
+  if (warp == PRODUCER) {
+    int stage = 0;
+    uint32_t phase = 0;
+    ArmedStages armed;
+    bool ok = true;
+    const int shift = min(J.page_shift, 7), boxes = BK >> shift;
+    const int outside = J.n_pages << J.page_shift;     // a box from there on reads zeros
+    while (ok && next_run(A, P, sp, at, u, before, R)) {
+      const int32_t* table = J.table + ((size_t)R.U.b * J.Hkv + R.U.h) * J.max_pages;
+      // this lane's box of a tile: its row of the pool
+      auto row_of = [&](int s) {
+        const int t = s * BK + (lane << shift);
+        if (lane >= boxes || s >= R.s1 || t >= R.U.keys) return outside;
+        const int row = page_row(table[t >> J.page_shift], J.n_pages, J.page_shift, t);
+        return row < 0 ? outside : row;
+      };
+      int next = row_of(R.s0);
+      for (int s = R.s0; ok && s < R.s1; ++s) {
+        const int row = next;
+        next = row_of(s + 1);                          // read a tile ahead
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv) {
+          if (!mbar_wait_warp(&empty[stage], phase ^ 1u, abort_)) { ok = false; break; }
+          if (lane == 0) mbar_expect_tx(&full[stage], SM::TILE);
+          armed.arm(stage, phase);
+          __syncwarp();
+          if (lane < boxes)
+#pragma unroll
+            for (int c = 0; c < SM::HALVES; ++c)
+              tma_load_3d(ring + stage * SM::TILE + c * SM::HALF + (lane << shift) * 128, kv ? &vmap : &kmap,
+                          &full[stage], c * 64, row, 0);
+          if (++stage == SM::STAGES) { stage = 0; phase ^= 1u; }
+        }
+      }
+    }
+    if (!armed.drain(full)) *abort_ = 1;
+  } else if (warp == ISSUER) {
+    const uint32_t id_s = idesc_bf16_f32(BQ, BK), id_o = idesc_bf16_f32(BQ, D) | (1u << 16);   // V: MN-major
+    const uint64_t qd = sdesc_k_sw128(smem_u32(sm)), kd = sdesc_k_sw128(smem_u32(ring));
+    const uint64_t vd = sdesc_mn_sw128(smem_u32(ring), SM::HALF);
+    int stage = 0;
+    uint32_t phase = 0, qp = 0, pp = 0, of = 0;        // bit i: phase of block i's barrier
+    bool ok = true, issued = false;
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      if (ok && !mbar_wait_warp(bar, parity & 1u, abort_)) ok = false;
+      return ok;
+    };
+    auto step = [&] {
+      if (++stage == SM::STAGES) { stage = 0; phase ^= 1u; }
+    };
+    // S of block x with the K tile of a stage
+    auto issue_s = [&](int x, int st) {
+      if (elect_one()) {
+        const uint64_t k = kd + (uint64_t)(st * (SM::TILE >> 4)), q = qd + (uint64_t)(x * (SM::TILE >> 4));
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) {
+          const uint64_t o = (uint64_t)(((ks / 4) * SM::HALF + (ks % 4) * 32) >> 4);
+          mma_bf16(tmem + x * BK, q + o, k + o, id_s, ks > 0 ? 1u : 0u);
+        }
+        mma_commit(&s_ready[x]);
+      }
+      __syncwarp();
+    };
+    auto issue_o = [&](int x, int st, bool add) {
+      if (elect_one()) {
+        const uint64_t v = vd + (uint64_t)(st * (SM::TILE >> 4));
+#pragma unroll
+        for (int ks = 0; ks < BK / 16; ++ks)
+          mma_p(tmem + SM::O_COL + x * SM::O_STRIDE, tmem + x * BK + ks * 8, v + (uint64_t)((ks * 2048) >> 4), id_o,
+                add || ks > 0 ? 1u : 0u);
+      }
+      __syncwarp();
+    };
+    auto commit = [&](uint64_t* bar) {
+      if (elect_one()) mma_commit(bar);
+      __syncwarp();
+    };
+    while (ok && next_run(A, P, sp, at, u, before, R)) {
+      const int nx = R.two ? 2 : 1;
+      if (!wait(&full[stage], phase)) break;
+      for (int x = 0; x < nx; ++x) {
+        if (!wait(&q_ready[x], qp >> x)) break;
+        qp ^= 1u << x;
+        fence_after();
+        issue_s(x, stage);
+        issued = true;
+      }
+      if (!ok) break;
+      commit(&empty[stage]);
+      step();
+      for (int s = R.s0; ok && s < R.s1; ++s) {
+        const int vst = stage;
+        if (!wait(&full[vst], phase)) break;
+        step();
+        const bool more = s + 1 < R.s1;
+        for (int x = 0; x < nx; ++x) {
+          if (s == R.s0) {                             // the last run's O has been read
+            if (!wait(&o_free[x], (of >> x) ^ 1u)) break;
+            of ^= 1u << x;
+          }
+          if (!wait(&p_ready[x], pp >> x)) break;
+          pp ^= 1u << x;
+          fence_after();
+          issue_o(x, vst, s > R.s0);
+          if (x == nx - 1) commit(&empty[vst]);
+          if (more) {
+            if (x == 0 && !wait(&full[stage], phase)) break;
+            issue_s(x, stage);
+          } else {
+            commit(&o_ready[x]);
+          }
+        }
+        if (!ok) break;
+        if (more) {
+          commit(&empty[stage]);
+          step();
+        }
+      }
+    }
+    if (issued) {
+      commit(&drain);
+      if (!mbar_wait_drain(&drain, 0)) *abort_ = 1;
+    }
+  } else if (warp < 8) {
+    const int x = warp / 4, lrow = threadIdx.x % 128;   // block, its row
+    const uint32_t lanes = (uint32_t)((warp % 4) * 32) << 16;
+    const uint32_t scol = tmem + lanes + x * BK, ocol = tmem + lanes + SM::O_COL + x * SM::O_STRIDE;
+    uint32_t sph = 0, oph = 0, vphase = 0;
+    int vstage = 0;                                      // ring stage of the next tile's K
+    bool ok = true;
+    while (ok && next_run(A, P, sp, at, u, before, R)) {
+      const AttendUnit& U = R.U;
+      const int ntiles = R.s1 - R.s0;
+      if (x == 1 && !R.two) {
+        vstage += 2 * ntiles;
+        vphase ^= (vstage / SM::STAGES) & 1;
+        vstage %= SM::STAGES;
+        continue;
+      }
+      const int brow = x * BQ + lrow, row = U.row0 + brow;
+      const bool live = brow < U.rows;
+      const int tok = row / J.r, j = row - tok * J.r;
+      {
+        const uint8_t* q = A.q + ((size_t)(J.off[U.b] + (live ? tok : 0)) * J.stride + (size_t)(U.h * J.r + j) * D) * 2;
+        unsigned char* dst = sm + x * SM::TILE + lrow * 128;
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) {
+          const uint4 w = live ? load_plain16(q + i * 16, A.qvec) : make_uint4(0, 0, 0, 0);
+          *reinterpret_cast<uint4*>(dst + (i / 8) * SM::HALF + ((i % 8) ^ (lrow % 8)) * 16) = w;
+        }
+        fence_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&q_ready[x]);
+      }
+      const int32_t* table = J.table + ((size_t)U.b * J.Hkv + U.h) * J.max_pages;
+      const int lim = live ? keys_of(A.causal, U.len, U.n, tok) : 0;
+      const int least = keys_of(A.causal, U.len, U.n, U.row0 / J.r);   // keys that every row attends to
+      // bit i: the tile's 16-key block i has no page
+      auto gone_of = [&](int s) {
+        const int t = s * BK + lane * 16;
+        const bool g = lane < 8 && s < R.s1 && t < U.keys &&
+                       page_row(table[t >> J.page_shift], J.n_pages, J.page_shift, t) < 0;
+        return __ballot_sync(0xffffffffu, g);
+      };
+      uint32_t next = gone_of(R.s0);
+      float m = -INFINITY, l = 0.f;
+      for (int s = R.s0; s < R.s1; ++s) {
+        const uint32_t gone = next;
+        next = gone_of(s + 1);
+        const int k0 = s * BK;
+        const bool special = k0 + BK > least;
+        if (!mbar_wait_warp(&s_ready[x], sph, abort_)) { ok = false; break; }
+        sph ^= 1u;
+        fence_after();
+        float v[BK];
+#pragma unroll
+        for (int i = 0; i < BK; i += 32) ld32(scol + i, v + i);
+        tmem_wait_ld();
+#pragma unroll
+        for (int i = 0; i < BK; i += 32) pin32(v + i);
+        if (special || gone) {
+          if (gone && x == 0 && warp == 0 && lane == 0) set_status(J.status, kStatusBadPage);
+#pragma unroll
+          for (int i = 0; i < BK; ++i)
+            if (k0 + i >= lim || ((gone >> (i / 16)) & 1u)) v[i] = -INFINITY;
+        }
+        float t4[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+        for (int i = 4; i < BK; i += 8)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) t4[c] = i + 4 + c < BK ? fmaxf(t4[c], fmaxf(v[i + c], v[i + 4 + c])) : fmaxf(t4[c], v[i + c]);
+        const float top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])) * A.alpha;
+        if (__any_sync(0xffffffffu, top > m + kRaise)) {
+          const float mn = fmaxf(m, top);
+          const float f = m == -INFINITY ? 0.f : fast_exp2(m - mn);
+          m = mn;
+          l *= f;
+          if (s > R.s0) {
+#pragma unroll 1
+            for (int i = 0; i < D; i += 32) {
+              float o[32];
+              ld32(ocol + i, o);
+              tmem_wait_ld();
+              pin32(o);
+              uint32_t w[32];
+#pragma unroll
+              for (int c = 0; c < 32; ++c) w[c] = __float_as_uint(o[c] * f);
+              st32(ocol + i, w);
+            }
+          }
+        }
+        const float mu = m == -INFINITY ? 0.f : m;
+        const uint64_t al2 = pk2(A.alpha, A.alpha), mu2 = pk2(-mu, -mu);
+        uint64_t sum2[2] = {pk2(0.f, 0.f), pk2(0.f, 0.f)};
+#pragma unroll
+        for (int i = 0; i < BK; i += 64) {
+          uint32_t w[32];
+#pragma unroll
+          for (int c = 0; c < 32; ++c) {
+            float a, b;
+            upk2(ffma2(pk2(v[i + 2 * c], v[i + 2 * c + 1]), al2, mu2), a, b);
+            a = fast_exp2(a);
+            b = fast_exp2(b);
+            sum2[c % 2] = fadd2(sum2[c % 2], pk2(a, b));
+            w[c] = pack_bf16(a, b);
+          }
+          st32(scol + i / 2, w);
+        }
+        float a, b;
+        upk2(fadd2(sum2[0], sum2[1]), a, b);
+        l += a + b;
+        // the tile's V, two stages on from its K
+        int vs = vstage + 1;
+        uint32_t vp = vphase;
+        if (vs == SM::STAGES) { vs = 0; vp ^= 1u; }
+        if (special && x == 0) {
+          // the first block's threads clean V: both blocks' products with it are
+          // issued after this block's P has been reported ready
+          if (!mbar_wait_warp(&full[vs], vp, abort_)) { ok = false; break; }
+          unsigned char* vt = ring + vs * SM::TILE;
+          bool odd = false;
+          for (int i = threadIdx.x; i < BK * SM::HALVES * 8; i += 128) {
+            const int key = i / (SM::HALVES * 8), ch = i % (SM::HALVES * 8);
+            if (k0 + key < least) continue;
+            uint4* p = reinterpret_cast<uint4*>(vt + (ch / 8) * SM::HALF + key * 128 + (ch % 8) * 16);
+            if (k0 + key >= U.keys) {
+              *p = make_uint4(0, 0, 0, 0);
+              continue;
+            }
+            const uint4 w = *p;
+            if (not_finite2(w.x) || not_finite2(w.y) || not_finite2(w.z) || not_finite2(w.w)) {
+              odd = true;
+              *p = make_uint4(finite2(w.x), finite2(w.y), finite2(w.z), finite2(w.w));
+            }
+          }
+          if (odd) *reinterpret_cast<volatile int*>(&odd_flag) = 1;
+          fence_async();
+        }
+        vstage = vs + 1;
+        vphase = vp;
+        if (vstage == SM::STAGES) { vstage = 0; vphase ^= 1u; }
+        wait_st();
+        fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&p_ready[x]);
+      }
+      if (!ok || !mbar_wait_warp(&o_ready[x], oph, abort_)) { ok = false; break; }
+      oph ^= 1u;
+      fence_after();
+      const bool fix = *reinterpret_cast<volatile int*>(&odd_flag) != 0;
+      const bool whole = R.s0 == 0 && R.s1 == U.pieces;
+      const float f = l == 0.f ? 0.f : 1.f / l;
+      const size_t orow = (size_t)(J.off[U.b] + tok) * J.Hq + U.h * J.r + j;
+      const size_t slot = (size_t)attend_slot(blockIdx.x, sp.begin, R.before) * P.rows + brow;
+#pragma unroll 1
+      for (int i = 0; i < D; i += 32) {
+        float o[32];
+        ld32(ocol + i, o);
+        tmem_wait_ld();
+        pin32(o);
+        if (!live) continue;
+        if (fix) {
+          float t[32];
+#pragma unroll
+          for (int c = 0; c < 32; ++c) t[c] = o[c];
+          add_not_finite<D>(A, R, row, lim, m == -INFINITY ? 0.f : m, i, t);
+#pragma unroll
+          for (int c = 0; c < 32; ++c) o[c] = t[c];
+        }
+        if (whole) {
+          __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(A.out) + orow * D + i;
+          uint32_t w[16];
+#pragma unroll
+          for (int c = 0; c < 16; ++c) w[c] = l == 0.f ? 0u : pack_bf16(o[2 * c] * f, o[2 * c + 1] * f);
+          if (A.ovec) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+              reinterpret_cast<uint4*>(out)[c] = make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
+          } else {
+#pragma unroll
+            for (int c = 0; c < 16; ++c) {
+              reinterpret_cast<uint16_t*>(out)[2 * c] = (uint16_t)w[c];
+              reinterpret_cast<uint16_t*>(out)[2 * c + 1] = (uint16_t)(w[c] >> 16);
+            }
+          }
+        } else {
+          float4* p = reinterpret_cast<float4*>(P.po + slot * D + i);
+#pragma unroll
+          for (int c = 0; c < 8; ++c) p[c] = make_float4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
+        }
+      }
+      if (live) {
+        if (!whole) P.pml[slot] = make_float2(m, l);
+        else if (A.lse) A.lse[orow] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+      }
+      fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&o_free[x]);
+    }
+  }
+
+  fence_before();
+  __syncthreads();
+  if (warp == ISSUER) tmem_dealloc(tmem, 512);
+  if (threadIdx.x == 0 && abort_flag) set_status(J.status, kStatusTimeout);
+}
+
+template <int D>
+cudaError_t launch(const AttendJob& A, const AttendPlan& P, cudaStream_t st) {
+  const CacheJob& J = A.c;
+  CUtensorMap kmap, vmap;
+  const uint64_t rows = (uint64_t)J.n_pages << J.page_shift;
+  const uint32_t box = std::min(1 << J.page_shift, BK);
+  if (!make_tmap_bf16_3d(&kmap, J.kp, D, rows, 1, D * 2, rows * D * 2, box) ||
+      !make_tmap_bf16_3d(&vmap, J.vp, D, rows, 1, D * 2, rows * D * 2, box))
+    return cudaErrorInvalidValue;
+  const cudaError_t e = cudaFuncSetAttribute(attend_chunk_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                             ChunkSmem<D>::BYTES);
+  if (e != cudaSuccess) return e;
+  return launch_kernel(attend_chunk_kernel<D>, dim3(P.workers), NT, ChunkSmem<D>::BYTES, st, true, 0, kmap, vmap, A, P);
+}
+
+}  // namespace
+
+cudaError_t launch_attend_chunk(const AttendJob& A, const AttendPlan& P, cudaStream_t st) {
+  return A.c.d == 128 ? launch<128>(A, P, st) : launch<64>(A, P, st);
+}
+
+}  // namespace mmshift
