@@ -230,7 +230,7 @@ cudaError_t launch_attend(const AttendJob& A, void* scratch, cudaStream_t st) {
   AttendPlan t = token_plan(J), c = chunk_plan(J);
   place(t, J, nsm * (t.rows <= 8 ? 4 : 3), at);
   place(c, J, nsm, at);
-  if (J.bf16 && !J.i8) {
+  if (J.bf16) {
     cudaError_t e = cudaSuccess;
     if (c.uoff[J.B]) {
       e = launch_attend_chunk(A, c, st);
@@ -242,19 +242,10 @@ cudaError_t launch_attend(const AttendJob& A, void* scratch, cudaStream_t st) {
     }
     return e;
   }
-  if (J.bf16 && !c.uoff[J.B]) {
-    const cudaError_t e = launch_attend_token(A, t, st);
-    return e == cudaSuccess ? launch_merge(A, t, st) : e;
-  }
   const long long rows = (long long)J.off[J.B] * J.Hq;
   auto go = [&](auto kernel) {
     return launch_kernel(kernel, dim3((unsigned)((rows + 3) / 4)), 128, 0, st, true, 0, A);
   };
-  if (J.bf16) {
-    if (J.d == 128)
-      return J.i8 ? go(attend_row_kernel<__nv_bfloat16, 128, true>) : go(attend_row_kernel<__nv_bfloat16, 128, false>);
-    return J.i8 ? go(attend_row_kernel<__nv_bfloat16, 64, true>) : go(attend_row_kernel<__nv_bfloat16, 64, false>);
-  }
   if (J.d == 128)
     return J.i8 ? go(attend_row_kernel<float, 128, true>) : go(attend_row_kernel<float, 128, false>);
   return J.i8 ? go(attend_row_kernel<float, 64, true>) : go(attend_row_kernel<float, 64, false>);

@@ -28,6 +28,7 @@
 #include <cudaTypedefs.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "attend.cuh"
 #include "umma.cuh"
@@ -37,18 +38,24 @@ namespace {
 
 using namespace umma;
 
-constexpr int NT = 384;
 constexpr int BQ = 128, BK = 128;      // rows of a block, keys of a tile
-constexpr int PRODUCER = 8, ISSUER = 9;
+constexpr int PRODUCER = 8, ISSUER = 9, CONVERT = 12;   // first warps of the roles
 constexpr float kRaise = 8.f;
 
-template <int D>
+template <int D, bool I8>
 struct ChunkSmem {
+  static constexpr int NT = I8 ? 512 : 384;
   static constexpr int HALVES = D / 64;
   static constexpr int HALF = BK * 128;              // 64 columns of 128 rows
   static constexpr int TILE = HALVES * HALF;         // a block of Q, a tile of K or V
-  static constexpr int STAGES = D == 128 ? 5 : 8;
-  static constexpr int BYTES = 2 * TILE + STAGES * TILE + 1024;
+  static constexpr int STAGES = D == 64 ? 8 : I8 ? 3 : 5;
+  static constexpr int RAW = BK * D;                 // a tile of codes
+  // Tiles whose scales are kept: those of tile j + SCALES are written when its K has a
+  // stage, which is after the V of tile j was freed, and so read by all.
+  static constexpr int SCALES = 8;
+  static_assert(2 * SCALES - STAGES >= 1, "scales would be overwritten while they are read");
+  static constexpr int RAWS = I8 ? (D == 64 ? 6 : 3) : 0;
+  static constexpr int BYTES = (2 + STAGES) * TILE + RAWS * RAW + 1024;
   static constexpr uint32_t O_COL = 256, O_STRIDE = D;
 };
 
@@ -93,15 +100,12 @@ __device__ __forceinline__ void pin32(float* v) {
                     "+f"(v[22]), "+f"(v[23]), "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]),
                     "+f"(v[29]), "+f"(v[30]), "+f"(v[31]));
 }
-__device__ __forceinline__ void st32(uint32_t taddr, const uint32_t* v) {
+__device__ __forceinline__ void st16(uint32_t taddr, const uint32_t* v) {
   asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(taddr),
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
       "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
-      "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]),
-      "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]),
-      "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31])
+      "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
       : "memory");
 }
 __device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -110,10 +114,33 @@ __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.
 __device__ __forceinline__ bool not_finite2(uint32_t w) {
   return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
 }
+// Two codes, in the low bytes of t's halves, as bfloat16.
+__device__ __forceinline__ uint32_t codes_bf16(uint32_t t) {
+  const uint32_t a = (t & 0x007f007fu) | 0x43004300u, c = (t & 0x00800080u) | 0x43004300u;
+  uint32_t x;
+  asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(x) : "r"(a), "r"(c));
+  return x;
+}
+__device__ __forceinline__ uint64_t fmul2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
 __device__ __forceinline__ uint32_t finite2(uint32_t w) {
   if ((w & 0x7f80u) == 0x7f80u) w &= 0xffff0000u;
   if ((w & 0x7f800000u) == 0x7f800000u) w &= 0xffffu;
   return w;
+}
+
+// The largest of N values (a NaN is passed over), N a multiple of 8.
+template <int N>
+__device__ __forceinline__ float max_of(const float* v) {
+  float t[4] = {fmaxf(v[0], v[4]), fmaxf(v[1], v[5]), fmaxf(v[2], v[6]), fmaxf(v[3], v[7])};
+#pragma unroll
+  for (int i = 8; i < N; i += 8)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) t[c] = fmaxf(t[c], fmaxf(v[i + c], v[i + 4 + c]));
+  return fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
 }
 
 // A role's walk over the CTA's runs of keys.
@@ -178,16 +205,20 @@ static __device__ __noinline__ void add_not_finite(const AttendJob& A, const Run
   }
 }
 
-template <int D>
-__global__ void __launch_bounds__(NT, 1) attend_chunk_kernel(const __grid_constant__ CUtensorMap kmap,
+template <int D, bool I8>
+__global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(const __grid_constant__ CUtensorMap kmap,
                                                              const __grid_constant__ CUtensorMap vmap,
                                                              const __grid_constant__ AttendJob A,
                                                              const __grid_constant__ AttendPlan P) {
-  using SM = ChunkSmem<D>;
+  using SM = ChunkSmem<D, I8>;
+  constexpr int NT = SM::NT;
   extern __shared__ unsigned char smraw[];
   unsigned char* sm =
       reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smraw) + 1023) & ~uintptr_t(1023));
   unsigned char* ring = sm + 2 * SM::TILE;
+  unsigned char* raw = ring + SM::STAGES * SM::TILE;
+  __shared__ uint64_t rfull[I8 ? SM::RAWS : 1], rempty[I8 ? SM::RAWS : 1];
+  __shared__ alignas(16) float scales[I8 ? SM::SCALES : 1][2][I8 ? BK : 1];   // K's (times alpha) and V's
   __shared__ uint64_t full[SM::STAGES], empty[SM::STAGES], q_ready[2], s_ready[2], p_ready[2], o_ready[2], o_free[2];
   __shared__ uint64_t drain;
   __shared__ uint32_t tbase;
@@ -200,8 +231,12 @@ __global__ void __launch_bounds__(NT, 1) attend_chunk_kernel(const __grid_consta
   if (threadIdx.x == 0) {
     abort_flag = odd_flag = 0;
     for (int s = 0; s < SM::STAGES; ++s) {
-      mbar_init(&full[s], 1);
+      mbar_init(&full[s], I8 ? 4 : 1);
       mbar_init(&empty[s], 1);
+    }
+    for (int s = 0; s < SM::RAWS; ++s) {
+      mbar_init(&rfull[s], 1);
+      mbar_init(&rempty[s], 4);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&q_ready[i], 4);     // a warpgroup's warps
@@ -228,8 +263,10 @@ __global__ void __launch_bounds__(NT, 1) attend_chunk_kernel(const __grid_consta
   int64_t at = sp.begin, before = sp.before;
   int u = sp.unit;
   Run R;
-
   if (warp == PRODUCER) {
+    // bfloat16 rows go where the MMAs read them, codes to a ring of their own
+    constexpr int NS = I8 ? SM::RAWS : SM::STAGES, BYTES = I8 ? SM::RAW : SM::TILE;
+    uint64_t *const got = I8 ? rfull : full, *const room = I8 ? rempty : empty;
     int stage = 0;
     uint32_t phase = 0;
     ArmedStages armed;
@@ -251,20 +288,25 @@ __global__ void __launch_bounds__(NT, 1) attend_chunk_kernel(const __grid_consta
         next = row_of(s + 1);                          // read a tile ahead
 #pragma unroll
         for (int kv = 0; kv < 2; ++kv) {
-          if (!mbar_wait_warp(&empty[stage], phase ^ 1u, abort_)) { ok = false; break; }
-          if (lane == 0) mbar_expect_tx(&full[stage], SM::TILE);
+          if (!mbar_wait_warp(&room[stage], phase ^ 1u, abort_)) { ok = false; break; }
+          if (lane == 0) mbar_expect_tx(&got[stage], BYTES);
           armed.arm(stage, phase);
           __syncwarp();
-          if (lane < boxes)
+          if (lane < boxes) {
+            if constexpr (I8) {
+              tma_load_3d(raw + stage * SM::RAW + (lane << shift) * D, kv ? &vmap : &kmap, &got[stage], 0, row, 0);
+            } else {
 #pragma unroll
-            for (int c = 0; c < SM::HALVES; ++c)
-              tma_load_3d(ring + stage * SM::TILE + c * SM::HALF + (lane << shift) * 128, kv ? &vmap : &kmap,
-                          &full[stage], c * 64, row, 0);
-          if (++stage == SM::STAGES) { stage = 0; phase ^= 1u; }
+              for (int c = 0; c < SM::HALVES; ++c)
+                tma_load_3d(ring + stage * SM::TILE + c * SM::HALF + (lane << shift) * 128, kv ? &vmap : &kmap,
+                            &got[stage], c * 64, row, 0);
+            }
+          }
+          if (++stage == NS) { stage = 0; phase ^= 1u; }
         }
       }
     }
-    if (!armed.drain(full)) *abort_ = 1;
+    if (!armed.drain(got)) *abort_ = 1;
   } else if (warp == ISSUER) {
     const uint32_t id_s = idesc_bf16_f32(BQ, BK), id_o = idesc_bf16_f32(BQ, D) | (1u << 16);   // V: MN-major
     const uint64_t qd = sdesc_k_sw128(smem_u32(sm)), kd = sdesc_k_sw128(smem_u32(ring));
@@ -352,12 +394,69 @@ __global__ void __launch_bounds__(NT, 1) attend_chunk_kernel(const __grid_consta
       commit(&drain);
       if (!mbar_wait_drain(&drain, 0)) *abort_ = 1;
     }
+  } else if (warp >= CONVERT) {
+    if constexpr (I8) {
+      // Codes to bfloat16, exactly: u = x & 127, x = (128 + u) - (128 or, below zero,
+      // 256), eight at a time into the swizzled tile. Thread t has key t's scales.
+      const int t = threadIdx.x - CONVERT * 32;
+      int stage = 0, rs = 0, tile = 0;
+      uint32_t phase = 0, rp = 0;
+      bool ok = true;
+      while (ok && next_run(A, P, sp, at, u, before, R)) {
+        const int32_t* table = J.table + ((size_t)R.U.b * J.Hkv + R.U.h) * J.max_pages;
+        auto row_of = [&](int s) {
+          const int k = s * BK + t;
+          return s < R.s1 && k < R.U.keys ? page_row(table[k >> J.page_shift], J.n_pages, J.page_shift, k) : -1;
+        };
+        auto scale_of = [&](int row) {
+          return row < 0 ? make_float2(0.f, 0.f) : make_float2(J.ks[row] * A.alpha, J.vs[row]);
+        };
+        float2 sc = scale_of(row_of(R.s0));
+        int next = row_of(R.s0 + 1);
+        for (int s = R.s0; ok && s < R.s1; ++s) {
+  #pragma unroll 1
+          for (int kv = 0; kv < 2; ++kv) {
+            if (!mbar_wait_warp(&empty[stage], phase ^ 1u, abort_) || !mbar_wait_warp(&rfull[rs], rp, abort_)) {
+              ok = false;
+              break;
+            }
+            if (kv == 0) {
+              // four tiles on, no block still reads these: K of this tile takes the place
+              // of a V two or more tiles back
+              scales[tile % SM::SCALES][0][t] = sc.x;
+              scales[tile % SM::SCALES][1][t] = sc.y;
+              sc = scale_of(next);                       // read a tile ahead
+              next = row_of(s + 2);
+            }
+            const unsigned char* src = raw + rs * SM::RAW;
+            unsigned char* dst = ring + stage * SM::TILE;
+  #pragma unroll 8
+            for (int i = t; i < BK * D / 8; i += 128) {
+              const int key = i / (D / 8), ch = i % (D / 8);
+              const uint2 w = *reinterpret_cast<const uint2*>(src + i * 8);
+              *reinterpret_cast<uint4*>(dst + (ch / 8) * SM::HALF + key * 128 + ((ch % 8) ^ (key % 8)) * 16) =
+                  make_uint4(codes_bf16(__byte_perm(w.x, 0, 0x1100)), codes_bf16(__byte_perm(w.x, 0, 0x3322)),
+                             codes_bf16(__byte_perm(w.y, 0, 0x1100)), codes_bf16(__byte_perm(w.y, 0, 0x3322)));
+            }
+            fence_async();
+            __syncwarp();
+            if (lane == 0) {
+              mbar_arrive(&rempty[rs]);
+              mbar_arrive(&full[stage]);
+            }
+            if (++stage == SM::STAGES) { stage = 0; phase ^= 1u; }
+            if (++rs == SM::RAWS) { rs = 0; rp ^= 1u; }
+          }
+          ++tile;
+        }
+      }
+    }
   } else if (warp < 8) {
     const int x = warp / 4, lrow = threadIdx.x % 128;   // block, its row
     const uint32_t lanes = (uint32_t)((warp % 4) * 32) << 16;
     const uint32_t scol = tmem + lanes + x * BK, ocol = tmem + lanes + SM::O_COL + x * SM::O_STRIDE;
     uint32_t sph = 0, oph = 0, vphase = 0;
-    int vstage = 0;                                      // ring stage of the next tile's K
+    int vstage = 0, tile = 0;                            // ring stage of the next tile's K, tiles so far
     bool ok = true;
     while (ok && next_run(A, P, sp, at, u, before, R)) {
       const AttendUnit& U = R.U;
@@ -366,6 +465,7 @@ __global__ void __launch_bounds__(NT, 1) attend_chunk_kernel(const __grid_consta
         vstage += 2 * ntiles;
         vphase ^= (vstage / SM::STAGES) & 1;
         vstage %= SM::STAGES;
+        tile += ntiles;
         continue;
       }
       const int brow = x * BQ + lrow, row = U.row0 + brow;
@@ -400,71 +500,135 @@ __global__ void __launch_bounds__(NT, 1) attend_chunk_kernel(const __grid_consta
         next = gone_of(s + 1);
         const int k0 = s * BK;
         const bool special = k0 + BK > least;
+        // the tile's V, the stage behind its K; it stays there until P is ready
+        int vs = vstage + 1;
+        uint32_t vp = vphase;
+        if (vs == SM::STAGES) { vs = 0; vp ^= 1u; }
         if (!mbar_wait_warp(&s_ready[x], sph, abort_)) { ok = false; break; }
         sph ^= 1u;
+        // 8-bit pages: the tile's scales were written before its V was
+        if (I8 && !mbar_wait_warp(&full[vs], vp, abort_)) { ok = false; break; }
         fence_after();
-        float v[BK];
-#pragma unroll
-        for (int i = 0; i < BK; i += 32) ld32(scol + i, v + i);
-        tmem_wait_ld();
-#pragma unroll
-        for (int i = 0; i < BK; i += 32) pin32(v + i);
-        if (special || gone) {
-          if (gone && x == 0 && warp == 0 && lane == 0) set_status(J.status, kStatusBadPage);
-#pragma unroll
-          for (int i = 0; i < BK; ++i)
-            if (k0 + i >= lim || ((gone >> (i / 16)) & 1u)) v[i] = -INFINITY;
-        }
-        float t4[4] = {v[0], v[1], v[2], v[3]};
-#pragma unroll
-        for (int i = 4; i < BK; i += 8)
-#pragma unroll
-          for (int c = 0; c < 4; ++c) t4[c] = i + 4 + c < BK ? fmaxf(t4[c], fmaxf(v[i + c], v[i + 4 + c])) : fmaxf(t4[c], v[i + c]);
-        const float top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])) * A.alpha;
-        if (__any_sync(0xffffffffu, top > m + kRaise)) {
+        const bool masked = special || gone;
+        if (gone && warp == 0 && lane == 0) set_status(J.status, kStatusBadPage);
+        auto hidden = [&](int i) { return k0 + i >= lim || ((gone >> (i / 16)) & 1u); };
+        // raises the maximum to `top` (base 2) where some row's passes it by enough
+        auto raise = [&](float top) {
+          if (!__any_sync(0xffffffffu, top > m + kRaise)) return;
           const float mn = fmaxf(m, top);
           const float f = m == -INFINITY ? 0.f : fast_exp2(m - mn);
           m = mn;
           l *= f;
-          if (s > R.s0) {
+          if (s == R.s0) return;
 #pragma unroll 1
-            for (int i = 0; i < D; i += 32) {
-              float o[32];
-              ld32(ocol + i, o);
-              tmem_wait_ld();
-              pin32(o);
-              uint32_t w[32];
+          for (int i = 0; i < D; i += 16) {
+            float o[16];
+            tmem_ld16(ocol + i, o);
+            tmem_wait_ld16(o);
+            uint32_t w[16];
 #pragma unroll
-              for (int c = 0; c < 32; ++c) w[c] = __float_as_uint(o[c] * f);
-              st32(ocol + i, w);
-            }
+            for (int c = 0; c < 16; ++c) w[c] = __float_as_uint(o[c] * f);
+            st16(ocol + i, w);
           }
-        }
-        const float mu = m == -INFINITY ? 0.f : m;
-        const uint64_t al2 = pk2(A.alpha, A.alpha), mu2 = pk2(-mu, -mu);
+        };
         uint64_t sum2[2] = {pk2(0.f, 0.f), pk2(0.f, 0.f)};
+        if constexpr (!I8) {
+          float v[BK];
 #pragma unroll
-        for (int i = 0; i < BK; i += 64) {
-          uint32_t w[32];
+          for (int i = 0; i < BK; i += 32) ld32(scol + i, v + i);
+          tmem_wait_ld();
 #pragma unroll
-          for (int c = 0; c < 32; ++c) {
-            float a, b;
-            upk2(ffma2(pk2(v[i + 2 * c], v[i + 2 * c + 1]), al2, mu2), a, b);
-            a = fast_exp2(a);
-            b = fast_exp2(b);
-            sum2[c % 2] = fadd2(sum2[c % 2], pk2(a, b));
-            w[c] = pack_bf16(a, b);
+          for (int i = 0; i < BK; i += 32) pin32(v + i);
+          if (masked) {
+#pragma unroll
+            for (int i = 0; i < BK; ++i)
+              if (hidden(i)) v[i] = -INFINITY;
           }
-          st32(scol + i / 2, w);
+          raise(max_of<BK>(v) * A.alpha);
+          const float mu = m == -INFINITY ? 0.f : m;
+          const uint64_t al2 = pk2(A.alpha, A.alpha), mu2 = pk2(-mu, -mu);
+#pragma unroll
+          for (int i = 0; i < BK; i += 32) {
+            uint32_t w[16];
+#pragma unroll
+            for (int c = 0; c < 16; ++c) {
+              float a, b;
+              upk2(ffma2(pk2(v[i + 2 * c], v[i + 2 * c + 1]), al2, mu2), a, b);
+              a = fast_exp2(a);
+              b = fast_exp2(b);
+              sum2[c % 2] = fadd2(sum2[c % 2], pk2(a, b));
+              w[c] = pack_bf16(a, b);
+            }
+            st16(scol + i / 2, w);
+          }
+        } else {
+          // 512 threads leave 128 registers: S is read twice, for the maximum and for the
+          // weights. K's scales (times alpha) go with the logits, V's with the weights.
+          const float4* sk = reinterpret_cast<const float4*>(scales[tile % SM::SCALES][0]);
+          const float4* sv = reinterpret_cast<const float4*>(scales[tile % SM::SCALES][1]);
+          float top = -INFINITY;
+#pragma unroll
+          for (int i = 0; i < BK; i += 32) {
+            float v[32];
+            ld32(scol + i, v);
+            tmem_wait_ld();
+            pin32(v);
+#pragma unroll
+            for (int c = 0; c < 32; c += 4) {
+              const float4 f = sk[(i + c) / 4];
+              upk2(fmul2(pk2(v[c], v[c + 1]), pk2(f.x, f.y)), v[c], v[c + 1]);
+              upk2(fmul2(pk2(v[c + 2], v[c + 3]), pk2(f.z, f.w)), v[c + 2], v[c + 3]);
+            }
+            if (masked) {
+#pragma unroll
+              for (int c = 0; c < 32; ++c)
+                if (hidden(i + c)) v[c] = -INFINITY;
+            }
+            top = fmaxf(top, max_of<32>(v));
+          }
+          raise(top);
+          const float mu = m == -INFINITY ? 0.f : m;
+          const uint64_t mu2 = pk2(-mu, -mu);
+#pragma unroll
+          for (int i = 0; i < BK; i += 32) {
+            float v[32];
+            ld32(scol + i, v);
+            tmem_wait_ld();
+            pin32(v);
+            uint32_t w[16];
+#pragma unroll
+            for (int c = 0; c < 32; c += 4) {
+              const float4 f = sk[(i + c) / 4], g = sv[(i + c) / 4];
+              float e[4];
+              upk2(ffma2(pk2(v[c], v[c + 1]), pk2(f.x, f.y), mu2), e[0], e[1]);
+              upk2(ffma2(pk2(v[c + 2], v[c + 3]), pk2(f.z, f.w), mu2), e[2], e[3]);
+#pragma unroll
+              for (int k = 0; k < 4; ++k) e[k] = fast_exp2(e[k]);
+              if (masked) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                  if (hidden(i + c + k)) e[k] = 0.f;
+              }
+              sum2[0] = fadd2(sum2[0], pk2(e[0], e[1]));
+              sum2[1] = fadd2(sum2[1], pk2(e[2], e[3]));
+              upk2(fmul2(pk2(e[0], e[1]), pk2(g.x, g.y)), e[0], e[1]);
+              upk2(fmul2(pk2(e[2], e[3]), pk2(g.z, g.w)), e[2], e[3]);
+              if (masked) {                            // a scale that no row may see can be a NaN
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                  if (hidden(i + c + k)) e[k] = 0.f;
+              }
+              w[c / 2] = pack_bf16(e[0], e[1]);
+              w[c / 2 + 1] = pack_bf16(e[2], e[3]);
+            }
+            st16(scol + i / 2, w);
+          }
         }
+        ++tile;
         float a, b;
         upk2(fadd2(sum2[0], sum2[1]), a, b);
         l += a + b;
-        // the tile's V, two stages on from its K
-        int vs = vstage + 1;
-        uint32_t vp = vphase;
-        if (vs == SM::STAGES) { vs = 0; vp ^= 1u; }
-        if (special && x == 0) {
+        if (!I8 && special && x == 0) {
           // the first block's threads clean V: both blocks' products with it are
           // issued after this block's P has been reported ready
           if (!mbar_wait_warp(&full[vs], vp, abort_)) { ok = false; break; }
@@ -498,7 +662,7 @@ __global__ void __launch_bounds__(NT, 1) attend_chunk_kernel(const __grid_consta
       if (!ok || !mbar_wait_warp(&o_ready[x], oph, abort_)) { ok = false; break; }
       oph ^= 1u;
       fence_after();
-      const bool fix = *reinterpret_cast<volatile int*>(&odd_flag) != 0;
+      const bool fix = !I8 && *reinterpret_cast<volatile int*>(&odd_flag) != 0;
       const bool whole = R.s0 == 0 && R.s1 == U.pieces;
       const float f = l == 0.f ? 0.f : 1.f / l;
       const size_t orow = (size_t)(J.off[U.b] + tok) * J.Hq + U.h * J.r + j;
@@ -556,25 +720,28 @@ __global__ void __launch_bounds__(NT, 1) attend_chunk_kernel(const __grid_consta
   if (threadIdx.x == 0 && abort_flag) set_status(J.status, kStatusTimeout);
 }
 
-template <int D>
+template <int D, bool I8>
 cudaError_t launch(const AttendJob& A, const AttendPlan& P, cudaStream_t st) {
+  using SM = ChunkSmem<D, I8>;
   const CacheJob& J = A.c;
   CUtensorMap kmap, vmap;
   const uint64_t rows = (uint64_t)J.n_pages << J.page_shift;
   const uint32_t box = std::min(1 << J.page_shift, BK);
-  if (!make_tmap_bf16_3d(&kmap, J.kp, D, rows, 1, D * 2, rows * D * 2, box) ||
-      !make_tmap_bf16_3d(&vmap, J.vp, D, rows, 1, D * 2, rows * D * 2, box))
-    return cudaErrorInvalidValue;
-  const cudaError_t e = cudaFuncSetAttribute(attend_chunk_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                             ChunkSmem<D>::BYTES);
+  auto make = [&](CUtensorMap* m, const void* base) {
+    return I8 ? make_tmap_u8_rows(m, base, D, rows, box) : make_tmap_bf16_3d(m, base, D, rows, 1, D * 2, rows * D * 2, box);
+  };
+  if (!make(&kmap, J.kp) || !make(&vmap, J.vp)) return cudaErrorInvalidValue;
+  const cudaError_t e =
+      cudaFuncSetAttribute(attend_chunk_kernel<D, I8>, cudaFuncAttributeMaxDynamicSharedMemorySize, SM::BYTES);
   if (e != cudaSuccess) return e;
-  return launch_kernel(attend_chunk_kernel<D>, dim3(P.workers), NT, ChunkSmem<D>::BYTES, st, true, 0, kmap, vmap, A, P);
+  return launch_kernel(attend_chunk_kernel<D, I8>, dim3(P.workers), SM::NT, SM::BYTES, st, true, 0, kmap, vmap, A, P);
 }
 
 }  // namespace
 
 cudaError_t launch_attend_chunk(const AttendJob& A, const AttendPlan& P, cudaStream_t st) {
-  return A.c.d == 128 ? launch<128>(A, P, st) : launch<64>(A, P, st);
+  if (A.c.i8) return A.c.d == 128 ? launch<128, true>(A, P, st) : launch<64, true>(A, P, st);
+  return A.c.d == 128 ? launch<128, false>(A, P, st) : launch<64, false>(A, P, st);
 }
 
 }  // namespace mmshift
