@@ -20,7 +20,8 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(BUILD, "libmmshift.so")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 SOURCES = ["api.cu", "proxy.cu", "score_simt.cu", "score_umma.cu", "select.cu", "stats.cu",
-           "hidden.cu", "coverage.cu", "noalloc.cu", "cache.cu", "attend.cu", "attend_token.cu", "attend_umma.cu"]
+           "hidden.cu", "coverage.cu", "noalloc.cu", "cache.cu", "attend.cu", "attend_token.cu", "attend_umma.cu",
+           "attend_simt.cu"]
 
 
 def _nvcc() -> str:

@@ -8,53 +8,6 @@
 namespace mmshift {
 namespace {
 
-template <typename T, int D, bool I8>
-__device__ __forceinline__ float row_value(const uint8_t* pages, const float* scales, int64_t slot, int j) {
-  if constexpr (I8) return (float)reinterpret_cast<const int8_t*>(pages)[slot * D + j] * scales[slot];
-  else return to_f32(reinterpret_cast<const T*>(pages)[slot * D + j]);
-}
-
-template <typename T, int D, bool I8>
-__global__ void __launch_bounds__(128) attend_row_kernel(const __grid_constant__ AttendJob A) {
-  dependent_start();
-  const CacheJob& J = A.c;
-  const long long row = (long long)blockIdx.x * 4 + threadIdx.x / 32;
-  const int lane = threadIdx.x % 32;
-  if (row >= (long long)J.off[J.B] * J.Hq) return;
-  const int tok = (int)(row / J.Hq), hq = (int)(row % J.Hq);
-  const int b = cache_request(J, tok);
-  const size_t u = (size_t)b * J.Hkv + hq / J.r;
-  const int end = keys_of(A.causal, cache_len(J, u), J.off[b + 1] - J.off[b], tok - J.off[b]);
-  float q[D / 32], o[D / 32] = {}, m = -INFINITY, z = 0.f;
-#pragma unroll
-  for (int i = 0; i < D / 32; ++i)
-    q[i] = to_f32(reinterpret_cast<const T*>(A.q)[(size_t)tok * J.stride + (size_t)hq * D + lane + 32 * i]);
-  for (int t = 0; t < end; ++t) {
-    const int64_t slot = cache_slot(J, u, t);
-    if (slot < 0) {
-      if (lane == 0) set_status(J.status, kStatusBadPage);
-      continue;
-    }
-    float s = 0.f;
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i) s += q[i] * row_value<T, D, I8>(J.kp, J.ks, slot, lane + 32 * i);
-#pragma unroll
-    for (int x = 16; x; x >>= 1) s += __shfl_xor_sync(0xffffffffu, s, x);
-    s *= A.alpha;
-    if (s == -INFINITY) continue;
-    const float mn = fmaxf(m, s);                    // a NaN stays out of the maximum
-    const float c = m == -INFINITY ? 0.f : fast_exp2(m - mn), p = fast_exp2(s - mn);
-    m = mn;
-    z = z * c + p;
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i) o[i] = o[i] * c + p * row_value<T, D, I8>(J.vp, J.vs, slot, lane + 32 * i);
-  }
-#pragma unroll
-  for (int i = 0; i < D / 32; ++i)
-    reinterpret_cast<T*>(A.out)[(size_t)row * D + lane + 32 * i] = from_f32<T>(z == 0.f ? 0.f : o[i] / z);
-  if (A.lse && lane == 0) A.lse[row] = z == 0.f ? -INFINITY : (m + log2f(z)) * 0.6931471805599453f;
-}
-
 // The partial sums of units that several workers share, and zeros for units
 // without keys. A block takes RPB rows: RPB = 1 with all its warps on the parts of
 // a row (few rows, many parts), else a warp a row.
@@ -152,25 +105,20 @@ cudaError_t launch_merge(const AttendJob& A, const AttendPlan& P, cudaStream_t s
   return A.c.d == 128 ? launch_merge_t<float, 128>(A, P, st) : launch_merge_t<float, 64>(A, P, st);
 }
 
-// Requests whose rows of a KV head are at most this many go to the token kernel.
+// Requests whose rows of a KV head are at most this many have a plan of their own:
+// bfloat16 rows go to the token kernel, float32 rows to tiles of 8 or 16 rows.
 constexpr int kTokenRows = 16;
+
+constexpr int kSMs = 152;              // the workspace is sized without asking the device
 
 int sm_count() {
   int dev = 0, n = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
     return 0;
-  return n;
+  return std::min(n, kSMs);
 }
 
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
-
-// Workers of the plans at most: the workspace is sized without asking the device.
-constexpr int kMostWorkers = 152 * 4, kMostChunkWorkers = 152;
-
-size_t plan_bytes(int units, int rows, int d, int workers) {
-  return align256((size_t)(units + 1) * sizeof(int64_t)) +
-         align256((size_t)2 * workers * rows * d * sizeof(float)) + align256((size_t)2 * workers * rows * sizeof(float2));
-}
 
 // The plan of the requests that `take`s, with tiles of at most `most` rows.
 template <class Take>
@@ -190,65 +138,64 @@ AttendPlan plan_of(const CacheJob& J, int most, Take take) {
   return P;
 }
 
-AttendPlan token_plan(const CacheJob& J) {
-  AttendPlan P = plan_of(J, kTokenRows, [&](int rows) { return J.bf16 && rows <= kTokenRows; });
-  const int row = J.i8 ? J.d : 2 * J.d;
-  while ((row << P.step_shift) < 4096) ++P.step_shift;   // a warp's piece: 4 KB of K
-  P.least = 4;
+// Plans for `nsm` SMs; a CTA a worker, as many as fit.
+AttendPlan token_plan(const CacheJob& J, int nsm) {
+  AttendPlan P = plan_of(J, kTokenRows, [&](int rows) { return rows <= kTokenRows; });
+  if (J.bf16) {
+    const int row = J.i8 ? J.d : 2 * J.d;
+    while ((row << P.step_shift) < 4096) ++P.step_shift;   // a warp's piece: 4 KB of K
+    P.least = 4;
+    P.workers = nsm * (P.rows <= 8 ? 4 : 3);
+  } else {
+    P.step_shift = 5;
+    P.least = 1;
+    P.workers = nsm * (P.rows <= 8 ? 3 : 2);
+  }
   return P;
 }
 
-AttendPlan chunk_plan(const CacheJob& J) {
-  AttendPlan P = plan_of(J, 256, [&](int rows) { return J.bf16 && rows > kTokenRows; });
-  P.step_shift = 7;
+AttendPlan chunk_plan(const CacheJob& J, int nsm) {
+  AttendPlan P = plan_of(J, J.bf16 ? 256 : 64, [&](int rows) { return rows > kTokenRows; });
+  P.step_shift = J.bf16 ? 7 : 5;
   P.least = 1;
+  P.workers = J.bf16 ? nsm : 2 * nsm;
   return P;
 }
 
-void place(AttendPlan& P, const CacheJob& J, int workers, char*& at) {
-  P.workers = workers;
+// The plan's buffers from `at` on; where they end.
+char* place(AttendPlan& P, const CacheJob& J, char* at) {
   P.pre = reinterpret_cast<int64_t*>(at);
   at += align256((size_t)(P.uoff[J.B] + 1) * sizeof(int64_t));
   P.po = reinterpret_cast<float*>(at);
-  at += align256((size_t)2 * workers * P.rows * J.d * sizeof(float));
+  at += align256((size_t)2 * P.workers * P.rows * J.d * sizeof(float));
   P.pml = reinterpret_cast<float2*>(at);
-  at += align256((size_t)2 * workers * P.rows * sizeof(float2));
+  return at + align256((size_t)2 * P.workers * P.rows * sizeof(float2));
 }
 
 }  // namespace
 
 size_t attend_scratch_bytes(const CacheJob& J) {
-  const AttendPlan t = token_plan(J), c = chunk_plan(J);
-  return plan_bytes(t.uoff[J.B], t.rows, J.d, kMostWorkers) + plan_bytes(c.uoff[J.B], c.rows, J.d, kMostChunkWorkers);
+  AttendPlan t = token_plan(J, kSMs), c = chunk_plan(J, kSMs);
+  char* const base = reinterpret_cast<char*>(uintptr_t(256));
+  return place(c, J, place(t, J, base)) - base;
 }
 
 cudaError_t launch_attend(const AttendJob& A, void* scratch, cudaStream_t st) {
   const CacheJob& J = A.c;
-  const int nsm = std::min(sm_count(), kMostChunkWorkers);
+  const int nsm = sm_count();
   if (nsm <= 0) return cudaErrorInvalidDevice;
-  char* at = static_cast<char*>(scratch);
-  AttendPlan t = token_plan(J), c = chunk_plan(J);
-  place(t, J, nsm * (t.rows <= 8 ? 4 : 3), at);
-  place(c, J, nsm, at);
-  if (J.bf16) {
-    cudaError_t e = cudaSuccess;
-    if (c.uoff[J.B]) {
-      e = launch_attend_chunk(A, c, st);
-      if (e == cudaSuccess) e = launch_merge(A, c, st);
-    }
-    if (e == cudaSuccess && t.uoff[J.B]) {
-      e = launch_attend_token(A, t, st);
-      if (e == cudaSuccess) e = launch_merge(A, t, st);
-    }
-    return e;
+  AttendPlan t = token_plan(J, nsm), c = chunk_plan(J, nsm);
+  place(c, J, place(t, J, static_cast<char*>(scratch)));
+  cudaError_t e = cudaSuccess;
+  if (c.uoff[J.B]) {
+    e = J.bf16 ? launch_attend_chunk(A, c, st) : launch_attend_simt(A, c, st);
+    if (e == cudaSuccess) e = launch_merge(A, c, st);
   }
-  const long long rows = (long long)J.off[J.B] * J.Hq;
-  auto go = [&](auto kernel) {
-    return launch_kernel(kernel, dim3((unsigned)((rows + 3) / 4)), 128, 0, st, true, 0, A);
-  };
-  if (J.d == 128)
-    return J.i8 ? go(attend_row_kernel<float, 128, true>) : go(attend_row_kernel<float, 128, false>);
-  return J.i8 ? go(attend_row_kernel<float, 64, true>) : go(attend_row_kernel<float, 64, false>);
+  if (e == cudaSuccess && t.uoff[J.B]) {
+    e = J.bf16 ? launch_attend_token(A, t, st) : launch_attend_simt(A, t, st);
+    if (e == cudaSuccess) e = launch_merge(A, t, st);
+  }
+  return e;
 }
 
 }  // namespace mmshift

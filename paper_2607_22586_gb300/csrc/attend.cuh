@@ -150,6 +150,7 @@ __device__ __forceinline__ void attend_write(const AttendJob& A, int b, int h, i
 }
 
 cudaError_t launch_attend_token(const AttendJob& A, const AttendPlan& P, cudaStream_t st);
+cudaError_t launch_attend_simt(const AttendJob& A, const AttendPlan& P, cudaStream_t st);
 cudaError_t launch_attend_chunk(const AttendJob& A, const AttendPlan& P, cudaStream_t st);
 
 }  // namespace mmshift

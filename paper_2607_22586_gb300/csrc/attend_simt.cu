@@ -1,0 +1,319 @@
+// Attention of float32 rows, over float32 or 8-bit pages: CUDA cores, fp32 FMAs.
+//
+// Tiles of 8 * TR query rows over tiles of 32 keys, 128 threads: thread (ty, tx)
+// has the TR rows of group ty; in S the keys tx and tx + 16, in O the dimensions
+// 4 tx .. of each 64. A row's threads are 16 lanes of one warp, so its weights
+// change hands through shared memory without a barrier of the CTA. K and V tiles
+// arrive through asynchronous copies, one tile ahead (8-bit codes through
+// registers, to be converted). With TR = 8 a thread's 16 and 64 sums make every
+// shared load feed 5 to 8 FMAs, packed in pairs: bound by the FMA rate. Few rows
+// (TR = 1, 2) are bound by the bytes of K and V.
+#include "attend.cuh"
+#include "umma.cuh"
+
+namespace mmshift {
+namespace {
+
+using umma::fadd2;
+using umma::ffma2;
+using umma::lds_2x64;
+using umma::pk2;
+using umma::smem_u32;
+using umma::upk2;
+
+constexpr int NT = 128, BK = 32;
+constexpr float kRaise = 8.f;
+
+template <int D, int TR>
+struct SimtSmem {
+  static constexpr int RT = 8 * TR;
+  static constexpr int QS = D + 4, PS = RT + 4;        // floats between rows: no bank conflicts
+  alignas(16) float q[RT][QS];
+  alignas(16) float k[2][BK][QS];
+  alignas(16) float v[2][BK][D];
+  alignas(16) float p[BK][PS];
+  float ks[2][BK], vs[2][BK];
+  AttendScan<NT> scan;
+};
+
+__device__ __forceinline__ void copy16(void* dst, const void* src, bool in) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(in ? 16 : 0)
+               : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group 0;" ::: "memory"); }
+
+template <int D, bool I8, int TR>
+__global__ void __launch_bounds__(NT, TR >= 4 ? 2 : 3) attend_simt_kernel(const __grid_constant__ AttendJob A,
+                                                                          const __grid_constant__ AttendPlan P) {
+  using SM = SimtSmem<D, TR>;
+  extern __shared__ __align__(16) unsigned char smraw[];
+  SM& sm = *reinterpret_cast<SM*>(smraw);
+  dependent_start();
+  const CacheJob& J = A.c;
+  const int tid = threadIdx.x, lane = tid % 32, tx = tid % 16, ty = tid / 16;
+  const AttendSpan sp = attend_span<NT>(A, P, &sm.scan, [] { __syncthreads(); });
+  int u = sp.unit;
+  int64_t before = sp.before;
+  for (int64_t at = sp.begin; at < sp.end;) {
+    const AttendUnit U = attend_unit(A, P, u);
+    const int64_t last = before + U.pieces;
+    if (last <= at) {
+      before = last;
+      ++u;
+      continue;
+    }
+    const int64_t stop = min(sp.end, last);
+    const int s0 = (int)(at - before), s1 = (int)(stop - before);
+    const int32_t* table = J.table + ((size_t)U.b * J.Hkv + U.h) * J.max_pages;
+
+    for (int i = tid; i < SM::RT * (D / 4); i += NT) {
+      const int r = i / (D / 4), d0 = i % (D / 4) * 4;
+      uint4 w = make_uint4(0, 0, 0, 0);
+      if (r < U.rows) {
+        const int tok = (U.row0 + r) / J.r, j = U.row0 + r - tok * J.r;
+        w = load_plain16(A.q + ((size_t)(J.off[U.b] + tok) * J.stride + (size_t)(U.h * J.r + j) * D + d0) * 4, A.qvec);
+      }
+      *reinterpret_cast<uint4*>(&sm.q[r][d0]) = w;
+    }
+    float m[TR], l[TR];
+    int lim[TR];
+    uint64_t o[TR][D / 64][2];
+#pragma unroll
+    for (int i = 0; i < TR; ++i) {
+      m[i] = -INFINITY;
+      l[i] = 0.f;
+      lim[i] = keys_of(A.causal, U.len, U.n, (U.row0 + min(ty * TR + i, U.rows - 1)) / J.r);
+#pragma unroll
+      for (int c = 0; c < D / 64; ++c) o[i][c][0] = o[i][c][1] = pk2(0.f, 0.f);
+    }
+    const int least = keys_of(A.causal, U.len, U.n, U.row0 / J.r);
+
+    // A thread brings 16 bytes of every (16 * NT / row bytes)-th key.
+    constexpr int ROWB = I8 ? D : 4 * D, LPR = ROWB / 16, STEP = NT / LPR;   // lanes of a row, keys a round
+    constexpr int N = BK / STEP;
+    const int lk = tid / LPR, part = tid % LPR;
+    uint4 ck[I8 ? N : 1], cv[I8 ? N : 1];
+    float2 sc;
+    auto row_of = [&](int t) {
+      return t < U.keys ? page_row(table[t >> J.page_shift], J.n_pages, J.page_shift, t) : -1;
+    };
+    auto fetch = [&](int s, int buf) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int key = lk + i * STEP, row = s < s1 ? row_of(s * BK + key) : -1;
+        const size_t src = (size_t)(row < 0 ? 0 : row) * ROWB + part * 16;
+        if constexpr (I8) {
+          ck[i] = row < 0 ? make_uint4(0, 0, 0, 0) : *reinterpret_cast<const uint4*>(J.kp + src);
+          cv[i] = row < 0 ? make_uint4(0, 0, 0, 0) : *reinterpret_cast<const uint4*>(J.vp + src);
+        } else {
+          copy16(&sm.k[buf][key][part * 4], J.kp + src, row >= 0);
+          copy16(&sm.v[buf][key][part * 4], J.vp + src, row >= 0);
+        }
+      }
+      if constexpr (I8) {
+        if (tid < BK) {
+          const int row = s < s1 ? row_of(s * BK + tid) : -1;
+          sc = row < 0 ? make_float2(0.f, 0.f) : make_float2(J.ks[row], J.vs[row]);
+        }
+      } else {
+        copies_commit();
+      }
+    };
+    auto store = [&](int buf) {                        // 8-bit pages: what fetch() left in registers
+      if constexpr (I8) {
+        auto put = [](float* dst, const uint4& w) {
+          const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            reinterpret_cast<float4*>(dst)[i] =
+                make_float4((float)(int8_t)x[i], (float)(int8_t)(x[i] >> 8), (float)(int8_t)(x[i] >> 16),
+                            (float)(int8_t)(x[i] >> 24));
+        };
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          put(&sm.k[buf][lk + i * STEP][part * 16], ck[i]);
+          put(&sm.v[buf][lk + i * STEP][part * 16], cv[i]);
+        }
+        if (tid < BK) {
+          sm.ks[buf][tid] = sc.x * A.alpha;
+          sm.vs[buf][tid] = sc.y;
+        }
+      }
+    };
+    fetch(s0, 0);
+    for (int s = s0; s < s1; ++s) {
+      const int buf = (s - s0) & 1, k0 = s * BK;
+      if constexpr (I8) store(buf); else copies_wait();
+      // the page of the tile's two 16-key blocks; the barrier also ends all reads of the other buffer
+      const bool none = lane < 2 && k0 + 16 * lane < U.keys && row_of(k0 + 16 * lane) < 0;
+      const uint32_t gone = __ballot_sync(0xffffffffu, none);
+      if (gone && tid == 0) set_status(J.status, kStatusBadPage);
+      __syncthreads();
+      fetch(s + 1, buf ^ 1);
+
+      uint64_t x2[TR][2];
+#pragma unroll
+      for (int i = 0; i < TR; ++i) x2[i][0] = x2[i][1] = pk2(0.f, 0.f);
+      const uint32_t qa = smem_u32(&sm.q[ty * TR][0]), ka = smem_u32(&sm.k[buf][tx][0]);
+#pragma unroll 4
+      for (int d = 0; d < D; d += 4) {
+        uint64_t kk[2][2];
+        lds_2x64(ka + d * 4, kk[0][0], kk[0][1]);
+        lds_2x64(ka + (16 * SM::QS + d) * 4, kk[1][0], kk[1][1]);
+#pragma unroll
+        for (int i = 0; i < TR; ++i) {
+          uint64_t q0, q1;
+          lds_2x64(qa + (i * SM::QS + d) * 4, q0, q1);
+#pragma unroll
+          for (int j = 0; j < 2; ++j) x2[i][j] = ffma2(q1, kk[j][1], ffma2(q0, kk[j][0], x2[i][j]));
+        }
+      }
+      const bool masked = k0 + BK > least || gone;
+      float x[TR][2];
+      bool raise = false;
+#pragma unroll
+      for (int i = 0; i < TR; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          float a, b;
+          upk2(x2[i][j], a, b);
+          x[i][j] = (a + b) * (I8 ? sm.ks[buf][tx + 16 * j] : A.alpha);
+          if (masked && (k0 + tx + 16 * j >= lim[i] || ((gone >> j) & 1u))) x[i][j] = -INFINITY;
+          raise |= x[i][j] > m[i] + kRaise;
+        }
+      if (__any_sync(0xffffffffu, raise)) {
+#pragma unroll
+        for (int i = 0; i < TR; ++i) {
+          float top = fmaxf(m[i], fmaxf(x[i][0], x[i][1]));
+#pragma unroll
+          for (int z = 1; z < 16; z <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, z));
+          const float f = m[i] == -INFINITY ? 0.f : fast_exp2(m[i] - top);
+          m[i] = top;
+          l[i] *= f;
+#pragma unroll
+          for (int c = 0; c < D / 64; ++c)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              float a, b;
+              upk2(o[i][c][e], a, b);
+              o[i][c][e] = pk2(a * f, b * f);
+            }
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int key = tx + 16 * j;
+        float w[TR];
+#pragma unroll
+        for (int i = 0; i < TR; ++i) {
+          w[i] = fast_exp2(x[i][j] - (m[i] == -INFINITY ? 0.f : m[i]));
+          l[i] += w[i];
+          if constexpr (I8) w[i] *= sm.vs[buf][key];
+          // below zero: a key that the row does not attend to
+          if (masked && (k0 + key >= lim[i] || ((gone >> j) & 1u))) w[i] = -1.f;
+        }
+#pragma unroll
+        for (int i = 0; i < TR; ++i) sm.p[key][ty * TR + i] = w[i];
+      }
+      __syncwarp();
+      const uint32_t va = smem_u32(&sm.v[buf][0][tx * 4]);
+      const float* pp = &sm.p[0][ty * TR];
+      if (!masked) {
+#pragma unroll 4
+        for (int key = 0; key < BK; ++key) {
+          uint64_t vv[D / 64][2];
+#pragma unroll
+          for (int c = 0; c < D / 64; ++c) lds_2x64(va + (key * D + 64 * c) * 4, vv[c][0], vv[c][1]);
+#pragma unroll
+          for (int i = 0; i < TR; ++i) {
+            const float w = pp[key * SM::PS + i];
+            const uint64_t w2 = pk2(w, w);
+#pragma unroll
+            for (int c = 0; c < D / 64; ++c) {
+              o[i][c][0] = ffma2(w2, vv[c][0], o[i][c][0]);
+              o[i][c][1] = ffma2(w2, vv[c][1], o[i][c][1]);
+            }
+          }
+        }
+      } else {
+        // a zero weight times a value that is not finite would be a NaN
+#pragma unroll 1
+        for (int key = 0; key < BK; ++key) {
+          uint64_t vv[D / 64][2];
+#pragma unroll
+          for (int c = 0; c < D / 64; ++c) lds_2x64(va + (key * D + 64 * c) * 4, vv[c][0], vv[c][1]);
+#pragma unroll
+          for (int i = 0; i < TR; ++i) {
+            const float w = pp[key * SM::PS + i];
+            if (w < 0.f) continue;
+            const uint64_t w2 = pk2(w, w);
+#pragma unroll
+            for (int c = 0; c < D / 64; ++c) {
+              o[i][c][0] = ffma2(w2, vv[c][0], o[i][c][0]);
+              o[i][c][1] = ffma2(w2, vv[c][1], o[i][c][1]);
+            }
+          }
+        }
+      }
+      __syncwarp();
+    }
+    if constexpr (!I8) copies_wait();                  // the fetch behind the last tile copied zeros
+
+    const bool whole = s0 == 0 && s1 == U.pieces;
+    const size_t slot = (size_t)attend_slot(blockIdx.x, sp.begin, before) * P.rows;
+#pragma unroll
+    for (int i = 0; i < TR; ++i) {
+      float z = l[i];
+#pragma unroll
+      for (int e = 1; e < 16; e <<= 1) z += __shfl_xor_sync(0xffffffffu, z, e);
+      const int r = ty * TR + i;
+      if (r < U.rows) {
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c) {
+          const int d0 = 64 * c + 4 * tx;
+          float4 a;
+          upk2(o[i][c][0], a.x, a.y);
+          upk2(o[i][c][1], a.z, a.w);
+          if (whole) {
+            attend_write<float, D>(A, U.b, U.h, U.row0 + r, d0, a, m[i], z);
+          } else {
+            *reinterpret_cast<float4*>(P.po + (slot + r) * D + d0) = a;
+            if (d0 == 0) P.pml[slot + r] = make_float2(m[i], z);
+          }
+        }
+      }
+    }
+    __syncthreads();
+    at = stop;
+    if (stop == last) {
+      before = last;
+      ++u;
+    }
+  }
+}
+
+template <int D, bool I8, int TR>
+cudaError_t launch(const AttendJob& A, const AttendPlan& P, cudaStream_t st) {
+  constexpr int bytes = (int)sizeof(SimtSmem<D, TR>);
+  const cudaError_t e =
+      cudaFuncSetAttribute(attend_simt_kernel<D, I8, TR>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e != cudaSuccess) return e;
+  return launch_kernel(attend_simt_kernel<D, I8, TR>, dim3(P.workers), NT, bytes, st, true, 0, A, P);
+}
+
+template <int D, bool I8>
+cudaError_t launch_rows(const AttendJob& A, const AttendPlan& P, cudaStream_t st) {
+  if (P.rows <= 8) return launch<D, I8, 1>(A, P, st);
+  if (P.rows <= 16) return launch<D, I8, 2>(A, P, st);
+  return launch<D, I8, 8>(A, P, st);
+}
+
+}  // namespace
+
+cudaError_t launch_attend_simt(const AttendJob& A, const AttendPlan& P, cudaStream_t st) {
+  if (A.c.d == 128) return A.c.i8 ? launch_rows<128, true>(A, P, st) : launch_rows<128, false>(A, P, st);
+  return A.c.i8 ? launch_rows<64, true>(A, P, st) : launch_rows<64, false>(A, P, st);
+}
+
+}  // namespace mmshift
