@@ -215,13 +215,10 @@ def default_params(**kw) -> Params:
 
 
 def _ptr(x) -> Optional[int]:
-    if x is None:
-        return None
-    if isinstance(x, int):
+    if x is None or isinstance(x, int):
         return x
-    if hasattr(x, "cuda_stream"):          # torch.cuda.Stream
-        return x.cuda_stream
-    return x.data_ptr()
+    address = getattr(x, "data_ptr", None)
+    return x.cuda_stream if address is None else address()   # torch.cuda.Stream, or a tensor
 
 
 def mmshift_output_rows(shape: Shape) -> int:

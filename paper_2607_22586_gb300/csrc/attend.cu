@@ -14,31 +14,46 @@ namespace {
 template <typename T, int D, int RPB>
 __global__ void __launch_bounds__(256) attend_merge_kernel(const __grid_constant__ AttendJob A,
                                                            const __grid_constant__ AttendPlan P) {
-  dependent_start();
   constexpr int LV = D / 32;                           // values of a lane
+  __shared__ AttendScan<256> scan;
+  __shared__ int64_t place[2];
   const int u = blockIdx.x, w = threadIdx.x / 32, lane = threadIdx.x % 32;
-  const int64_t a = P.pre[u], b = P.pre[u + 1], W = P.pre[P.uoff[A.c.B]];
-  int n = 0, i0 = 0, i1 = -1;
-  if (a < b) {
-    n = span_workers(W, P.workers, P.least);
-    i0 = span_of(W, n, a);
-    i1 = span_of(W, n, b - 1);
-    if (i0 == i1) return;                              // one worker had it all
+  // Which workers share the unit follows from the lengths, which were there before the
+  // attention kernel began: worked out while that still runs.
+  {
+    const AttendSums x(A, P, &scan);
+    if (u >= x.u0 && u < x.u1) {
+      int64_t a = x.before;
+      for (int k = x.u0; k < u; ++k) a += attend_unit(A, P, scan.lengths(A.c), k).pieces;
+      place[0] = a;
+      place[1] = x.W;
+    }
+    __syncthreads();
   }
-  const AttendUnit U = attend_unit(A, P, u);
+  const AttendUnit U = attend_unit(A, P, scan.lengths(A.c), u);
+  const int64_t a = place[0], b = a + U.pieces;
+  int i0 = 0, i1 = -1, first = 0;
+  bool whole = false;
+  if (a < b) {
+    const Shares sh = shares_of(place[1], P.workers, P.least);
+    i0 = sh.of(a);
+    whole = b <= sh.begin(i0 + 1);                     // one worker had it all
+    i1 = sh.of(b - 1);
+    first = attend_slot(i0, sh.begin(i0), a);
+  }
   const int r = RPB == 1 ? blockIdx.y : blockIdx.y * RPB + w;
-  if (r >= U.rows) return;
+  dependent_start();
+  if (whole || r >= U.rows) return;
   const int parts = i1 - i0 + 1;
-  auto at = [&](int k) {
-    return (size_t)attend_slot(i0 + k, span_begin(W, n, i0 + k), a) * P.rows + r;
-  };
+  // a worker's first piece has an even slot; only the unit's first part can be a last piece
+  auto at = [&](int k) { return (size_t)(k ? 2 * (i0 + k) : first) * P.rows + r; };
   float top = -INFINITY;
   for (int k = lane; k < parts; k += 32) top = fmaxf(top, P.pml[at(k)].x);
 #pragma unroll
   for (int s = 16; s; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
   float z = 0.f, o[LV] = {};
   constexpr int STEP = RPB == 1 ? 8 : 1;
-#pragma unroll 4
+#pragma unroll 8
   for (int k = RPB == 1 ? w : 0; k < parts; k += STEP) {
     const size_t slot = at(k);
     const float2 ml = P.pml[slot];
@@ -94,7 +109,8 @@ __global__ void __launch_bounds__(256) attend_merge_kernel(const __grid_constant
 template <typename T, int D>
 cudaError_t launch_merge_t(const AttendJob& A, const AttendPlan& P, cudaStream_t st) {
   const unsigned units = P.uoff[A.c.B];
-  if (P.rows <= 16)
+  // few units, then many parts each: 4 units of 114 parts
+  if (8 * units <= (unsigned)P.workers)
     return launch_kernel(attend_merge_kernel<T, D, 1>, dim3(units, P.rows), 256, 0, st, true, 0, A, P);
   return launch_kernel(attend_merge_kernel<T, D, 8>, dim3(units, (P.rows + 7) / 8), 256, 0, st, true, 0, A, P);
 }
@@ -133,7 +149,8 @@ AttendPlan plan_of(const CacheJob& J, int most, Take take) {
   P.rows = std::min(widest, most);
   for (int b = 0; b < J.B; ++b) {
     const int rows = (J.off[b + 1] - J.off[b]) * J.r;
-    P.uoff[b + 1] = P.uoff[b] + (rows && take(rows) ? J.Hkv * ((rows + P.rows - 1) / P.rows) : 0);
+    P.tiles[b] = rows && take(rows) ? (rows + P.rows - 1) / P.rows : 0;
+    P.uoff[b + 1] = P.uoff[b] + J.Hkv * P.tiles[b];
   }
   return P;
 }
@@ -144,11 +161,10 @@ AttendPlan token_plan(const CacheJob& J, int nsm) {
   if (J.bf16) {
     const int row = J.i8 ? J.d : 2 * J.d;
     while ((row << P.step_shift) < 4096) ++P.step_shift;   // a warp's piece: 4 KB of K
-    P.least = 4;
-    P.workers = nsm * (P.rows <= 8 ? 4 : 3);
+    P.least = 2;
+    P.workers = nsm * (P.rows <= 8 ? 3 : 2);
   } else {
     P.step_shift = 5;
-    P.least = 1;
     P.workers = nsm * (P.rows <= 8 ? 3 : 2);
   }
   return P;
@@ -157,15 +173,12 @@ AttendPlan token_plan(const CacheJob& J, int nsm) {
 AttendPlan chunk_plan(const CacheJob& J, int nsm) {
   AttendPlan P = plan_of(J, J.bf16 ? 256 : 64, [&](int rows) { return rows > kTokenRows; });
   P.step_shift = J.bf16 ? 7 : 5;
-  P.least = 1;
   P.workers = J.bf16 ? nsm : 2 * nsm;
   return P;
 }
 
 // The plan's buffers from `at` on; where they end.
 char* place(AttendPlan& P, const CacheJob& J, char* at) {
-  P.pre = reinterpret_cast<int64_t*>(at);
-  at += align256((size_t)(P.uoff[J.B] + 1) * sizeof(int64_t));
   P.po = reinterpret_cast<float*>(at);
   at += align256((size_t)2 * P.workers * P.rows * J.d * sizeof(float));
   P.pml = reinterpret_cast<float2*>(at);

@@ -16,10 +16,10 @@ namespace mmshift {
 
 struct AttendPlan {
   int32_t uoff[MMSHIFT_MAX_BATCH + 1];  // units, prefix over requests
+  int32_t tiles[MMSHIFT_MAX_BATCH];     // a request's row tiles per KV head
   int32_t rows;                         // query rows of a tile
   int32_t step_shift;
-  int32_t workers, least;               // workers at most; pieces that one has at least, if there are so many
-  int64_t* pre;                         // [units + 1] pieces before each unit (written by the first CTA)
+  int32_t workers, least;               // workers at most; one has 2^least pieces where there are as many
   float* po;                            // [2 * workers][rows][d] sums of weights times values
   float2* pml;                          // [2 * workers][rows] their maximum (base 2) and sum of weights
 };
@@ -31,16 +31,25 @@ struct AttendUnit {
   int pieces;
 };
 
-__device__ __forceinline__ AttendUnit attend_unit(const AttendJob& A, const AttendPlan& P, int u) {
+// Start of an attention kernel: everything before it in the stream is done, and the
+// merge kernel may start and read the lengths too.
+__device__ __forceinline__ void attend_start() {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
+// lens: the sequences' lengths (AttendScan::lengths), or null to read them from the cache.
+__device__ __forceinline__ AttendUnit attend_unit(const AttendJob& A, const AttendPlan& P, const int32_t* lens, int u) {
   const CacheJob& J = A.c;
   AttendUnit x;
   x.b = range_of(P.uoff, J.B, u);
   x.n = J.off[x.b + 1] - J.off[x.b];
-  const int all = x.n * J.r, tiles = (all + P.rows - 1) / P.rows, rem = u - P.uoff[x.b];
-  x.h = rem / tiles;
+  const int all = x.n * J.r, tiles = P.tiles[x.b], rem = u - P.uoff[x.b];
+  x.h = tiles == 1 ? rem : rem / tiles;
   x.row0 = (rem - x.h * tiles) * P.rows;
   x.rows = min(P.rows, all - x.row0);
-  x.len = cache_len(J, (size_t)x.b * J.Hkv + x.h);
+  const int seq = x.b * J.Hkv + x.h;
+  x.len = lens ? lens[seq] : cache_len(J, seq);
   x.keys = keys_of(A.causal, x.len, x.n, (x.row0 + x.rows - 1) / J.r);
   x.pieces = (x.keys + (1 << P.step_shift) - 1) >> P.step_shift;
   return x;
@@ -53,61 +62,72 @@ struct AttendSpan {
   int unit;
 };
 
-template <int NT>
+// LENS: up to so many sequences' lengths are kept in shared memory.
+template <int NT, int LENS = 1024>
 struct AttendScan {
   int64_t warp[NT / 32];
   AttendSpan span;
+  int32_t lens[LENS];
+  __device__ __forceinline__ const int32_t* lengths(const CacheJob& J) const {
+    return J.B * J.Hkv <= LENS ? lens : nullptr;
+  }
 };
 
-// Called by the CTA's first NT threads together (`bar` is their barrier).
-// Every thread adds up a run of units; a scan over the threads gives the pieces
-// before each run.
-template <int NT, class Barrier>
-__device__ __forceinline__ AttendSpan attend_span(const AttendJob& A, const AttendPlan& P, AttendScan<NT>* s,
-                                                  Barrier bar) {
-  const int tid = threadIdx.x, lane = tid % 32, w = tid / 32, U = P.uoff[A.c.B];
-  const int per = (U + NT - 1) / NT, u0 = min(tid * per, U), u1 = min(u0 + per, U);
-  int64_t sum = 0;
-  for (int u = u0; u < u1; ++u) sum += attend_unit(A, P, u).pieces;
-  int64_t x = sum;
+// Called by all NT threads of a CTA. Every thread adds up a run of units, [u0, u1);
+// `before` are the pieces before its run, `sum` the run's, W all units'.
+struct AttendSums {
+  int u0, u1;
+  int64_t before, sum, W;
+  template <int NT, int LENS>
+  __device__ __forceinline__ AttendSums(const AttendJob& A, const AttendPlan& P, AttendScan<NT, LENS>* s) {
+    const CacheJob& J = A.c;
+    const int tid = threadIdx.x, lane = tid % 32, w = tid / 32, U = P.uoff[J.B];
+    if (s->lengths(J))
+      for (int i = tid; i < J.B * J.Hkv; i += NT) s->lens[i] = cache_len(J, i);
+    __syncthreads();
+    const int per = (U + NT - 1) / NT;
+    u0 = min(tid * per, U);
+    u1 = min(u0 + per, U);
+    sum = 0;
+    for (int u = u0; u < u1; ++u) sum += attend_unit(A, P, s->lengths(A.c), u).pieces;
+    int64_t x = sum;
 #pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    const int64_t y = __shfl_up_sync(0xffffffffu, x, d);
-    if (lane >= d) x += y;
-  }
-  if (lane == 31) s->warp[w] = x;
-  bar();
-  int64_t W = 0, before = x - sum;
-#pragma unroll
-  for (int i = 0; i < NT / 32; ++i) {
-    if (i < w) before += s->warp[i];
-    W += s->warp[i];
-  }
-  const int n = span_workers(W, P.workers, P.least), i = blockIdx.x;
-  const int64_t begin = i < n ? span_begin(W, n, i) : W, end = i < n ? span_begin(W, n, i + 1) : W;
-  if (i == 0) {
-    int64_t a = before;
-    for (int u = u0; u < u1; ++u) {
-      P.pre[u] = a;
-      a += attend_unit(A, P, u).pieces;
+    for (int d = 1; d < 32; d <<= 1) {
+      const int64_t y = __shfl_up_sync(0xffffffffu, x, d);
+      if (lane >= d) x += y;
     }
-    if (tid == 0) P.pre[U] = W;
+    if (lane == 31) s->warp[w] = x;
+    __syncthreads();
+    W = 0;
+    before = x - sum;
+#pragma unroll
+    for (int i = 0; i < NT / 32; ++i) {
+      if (i < w) before += s->warp[i];
+      W += s->warp[i];
+    }
   }
-  if (tid == 0) s->span = AttendSpan{begin, end, 0, 0};
-  bar();
-  if (begin < end && begin >= before && begin < before + sum) {
-    int u = u0;
-    int64_t a = before;
+};
+
+// The CTA's share of the work, as a worker.
+template <int NT, int LENS>
+__device__ __forceinline__ AttendSpan attend_span(const AttendJob& A, const AttendPlan& P, AttendScan<NT, LENS>* s) {
+  const AttendSums x(A, P, s);
+  const Shares sh = shares_of(x.W, P.workers, P.least);
+  const int i = blockIdx.x;
+  const int64_t begin = i < sh.n ? sh.begin(i) : x.W, end = i < sh.n ? sh.begin(i + 1) : x.W;
+  if (begin >= end) return AttendSpan{begin, end, 0, 0};
+  if (begin >= x.before && begin < x.before + x.sum) {
+    int u = x.u0;
+    int64_t a = x.before;
     for (;;) {
-      const int p = attend_unit(A, P, u).pieces;
+      const int p = attend_unit(A, P, s->lengths(A.c), u).pieces;
       if (a + p > begin) break;
       a += p;
       ++u;
     }
-    s->span.before = a;
-    s->span.unit = u;
+    s->span = AttendSpan{begin, end, a, u};
   }
-  bar();
+  __syncthreads();
   return s->span;
 }
 

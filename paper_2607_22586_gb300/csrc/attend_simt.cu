@@ -33,7 +33,7 @@ struct SimtSmem {
   alignas(16) float v[2][BK][D];
   alignas(16) float p[BK][PS];
   float ks[2][BK], vs[2][BK];
-  AttendScan<NT> scan;
+  AttendScan<NT, 256> scan;
 };
 
 __device__ __forceinline__ void copy16(void* dst, const void* src, bool in) {
@@ -49,14 +49,14 @@ __global__ void __launch_bounds__(NT, TR >= 4 ? 2 : 3) attend_simt_kernel(const 
   using SM = SimtSmem<D, TR>;
   extern __shared__ __align__(16) unsigned char smraw[];
   SM& sm = *reinterpret_cast<SM*>(smraw);
-  dependent_start();
+  attend_start();
   const CacheJob& J = A.c;
   const int tid = threadIdx.x, lane = tid % 32, tx = tid % 16, ty = tid / 16;
-  const AttendSpan sp = attend_span<NT>(A, P, &sm.scan, [] { __syncthreads(); });
+  const AttendSpan sp = attend_span(A, P, &sm.scan);
   int u = sp.unit;
   int64_t before = sp.before;
   for (int64_t at = sp.begin; at < sp.end;) {
-    const AttendUnit U = attend_unit(A, P, u);
+    const AttendUnit U = attend_unit(A, P, sm.scan.lengths(A.c), u);
     const int64_t last = before + U.pieces;
     if (last <= at) {
       before = last;

@@ -12,12 +12,19 @@
 // dimensions is free too, so both are chosen such that a lane's fragment is 16
 // (or 8) consecutive bytes of a row: lane (g, c) holds key g's dimensions of
 // chunk c for S, and, for O, the keys 2c, 2c + 1, 2c + 8, 2c + 9 of dimension
-// chunk g, whose pairs of keys one byte permutation brings together. An 8-bit
-// code x becomes bfloat16 without rounding: with u = x & 127, 128 + u is
-// the pattern 0x4300 | u, and x = (128 + u) - (128 or, for a negative x, 256). K's
-// scale goes to the logit and V's into the weight, before it is rounded.
+// chunk g, whose pairs of keys one byte permutation brings together.
 //
-// The maximum is only raised when a logit passes it by 8 (base 2), so the common
+// 8-bit pages: both products take float16. A code x becomes float16 without
+// rounding, three instructions for two: with u = x + 128, 1024 + u is the pattern
+// 0x6400 | u, less 1152. (bfloat16 holds no 8 bits beside a leading one: five
+// instructions, and this kernel was bound by them, 468 us for 64 requests of 2 to 24
+// thousand rows.) A query row is scaled by a power of two that brings its largest
+// value to 2^14, so what float16 cannot hold of it is below 2^-39 of that. K's scale
+// goes to the logit. V's goes into the weight, whose float16 form is relative to the
+// row's largest such product: w = e^(z + ln vs - M), while the sum of weights is
+// taken of e^(z - m) as ever.
+//
+// The maxima are only raised when a value passes them by 8 (base 2), so the common
 // step has one vote and no reduction: weights then stay below 2^8.
 #include "attend.cuh"
 
@@ -41,12 +48,29 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
   return y;
 }
 
-// Two codes, in the low bytes of t's halves, as bfloat16.
-__device__ __forceinline__ uint32_t codes_bf16(uint32_t t) {
-  const uint32_t a = (t & 0x007f007fu) | 0x43004300u, c = (t & 0x00800080u) | 0x43004300u;
-  uint32_t x;
-  asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(x) : "r"(a), "r"(c));
-  return x;
+__device__ __forceinline__ void mma16816_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                             uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// Bytes b0, b1 of x (codes + 128), picked by `sel` as b0 64 b1 64, as two float16 codes.
+template <int SEL>
+__device__ __forceinline__ uint32_t codes_f16(uint32_t x) {
+  uint32_t y;
+  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(y) : "r"(__byte_perm(x, 0x64646464u, SEL)), "r"(0x64806480u));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ float fast_log2(float x) {
+  float y;
+  asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
 }
 
 __device__ __forceinline__ bool not_finite2(uint32_t w) {
@@ -140,32 +164,41 @@ struct Token {
       a[2] = x.w[0][2 * s + 1];
       a[3] = x.w[1][2 * s + 1];
     } else {
-      a[0] = codes_bf16(__byte_perm(x.w[0][s], 0, 0x1100));
-      a[1] = codes_bf16(__byte_perm(x.w[1][s], 0, 0x1100));
-      a[2] = codes_bf16(__byte_perm(x.w[0][s], 0, 0x3322));
-      a[3] = codes_bf16(__byte_perm(x.w[1][s], 0, 0x3322));
+      const uint32_t u0 = x.w[0][s] ^ 0x80808080u, u1 = x.w[1][s] ^ 0x80808080u;
+      a[0] = codes_f16<0x4140>(u0);
+      a[1] = codes_f16<0x4140>(u1);
+      a[2] = codes_f16<0x4342>(u0);
+      a[3] = codes_f16<0x4342>(u1);
     }
   }
 
-  // A fragments of dimension block m of O^T: its rows g and g + 8 are two
-  // neighbouring dimensions of chunk g.
-  static __device__ __forceinline__ void v_frag(const VBlock& x, int m, uint32_t (&a)[4]) {
+  // A fragments of dimension blocks 2j and 2j + 1 of O^T: rows g and g + 8 of a block
+  // are two neighbouring dimensions of chunk g.
+  static __device__ __forceinline__ void v_frag(const VBlock& x, int j, uint32_t (&a)[2][4]) {
     if constexpr (!I8) {
-      a[0] = __byte_perm(x.w[0][m], x.w[1][m], 0x5410);
-      a[1] = __byte_perm(x.w[0][m], x.w[1][m], 0x7632);
-      a[2] = __byte_perm(x.w[2][m], x.w[3][m], 0x5410);
-      a[3] = __byte_perm(x.w[2][m], x.w[3][m], 0x7632);
-    } else if (m % 2 == 0) {
-      a[0] = codes_bf16(__byte_perm(x.w[0][m / 2], x.w[1][m / 2], 0x4400));
-      a[1] = codes_bf16(__byte_perm(x.w[0][m / 2], x.w[1][m / 2], 0x5511));
-      a[2] = codes_bf16(__byte_perm(x.w[2][m / 2], x.w[3][m / 2], 0x4400));
-      a[3] = codes_bf16(__byte_perm(x.w[2][m / 2], x.w[3][m / 2], 0x5511));
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int m = 2 * j + e;
+        a[e][0] = __byte_perm(x.w[0][m], x.w[1][m], 0x5410);
+        a[e][1] = __byte_perm(x.w[0][m], x.w[1][m], 0x7632);
+        a[e][2] = __byte_perm(x.w[2][m], x.w[3][m], 0x5410);
+        a[e][3] = __byte_perm(x.w[2][m], x.w[3][m], 0x7632);
+      }
     } else {
-      a[0] = codes_bf16(__byte_perm(x.w[0][m / 2], x.w[1][m / 2], 0x6622));
-      a[1] = codes_bf16(__byte_perm(x.w[0][m / 2], x.w[1][m / 2], 0x7733));
-      a[2] = codes_bf16(__byte_perm(x.w[2][m / 2], x.w[3][m / 2], 0x6622));
-      a[3] = codes_bf16(__byte_perm(x.w[2][m / 2], x.w[3][m / 2], 0x7733));
+#pragma unroll
+      for (int k = 0; k < 4; k += 2) {                 // keys 2c, 2c + 1, then 2c + 8, 2c + 9
+        const uint32_t p = x.w[k][j] ^ 0x80808080u, q = x.w[k + 1][j] ^ 0x80808080u;
+        const uint32_t lo = __byte_perm(p, q, 0x5140), hi = __byte_perm(p, q, 0x7362);
+        a[0][k] = codes_f16<0x4140>(lo);
+        a[0][k + 1] = codes_f16<0x4342>(lo);
+        a[1][k] = codes_f16<0x4140>(hi);
+        a[1][k + 1] = codes_f16<0x4342>(hi);
+      }
     }
+  }
+  static __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    if constexpr (I8) mma16816_f16(d, a[0], a[1], a[2], a[3], b0, b1);
+    else mma16816(d, a[0], a[1], a[2], a[3], b0, b1);
   }
 
   // The first of the two dimensions of block m in lanes of chunk g.
@@ -176,18 +209,18 @@ struct Token {
 };
 
 template <int D, bool I8, int NQ>
-__global__ void __launch_bounds__(NT, NQ == 1 ? 4 : 3) attend_token_kernel(const __grid_constant__ AttendJob A,
+__global__ void __launch_bounds__(NT, NQ == 1 ? 3 : 2) attend_token_kernel(const __grid_constant__ AttendJob A,
                                                                            const __grid_constant__ AttendPlan P) {
   using T = Token<D, I8, NQ>;
   __shared__ typename T::Smem sm;
-  dependent_start();
+  attend_start();
   const CacheJob& J = A.c;
   const int lane = threadIdx.x % 32, w = threadIdx.x / 32, g = lane / 4, c = lane % 4;
-  const AttendSpan sp = attend_span<NT>(A, P, &sm.scan, [] { __syncthreads(); });
+  const AttendSpan sp = attend_span(A, P, &sm.scan);
   int u = sp.unit;
   int64_t before = sp.before;
   for (int64_t at = sp.begin; at < sp.end;) {
-    const AttendUnit U = attend_unit(A, P, u);
+    const AttendUnit U = attend_unit(A, P, sm.scan.lengths(A.c), u);
     const int64_t last = before + U.pieces;
     if (last <= at) {                                  // a unit without pieces
       before = last;
@@ -197,6 +230,36 @@ __global__ void __launch_bounds__(NT, NQ == 1 ? 4 : 3) attend_token_kernel(const
     const int64_t stop = min(sp.end, last);
     const int s0 = (int)(at - before), s1 = (int)(stop - before);
     const int32_t* table = J.table + ((size_t)U.b * J.Hkv + U.h) * J.max_pages;
+
+    // row of the pool of each 16-key block, -1 behind the end and without a page
+    // raises a maximum to its row's of the step; what sums relative to it have to be multiplied by
+    auto raise_max = [&](float& m, auto&& value) {
+      float top = m;
+#pragma unroll
+      for (int nb = 0; nb < T::NB; ++nb) top = fmaxf(top, fmaxf(value(nb, 0), value(nb, 1)));
+#pragma unroll
+      for (int z = 4; z < 32; z <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, z));
+      const float f = m == -INFINITY ? 0.f : fast_exp2(m - top);
+      m = top;
+      return f;
+    };
+    auto rows_of = [&](int s, int (&row)[T::NB]) {
+#pragma unroll
+      for (int nb = 0; nb < T::NB; ++nb) {
+        const int t = s * T::KEYS + 16 * nb;
+        row[nb] = s < s1 && t < U.keys ? page_row(table[t >> J.page_shift], J.n_pages, J.page_shift, t) : -1;
+      }
+    };
+    typename T::KBlock kb[T::NB];
+    typename T::VBlock vb[T::NB];
+    int row[T::NB], next[T::NB];
+    int s = s0 + w;
+    rows_of(s, row);
+    rows_of(s + NW, next);
+#pragma unroll
+    for (int nb = 0; nb < T::NB; ++nb) T::load_k(J, kb[nb], row[nb], s * T::KEYS + 16 * nb, U.keys, g, c);
+#pragma unroll
+    for (int nb = 0; nb < T::NB; ++nb) T::load_v(J, vb[nb], row[nb], s * T::KEYS + 16 * nb, U.keys, g, c);
 
     // query rows as B fragments: row 8 * nq + g
     uint32_t q[NQ][2 * T::KS];
@@ -219,6 +282,28 @@ __global__ void __launch_bounds__(NT, NQ == 1 ? 4 : 3) attend_token_kernel(const
     }
     // rows 8 * nq + 2c and + 1 as columns of the products
     float m[NQ][2], l[NQ][2], o[NQ][T::MT][4];
+    float mw[NQ][2], alpha[NQ][2];                     // 8-bit pages: M, and alpha over the row's power of two
+    if constexpr (I8) {
+#pragma unroll
+      for (int nq = 0; nq < NQ; ++nq) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 2 * T::KS; ++i) top = max(top, max(q[nq][i] & 0x7fffu, (q[nq][i] >> 16) & 0x7fffu));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        // 2^k with k = 14 - exponent of the largest, at most 126 (a largest below 2^-112 or a row of zeros)
+        const int k = min(14 - ((int)(top >> 7) - 127), 126);
+        const float f = __uint_as_float((uint32_t)(127 + k) << 23);
+#pragma unroll
+        for (int i = 0; i < 2 * T::KS; ++i) q[nq][i] = pack_f16(bf16_lo(q[nq][i]) * f, bf16_hi(q[nq][i]) * f);
+        const float back = A.alpha * __uint_as_float((uint32_t)(127 - k) << 23);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          alpha[nq][e] = __shfl_sync(0xffffffffu, back, 4 * (2 * c + e));
+          mw[nq][e] = -INFINITY;
+        }
+      }
+    }
     int lim[NQ][2];
 #pragma unroll
     for (int nq = 0; nq < NQ; ++nq)
@@ -231,25 +316,6 @@ __global__ void __launch_bounds__(NT, NQ == 1 ? 4 : 3) attend_token_kernel(const
         for (int mt = 0; mt < T::MT; ++mt) o[nq][mt][e] = o[nq][mt][2 + e] = 0.f;
       }
     const int least = keys_of(A.causal, U.len, U.n, 0);   // keys that every row attends to
-
-    // row of the pool of each 16-key block, -1 behind the end and without a page
-    auto rows_of = [&](int s, int (&row)[T::NB]) {
-#pragma unroll
-      for (int nb = 0; nb < T::NB; ++nb) {
-        const int t = s * T::KEYS + 16 * nb;
-        row[nb] = s < s1 && t < U.keys ? page_row(table[t >> J.page_shift], J.n_pages, J.page_shift, t) : -1;
-      }
-    };
-    typename T::KBlock kb[T::NB];
-    typename T::VBlock vb[T::NB];
-    int row[T::NB], next[T::NB];
-    int s = s0 + w;
-    rows_of(s, row);
-    rows_of(s + NW, next);
-#pragma unroll
-    for (int nb = 0; nb < T::NB; ++nb) T::load_k(J, kb[nb], row[nb], s * T::KEYS + 16 * nb, U.keys, g, c);
-#pragma unroll
-    for (int nb = 0; nb < T::NB; ++nb) T::load_v(J, vb[nb], row[nb], s * T::KEYS + 16 * nb, U.keys, g, c);
 
     for (; s < s1; s += NW) {
       const int t0 = s * T::KEYS;
@@ -265,12 +331,23 @@ __global__ void __launch_bounds__(NT, NQ == 1 ? 4 : 3) attend_token_kernel(const
           uint32_t a[4];
           T::k_frag(kb[nb], ks, a);
 #pragma unroll
-          for (int nq = 0; nq < NQ; ++nq) mma16816(x[nq][nb], a[0], a[1], a[2], a[3], q[nq][2 * ks], q[nq][2 * ks + 1]);
+          for (int nq = 0; nq < NQ; ++nq) T::mma(x[nq][nb], a, q[nq][2 * ks], q[nq][2 * ks + 1]);
         }
 #pragma unroll
         for (int nq = 0; nq < NQ; ++nq)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x[nq][nb][i] *= I8 ? A.alpha * kb[nb].s[i / 2] : A.alpha;
+          for (int i = 0; i < 4; ++i) x[nq][nb][i] *= I8 ? kb[nb].s[i / 2] * alpha[nq][i % 2] : A.alpha;
+      }
+      float y[I8 ? NQ : 1][T::NB][4];                  // 8-bit pages: with V's scales
+      if constexpr (I8) {
+#pragma unroll
+        for (int nb = 0; nb < T::NB; ++nb) {
+          const float lv[2] = {fast_log2(vb[nb].s[0]), fast_log2(vb[nb].s[1])};
+#pragma unroll
+          for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[nq][nb][i] = x[nq][nb][i] + lv[i / 2];
+        }
       }
       const int tn = t0 + NW * T::KEYS;
 #pragma unroll
@@ -288,7 +365,10 @@ __global__ void __launch_bounds__(NT, NQ == 1 ? 4 : 3) attend_token_kernel(const
           for (int nb = 0; nb < T::NB; ++nb)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-              if (row[nb] < 0 || t0 + 16 * nb + 8 * (i / 2) + g >= lim[nq][i % 2]) x[nq][nb][i] = -INFINITY;
+              if (row[nb] < 0 || t0 + 16 * nb + 8 * (i / 2) + g >= lim[nq][i % 2]) {
+                x[nq][nb][i] = -INFINITY;
+                if constexpr (I8) y[nq][nb][i] = -INFINITY;
+              }
       }
       bool raise = false;
 #pragma unroll
@@ -296,20 +376,18 @@ __global__ void __launch_bounds__(NT, NQ == 1 ? 4 : 3) attend_token_kernel(const
 #pragma unroll
         for (int nb = 0; nb < T::NB; ++nb)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) raise |= x[nq][nb][i] > m[nq][i % 2] + kRaise;
+          for (int i = 0; i < 4; ++i) {
+            raise |= x[nq][nb][i] > m[nq][i % 2] + kRaise;
+            if constexpr (I8) raise |= y[nq][nb][i] > mw[nq][i % 2] + kRaise;
+          }
       if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
         for (int nq = 0; nq < NQ; ++nq)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            float top = m[nq][e];
-#pragma unroll
-            for (int nb = 0; nb < T::NB; ++nb) top = fmaxf(top, fmaxf(x[nq][nb][e], x[nq][nb][2 + e]));
-#pragma unroll
-            for (int z = 4; z < 32; z <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, z));
-            const float f = m[nq][e] == -INFINITY ? 0.f : fast_exp2(m[nq][e] - top);
-            m[nq][e] = top;
+            float f = raise_max(m[nq][e], [&](int nb, int hf) { return x[nq][nb][2 * hf + e]; });
             l[nq][e] *= f;
+            if constexpr (I8) f = raise_max(mw[nq][e], [&](int nb, int hf) { return y[nq][nb][2 * hf + e]; });
 #pragma unroll
             for (int mt = 0; mt < T::MT; ++mt) {
               o[nq][mt][e] *= f;
@@ -321,6 +399,11 @@ __global__ void __launch_bounds__(NT, NQ == 1 ? 4 : 3) attend_token_kernel(const
 #pragma unroll
       for (int nq = 0; nq < NQ; ++nq) {
         const float m0 = m[nq][0] == -INFINITY ? 0.f : m[nq][0], m1 = m[nq][1] == -INFINITY ? 0.f : m[nq][1];
+        float w0 = 0.f, w1 = 0.f;
+        if constexpr (I8) {
+          w0 = mw[nq][0] == -INFINITY ? 0.f : mw[nq][0];
+          w1 = mw[nq][1] == -INFINITY ? 0.f : mw[nq][1];
+        }
 #pragma unroll
         for (int nb = 0; nb < T::NB; ++nb) {
           float e[4];
@@ -328,14 +411,10 @@ __global__ void __launch_bounds__(NT, NQ == 1 ? 4 : 3) attend_token_kernel(const
           for (int i = 0; i < 4; ++i) {
             e[i] = fast_exp2(x[nq][nb][i] - (i % 2 ? m1 : m0));
             l[nq][i % 2] += e[i];
+            if constexpr (I8) e[i] = fast_exp2(y[nq][nb][i] - (i % 2 ? w1 : w0));
           }
-          if constexpr (I8) {
-            // a key that is masked has no part in the result, whatever its scale
-#pragma unroll
-            for (int i = 0; i < 4; ++i) e[i] = masked && x[nq][nb][i] == -INFINITY ? 0.f : e[i] * vb[nb].s[i / 2];
-          }
-          p[nq][nb][0] = transpose8(pack_bf16(e[0], e[1]));
-          p[nq][nb][1] = transpose8(pack_bf16(e[2], e[3]));
+          p[nq][nb][0] = transpose8(I8 ? pack_f16(e[0], e[1]) : pack_bf16(e[0], e[1]));
+          p[nq][nb][1] = transpose8(I8 ? pack_f16(e[2], e[3]) : pack_bf16(e[2], e[3]));
         }
       }
       bool plain = true;
@@ -358,11 +437,13 @@ __global__ void __launch_bounds__(NT, NQ == 1 ? 4 : 3) attend_token_kernel(const
 #pragma unroll
         for (int nb = 0; nb < T::NB; ++nb)
 #pragma unroll
-          for (int mt = 0; mt < T::MT; ++mt) {
-            uint32_t a[4];
-            T::v_frag(vb[nb], mt, a);
+          for (int j = 0; j < T::MT / 2; ++j) {
+            uint32_t a[2][4];
+            T::v_frag(vb[nb], j, a);
 #pragma unroll
-            for (int nq = 0; nq < NQ; ++nq) mma16816(o[nq][mt], a[0], a[1], a[2], a[3], p[nq][nb][0], p[nq][nb][1]);
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+              for (int nq = 0; nq < NQ; ++nq) T::mma(o[nq][2 * j + e], a[e], p[nq][nb][0], p[nq][nb][1]);
           }
       } else {
 #pragma unroll
@@ -372,16 +453,20 @@ __global__ void __launch_bounds__(NT, NQ == 1 ? 4 : 3) attend_token_kernel(const
             const uint32_t half = (k & 7) >> 1 == c ? (k & 1 ? 0xffff0000u : 0xffffu) : 0u;
             const uint32_t lo = k < 8 ? half : 0u, hi = k < 8 ? 0u : half;
 #pragma unroll
-            for (int mt = 0; mt < T::MT; ++mt) {
-              uint32_t a[4];
-              T::v_frag(vb[nb], mt, a);
+            for (int j = 0; j < T::MT / 2; ++j) {
+              uint32_t a[2][4];
+              T::v_frag(vb[nb], j, a);
 #pragma unroll
-              for (int nq = 0; nq < NQ; ++nq) {
-                float d[4] = {};
-                mma16816(d, a[0] & lo, a[1] & lo, a[2] & hi, a[3] & hi, p[nq][nb][0], p[nq][nb][1]);
+              for (int e = 0; e < 2; ++e) {
+                const uint32_t b[4] = {a[e][0] & lo, a[e][1] & lo, a[e][2] & hi, a[e][3] & hi};
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                  if (t0 + 16 * nb + k < lim[nq][i % 2]) o[nq][mt][i] += d[i];
+                for (int nq = 0; nq < NQ; ++nq) {
+                  float d[4] = {};
+                  T::mma(d, b, p[nq][nb][0], p[nq][nb][1]);
+#pragma unroll
+                  for (int i = 0; i < 4; ++i)
+                    if (t0 + 16 * nb + k < lim[nq][i % 2]) o[nq][2 * j + e][i] += d[i];
+                }
               }
             }
           }
@@ -402,6 +487,14 @@ __global__ void __launch_bounds__(NT, NQ == 1 ? 4 : 3) attend_token_kernel(const
 #pragma unroll
         for (int d = 4; d < 32; d <<= 1) z += __shfl_xor_sync(0xffffffffu, z, d);
         const int r = 8 * nq + 2 * c + e;
+        if constexpr (I8) {                            // O relative to m
+          const float f = mw[nq][e] == -INFINITY ? 1.f : exp2f(mw[nq][e] - m[nq][e]);
+#pragma unroll
+          for (int mt = 0; mt < T::MT; ++mt) {
+            o[nq][mt][e] *= f;
+            o[nq][mt][2 + e] *= f;
+          }
+        }
         if (g == 0) sm.ml[w][r] = make_float2(m[nq][e], z);
 #pragma unroll
         for (int mt = 0; mt < T::MT; ++mt)

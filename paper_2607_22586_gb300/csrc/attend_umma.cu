@@ -151,10 +151,11 @@ struct Run {
   bool two;              // the second block has rows
 };
 
-__device__ __forceinline__ bool next_run(const AttendJob& A, const AttendPlan& P, const AttendSpan& sp, int64_t& at,
+__device__ __forceinline__ bool next_run(const AttendJob& A, const AttendPlan& P, const int32_t* lens,
+                                         const AttendSpan& sp, int64_t& at,
                                          int& u, int64_t& before, Run& R) {
   while (at < sp.end) {
-    R.U = attend_unit(A, P, u);
+    R.U = attend_unit(A, P, lens, u);
     const int64_t last = before + R.U.pieces;
     if (last > at) {
       const int64_t stop = min(sp.end, last);
@@ -223,7 +224,7 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
   __shared__ uint64_t drain;
   __shared__ uint32_t tbase;
   __shared__ int abort_flag, odd_flag;
-  __shared__ AttendScan<NT> scan;
+  __shared__ AttendScan<NT, 256> scan;
   volatile int* abort_ = &abort_flag;
   const CacheJob& J = A.c;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -258,10 +259,11 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
   __syncthreads();
   fence_after();
   const uint32_t tmem = tbase;
-  dependent_start();
-  const AttendSpan sp = attend_span<NT>(A, P, &scan, [] { __syncthreads(); });
+  attend_start();
+  const AttendSpan sp = attend_span(A, P, &scan);
   int64_t at = sp.begin, before = sp.before;
   int u = sp.unit;
+  const int32_t* lens = scan.lengths(A.c);
   Run R;
   if (warp == PRODUCER) {
     // bfloat16 rows go where the MMAs read them, codes to a ring of their own
@@ -273,7 +275,7 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
     bool ok = true;
     const int shift = min(J.page_shift, 7), boxes = BK >> shift;
     const int outside = J.n_pages << J.page_shift;     // a box from there on reads zeros
-    while (ok && next_run(A, P, sp, at, u, before, R)) {
+    while (ok && next_run(A, P, lens, sp, at, u, before, R)) {
       const int32_t* table = J.table + ((size_t)R.U.b * J.Hkv + R.U.h) * J.max_pages;
       // this lane's box of a tile: its row of the pool
       auto row_of = [&](int s) {
@@ -348,7 +350,7 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
       if (elect_one()) mma_commit(bar);
       __syncwarp();
     };
-    while (ok && next_run(A, P, sp, at, u, before, R)) {
+    while (ok && next_run(A, P, lens, sp, at, u, before, R)) {
       const int nx = R.two ? 2 : 1;
       if (!wait(&full[stage], phase)) break;
       for (int x = 0; x < nx; ++x) {
@@ -402,7 +404,7 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
       int stage = 0, rs = 0, tile = 0;
       uint32_t phase = 0, rp = 0;
       bool ok = true;
-      while (ok && next_run(A, P, sp, at, u, before, R)) {
+      while (ok && next_run(A, P, lens, sp, at, u, before, R)) {
         const int32_t* table = J.table + ((size_t)R.U.b * J.Hkv + R.U.h) * J.max_pages;
         auto row_of = [&](int s) {
           const int k = s * BK + t;
@@ -458,7 +460,7 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
     uint32_t sph = 0, oph = 0, vphase = 0;
     int vstage = 0, tile = 0;                            // ring stage of the next tile's K, tiles so far
     bool ok = true;
-    while (ok && next_run(A, P, sp, at, u, before, R)) {
+    while (ok && next_run(A, P, lens, sp, at, u, before, R)) {
       const AttendUnit& U = R.U;
       const int ntiles = R.s1 - R.s0;
       if (x == 1 && !R.two) {

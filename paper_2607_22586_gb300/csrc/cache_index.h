@@ -36,17 +36,32 @@ MMSHIFT_HD int keys_of(int causal, int len, int n, int i) {
   return e > 0 ? e : 0;
 }
 
-// W pieces of work are shared out to n workers in order: worker i takes
-// [span_begin(W, n, i), span_begin(W, n, i + 1)), which differ by one piece at most.
-MMSHIFT_HD int64_t span_begin(int64_t W, int n, int i) { return W * i / n; }
+// x / y for 0 <= x, 0 < y; 64-bit division only where it is needed.
+MMSHIFT_HD int64_t quotient(int64_t x, int64_t y) {
+  if (((uint64_t)x | (uint64_t)y) >> 32) return x / y;
+  return (uint32_t)x / (uint32_t)y;
+}
 
-// The worker that has piece x.
-MMSHIFT_HD int span_of(int64_t W, int n, int64_t x) { return (int)(((x + 1) * n - 1) / W); }
+// W pieces of work shared out in order to n workers, `most` at most and each with
+// 2^least pieces where there are as many: the first `more` get base + 1, the others
+// base. Worker i has [begin(i), begin(i + 1)); of(x) is the worker that has piece x.
+struct Shares {
+  int64_t base;
+  int32_t n, more;
+  MMSHIFT_HD int64_t begin(int i) const { return base * i + (i < more ? i : more); }
+  MMSHIFT_HD int of(int64_t x) const {
+    const int64_t t = (base + 1) * more;
+    return (int)(x < t ? quotient(x, base + 1) : more + quotient(x - t, base));
+  }
+};
 
-// Workers that W pieces occupy, each with `least` pieces where there are as many.
-MMSHIFT_HD int span_workers(int64_t W, int most, int least) {
-  const int64_t n = (W + least - 1) / least;
-  return n < 1 ? 1 : n < most ? (int)n : most;
+MMSHIFT_HD Shares shares_of(int64_t W, int most, int least) {
+  const int64_t want = (W + (1 << least) - 1) >> least;
+  Shares s;
+  s.n = want < 1 ? 1 : want < most ? (int)want : most;
+  s.base = quotient(W, s.n);
+  s.more = (int)(W - s.base * s.n);
+  return s;
 }
 
 }  // namespace mmshift

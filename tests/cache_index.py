@@ -15,9 +15,10 @@ extern "C" {
 int t_range_of(const int32_t* off, int n, int x) { return range_of(off, n, x); }
 int t_page_row(int page, int n_pages, int shift, int t) { return page_row(page, n_pages, shift, t); }
 int t_keys_of(int causal, int len, int n, int i) { return keys_of(causal, len, n, i); }
-long long t_span_begin(long long W, int n, int i) { return span_begin(W, n, i); }
-int t_span_of(long long W, int n, long long x) { return span_of(W, n, x); }
-int t_span_workers(long long W, int most, int least) { return span_workers(W, most, least); }
+long long t_begin(long long W, int most, int least, int i) { return shares_of(W, most, least).begin(i); }
+int t_of(long long W, int most, int least, long long x) { return shares_of(W, most, least).of(x); }
+int t_workers(long long W, int most, int least) { return shares_of(W, most, least).n; }
+long long t_quotient(long long x, long long y) { return quotient(x, y); }
 }
 """
 
@@ -32,8 +33,8 @@ def library():
         subprocess.run([cxx, "-std=c++17", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", "-I", CSRC, src, "-o", so],
                        check=True)
         lib = ctypes.CDLL(so)
-    lib.t_span_begin.restype = ctypes.c_longlong
-    lib.t_span_begin.argtypes = [ctypes.c_longlong, ctypes.c_int, ctypes.c_int]
-    lib.t_span_of.argtypes = [ctypes.c_longlong, ctypes.c_int, ctypes.c_longlong]
-    lib.t_span_workers.argtypes = [ctypes.c_longlong, ctypes.c_int, ctypes.c_int]
+    ll, i = ctypes.c_longlong, ctypes.c_int
+    lib.t_begin.restype = lib.t_quotient.restype = ll
+    lib.t_begin.argtypes, lib.t_of.argtypes, lib.t_workers.argtypes = [ll, i, i, i], [ll, i, i, ll], [ll, i, i]
+    lib.t_quotient.argtypes = [ll, ll]
     return lib

@@ -47,20 +47,28 @@ def test_keys_of_a_token(lib):
 def test_shares_cover_all_work_once(lib):
     rng = random.Random(2)
     for _ in range(400):
-        W, n = rng.choice([1, 2, 151, 152, 1000, rng.randint(1, 3000)]), rng.choice([1, 2, 152, 456])
-        begins = [lib.t_span_begin(W, n, i) for i in range(n + 1)]
+        W, most, least = rng.choice([1, 2, 151, 152, 1000, rng.randint(1, 3000)]), rng.choice([1, 2, 152, 456]), rng.choice([0, 2])
+        n = lib.t_workers(W, most, least)
+        assert n == max(1, min(most, -(-W // 2 ** least)))
+        begins = [lib.t_begin(W, most, least, i) for i in range(n + 1)]
         assert begins[0] == 0 and begins[-1] == W
         sizes = [b - a for a, b in zip(begins, begins[1:])]
-        assert max(sizes) - min(sizes) <= 1
+        assert max(sizes) - min(sizes) <= 1 and min(sizes) >= 1
         owner = [i for i, s in enumerate(sizes) for _ in range(s)]
-        assert [lib.t_span_of(W, n, x) for x in range(W)] == owner
-    big = 2 ** 40                                    # pieces past 32 bits
-    for x in (0, 1, 2 ** 33 + 5, big - 1):
-        i = lib.t_span_of(big, 456, x)
-        assert lib.t_span_begin(big, 456, i) <= x < lib.t_span_begin(big, 456, i + 1)
+        assert [lib.t_of(W, most, least, x) for x in range(W)] == owner
+    for big in (2 ** 31 - 1, 2 ** 32 + 7, 2 ** 40):      # pieces past 32 bits
+        for x in (0, 1, 2 ** 31 - 5, big - 1):
+            i = lib.t_of(big, 456, 0, x)
+            assert lib.t_begin(big, 456, 0, i) <= x < lib.t_begin(big, 456, 0, i + 1)
 
 
-def test_workers(lib):
-    assert lib.t_span_workers(0, 152, 4) == 1
-    assert lib.t_span_workers(9, 152, 4) == 3
-    assert lib.t_span_workers(10 ** 9, 152, 4) == 152
+def test_no_work_has_one_worker(lib):
+    assert lib.t_workers(0, 152, 2) == 1
+    assert lib.t_begin(0, 152, 2, 1) == 0
+
+
+def test_quotients(lib):
+    rng = random.Random(3)
+    for _ in range(2000):
+        x, y = rng.randrange(2 ** rng.randint(1, 62)), 1 + rng.randrange(2 ** rng.randint(1, 40))
+        assert lib.t_quotient(x, y) == x // y
