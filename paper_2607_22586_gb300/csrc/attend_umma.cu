@@ -7,9 +7,10 @@
 //               shared memory as it lies in the page (keys by dimensions: the
 //               MN-major B operand), O in tensor memory for the whole run of keys.
 // Roles (384 threads, one CTA per SM):
-//   warps 0-7   softmax, one warpgroup a block, one thread a row: its maximum
-//               and sum need no reduction across threads. It reads S, writes P
-//               and, at the end of the run, O;
+//   warps 0-7   softmax, one warpgroup a block, one thread a row (its maximum and
+//               sum need no reduction across threads; over 8-bit pages four
+//               threads have four rows). They read S, write P and, at the end of
+//               the run, O;
 //   warp 8      TMA producer: a ring of K and V tiles. A page is a box of up to
 //               128 rows, so a tile is 1 to 8 boxes and 64 columns wide halves;
 //   warp 9      MMA issuer.
@@ -100,6 +101,11 @@ __device__ __forceinline__ void pin32(float* v) {
                     "+f"(v[22]), "+f"(v[23]), "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]),
                     "+f"(v[29]), "+f"(v[30]), "+f"(v[31]));
 }
+__device__ __forceinline__ void pin16(float* v) {
+  asm volatile("" : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]),
+                    "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]),
+                    "+f"(v[15]));
+}
 __device__ __forceinline__ void st16(uint32_t taddr, const uint32_t* v) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
@@ -107,6 +113,22 @@ __device__ __forceinline__ void st16(uint32_t taddr, const uint32_t* v) {
       "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
       "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
       : "memory");
+}
+// 16 lanes by 32 columns, spread as an MMA's accumulator: v[4k], v[4k + 1] are row
+// lane / 4, columns 8k + 2 (lane % 4) and the next; v[4k + 2], v[4k + 3] row lane / 4 + 8.
+__device__ __forceinline__ void ld_quads(uint32_t taddr, float* v) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.16x256b.x4.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]),
+        "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
+      : "r"(taddr));
+}
+// 16 lanes by 16 columns: w[2k] is row lane / 4, column 4k + lane % 4, w[2k + 1] row lane / 4 + 8.
+__device__ __forceinline__ void st_quads(uint32_t taddr, const uint32_t* w) {
+  asm volatile("tcgen05.st.sync.aligned.16x128b.x4.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(w[0]),
+               "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+               : "memory");
 }
 __device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
@@ -363,27 +385,25 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
       if (!ok) break;
       commit(&empty[stage]);
       step();
+      for (int x = 0; x < nx; ++x) {                   // the last run's O has been read
+        if (!wait(&o_free[x], (of >> x) ^ 1u)) break;
+        of ^= 1u << x;
+      }
       for (int s = R.s0; ok && s < R.s1; ++s) {
+        // V of this tile and K of the next are there long before the weights are
         const int vst = stage;
         if (!wait(&full[vst], phase)) break;
         step();
         const bool more = s + 1 < R.s1;
+        if (more && !wait(&full[stage], phase)) break;
         for (int x = 0; x < nx; ++x) {
-          if (s == R.s0) {                             // the last run's O has been read
-            if (!wait(&o_free[x], (of >> x) ^ 1u)) break;
-            of ^= 1u << x;
-          }
           if (!wait(&p_ready[x], pp >> x)) break;
           pp ^= 1u << x;
           fence_after();
           issue_o(x, vst, s > R.s0);
           if (x == nx - 1) commit(&empty[vst]);
-          if (more) {
-            if (x == 0 && !wait(&full[stage], phase)) break;
-            issue_s(x, stage);
-          } else {
-            commit(&o_ready[x]);
-          }
+          if (more) issue_s(x, stage);
+          else commit(&o_ready[x]);
         }
         if (!ok) break;
         if (more) {
@@ -474,19 +494,28 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
       const bool live = brow < U.rows;
       const int tok = row / J.r, j = row - tok * J.r;
       {
-        const uint8_t* q = A.q + ((size_t)(J.off[U.b] + (live ? tok : 0)) * J.stride + (size_t)(U.h * J.r + j) * D) * 2;
-        unsigned char* dst = sm + x * SM::TILE + lrow * 128;
+        // the warp's 32 rows, LPR lanes a row; a row's offset comes from the lane that owns it
+        constexpr int LPR = D / 8;
+        const int64_t off = live ? ((int64_t)(J.off[U.b] + tok) * J.stride + (int64_t)(U.h * J.r + j) * D) * 2 : -1;
+        unsigned char* dst = sm + x * SM::TILE + warp % 4 * 32 * 128;
+        auto put = [&](int i, bool vec) {
+          const int r = i * (32 / LPR) + lane / LPR, ch = lane % LPR;
+          const int64_t o = __shfl_sync(0xffffffffu, off, r);
+          const uint4 w = o >= 0 ? load_plain16(A.q + o + ch * 16, vec) : make_uint4(0, 0, 0, 0);
+          *reinterpret_cast<uint4*>(dst + (ch / 8) * SM::HALF + r * 128 + ((ch % 8) ^ (r % 8)) * 16) = w;
+        };
+        if (A.qvec) {
 #pragma unroll
-        for (int i = 0; i < D / 8; ++i) {
-          const uint4 w = live ? load_plain16(q + i * 16, A.qvec) : make_uint4(0, 0, 0, 0);
-          *reinterpret_cast<uint4*>(dst + (i / 8) * SM::HALF + ((i % 8) ^ (lrow % 8)) * 16) = w;
+          for (int i = 0; i < LPR; ++i) put(i, true);
+        } else {
+#pragma unroll 1
+          for (int i = 0; i < LPR; ++i) put(i, false);
         }
         fence_async();
         __syncwarp();
         if (lane == 0) mbar_arrive(&q_ready[x]);
       }
       const int32_t* table = J.table + ((size_t)U.b * J.Hkv + U.h) * J.max_pages;
-      const int lim = live ? keys_of(A.causal, U.len, U.n, tok) : 0;
       const int least = keys_of(A.causal, U.len, U.n, U.row0 / J.r);   // keys that every row attends to
       // bit i: the tile's 16-key block i has no page
       auto gone_of = [&](int s) {
@@ -496,7 +525,30 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
         return __ballot_sync(0xffffffffu, g);
       };
       uint32_t next = gone_of(R.s0);
-      float m = -INFINITY, l = 0.f;
+      // bfloat16 pages: the thread's row. 8-bit pages: rows g + 8i of the warp's 32, with
+      // the lanes of a quad sharing them (and their sums).
+      constexpr int NR = I8 ? 4 : 1;
+      const int g = lane / 4, c = lane % 4;
+      float m[NR], l[NR];
+      int lim[NR];
+#pragma unroll
+      for (int i = 0; i < NR; ++i) {
+        m[i] = -INFINITY;
+        l[i] = 0.f;
+        const int r = U.row0 + x * BQ + (I8 ? warp % 4 * 32 + g + 8 * i : lrow);
+        lim[i] = r < U.row0 + U.rows ? keys_of(A.causal, U.len, U.n, r / J.r) : 0;
+      }
+      // a value of the thread's row, of those that the quads hold
+      auto of_row = [&](const float* v) {
+        if constexpr (!I8) return v[0];
+        float got = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float w = __shfl_sync(0xffffffffu, v[I8 ? i : 0], lane % 8 * 4);
+          if (lane / 8 == i) got = w;
+        }
+        return got;
+      };
       for (int s = R.s0; s < R.s1; ++s) {
         const uint32_t gone = next;
         next = gone_of(s + 1);
@@ -506,6 +558,25 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
         int vs = vstage + 1;
         uint32_t vp = vphase;
         if (vs == SM::STAGES) { vs = 0; vp ^= 1u; }
+        if (!I8 && special && x == 0) {
+          // the first block's threads clean V: both blocks' products with it are
+          // issued after this block's P has been reported ready
+          if (!mbar_wait_warp(&full[vs], vp, abort_)) { ok = false; break; }
+          unsigned char* vt = ring + vs * SM::TILE;
+          constexpr int CH = SM::HALVES * 8;             // 16-byte chunks of a row
+          bool odd = false;
+#pragma unroll 4
+          for (int i = max(least - k0, 0) * CH + threadIdx.x; i < BK * CH; i += 128) {
+            const int key = i / CH, ch = i % CH;
+            uint4* p = reinterpret_cast<uint4*>(vt + (ch / 8) * SM::HALF + key * 128 + (ch % 8) * 16);
+            const uint4 w = k0 + key < U.keys ? *p : make_uint4(0, 0, 0, 0);
+            const bool bad = not_finite2(w.x) || not_finite2(w.y) || not_finite2(w.z) || not_finite2(w.w);
+            odd |= bad;
+            if (bad || k0 + key >= U.keys) *p = make_uint4(finite2(w.x), finite2(w.y), finite2(w.z), finite2(w.w));
+          }
+          if (odd) *reinterpret_cast<volatile int*>(&odd_flag) = 1;
+          fence_async();
+        }
         if (!mbar_wait_warp(&s_ready[x], sph, abort_)) { ok = false; break; }
         sph ^= 1u;
         // 8-bit pages: the tile's scales were written before its V was
@@ -513,15 +584,27 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
         fence_after();
         const bool masked = special || gone;
         if (gone && warp == 0 && lane == 0) set_status(J.status, kStatusBadPage);
-        auto hidden = [&](int i) { return k0 + i >= lim || ((gone >> (i / 16)) & 1u); };
-        // raises the maximum to `top` (base 2) where some row's passes it by enough
-        auto raise = [&](float top) {
-          if (!__any_sync(0xffffffffu, top > m + kRaise)) return;
-          const float mn = fmaxf(m, top);
-          const float f = m == -INFINITY ? 0.f : fast_exp2(m - mn);
-          m = mn;
-          l *= f;
+        auto hidden = [&](int i, int r) { return k0 + i >= lim[r] || ((gone >> (i / 16)) & 1u); };
+        // raises the maxima to `top` (base 2) where some row's passes them by enough
+        auto raise = [&](float (&top)[NR]) {
+          bool over = false;
+#pragma unroll
+          for (int i = 0; i < NR; ++i) over |= top[i] > m[i] + kRaise;
+          if (!__any_sync(0xffffffffu, over)) return;
+          float f[NR];
+#pragma unroll
+          for (int i = 0; i < NR; ++i) {
+            if constexpr (I8) {
+              top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
+              top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
+            }
+            const float mn = fmaxf(m[i], top[i]);
+            f[i] = m[i] == -INFINITY ? 0.f : fast_exp2(m[i] - mn);
+            m[i] = mn;
+            l[i] *= f[i];
+          }
           if (s == R.s0) return;
+          const float fr = of_row(f);
 #pragma unroll 1
           for (int i = 0; i < D; i += 16) {
             float o[16];
@@ -529,130 +612,162 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
             tmem_wait_ld16(o);
             uint32_t w[16];
 #pragma unroll
-            for (int c = 0; c < 16; ++c) w[c] = __float_as_uint(o[c] * f);
+            for (int k = 0; k < 16; ++k) w[k] = __float_as_uint(o[k] * fr);
             st16(ocol + i, w);
           }
         };
-        uint64_t sum2[2] = {pk2(0.f, 0.f), pk2(0.f, 0.f)};
         if constexpr (!I8) {
-          float v[BK];
+          uint64_t sum2[2] = {pk2(0.f, 0.f), pk2(0.f, 0.f)};
+          const uint64_t al2 = pk2(A.alpha, A.alpha);
+          auto weights = [&](const float* v, float mu, uint32_t* w) {   // 32 columns
+            const uint64_t mu2 = pk2(-mu, -mu);
 #pragma unroll
-          for (int i = 0; i < BK; i += 32) ld32(scol + i, v + i);
-          tmem_wait_ld();
-#pragma unroll
-          for (int i = 0; i < BK; i += 32) pin32(v + i);
-          if (masked) {
-#pragma unroll
-            for (int i = 0; i < BK; ++i)
-              if (hidden(i)) v[i] = -INFINITY;
-          }
-          raise(max_of<BK>(v) * A.alpha);
-          const float mu = m == -INFINITY ? 0.f : m;
-          const uint64_t al2 = pk2(A.alpha, A.alpha), mu2 = pk2(-mu, -mu);
-#pragma unroll
-          for (int i = 0; i < BK; i += 32) {
-            uint32_t w[16];
-#pragma unroll
-            for (int c = 0; c < 16; ++c) {
+            for (int k = 0; k < 16; ++k) {
               float a, b;
-              upk2(ffma2(pk2(v[i + 2 * c], v[i + 2 * c + 1]), al2, mu2), a, b);
+              upk2(ffma2(pk2(v[2 * k], v[2 * k + 1]), al2, mu2), a, b);
               a = fast_exp2(a);
               b = fast_exp2(b);
-              sum2[c % 2] = fadd2(sum2[c % 2], pk2(a, b));
-              w[c] = pack_bf16(a, b);
+              sum2[k % 2] = fadd2(sum2[k % 2], pk2(a, b));
+              w[k] = pack_bf16(a, b);
             }
-            st16(scol + i / 2, w);
+          };
+          if (!masked) {
+            float v[BK];
+#pragma unroll
+            for (int i = 0; i < BK; i += 32) ld32(scol + i, v + i);
+            tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < BK; i += 32) pin32(v + i);
+            float top[1] = {max_of<BK>(v) * A.alpha};
+            raise(top);
+            const float mu = m[0] == -INFINITY ? 0.f : m[0];
+#pragma unroll
+            for (int i = 0; i < BK; i += 32) {
+              uint32_t w[16];
+              weights(v + i, mu, w);
+              st16(scol + i / 2, w);
+            }
+          } else {
+            // few tiles: a short loop, which reads S twice (its code is fetched once a call)
+            float v[32], top[1] = {-INFINITY};
+            auto load = [&](int i) {
+              ld32(scol + i, v);
+              tmem_wait_ld();
+              pin32(v);
+              const uint32_t none = gone >> (i / 16);
+              const int n = lim[0] - (k0 + i);
+#pragma unroll
+              for (int k = 0; k < 32; ++k)
+                if (k >= n || ((none >> (k / 16)) & 1u)) v[k] = -INFINITY;
+            };
+#pragma unroll 1
+            for (int i = 0; i < BK; i += 32) {
+              load(i);
+              top[0] = fmaxf(top[0], max_of<32>(v) * A.alpha);
+            }
+            raise(top);
+            const float mu = m[0] == -INFINITY ? 0.f : m[0];
+#pragma unroll 1
+            for (int i = 0; i < BK; i += 32) {
+              load(i);
+              uint32_t w[16];
+              weights(v, mu, w);
+              st16(scol + i / 2, w);
+            }
           }
+          float a, b;
+          upk2(fadd2(sum2[0], sum2[1]), a, b);
+          l[0] += a + b;
         } else {
-          // 512 threads leave 128 registers: S is read twice, for the maximum and for the
-          // weights. K's scales (times alpha) go with the logits, V's with the weights.
-          const float4* sk = reinterpret_cast<const float4*>(scales[tile % SM::SCALES][0]);
-          const float4* sv = reinterpret_cast<const float4*>(scales[tile % SM::SCALES][1]);
-          float top = -INFINITY;
-#pragma unroll
-          for (int i = 0; i < BK; i += 32) {
-            float v[32];
-            ld32(scol + i, v);
+          // A thread of a quad has a fourth of the columns of four rows, so it reads a fourth of
+          // the scales from shared memory (with whole rows, 3 KB a thread and tile, that took
+          // longer than the products). S is read twice, for the maxima and for the weights: 512
+          // threads leave 128 registers. K's scales hold alpha; V's go with the weights.
+          const float2* sk = reinterpret_cast<const float2*>(scales[tile % SM::SCALES][0]) + c;
+          const float2* sv = reinterpret_cast<const float2*>(scales[tile % SM::SCALES][1]) + c;
+          float v[2][16], top[NR];
+          auto load = [&](int i) {
+            ld_quads(scol + i, v[0]);
+            ld_quads(scol + i + (16u << 16), v[1]);
             tmem_wait_ld();
-            pin32(v);
+            pin16(v[0]);
+            pin16(v[1]);
+          };
+          auto pair = [&](int r, int k) { return pk2(v[r / 2][4 * k + 2 * (r % 2)], v[r / 2][4 * k + 2 * (r % 2) + 1]); };
+          uint64_t mu2[NR], sum2[NR];
+          auto maxima = [&](auto mask) {
+#pragma unroll 1
+            for (int i = 0; i < BK; i += 32) {
+              load(i);
 #pragma unroll
-            for (int c = 0; c < 32; c += 4) {
-              const float4 f = sk[(i + c) / 4];
-              upk2(fmul2(pk2(v[c], v[c + 1]), pk2(f.x, f.y)), v[c], v[c + 1]);
-              upk2(fmul2(pk2(v[c + 2], v[c + 3]), pk2(f.z, f.w)), v[c + 2], v[c + 3]);
-            }
-            if (masked) {
+              for (int k = 0; k < 4; ++k) {
+                const float2 f = sk[i / 2 + 4 * k];
 #pragma unroll
-              for (int c = 0; c < 32; ++c)
-                if (hidden(i + c)) v[c] = -INFINITY;
+                for (int r = 0; r < 4; ++r) {
+                  float a, b;
+                  upk2(fmul2(pair(r, k), pk2(f.x, f.y)), a, b);
+                  if constexpr (decltype(mask)::value) {
+                    if (hidden(i + 8 * k + 2 * c, r)) a = -INFINITY;
+                    if (hidden(i + 8 * k + 2 * c + 1, r)) b = -INFINITY;
+                  }
+                  top[r] = fmaxf(top[r], fmaxf(a, b));
+                }
+              }
             }
-            top = fmaxf(top, max_of<32>(v));
-          }
+          };
+          auto weights = [&](auto mask) {
+#pragma unroll 1
+            for (int i = 0; i < BK; i += 32) {
+              load(i);
+              uint32_t w[2][8];
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const float2 f = sk[i / 2 + 4 * k], h = sv[i / 2 + 4 * k];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                  float a, b;
+                  upk2(ffma2(pair(r, k), pk2(f.x, f.y), mu2[r]), a, b);
+                  a = fast_exp2(a);
+                  b = fast_exp2(b);
+                  bool ha = false, hb = false;
+                  if constexpr (decltype(mask)::value) {
+                    ha = hidden(i + 8 * k + 2 * c, r);
+                    hb = hidden(i + 8 * k + 2 * c + 1, r);
+                    if (ha) a = 0.f;
+                    if (hb) b = 0.f;
+                  }
+                  sum2[r] = fadd2(sum2[r], pk2(a, b));
+                  upk2(fmul2(pk2(a, b), pk2(h.x, h.y)), a, b);
+                  if (ha) a = 0.f;                     // a scale that no row may see can be a NaN
+                  if (hb) b = 0.f;
+                  w[r / 2][2 * k + r % 2] = pack_bf16(a, b);
+                }
+              }
+              st_quads(scol + i / 2, w[0]);
+              st_quads(scol + i / 2 + (16u << 16), w[1]);
+            }
+          };
+#pragma unroll
+          for (int r = 0; r < NR; ++r) top[r] = -INFINITY;
+          if (masked) maxima(std::true_type());
+          else maxima(std::false_type());
           raise(top);
-          const float mu = m == -INFINITY ? 0.f : m;
-          const uint64_t mu2 = pk2(-mu, -mu);
 #pragma unroll
-          for (int i = 0; i < BK; i += 32) {
-            float v[32];
-            ld32(scol + i, v);
-            tmem_wait_ld();
-            pin32(v);
-            uint32_t w[16];
+          for (int r = 0; r < NR; ++r) {
+            const float mu = m[r] == -INFINITY ? 0.f : m[r];
+            mu2[r] = pk2(-mu, -mu);
+            sum2[r] = pk2(0.f, 0.f);
+          }
+          if (masked) weights(std::true_type());
+          else weights(std::false_type());
 #pragma unroll
-            for (int c = 0; c < 32; c += 4) {
-              const float4 f = sk[(i + c) / 4], g = sv[(i + c) / 4];
-              float e[4];
-              upk2(ffma2(pk2(v[c], v[c + 1]), pk2(f.x, f.y), mu2), e[0], e[1]);
-              upk2(ffma2(pk2(v[c + 2], v[c + 3]), pk2(f.z, f.w), mu2), e[2], e[3]);
-#pragma unroll
-              for (int k = 0; k < 4; ++k) e[k] = fast_exp2(e[k]);
-              if (masked) {
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                  if (hidden(i + c + k)) e[k] = 0.f;
-              }
-              sum2[0] = fadd2(sum2[0], pk2(e[0], e[1]));
-              sum2[1] = fadd2(sum2[1], pk2(e[2], e[3]));
-              upk2(fmul2(pk2(e[0], e[1]), pk2(g.x, g.y)), e[0], e[1]);
-              upk2(fmul2(pk2(e[2], e[3]), pk2(g.z, g.w)), e[2], e[3]);
-              if (masked) {                            // a scale that no row may see can be a NaN
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                  if (hidden(i + c + k)) e[k] = 0.f;
-              }
-              w[c / 2] = pack_bf16(e[0], e[1]);
-              w[c / 2 + 1] = pack_bf16(e[2], e[3]);
-            }
-            st16(scol + i / 2, w);
+          for (int r = 0; r < NR; ++r) {
+            float a, b;
+            upk2(sum2[r], a, b);
+            l[r] += a + b;
           }
         }
         ++tile;
-        float a, b;
-        upk2(fadd2(sum2[0], sum2[1]), a, b);
-        l += a + b;
-        if (!I8 && special && x == 0) {
-          // the first block's threads clean V: both blocks' products with it are
-          // issued after this block's P has been reported ready
-          if (!mbar_wait_warp(&full[vs], vp, abort_)) { ok = false; break; }
-          unsigned char* vt = ring + vs * SM::TILE;
-          bool odd = false;
-          for (int i = threadIdx.x; i < BK * SM::HALVES * 8; i += 128) {
-            const int key = i / (SM::HALVES * 8), ch = i % (SM::HALVES * 8);
-            if (k0 + key < least) continue;
-            uint4* p = reinterpret_cast<uint4*>(vt + (ch / 8) * SM::HALF + key * 128 + (ch % 8) * 16);
-            if (k0 + key >= U.keys) {
-              *p = make_uint4(0, 0, 0, 0);
-              continue;
-            }
-            const uint4 w = *p;
-            if (not_finite2(w.x) || not_finite2(w.y) || not_finite2(w.z) || not_finite2(w.w)) {
-              odd = true;
-              *p = make_uint4(finite2(w.x), finite2(w.y), finite2(w.z), finite2(w.w));
-            }
-          }
-          if (odd) *reinterpret_cast<volatile int*>(&odd_flag) = 1;
-          fence_async();
-        }
         vstage = vs + 1;
         vphase = vp;
         if (vstage == SM::STAGES) { vstage = 0; vphase ^= 1u; }
@@ -664,51 +779,75 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
       if (!ok || !mbar_wait_warp(&o_ready[x], oph, abort_)) { ok = false; break; }
       oph ^= 1u;
       fence_after();
+      if constexpr (I8) {
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+          l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
+          l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
+        }
+      }
+      const float lr = of_row(l), mr = of_row(m);
       const bool fix = !I8 && *reinterpret_cast<volatile int*>(&odd_flag) != 0;
       const bool whole = R.s0 == 0 && R.s1 == U.pieces;
-      const float f = l == 0.f ? 0.f : 1.f / l;
-      const size_t orow = (size_t)(J.off[U.b] + tok) * J.Hq + U.h * J.r + j;
-      const size_t slot = (size_t)attend_slot(blockIdx.x, sp.begin, R.before) * P.rows + brow;
+      const float f = lr == 0.f ? 0.f : 1.f / lr;
+      const int64_t orow = (int64_t)(J.off[U.b] + tok) * J.Hq + U.h * J.r + j;
+      const int64_t slot = (int64_t)attend_slot(blockIdx.x, sp.begin, R.before) * P.rows + brow;
+      // Rows leave by way of the block's place for Q, which no product reads any more: a
+      // thread puts 16-byte chunks of its row there, then 2 * D bytes of a row at a time
+      // (all of it, or half of its float32 sums) go out by consecutive lanes.
+      constexpr int LPR = D / 8;
+      unsigned char* mine = sm + x * SM::TILE + warp % 4 * 32 * 128;   // the warp's rows of Q
+      auto chunk = [&](int r, int ch) {
+        return reinterpret_cast<uint4*>(mine + (ch / 8) * SM::HALF + r * 128 + ((ch % 8) ^ (r % 8)) * 16);
+      };
+      const int64_t to = live ? (whole ? orow : slot) : -1;
+      auto flush = [&](int half) {
+        __syncwarp();
+#pragma unroll 2
+        for (int i = 0; i < LPR; ++i) {
+          const int r = i * (32 / LPR) + lane / LPR, ch = lane % LPR;
+          const int64_t t = __shfl_sync(0xffffffffu, to, r);
+          const uint4 w = *chunk(r, ch);
+          if (t < 0) continue;
+          if (whole) store_row16(A.out + t * (2 * D) + ch * 16, w, A.ovec);
+          else *reinterpret_cast<uint4*>(reinterpret_cast<uint8_t*>(P.po + t * D) + half * (2 * D) + ch * 16) = w;
+        }
+        __syncwarp();
+      };
 #pragma unroll 1
       for (int i = 0; i < D; i += 32) {
         float o[32];
         ld32(ocol + i, o);
         tmem_wait_ld();
         pin32(o);
-        if (!live) continue;
-        if (fix) {
+        if (fix && live) {
           float t[32];
 #pragma unroll
           for (int c = 0; c < 32; ++c) t[c] = o[c];
-          add_not_finite<D>(A, R, row, lim, m == -INFINITY ? 0.f : m, i, t);
+          add_not_finite<D>(A, R, row, lim[0], mr == -INFINITY ? 0.f : mr, i, t);
 #pragma unroll
           for (int c = 0; c < 32; ++c) o[c] = t[c];
         }
         if (whole) {
-          __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(A.out) + orow * D + i;
           uint32_t w[16];
 #pragma unroll
-          for (int c = 0; c < 16; ++c) w[c] = l == 0.f ? 0u : pack_bf16(o[2 * c] * f, o[2 * c + 1] * f);
-          if (A.ovec) {
+          for (int c = 0; c < 16; ++c) w[c] = lr == 0.f ? 0u : pack_bf16(o[2 * c] * f, o[2 * c + 1] * f);
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
-              reinterpret_cast<uint4*>(out)[c] = make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
-          } else {
-#pragma unroll
-            for (int c = 0; c < 16; ++c) {
-              reinterpret_cast<uint16_t*>(out)[2 * c] = (uint16_t)w[c];
-              reinterpret_cast<uint16_t*>(out)[2 * c + 1] = (uint16_t)(w[c] >> 16);
-            }
-          }
+          for (int c = 0; c < 4; ++c)
+            *chunk(lane, i / 8 + c) = make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
         } else {
-          float4* p = reinterpret_cast<float4*>(P.po + slot * D + i);
 #pragma unroll
-          for (int c = 0; c < 8; ++c) p[c] = make_float4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
+          for (int c = 0; c < 8; ++c)
+            *chunk(lane, i % (D / 2) / 4 + c) =
+                make_uint4(__float_as_uint(o[4 * c]), __float_as_uint(o[4 * c + 1]), __float_as_uint(o[4 * c + 2]),
+                           __float_as_uint(o[4 * c + 3]));
+          if ((i + 32) % (D / 2) == 0) flush(i >= D / 2);
         }
       }
+      if (whole) flush(0);
       if (live) {
-        if (!whole) P.pml[slot] = make_float2(m, l);
-        else if (A.lse) A.lse[orow] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+        if (!whole) P.pml[slot] = make_float2(mr, lr);
+        else if (A.lse) A.lse[orow] = lr == 0.f ? -INFINITY : (mr + log2f(lr)) * 0.6931471805599453f;
       }
       fence_before();
       __syncwarp();
