@@ -150,6 +150,7 @@ AttendPlan plan_of(const CacheJob& J, int most, Take take) {
   for (int b = 0; b < J.B; ++b) {
     const int rows = (J.off[b + 1] - J.off[b]) * J.r;
     P.tiles[b] = rows && take(rows) ? (rows + P.rows - 1) / P.rows : 0;
+    P.by_tiles[b] = divisor_of(P.tiles[b]);
     P.uoff[b + 1] = P.uoff[b] + J.Hkv * P.tiles[b];
   }
   return P;

@@ -17,6 +17,7 @@ namespace mmshift {
 struct AttendPlan {
   int32_t uoff[MMSHIFT_MAX_BATCH + 1];  // units, prefix over requests
   int32_t tiles[MMSHIFT_MAX_BATCH];     // a request's row tiles per KV head
+  Divisor by_tiles[MMSHIFT_MAX_BATCH];
   int32_t rows;                         // query rows of a tile
   int32_t step_shift;
   int32_t workers, least;               // workers at most; one has 2^least pieces where there are as many
@@ -45,12 +46,12 @@ __device__ __forceinline__ AttendUnit attend_unit(const AttendJob& A, const Atte
   x.b = range_of(P.uoff, J.B, u);
   x.n = J.off[x.b + 1] - J.off[x.b];
   const int all = x.n * J.r, tiles = P.tiles[x.b], rem = u - P.uoff[x.b];
-  x.h = tiles == 1 ? rem : rem / tiles;
+  x.h = P.by_tiles[x.b](rem);
   x.row0 = (rem - x.h * tiles) * P.rows;
   x.rows = min(P.rows, all - x.row0);
   const int seq = x.b * J.Hkv + x.h;
   x.len = lens ? lens[seq] : cache_len(J, seq);
-  x.keys = keys_of(A.causal, x.len, x.n, (x.row0 + x.rows - 1) / J.r);
+  x.keys = keys_of(A.causal, x.len, x.n, J.by_r(x.row0 + x.rows - 1));
   x.pieces = (x.keys + (1 << P.step_shift) - 1) >> P.step_shift;
   return x;
 }
@@ -119,7 +120,7 @@ __device__ __forceinline__ AttendSpan attend_span(const AttendJob& A, const Atte
   if (begin >= x.before && begin < x.before + x.sum) {
     int u = x.u0;
     int64_t a = x.before;
-    for (;;) {
+    while (x.u1 - x.u0 > 1) {
       const int p = attend_unit(A, P, s->lengths(A.c), u).pieces;
       if (a + p > begin) break;
       a += p;
@@ -142,7 +143,7 @@ template <typename T, int D>
 __device__ __forceinline__ void attend_write(const AttendJob& A, int b, int h, int row, int d0, float4 v, float top,
                                              float z) {
   const CacheJob& J = A.c;
-  const int tok = row / J.r;
+  const int tok = J.by_r(row);
   const size_t at = (size_t)(J.off[b] + tok) * J.Hq + h * J.r + row - tok * J.r;
   const float f = z == 0.f ? 0.f : 1.f / z;
   T* out = reinterpret_cast<T*>(A.out) + at * D + d0;

@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(NT, TR >= 4 ? 2 : 3) attend_simt_kernel(const 
       const int r = i / (D / 4), d0 = i % (D / 4) * 4;
       uint4 w = make_uint4(0, 0, 0, 0);
       if (r < U.rows) {
-        const int tok = (U.row0 + r) / J.r, j = U.row0 + r - tok * J.r;
+        const int tok = J.by_r(U.row0 + r), j = U.row0 + r - tok * J.r;
         w = load_plain16(A.q + ((size_t)(J.off[U.b] + tok) * J.stride + (size_t)(U.h * J.r + j) * D + d0) * 4, A.qvec);
       }
       *reinterpret_cast<uint4*>(&sm.q[r][d0]) = w;
@@ -83,11 +83,11 @@ __global__ void __launch_bounds__(NT, TR >= 4 ? 2 : 3) attend_simt_kernel(const 
     for (int i = 0; i < TR; ++i) {
       m[i] = -INFINITY;
       l[i] = 0.f;
-      lim[i] = keys_of(A.causal, U.len, U.n, (U.row0 + min(ty * TR + i, U.rows - 1)) / J.r);
+      lim[i] = keys_of(A.causal, U.len, U.n, J.by_r(U.row0 + min(ty * TR + i, U.rows - 1)));
 #pragma unroll
       for (int c = 0; c < D / 64; ++c) o[i][c][0] = o[i][c][1] = pk2(0.f, 0.f);
     }
-    const int least = keys_of(A.causal, U.len, U.n, U.row0 / J.r);
+    const int least = keys_of(A.causal, U.len, U.n, J.by_r(U.row0));
 
     // A thread brings 16 bytes of every (16 * NT / row bytes)-th key.
     constexpr int ROWB = I8 ? D : 4 * D, LPR = ROWB / 16, STEP = NT / LPR;   // lanes of a row, keys a round

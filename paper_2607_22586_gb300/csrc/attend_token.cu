@@ -267,7 +267,7 @@ __global__ void __launch_bounds__(NT, NQ == 1 ? 3 : 2) attend_token_kernel(const
     for (int nq = 0; nq < NQ; ++nq) {
       const int row = 8 * nq + g;
       const bool in = row < U.rows;
-      const int tok = in ? row / J.r : 0, j = in ? row - tok * J.r : 0;
+      const int tok = in ? J.by_r(row) : 0, j = in ? row - tok * J.r : 0;
       const uint8_t* p = A.q + ((size_t)(J.off[U.b] + tok) * J.stride + (size_t)(U.h * J.r + j) * D) * 2;
 #pragma unroll
       for (int i = 0; i < 2 * T::KS / 4; ++i) {
@@ -311,7 +311,7 @@ __global__ void __launch_bounds__(NT, NQ == 1 ? 3 : 2) attend_token_kernel(const
       for (int e = 0; e < 2; ++e) {
         m[nq][e] = -INFINITY;
         l[nq][e] = 0.f;
-        lim[nq][e] = keys_of(A.causal, U.len, U.n, min(8 * nq + 2 * c + e, U.rows - 1) / J.r);
+        lim[nq][e] = keys_of(A.causal, U.len, U.n, J.by_r(min(8 * nq + 2 * c + e, U.rows - 1)));
 #pragma unroll
         for (int mt = 0; mt < T::MT; ++mt) o[nq][mt][e] = o[nq][mt][2 + e] = 0.f;
       }

@@ -6,14 +6,15 @@
 //   O += P V    [128 x d]    P in tensor memory, over the columns of its S, V in
 //               shared memory as it lies in the page (keys by dimensions: the
 //               MN-major B operand), O in tensor memory for the whole run of keys.
-// Roles (384 threads, one CTA per SM):
+// Roles (384 threads, 512 over 8-bit pages, one CTA per SM):
 //   warps 0-7   softmax, one warpgroup a block, one thread a row (its maximum and
 //               sum need no reduction across threads; over 8-bit pages four
 //               threads have four rows). They read S, write P and, at the end of
 //               the run, O;
 //   warp 8      TMA producer: a ring of K and V tiles. A page is a box of up to
 //               128 rows, so a tile is 1 to 8 boxes and 64 columns wide halves;
-//   warp 9      MMA issuer.
+//   warp 9      MMA issuer;
+//   warps 12-15 (8-bit pages) make codes bfloat16.
 // The blocks alternate: while one block's softmax runs, the tensor cores have
 // the other block's products. A row's maximum is only raised when a logit passes it
 // by 8 (base 2); then the thread rescales its row of O itself, which is idle at
@@ -165,6 +166,12 @@ __device__ __forceinline__ float max_of(const float* v) {
   return fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
 }
 
+// A converged warp's wait, as umma.cuh's, without a vote a poll (2 % of a long chunk).
+__device__ __forceinline__ bool wait_bar(uint64_t* bar, uint32_t parity, volatile int* abort) {
+  const bool ok = mbar_try_wait_fast(bar, parity) || mbar_wait(bar, parity, abort);
+  return __all_sync(0xffffffffu, ok);
+}
+
 // A role's walk over the CTA's runs of keys.
 struct Run {
   AttendUnit U;
@@ -206,10 +213,10 @@ static __device__ __noinline__ void add_not_finite(const AttendJob& A, const Run
                                                    float* o) {
   const CacheJob& J = A.c;
   const size_t seq = (size_t)R.U.b * J.Hkv + R.U.h;
-  const int tok = row / J.r, j = row - tok * J.r;
+  const int tok = J.by_r(row), j = row - tok * J.r;
   const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(A.q) +
                            (size_t)(J.off[R.U.b] + tok) * J.stride + (size_t)(R.U.h * J.r + j) * D;
-  const int first = keys_of(A.causal, R.U.len, R.U.n, R.U.row0 / J.r);
+  const int first = keys_of(A.causal, R.U.len, R.U.n, J.by_r(R.U.row0));
   for (int t = max(R.s0 * BK, first / BK * BK); t < min(R.s1 * BK, lim); ++t) {
     const int64_t slot = cache_slot(J, seq, t);
     if (slot < 0) continue;
@@ -242,8 +249,8 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
   unsigned char* raw = ring + SM::STAGES * SM::TILE;
   __shared__ uint64_t rfull[I8 ? SM::RAWS : 1], rempty[I8 ? SM::RAWS : 1];
   __shared__ alignas(16) float scales[I8 ? SM::SCALES : 1][2][I8 ? BK : 1];   // K's (times alpha) and V's
-  __shared__ uint64_t full[SM::STAGES], empty[SM::STAGES], q_ready[2], s_ready[2], p_ready[2], o_ready[2], o_free[2];
-  __shared__ uint64_t drain;
+  __shared__ uint64_t full[SM::STAGES], empty[SM::STAGES], q_ready[2], s_ready[2], o_ready[2], o_free[2];
+  __shared__ uint64_t p_ready[2], drain;
   __shared__ uint32_t tbase;
   __shared__ int abort_flag, odd_flag;
   __shared__ AttendScan<NT, 256> scan;
@@ -300,19 +307,18 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
     while (ok && next_run(A, P, lens, sp, at, u, before, R)) {
       const int32_t* table = J.table + ((size_t)R.U.b * J.Hkv + R.U.h) * J.max_pages;
       // this lane's box of a tile: its row of the pool
-      auto row_of = [&](int s) {
+      auto entry_of = [&](int s) {
         const int t = s * BK + (lane << shift);
-        if (lane >= boxes || s >= R.s1 || t >= R.U.keys) return outside;
-        const int row = page_row(table[t >> J.page_shift], J.n_pages, J.page_shift, t);
-        return row < 0 ? outside : row;
+        return lane < boxes && s < R.s1 && t < R.U.keys ? table[t >> J.page_shift] : -1;
       };
-      int next = row_of(R.s0);
+      int next = entry_of(R.s0);
       for (int s = R.s0; ok && s < R.s1; ++s) {
-        const int row = next;
-        next = row_of(s + 1);                          // read a tile ahead
+        const int got_row = page_row(next, J.n_pages, J.page_shift, s * BK + (lane << shift));
+        const int row = got_row < 0 ? outside : got_row;
+        next = entry_of(s + 1);                        // read a tile ahead
 #pragma unroll
         for (int kv = 0; kv < 2; ++kv) {
-          if (!mbar_wait_warp(&room[stage], phase ^ 1u, abort_)) { ok = false; break; }
+          if (!wait_bar(&room[stage], phase ^ 1u, abort_)) { ok = false; break; }
           if (lane == 0) mbar_expect_tx(&got[stage], BYTES);
           armed.arm(stage, phase);
           __syncwarp();
@@ -336,19 +342,23 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
     const uint64_t qd = sdesc_k_sw128(smem_u32(sm)), kd = sdesc_k_sw128(smem_u32(ring));
     const uint64_t vd = sdesc_mn_sw128(smem_u32(ring), SM::HALF);
     int stage = 0;
-    uint32_t phase = 0, qp = 0, pp = 0, of = 0;        // bit i: phase of block i's barrier
+    uint32_t phase = 0, qp = 0, pp = 0, of = 0;        // of the ring; bit i: of block i's barriers
     bool ok = true, issued = false;
     auto wait = [&](uint64_t* bar, uint32_t parity) {
-      if (ok && !mbar_wait_warp(bar, parity & 1u, abort_)) ok = false;
+      ok = ok && wait_bar(bar, parity & 1u, abort_);
       return ok;
     };
     auto step = [&] {
       if (++stage == SM::STAGES) { stage = 0; phase ^= 1u; }
     };
-    // S of block x with the K tile of a stage
-    auto issue_s = [&](int x, int st) {
+    auto commit = [&](uint64_t* bar) {
+      if (elect_one()) mma_commit(bar);
+      __syncwarp();
+    };
+    // S of block x with the K tile of the stage
+    auto issue_s = [&](int x) {
       if (elect_one()) {
-        const uint64_t k = kd + (uint64_t)(st * (SM::TILE >> 4)), q = qd + (uint64_t)(x * (SM::TILE >> 4));
+        const uint64_t k = kd + (uint64_t)(stage * (SM::TILE >> 4)), q = qd + (uint64_t)(x * (SM::TILE >> 4));
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks) {
           const uint64_t o = (uint64_t)(((ks / 4) * SM::HALF + (ks % 4) * 32) >> 4);
@@ -368,10 +378,6 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
       }
       __syncwarp();
     };
-    auto commit = [&](uint64_t* bar) {
-      if (elect_one()) mma_commit(bar);
-      __syncwarp();
-    };
     while (ok && next_run(A, P, lens, sp, at, u, before, R)) {
       const int nx = R.two ? 2 : 1;
       if (!wait(&full[stage], phase)) break;
@@ -379,7 +385,7 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
         if (!wait(&q_ready[x], qp >> x)) break;
         qp ^= 1u << x;
         fence_after();
-        issue_s(x, stage);
+        issue_s(x);
         issued = true;
       }
       if (!ok) break;
@@ -390,20 +396,24 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
         of ^= 1u << x;
       }
       for (int s = R.s0; ok && s < R.s1; ++s) {
-        // V of this tile and K of the next are there long before the weights are
+        // In order: P V of a tile reads P before S of the next tile takes its place. While
+        // one block's products run, the other's softmax does.
         const int vst = stage;
+        const bool more = s + 1 < R.s1;
         if (!wait(&full[vst], phase)) break;
         step();
-        const bool more = s + 1 < R.s1;
-        if (more && !wait(&full[stage], phase)) break;
         for (int x = 0; x < nx; ++x) {
           if (!wait(&p_ready[x], pp >> x)) break;
           pp ^= 1u << x;
           fence_after();
           issue_o(x, vst, s > R.s0);
           if (x == nx - 1) commit(&empty[vst]);
-          if (more) issue_s(x, stage);
-          else commit(&o_ready[x]);
+          if (more) {
+            if (x == 0 && !wait(&full[stage], phase)) break;
+            issue_s(x);
+          } else {
+            commit(&o_ready[x]);
+          }
         }
         if (!ok) break;
         if (more) {
@@ -425,40 +435,48 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
       uint32_t phase = 0, rp = 0;
       bool ok = true;
       while (ok && next_run(A, P, lens, sp, at, u, before, R)) {
+        // what is read for the tiles ahead is worked on a tile later: page entries two
+        // tiles ahead, scales one
         const int32_t* table = J.table + ((size_t)R.U.b * J.Hkv + R.U.h) * J.max_pages;
-        auto row_of = [&](int s) {
+        auto entry_of = [&](int s) {
           const int k = s * BK + t;
-          return s < R.s1 && k < R.U.keys ? page_row(table[k >> J.page_shift], J.n_pages, J.page_shift, k) : -1;
+          return s < R.s1 && k < R.U.keys ? table[k >> J.page_shift] : -1;
         };
-        auto scale_of = [&](int row) {
-          return row < 0 ? make_float2(0.f, 0.f) : make_float2(J.ks[row] * A.alpha, J.vs[row]);
+        float ks, vs;
+        auto read = [&](int s, int entry) {
+          const int row = page_row(entry, J.n_pages, J.page_shift, s * BK + t);
+          ks = row < 0 ? 0.f : J.ks[row];
+          vs = row < 0 ? 0.f : J.vs[row];
         };
-        float2 sc = scale_of(row_of(R.s0));
-        int next = row_of(R.s0 + 1);
+        read(R.s0, entry_of(R.s0));
+        int entry = entry_of(R.s0 + 1);
         for (int s = R.s0; ok && s < R.s1; ++s) {
-  #pragma unroll 1
+#pragma unroll 1
           for (int kv = 0; kv < 2; ++kv) {
-            if (!mbar_wait_warp(&empty[stage], phase ^ 1u, abort_) || !mbar_wait_warp(&rfull[rs], rp, abort_)) {
+            if (!wait_bar(&empty[stage], phase ^ 1u, abort_) || !wait_bar(&rfull[rs], rp, abort_)) {
               ok = false;
               break;
             }
             if (kv == 0) {
-              // four tiles on, no block still reads these: K of this tile takes the place
-              // of a V two or more tiles back
-              scales[tile % SM::SCALES][0][t] = sc.x;
-              scales[tile % SM::SCALES][1][t] = sc.y;
-              sc = scale_of(next);                       // read a tile ahead
-              next = row_of(s + 2);
+              scales[tile % SM::SCALES][0][t] = ks * A.alpha;
+              scales[tile % SM::SCALES][1][t] = vs;
+              read(s + 1, entry);
+              entry = entry_of(s + 2);
             }
             const unsigned char* src = raw + rs * SM::RAW;
             unsigned char* dst = ring + stage * SM::TILE;
-  #pragma unroll 8
-            for (int i = t; i < BK * D / 8; i += 128) {
-              const int key = i / (D / 8), ch = i % (D / 8);
-              const uint2 w = *reinterpret_cast<const uint2*>(src + i * 8);
-              *reinterpret_cast<uint4*>(dst + (ch / 8) * SM::HALF + key * 128 + ((ch % 8) ^ (key % 8)) * 16) =
-                  make_uint4(codes_bf16(__byte_perm(w.x, 0, 0x1100)), codes_bf16(__byte_perm(w.x, 0, 0x3322)),
-                             codes_bf16(__byte_perm(w.y, 0, 0x1100)), codes_bf16(__byte_perm(w.y, 0, 0x3322)));
+#pragma unroll
+            for (int i = 0; i < BK * D / 8; i += 8 * 128) {
+              uint2 w[8];
+#pragma unroll
+              for (int e = 0; e < 8; ++e) w[e] = *reinterpret_cast<const uint2*>(src + (i + e * 128 + t) * 8);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                const int n = i + e * 128 + t, key = n / (D / 8), ch = n % (D / 8);
+                *reinterpret_cast<uint4*>(dst + (ch / 8) * SM::HALF + key * 128 + ((ch % 8) ^ (key % 8)) * 16) =
+                    make_uint4(codes_bf16(__byte_perm(w[e].x, 0, 0x1100)), codes_bf16(__byte_perm(w[e].x, 0, 0x3322)),
+                               codes_bf16(__byte_perm(w[e].y, 0, 0x1100)), codes_bf16(__byte_perm(w[e].y, 0, 0x3322)));
+              }
             }
             fence_async();
             __syncwarp();
@@ -492,39 +510,48 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
       }
       const int brow = x * BQ + lrow, row = U.row0 + brow;
       const bool live = brow < U.rows;
-      const int tok = row / J.r, j = row - tok * J.r;
+      const int tok = J.by_r(row), j = row - tok * J.r;
       {
         // the warp's 32 rows, LPR lanes a row; a row's offset comes from the lane that owns it
         constexpr int LPR = D / 8;
         const int64_t off = live ? ((int64_t)(J.off[U.b] + tok) * J.stride + (int64_t)(U.h * J.r + j) * D) * 2 : -1;
         unsigned char* dst = sm + x * SM::TILE + warp % 4 * 32 * 128;
-        auto put = [&](int i, bool vec) {
+        auto offset = [&](int i) { return __shfl_sync(0xffffffffu, off, i * (32 / LPR) + lane / LPR); };
+        auto put = [&](int i, const uint4& w) {
           const int r = i * (32 / LPR) + lane / LPR, ch = lane % LPR;
-          const int64_t o = __shfl_sync(0xffffffffu, off, r);
-          const uint4 w = o >= 0 ? load_plain16(A.q + o + ch * 16, vec) : make_uint4(0, 0, 0, 0);
           *reinterpret_cast<uint4*>(dst + (ch / 8) * SM::HALF + r * 128 + ((ch % 8) ^ (r % 8)) * 16) = w;
         };
         if (A.qvec) {
 #pragma unroll
-          for (int i = 0; i < LPR; ++i) put(i, true);
+          for (int i = 0; i < LPR; i += 8) {           // eight loads, then their stores
+            uint4 w[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const int64_t o = offset(i + e);
+              w[e] = o >= 0 ? *reinterpret_cast<const uint4*>(A.q + o + lane % LPR * 16) : make_uint4(0, 0, 0, 0);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) put(i + e, w[e]);
+          }
         } else {
 #pragma unroll 1
-          for (int i = 0; i < LPR; ++i) put(i, false);
+          for (int i = 0; i < LPR; ++i) {
+            const int64_t o = offset(i);
+            put(i, o >= 0 ? load_plain16(A.q + o + lane % LPR * 16, false) : make_uint4(0, 0, 0, 0));
+          }
         }
         fence_async();
         __syncwarp();
         if (lane == 0) mbar_arrive(&q_ready[x]);
       }
       const int32_t* table = J.table + ((size_t)U.b * J.Hkv + U.h) * J.max_pages;
-      const int least = keys_of(A.causal, U.len, U.n, U.row0 / J.r);   // keys that every row attends to
+      const int least = keys_of(A.causal, U.len, U.n, J.by_r(U.row0));   // keys that every row attends to
       // bit i: the tile's 16-key block i has no page
-      auto gone_of = [&](int s) {
+      auto entry_of = [&](int s) {
         const int t = s * BK + lane * 16;
-        const bool g = lane < 8 && s < R.s1 && t < U.keys &&
-                       page_row(table[t >> J.page_shift], J.n_pages, J.page_shift, t) < 0;
-        return __ballot_sync(0xffffffffu, g);
+        return lane < 8 && s < R.s1 && t < U.keys ? table[t >> J.page_shift] : 0;
       };
-      uint32_t next = gone_of(R.s0);
+      int next = entry_of(R.s0);
       // bfloat16 pages: the thread's row. 8-bit pages: rows g + 8i of the warp's 32, with
       // the lanes of a quad sharing them (and their sums).
       constexpr int NR = I8 ? 4 : 1;
@@ -536,7 +563,7 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
         m[i] = -INFINITY;
         l[i] = 0.f;
         const int r = U.row0 + x * BQ + (I8 ? warp % 4 * 32 + g + 8 * i : lrow);
-        lim[i] = r < U.row0 + U.rows ? keys_of(A.causal, U.len, U.n, r / J.r) : 0;
+        lim[i] = r < U.row0 + U.rows ? keys_of(A.causal, U.len, U.n, J.by_r(r)) : 0;
       }
       // a value of the thread's row, of those that the quads hold
       auto of_row = [&](const float* v) {
@@ -550,37 +577,38 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
         return got;
       };
       for (int s = R.s0; s < R.s1; ++s) {
-        const uint32_t gone = next;
-        next = gone_of(s + 1);
+        const uint32_t gone = __ballot_sync(0xffffffffu, next < 0 || next >= J.n_pages);
+        next = entry_of(s + 1);
         const int k0 = s * BK;
         const bool special = k0 + BK > least;
         // the tile's V, the stage behind its K; it stays there until P is ready
         int vs = vstage + 1;
         uint32_t vp = vphase;
         if (vs == SM::STAGES) { vs = 0; vp ^= 1u; }
-        if (!I8 && special && x == 0) {
-          // the first block's threads clean V: both blocks' products with it are
-          // issued after this block's P has been reported ready
-          if (!mbar_wait_warp(&full[vs], vp, abort_)) { ok = false; break; }
+        if (!I8 && special) {
+          // Both blocks clean V, each before it reports its P: what one finds clean the
+          // other has cleaned, after it set the flag.
+          if (!wait_bar(&full[vs], vp, abort_)) { ok = false; break; }
           unsigned char* vt = ring + vs * SM::TILE;
           constexpr int CH = SM::HALVES * 8;             // 16-byte chunks of a row
-          bool odd = false;
 #pragma unroll 4
-          for (int i = max(least - k0, 0) * CH + threadIdx.x; i < BK * CH; i += 128) {
+          for (int i = max(least - k0, 0) * CH + lrow; i < BK * CH; i += 128) {
             const int key = i / CH, ch = i % CH;
             uint4* p = reinterpret_cast<uint4*>(vt + (ch / 8) * SM::HALF + key * 128 + (ch % 8) * 16);
             const uint4 w = k0 + key < U.keys ? *p : make_uint4(0, 0, 0, 0);
             const bool bad = not_finite2(w.x) || not_finite2(w.y) || not_finite2(w.z) || not_finite2(w.w);
-            odd |= bad;
+            if (bad) {
+              *reinterpret_cast<volatile int*>(&odd_flag) = 1;
+              __threadfence_block();
+            }
             if (bad || k0 + key >= U.keys) *p = make_uint4(finite2(w.x), finite2(w.y), finite2(w.z), finite2(w.w));
           }
-          if (odd) *reinterpret_cast<volatile int*>(&odd_flag) = 1;
           fence_async();
         }
-        if (!mbar_wait_warp(&s_ready[x], sph, abort_)) { ok = false; break; }
+        if (!wait_bar(&s_ready[x], sph, abort_)) { ok = false; break; }
         sph ^= 1u;
         // 8-bit pages: the tile's scales were written before its V was
-        if (I8 && !mbar_wait_warp(&full[vs], vp, abort_)) { ok = false; break; }
+        if (I8 && !wait_bar(&full[vs], vp, abort_)) { ok = false; break; }
         fence_after();
         const bool masked = special || gone;
         if (gone && warp == 0 && lane == 0) set_status(J.status, kStatusBadPage);
@@ -776,7 +804,7 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
         __syncwarp();
         if (lane == 0) mbar_arrive(&p_ready[x]);
       }
-      if (!ok || !mbar_wait_warp(&o_ready[x], oph, abort_)) { ok = false; break; }
+      if (!ok || !wait_bar(&o_ready[x], oph, abort_)) { ok = false; break; }
       oph ^= 1u;
       fence_after();
       if constexpr (I8) {

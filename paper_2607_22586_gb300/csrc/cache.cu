@@ -219,6 +219,7 @@ void fill_job(const mmshift_shape* s, const mmshift_cache* c, void* ws, CacheJob
   J->Hq = s->n_q_heads;
   J->Hkv = s->n_kv_heads;
   J->r = s->n_q_heads / s->n_kv_heads;
+  J->by_r = divisor_of(J->r);
   J->d = s->head_dim;
   J->bf16 = s->dtype == MMSHIFT_BF16;
   J->i8 = c->dtype == MMSHIFT_I8;

@@ -36,6 +36,31 @@ MMSHIFT_HD int keys_of(int causal, int len, int n, int i) {
   return e > 0 ? e : 0;
 }
 
+// Division of 0 <= x < 2^31 by a number d >= 1 known on the host, as one high product:
+// with L the least L such that d <= 2^L, m = ceil(2^(31 + L) / d) < 2^32 gives
+// floor(x / d) = floor(x m / 2^(31 + L)) (Granlund and Montgomery, 1994).
+struct Divisor {
+  uint32_t m;      // 0: d = 1
+  int32_t shift;   // L - 1
+  MMSHIFT_HD int operator()(int x) const {
+#if defined(__CUDA_ARCH__)
+    return m ? (int)(__umulhi((uint32_t)x, m) >> shift) : x;
+#else
+    return m ? (int)((uint32_t)(((uint64_t)(uint32_t)x * m) >> 32) >> shift) : x;
+#endif
+  }
+};
+
+inline Divisor divisor_of(int32_t d) {
+  Divisor r = {0, 0};
+  if (d <= 1) return r;
+  int L = 1;
+  while (((int64_t)1 << L) < d) ++L;
+  r.m = (uint32_t)((((uint64_t)1 << (31 + L)) + d - 1) / d);
+  r.shift = L - 1;
+  return r;
+}
+
 // x / y for 0 <= x, 0 < y; 64-bit division only where it is needed.
 MMSHIFT_HD int64_t quotient(int64_t x, int64_t y) {
   if (((uint64_t)x | (uint64_t)y) >> 32) return x / y;

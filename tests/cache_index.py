@@ -18,6 +18,7 @@ int t_keys_of(int causal, int len, int n, int i) { return keys_of(causal, len, n
 long long t_begin(long long W, int most, int least, int i) { return shares_of(W, most, least).begin(i); }
 int t_of(long long W, int most, int least, long long x) { return shares_of(W, most, least).of(x); }
 int t_workers(long long W, int most, int least) { return shares_of(W, most, least).n; }
+int t_divide(int d, int x) { return divisor_of(d)(x); }
 long long t_quotient(long long x, long long y) { return quotient(x, y); }
 }
 """

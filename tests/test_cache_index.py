@@ -72,3 +72,14 @@ def test_quotients(lib):
     for _ in range(2000):
         x, y = rng.randrange(2 ** rng.randint(1, 62)), 1 + rng.randrange(2 ** rng.randint(1, 40))
         assert lib.t_quotient(x, y) == x // y
+
+
+def test_division_by_a_known_number(lib):
+    rng = random.Random(4)
+    ds = list(range(1, 130)) + [2 ** k + e for k in range(1, 31) for e in (-1, 0, 1) if 2 ** k + e <= 2 ** 31 - 1]
+    for d in ds:
+        xs = [0, 1, d - 1, d, d + 1, 2 ** 31 - 1, 2 ** 31 - 2, (2 ** 31 - 1) // d * d, (2 ** 31 - 1) // d * d - 1]
+        xs += [rng.randrange(2 ** 31) for _ in range(20)]
+        for x in xs:
+            if 0 <= x < 2 ** 31:
+                assert lib.t_divide(d, x) == x // d, (d, x)
