@@ -172,36 +172,81 @@ __device__ __forceinline__ bool wait_bar(uint64_t* bar, uint32_t parity, volatil
   return __all_sync(0xffffffffu, ok);
 }
 
-// A role's walk over the CTA's runs of keys.
+// A run: consecutive key tiles [s0, s1) of a unit that the CTA works on together.
 struct Run {
   AttendUnit U;
-  int64_t before;
-  int unit, s0, s1;      // key tiles [s0, s1) of the unit
+  int64_t before;        // pieces before the unit
+  int s0, s1;
   bool two;              // the second block has rows
 };
 
-__device__ __forceinline__ bool next_run(const AttendJob& A, const AttendPlan& P, const int32_t* lens,
-                                         const AttendSpan& sp, int64_t& at,
-                                         int& u, int64_t& before, Run& R) {
-  while (at < sp.end) {
-    R.U = attend_unit(A, P, lens, u);
-    const int64_t last = before + R.U.pieces;
-    if (last > at) {
-      const int64_t stop = min(sp.end, last);
-      R.before = before;
-      R.unit = u;
-      R.s0 = (int)(at - before);
-      R.s1 = (int)(stop - before);
-      R.two = R.U.rows > BQ;
-      at = stop;
-      if (stop == last) {
-        before = last;
-        ++u;
-      }
+// A role's walk over the CTA's runs. A warp works the first ones out for all roles, a
+// lane a unit; a role itself those behind them (units of few keys).
+constexpr int RUNS = 16;
+struct Walk {
+  int k, unit;           // runs so far; behind the list, the next unit and the pieces before it
+  int64_t before;
+};
+struct RunList {
+  Run run[RUNS];
+  Walk rest;
+  int n;
+};
+
+__device__ __forceinline__ Run run_of(const AttendSpan& sp, const AttendUnit& U, int64_t before) {
+  Run R;
+  R.U = U;
+  R.before = before;
+  R.s0 = (int)(max(sp.begin, before) - before);
+  R.s1 = (int)(min(sp.end, before + U.pieces) - before);
+  R.two = U.rows > BQ;
+  return R;
+}
+
+// By a whole warp: the first runs of the CTA.
+__device__ __forceinline__ void list_runs(const AttendJob& A, const AttendPlan& P, const AttendSpan& sp, int lane,
+                                          RunList* list) {
+  const int u = sp.unit + lane;
+  const bool in = sp.begin < sp.end && lane < RUNS && u < P.uoff[A.c.B];
+  AttendUnit U;
+  U.pieces = 0;
+  if (in) U = attend_unit(A, P, nullptr, u);
+  int64_t x = U.pieces;
+#pragma unroll
+  for (int d = 1; d < RUNS; d <<= 1) {
+    const int64_t y = __shfl_up_sync(0xffffffffu, x, d);
+    if (lane >= d) x += y;
+  }
+  const int64_t before = sp.before + x - U.pieces;
+  const bool mine = in && U.pieces > 0 && before < sp.end;
+  const unsigned all = __ballot_sync(0xffffffffu, mine);
+  if (mine) list->run[__popc(all & ((1u << lane) - 1u))] = run_of(sp, U, before);
+  if (lane == RUNS - 1) {                              // where the walk goes on
+    list->n = __popc(all);
+    list->rest = Walk{0, u + 1, in ? sp.before + x : sp.end};
+  }
+}
+
+__device__ __forceinline__ bool next_run(const AttendJob& A, const AttendPlan& P, const AttendSpan& sp,
+                                         const RunList& list, Walk& w, Run& R) {
+  if (w.k < list.n) {
+    R = list.run[w.k];
+    ++w.k;
+    return true;
+  }
+  if (w.k == list.n) {
+    w = list.rest;
+    w.k = RUNS + 1;
+  }
+  while (w.before < sp.end) {
+    const AttendUnit U = attend_unit(A, P, nullptr, w.unit);
+    const int64_t before = w.before;
+    w.before += U.pieces;
+    ++w.unit;
+    if (U.pieces) {
+      R = run_of(sp, U, before);
       return true;
     }
-    before = last;
-    ++u;
   }
   return false;
 }
@@ -253,7 +298,8 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
   __shared__ uint64_t p_ready[2], drain;
   __shared__ uint32_t tbase;
   __shared__ int abort_flag, odd_flag;
-  __shared__ AttendScan<NT, 256> scan;
+  __shared__ AttendScan<NT, 1> scan;
+  __shared__ RunList runs;
   volatile int* abort_ = &abort_flag;
   const CacheJob& J = A.c;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -290,9 +336,9 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
   const uint32_t tmem = tbase;
   attend_start();
   const AttendSpan sp = attend_span(A, P, &scan);
-  int64_t at = sp.begin, before = sp.before;
-  int u = sp.unit;
-  const int32_t* lens = scan.lengths(A.c);
+  if (warp == 0) list_runs(A, P, sp, lane, &runs);
+  __syncthreads();
+  Walk walk = {0, 0, 0};
   Run R;
   if (warp == PRODUCER) {
     // bfloat16 rows go where the MMAs read them, codes to a ring of their own
@@ -304,7 +350,7 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
     bool ok = true;
     const int shift = min(J.page_shift, 7), boxes = BK >> shift;
     const int outside = J.n_pages << J.page_shift;     // a box from there on reads zeros
-    while (ok && next_run(A, P, lens, sp, at, u, before, R)) {
+    while (ok && next_run(A, P, sp, runs, walk, R)) {
       const int32_t* table = J.table + ((size_t)R.U.b * J.Hkv + R.U.h) * J.max_pages;
       // this lane's box of a tile: its row of the pool
       auto entry_of = [&](int s) {
@@ -378,7 +424,7 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
       }
       __syncwarp();
     };
-    while (ok && next_run(A, P, lens, sp, at, u, before, R)) {
+    while (ok && next_run(A, P, sp, runs, walk, R)) {
       const int nx = R.two ? 2 : 1;
       if (!wait(&full[stage], phase)) break;
       for (int x = 0; x < nx; ++x) {
@@ -434,7 +480,7 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
       int stage = 0, rs = 0, tile = 0;
       uint32_t phase = 0, rp = 0;
       bool ok = true;
-      while (ok && next_run(A, P, lens, sp, at, u, before, R)) {
+      while (ok && next_run(A, P, sp, runs, walk, R)) {
         // what is read for the tiles ahead is worked on a tile later: page entries two
         // tiles ahead, scales one
         const int32_t* table = J.table + ((size_t)R.U.b * J.Hkv + R.U.h) * J.max_pages;
@@ -498,7 +544,7 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
     uint32_t sph = 0, oph = 0, vphase = 0;
     int vstage = 0, tile = 0;                            // ring stage of the next tile's K, tiles so far
     bool ok = true;
-    while (ok && next_run(A, P, lens, sp, at, u, before, R)) {
+    while (ok && next_run(A, P, sp, runs, walk, R)) {
       const AttendUnit& U = R.U;
       const int ntiles = R.s1 - R.s0;
       if (x == 1 && !R.two) {
@@ -508,12 +554,20 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
         tile += ntiles;
         continue;
       }
+      const int32_t* table = J.table + ((size_t)U.b * J.Hkv + U.h) * J.max_pages;
+      const int least = keys_of(A.causal, U.len, U.n, J.by_r(U.row0));   // keys that every row attends to
+      // bit i: the tile's 16-key block i has no page
+      auto entry_of = [&](int s) {
+        const int t = s * BK + lane * 16;
+        return lane < 8 && s < R.s1 && t < U.keys ? table[t >> J.page_shift] : 0;
+      };
+      int next = entry_of(R.s0);
       const int brow = x * BQ + lrow, row = U.row0 + brow;
       const bool live = brow < U.rows;
       const int tok = J.by_r(row), j = row - tok * J.r;
       {
         // the warp's 32 rows, LPR lanes a row; a row's offset comes from the lane that owns it
-        constexpr int LPR = D / 8;
+        constexpr int LPR = D / 8, QN = I8 ? 8 : LPR;
         const int64_t off = live ? ((int64_t)(J.off[U.b] + tok) * J.stride + (int64_t)(U.h * J.r + j) * D) * 2 : -1;
         unsigned char* dst = sm + x * SM::TILE + warp % 4 * 32 * 128;
         auto offset = [&](int i) { return __shfl_sync(0xffffffffu, off, i * (32 / LPR) + lane / LPR); };
@@ -523,15 +577,15 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
         };
         if (A.qvec) {
 #pragma unroll
-          for (int i = 0; i < LPR; i += 8) {           // eight loads, then their stores
-            uint4 w[8];
+          for (int i = 0; i < LPR; i += QN) {          // loads, then their stores
+            uint4 w[QN];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
+            for (int e = 0; e < QN; ++e) {
               const int64_t o = offset(i + e);
               w[e] = o >= 0 ? *reinterpret_cast<const uint4*>(A.q + o + lane % LPR * 16) : make_uint4(0, 0, 0, 0);
             }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) put(i + e, w[e]);
+            for (int e = 0; e < QN; ++e) put(i + e, w[e]);
           }
         } else {
 #pragma unroll 1
@@ -544,14 +598,6 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
         __syncwarp();
         if (lane == 0) mbar_arrive(&q_ready[x]);
       }
-      const int32_t* table = J.table + ((size_t)U.b * J.Hkv + U.h) * J.max_pages;
-      const int least = keys_of(A.causal, U.len, U.n, J.by_r(U.row0));   // keys that every row attends to
-      // bit i: the tile's 16-key block i has no page
-      auto entry_of = [&](int s) {
-        const int t = s * BK + lane * 16;
-        return lane < 8 && s < R.s1 && t < U.keys ? table[t >> J.page_shift] : 0;
-      };
-      int next = entry_of(R.s0);
       // bfloat16 pages: the thread's row. 8-bit pages: rows g + 8i of the warp's 32, with
       // the lanes of a quad sharing them (and their sums).
       constexpr int NR = I8 ? 4 : 1;
@@ -831,14 +877,20 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
       const int64_t to = live ? (whole ? orow : slot) : -1;
       auto flush = [&](int half) {
         __syncwarp();
-#pragma unroll 2
-        for (int i = 0; i < LPR; ++i) {
-          const int r = i * (32 / LPR) + lane / LPR, ch = lane % LPR;
-          const int64_t t = __shfl_sync(0xffffffffu, to, r);
-          const uint4 w = *chunk(r, ch);
-          if (t < 0) continue;
-          if (whole) store_row16(A.out + t * (2 * D) + ch * 16, w, A.ovec);
-          else *reinterpret_cast<uint4*>(reinterpret_cast<uint8_t*>(P.po + t * D) + half * (2 * D) + ch * 16) = w;
+        const int ch = lane % LPR;
+        uint8_t* const base = whole ? A.out + ch * 16 : reinterpret_cast<uint8_t*>(P.po) + half * (2 * D) + ch * 16;
+        const int64_t pitch = whole ? 2 * D : 4 * D;
+        const bool vec = !whole || A.ovec;
+#pragma unroll 1
+        for (int i = 0; i < LPR; i += 8) {
+          uint4 w[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) w[e] = *chunk((i + e) * (32 / LPR) + lane / LPR, ch);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int64_t t = __shfl_sync(0xffffffffu, to, (i + e) * (32 / LPR) + lane / LPR);
+            if (t >= 0) store_row16(base + t * pitch, w[e], vec);
+          }
         }
         __syncwarp();
       };
