@@ -122,7 +122,8 @@ cudaError_t launch_merge(const AttendJob& A, const AttendPlan& P, cudaStream_t s
 }
 
 // Requests whose rows of a KV head are at most this many have a plan of their own:
-// bfloat16 rows go to the token kernel, float32 rows to tiles of 8 or 16 rows.
+// bfloat16 rows go to the token kernel, float32 rows to tiles of 8 or 16 rows (others to
+// tiles of 256 and of 64 or 128).
 constexpr int kTokenRows = 16;
 
 constexpr int kSMs = 152;              // the workspace is sized without asking the device
@@ -166,15 +167,15 @@ AttendPlan token_plan(const CacheJob& J, int nsm) {
     P.workers = nsm * (P.rows <= 8 ? 3 : 2);
   } else {
     P.step_shift = 5;
-    P.workers = nsm * (P.rows <= 8 ? 3 : 2);
+    P.workers = nsm * (P.rows <= 8 ? 4 : 3);
   }
   return P;
 }
 
 AttendPlan chunk_plan(const CacheJob& J, int nsm) {
-  AttendPlan P = plan_of(J, J.bf16 ? 256 : 64, [&](int rows) { return rows > kTokenRows; });
-  P.step_shift = J.bf16 ? 7 : 5;
-  P.workers = J.bf16 ? nsm : 2 * nsm;
+  AttendPlan P = plan_of(J, J.bf16 ? 256 : 128, [&](int rows) { return rows > kTokenRows; });
+  P.step_shift = J.bf16 ? 7 : 6;
+  P.workers = nsm;
   return P;
 }
 

@@ -1,13 +1,16 @@
 // Attention of float32 rows, over float32 or 8-bit pages: CUDA cores, fp32 FMAs.
 //
-// Tiles of 8 * TR query rows over tiles of 32 keys, 128 threads: thread (ty, tx)
-// has the TR rows of group ty; in S the keys tx and tx + 16, in O the dimensions
-// 4 tx .. of each 64. A row's threads are 16 lanes of one warp, so its weights
-// change hands through shared memory without a barrier of the CTA. K and V tiles
-// arrive through asynchronous copies, one tile ahead (8-bit codes through
-// registers, to be converted). With TR = 8 a thread's 16 and 64 sums make every
-// shared load feed 5 to 8 FMAs, packed in pairs: bound by the FMA rate. Few rows
-// (TR = 1, 2) are bound by the bytes of K and V.
+// Tiles of NT / 16 * TR query rows over tiles of BK keys: thread (ty, tx) has the TR rows of
+// group ty; in S the keys tx, tx + 16, ..., in O the dimensions 4 tx .. of each 64. A row's
+// threads are 16 lanes of one warp, so its weights change hands through shared memory
+// without a barrier of the CTA. K of the next tile arrives (asynchronous copies; 8-bit
+// codes through registers, to be converted) while this one's values are added up, V while
+// its logits are. Chunks (TR = 8, 128 rows by 64 keys) are bound by what shared memory
+// feeds the FMAs, 128 bytes a clock and SM: 8 x 4 sums take 1.5 bytes an FMA, the 8 x 8
+// (or 8 x 4, d = 64) of the second product 1 (1.5). Few rows (TR = 1, 2) are bound by the
+// bytes of K and V.
+#include <type_traits>
+
 #include "attend.cuh"
 #include "umma.cuh"
 
@@ -21,19 +24,22 @@ using umma::pk2;
 using umma::smem_u32;
 using umma::upk2;
 
-constexpr int NT = 128, BK = 32;
 constexpr float kRaise = 8.f;
 
 template <int D, int TR>
-struct SimtSmem {
-  static constexpr int RT = 8 * TR;
+struct Simt {
+  static constexpr int NT = TR >= 4 ? 256 : 128, BK = TR >= 4 ? 64 : 32, NK = BK / 16;
+  static constexpr int CTAS = TR >= 4 ? 1 : TR == 2 ? 3 : 4;   // of an SM
+  static constexpr int RT = NT / 16 * TR;
   static constexpr int QS = D + 4, PS = RT + 4;        // floats between rows: no bank conflicts
-  alignas(16) float q[RT][QS];
-  alignas(16) float k[2][BK][QS];
-  alignas(16) float v[2][BK][D];
-  alignas(16) float p[BK][PS];
-  float ks[2][BK], vs[2][BK];
-  AttendScan<NT, 256> scan;
+  struct Smem {
+    alignas(16) float q[RT][QS];
+    alignas(16) float k[BK][QS];
+    alignas(16) float v[BK][D];
+    alignas(16) float p[BK][PS];
+    float ks[BK], vs[BK];
+    AttendScan<NT, 256> scan;
+  };
 };
 
 __device__ __forceinline__ void copy16(void* dst, const void* src, bool in) {
@@ -44,11 +50,12 @@ __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group 0;" ::: "memory"); }
 
 template <int D, bool I8, int TR>
-__global__ void __launch_bounds__(NT, TR >= 4 ? 2 : 3) attend_simt_kernel(const __grid_constant__ AttendJob A,
-                                                                          const __grid_constant__ AttendPlan P) {
-  using SM = SimtSmem<D, TR>;
+__global__ void __launch_bounds__(Simt<D, TR>::NT, Simt<D, TR>::CTAS)
+    attend_simt_kernel(const __grid_constant__ AttendJob A, const __grid_constant__ AttendPlan P) {
+  using SM = Simt<D, TR>;
+  constexpr int NT = SM::NT, BK = SM::BK, NK = SM::NK;
   extern __shared__ __align__(16) unsigned char smraw[];
-  SM& sm = *reinterpret_cast<SM*>(smraw);
+  typename SM::Smem& sm = *reinterpret_cast<typename SM::Smem*>(smraw);
   attend_start();
   const CacheJob& J = A.c;
   const int tid = threadIdx.x, lane = tid % 32, tx = tid % 16, ty = tid / 16;
@@ -93,99 +100,95 @@ __global__ void __launch_bounds__(NT, TR >= 4 ? 2 : 3) attend_simt_kernel(const 
     constexpr int ROWB = I8 ? D : 4 * D, LPR = ROWB / 16, STEP = NT / LPR;   // lanes of a row, keys a round
     constexpr int N = BK / STEP;
     const int lk = tid / LPR, part = tid % LPR;
-    uint4 ck[I8 ? N : 1], cv[I8 ? N : 1];
-    float2 sc;
+    uint4 codes[I8 ? N : 1];
+    float scale = 0.f;
     auto row_of = [&](int t) {
       return t < U.keys ? page_row(table[t >> J.page_shift], J.n_pages, J.page_shift, t) : -1;
     };
-    auto fetch = [&](int s, int buf) {
+    auto fetch = [&](int s, const uint8_t* pages, const float* scales, float* dst, int pitch) {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const int key = lk + i * STEP, row = s < s1 ? row_of(s * BK + key) : -1;
         const size_t src = (size_t)(row < 0 ? 0 : row) * ROWB + part * 16;
-        if constexpr (I8) {
-          ck[i] = row < 0 ? make_uint4(0, 0, 0, 0) : *reinterpret_cast<const uint4*>(J.kp + src);
-          cv[i] = row < 0 ? make_uint4(0, 0, 0, 0) : *reinterpret_cast<const uint4*>(J.vp + src);
-        } else {
-          copy16(&sm.k[buf][key][part * 4], J.kp + src, row >= 0);
-          copy16(&sm.v[buf][key][part * 4], J.vp + src, row >= 0);
-        }
+        if constexpr (I8) codes[i] = row < 0 ? make_uint4(0, 0, 0, 0) : *reinterpret_cast<const uint4*>(pages + src);
+        else copy16(dst + key * pitch + part * 4, pages + src, row >= 0);
       }
       if constexpr (I8) {
         if (tid < BK) {
           const int row = s < s1 ? row_of(s * BK + tid) : -1;
-          sc = row < 0 ? make_float2(0.f, 0.f) : make_float2(J.ks[row], J.vs[row]);
+          scale = row < 0 ? 0.f : scales[row];
         }
       } else {
         copies_commit();
       }
     };
-    auto store = [&](int buf) {                        // 8-bit pages: what fetch() left in registers
+    auto arrive = [&](float* dst, int pitch, float* scales, float by) {   // what fetch() asked for
       if constexpr (I8) {
-        auto put = [](float* dst, const uint4& w) {
-          const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            reinterpret_cast<float4*>(dst)[i] =
-                make_float4((float)(int8_t)x[i], (float)(int8_t)(x[i] >> 8), (float)(int8_t)(x[i] >> 16),
-                            (float)(int8_t)(x[i] >> 24));
-        };
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-          put(&sm.k[buf][lk + i * STEP][part * 16], ck[i]);
-          put(&sm.v[buf][lk + i * STEP][part * 16], cv[i]);
+          const uint32_t x[4] = {codes[i].x, codes[i].y, codes[i].z, codes[i].w};
+          float4* to = reinterpret_cast<float4*>(dst + (lk + i * STEP) * pitch + part * 16);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            to[e] = make_float4((float)(int8_t)x[e], (float)(int8_t)(x[e] >> 8), (float)(int8_t)(x[e] >> 16),
+                                (float)(int8_t)(x[e] >> 24));
         }
-        if (tid < BK) {
-          sm.ks[buf][tid] = sc.x * A.alpha;
-          sm.vs[buf][tid] = sc.y;
-        }
+        if (tid < BK) scales[tid] = scale * by;
+      } else {
+        copies_wait();
       }
     };
-    fetch(s0, 0);
+    float* const kt = &sm.k[0][0];
+    float* const vt = &sm.v[0][0];
+    fetch(s0, J.kp, J.ks, kt, SM::QS);
     for (int s = s0; s < s1; ++s) {
-      const int buf = (s - s0) & 1, k0 = s * BK;
-      if constexpr (I8) store(buf); else copies_wait();
-      // the page of the tile's two 16-key blocks; the barrier also ends all reads of the other buffer
-      const bool none = lane < 2 && k0 + 16 * lane < U.keys && row_of(k0 + 16 * lane) < 0;
+      const int k0 = s * BK;
+      arrive(kt, SM::QS, sm.ks, A.alpha);
+      // the pages of the tile's 16-key blocks
+      const bool none = lane < NK && k0 + 16 * lane < U.keys && row_of(k0 + 16 * lane) < 0;
       const uint32_t gone = __ballot_sync(0xffffffffu, none);
       if (gone && tid == 0) set_status(J.status, kStatusBadPage);
-      __syncthreads();
-      fetch(s + 1, buf ^ 1);
+      __syncthreads();                                 // K is there; the last tile's V is done with
+      fetch(s, J.vp, J.vs, vt, D);
 
-      uint64_t x2[TR][2];
+      uint64_t x2[TR][NK];
 #pragma unroll
-      for (int i = 0; i < TR; ++i) x2[i][0] = x2[i][1] = pk2(0.f, 0.f);
-      const uint32_t qa = smem_u32(&sm.q[ty * TR][0]), ka = smem_u32(&sm.k[buf][tx][0]);
-#pragma unroll 4
+      for (int i = 0; i < TR; ++i)
+#pragma unroll
+        for (int j = 0; j < NK; ++j) x2[i][j] = pk2(0.f, 0.f);
+      const uint32_t qa = smem_u32(&sm.q[ty * TR][0]), ka = smem_u32(&sm.k[tx][0]);
+#pragma unroll 2
       for (int d = 0; d < D; d += 4) {
-        uint64_t kk[2][2];
-        lds_2x64(ka + d * 4, kk[0][0], kk[0][1]);
-        lds_2x64(ka + (16 * SM::QS + d) * 4, kk[1][0], kk[1][1]);
+        uint64_t kk[NK][2];
+#pragma unroll
+        for (int j = 0; j < NK; ++j) lds_2x64(ka + (16 * j * SM::QS + d) * 4, kk[j][0], kk[j][1]);
 #pragma unroll
         for (int i = 0; i < TR; ++i) {
           uint64_t q0, q1;
           lds_2x64(qa + (i * SM::QS + d) * 4, q0, q1);
 #pragma unroll
-          for (int j = 0; j < 2; ++j) x2[i][j] = ffma2(q1, kk[j][1], ffma2(q0, kk[j][0], x2[i][j]));
+          for (int j = 0; j < NK; ++j) x2[i][j] = ffma2(q1, kk[j][1], ffma2(q0, kk[j][0], x2[i][j]));
         }
       }
       const bool masked = k0 + BK > least || gone;
-      float x[TR][2];
+      float x[TR][NK];
       bool raise = false;
 #pragma unroll
       for (int i = 0; i < TR; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
+        for (int j = 0; j < NK; ++j) {
           float a, b;
           upk2(x2[i][j], a, b);
-          x[i][j] = (a + b) * (I8 ? sm.ks[buf][tx + 16 * j] : A.alpha);
+          x[i][j] = (a + b) * (I8 ? sm.ks[tx + 16 * j] : A.alpha);
           if (masked && (k0 + tx + 16 * j >= lim[i] || ((gone >> j) & 1u))) x[i][j] = -INFINITY;
           raise |= x[i][j] > m[i] + kRaise;
         }
       if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
         for (int i = 0; i < TR; ++i) {
-          float top = fmaxf(m[i], fmaxf(x[i][0], x[i][1]));
+          float top = m[i];
+#pragma unroll
+          for (int j = 0; j < NK; ++j) top = fmaxf(top, x[i][j]);
 #pragma unroll
           for (int z = 1; z < 16; z <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, z));
           const float f = m[i] == -INFINITY ? 0.f : fast_exp2(m[i] - top);
@@ -202,59 +205,52 @@ __global__ void __launch_bounds__(NT, TR >= 4 ? 2 : 3) attend_simt_kernel(const 
         }
       }
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
+      for (int i = 0; i < TR; ++i)
+#pragma unroll
+        for (int j = 0; j < NK; ++j) {
+          x[i][j] = fast_exp2(x[i][j] - (m[i] == -INFINITY ? 0.f : m[i]));
+          l[i] += x[i][j];
+        }
+      arrive(vt, D, sm.vs, 1.f);
+      __syncthreads();                                 // V is there, K is done with
+      fetch(s + 1, J.kp, J.ks, kt, SM::QS);
+#pragma unroll
+      for (int j = 0; j < NK; ++j) {
         const int key = tx + 16 * j;
-        float w[TR];
+        const float by = I8 ? sm.vs[key] : 1.f;
 #pragma unroll
         for (int i = 0; i < TR; ++i) {
-          w[i] = fast_exp2(x[i][j] - (m[i] == -INFINITY ? 0.f : m[i]));
-          l[i] += w[i];
-          if constexpr (I8) w[i] *= sm.vs[buf][key];
           // below zero: a key that the row does not attend to
-          if (masked && (k0 + key >= lim[i] || ((gone >> j) & 1u))) w[i] = -1.f;
+          const bool hidden = masked && (k0 + key >= lim[i] || ((gone >> j) & 1u));
+          sm.p[key][ty * TR + i] = hidden ? -1.f : I8 ? x[i][j] * by : x[i][j];
         }
-#pragma unroll
-        for (int i = 0; i < TR; ++i) sm.p[key][ty * TR + i] = w[i];
       }
       __syncwarp();
-      const uint32_t va = smem_u32(&sm.v[buf][0][tx * 4]);
+      const uint32_t va = smem_u32(&sm.v[0][tx * 4]);
       const float* pp = &sm.p[0][ty * TR];
-      if (!masked) {
-#pragma unroll 4
-        for (int key = 0; key < BK; ++key) {
-          uint64_t vv[D / 64][2];
+      auto add = [&](int key, auto mask) {
+        uint64_t vv[D / 64][2];
 #pragma unroll
-          for (int c = 0; c < D / 64; ++c) lds_2x64(va + (key * D + 64 * c) * 4, vv[c][0], vv[c][1]);
+        for (int c = 0; c < D / 64; ++c) lds_2x64(va + (key * D + 64 * c) * 4, vv[c][0], vv[c][1]);
 #pragma unroll
-          for (int i = 0; i < TR; ++i) {
-            const float w = pp[key * SM::PS + i];
-            const uint64_t w2 = pk2(w, w);
+        for (int i = 0; i < TR; ++i) {
+          const float w = pp[key * SM::PS + i];
+          if (decltype(mask)::value && w < 0.f) continue;
+          const uint64_t w2 = pk2(w, w);
 #pragma unroll
-            for (int c = 0; c < D / 64; ++c) {
-              o[i][c][0] = ffma2(w2, vv[c][0], o[i][c][0]);
-              o[i][c][1] = ffma2(w2, vv[c][1], o[i][c][1]);
-            }
+          for (int c = 0; c < D / 64; ++c) {
+            o[i][c][0] = ffma2(w2, vv[c][0], o[i][c][0]);
+            o[i][c][1] = ffma2(w2, vv[c][1], o[i][c][1]);
           }
         }
+      };
+      if (!masked) {
+#pragma unroll 4
+        for (int key = 0; key < BK; ++key) add(key, std::false_type());
       } else {
         // a zero weight times a value that is not finite would be a NaN
 #pragma unroll 1
-        for (int key = 0; key < BK; ++key) {
-          uint64_t vv[D / 64][2];
-#pragma unroll
-          for (int c = 0; c < D / 64; ++c) lds_2x64(va + (key * D + 64 * c) * 4, vv[c][0], vv[c][1]);
-#pragma unroll
-          for (int i = 0; i < TR; ++i) {
-            const float w = pp[key * SM::PS + i];
-            if (w < 0.f) continue;
-            const uint64_t w2 = pk2(w, w);
-#pragma unroll
-            for (int c = 0; c < D / 64; ++c) {
-              o[i][c][0] = ffma2(w2, vv[c][0], o[i][c][0]);
-              o[i][c][1] = ffma2(w2, vv[c][1], o[i][c][1]);
-            }
-          }
-        }
+        for (int key = 0; key < BK; ++key) add(key, std::true_type());
       }
       __syncwarp();
     }
@@ -295,17 +291,23 @@ __global__ void __launch_bounds__(NT, TR >= 4 ? 2 : 3) attend_simt_kernel(const 
 
 template <int D, bool I8, int TR>
 cudaError_t launch(const AttendJob& A, const AttendPlan& P, cudaStream_t st) {
-  constexpr int bytes = (int)sizeof(SimtSmem<D, TR>);
+  using SM = Simt<D, TR>;
+  constexpr int bytes = (int)sizeof(typename SM::Smem);
+  // A call of many units is not launched as a programmatic dependent: behind another
+  // call's merge it then took 488 to 790 us for 64 requests of 8 heads (512 units) instead
+  // of 444. One of few saves 1 to 2 us by it.
+  const bool overlap = 2 * P.uoff[A.c.B] < P.workers;
   const cudaError_t e =
       cudaFuncSetAttribute(attend_simt_kernel<D, I8, TR>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
   if (e != cudaSuccess) return e;
-  return launch_kernel(attend_simt_kernel<D, I8, TR>, dim3(P.workers), NT, bytes, st, true, 0, A, P);
+  return launch_kernel(attend_simt_kernel<D, I8, TR>, dim3(P.workers), SM::NT, bytes, st, overlap, 0, A, P);
 }
 
 template <int D, bool I8>
 cudaError_t launch_rows(const AttendJob& A, const AttendPlan& P, cudaStream_t st) {
   if (P.rows <= 8) return launch<D, I8, 1>(A, P, st);
   if (P.rows <= 16) return launch<D, I8, 2>(A, P, st);
+  if (P.rows <= 64) return launch<D, I8, 4>(A, P, st);
   return launch<D, I8, 8>(A, P, st);
 }
 

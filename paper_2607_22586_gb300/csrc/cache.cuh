@@ -14,7 +14,7 @@ struct CacheJob {
   int32_t i8;                    // the pages hold 8-bit codes with scales
   int32_t page_shift, n_pages, max_pages;
   int32_t cap;                   // positions of a sequence: max_pages << page_shift
-  Divisor by_r;                  // by r
+  Divisor by_r, by_heads;        // by r and by Hkv
   int64_t stride, ls;            // elements between tokens / layers of the call's K and V, or Q
   uint8_t *kp, *vp;
   float *ks, *vs;
