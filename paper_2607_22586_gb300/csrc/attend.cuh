@@ -5,9 +5,10 @@
 // row's, are cut into pieces of 2^step_shift, and the pieces of all units in
 // their order are shared out evenly to the workers (CTAs), however long the
 // sequences are: their lengths are read on the device, so every CTA adds up
-// the pieces itself. A worker's range covers whole units, whose results it
-// writes, and at most two pieces of units, its first and its last, whose
-// partial sums it leaves for the merge kernel.
+// the pieces itself. A unit counts for `extra` pieces more, before its first: its
+// start and end take a worker about as long. A worker's range covers whole units,
+// whose results it writes, and at most two parts of units, its first and its last,
+// whose partial sums it leaves for the merge kernel.
 #pragma once
 
 #include "cache.cuh"
@@ -19,7 +20,7 @@ struct AttendPlan {
   int32_t tiles[MMSHIFT_MAX_BATCH];     // a request's row tiles per KV head
   Divisor by_tiles[MMSHIFT_MAX_BATCH];
   int32_t rows;                         // query rows of a tile
-  int32_t step_shift;
+  int32_t step_shift, extra;
   int32_t workers, least;               // workers at most; one has 2^least pieces where there are as many
   float* po;                            // [2 * workers][rows][d] sums of weights times values
   float2* pml;                          // [2 * workers][rows] their maximum (base 2) and sum of weights
@@ -29,7 +30,7 @@ struct AttendUnit {
   int b, h, n;         // request, KV head, the request's tokens
   int row0, rows;      // the tile's first row, its rows
   int len, keys;       // rows of the sequence; keys that the tile's last row attends to
-  int pieces;
+  int pieces, cost;    // cost: pieces and extra, 0 without keys
 };
 
 // Start of an attention kernel: everything before it in the stream is done, and the
@@ -53,11 +54,12 @@ __device__ __forceinline__ AttendUnit attend_unit(const AttendJob& A, const Atte
   x.len = lens ? lens[seq] : cache_len(J, seq);
   x.keys = keys_of(A.causal, x.len, x.n, J.by_r(x.row0 + x.rows - 1));
   x.pieces = (x.keys + (1 << P.step_shift) - 1) >> P.step_shift;
+  x.cost = x.pieces ? x.pieces + P.extra : 0;
   return x;
 }
 
-// A worker's place in the work: pieces [begin, end) of all, the unit that
-// holds the first of them and the pieces before that unit.
+// A worker's place in the work: [begin, end) of all units' costs, the unit that
+// holds the first of them and the costs before that unit.
 struct AttendSpan {
   int64_t begin, end, before;
   int unit;
@@ -75,7 +77,7 @@ struct AttendScan {
 };
 
 // Called by all NT threads of a CTA. Every thread adds up a run of units, [u0, u1);
-// `before` are the pieces before its run, `sum` the run's, W all units'.
+// `before` are the costs before its run, `sum` the run's, W all units'.
 struct AttendSums {
   int u0, u1;
   int64_t before, sum, W;
@@ -90,7 +92,7 @@ struct AttendSums {
     u0 = min(tid * per, U);
     u1 = min(u0 + per, U);
     sum = 0;
-    for (int u = u0; u < u1; ++u) sum += attend_unit(A, P, s->lengths(A.c), u).pieces;
+    for (int u = u0; u < u1; ++u) sum += attend_unit(A, P, s->lengths(A.c), u).cost;
     int64_t x = sum;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -121,7 +123,7 @@ __device__ __forceinline__ AttendSpan attend_span(const AttendJob& A, const Atte
     int u = x.u0;
     int64_t a = x.before;
     while (x.u1 - x.u0 > 1) {
-      const int p = attend_unit(A, P, s->lengths(A.c), u).pieces;
+      const int p = attend_unit(A, P, s->lengths(A.c), u).cost;
       if (a + p > begin) break;
       a += p;
       ++u;
@@ -132,7 +134,15 @@ __device__ __forceinline__ AttendSpan attend_span(const AttendJob& A, const Atte
   return s->span;
 }
 
-// The partial sums' slot of a worker's piece of the unit with `before` pieces before it.
+// The unit's pieces [s0, s1) among a worker's [begin, end), with `before` before the unit.
+__device__ __forceinline__ void attend_pieces(const AttendPlan& P, const AttendUnit& U, int64_t begin, int64_t end,
+                                              int64_t before, int& s0, int& s1) {
+  const int64_t first = before + P.extra;
+  s0 = (int)(max(begin, first) - first);
+  s1 = (int)max(min(end, first + U.pieces) - first, (int64_t)0);
+}
+
+// The partial sums' slot of a worker's part of the unit with `before` before it.
 __device__ __forceinline__ int attend_slot(int worker, int64_t begin, int64_t before) {
   return 2 * worker + (before > begin);
 }
@@ -170,7 +180,7 @@ __device__ __forceinline__ void attend_write(const AttendJob& A, int b, int h, i
   if (d0 == 0 && A.lse) A.lse[at] = z == 0.f ? -INFINITY : (top + log2f(z)) * 0.6931471805599453f;
 }
 
-cudaError_t launch_attend_token(const AttendJob& A, const AttendPlan& P, cudaStream_t st);
+cudaError_t launch_attend_token(const AttendJob& A, const AttendPlan& P, bool cluster, cudaStream_t st);
 cudaError_t launch_attend_simt(const AttendJob& A, const AttendPlan& P, cudaStream_t st);
 cudaError_t launch_attend_chunk(const AttendJob& A, const AttendPlan& P, cudaStream_t st);
 

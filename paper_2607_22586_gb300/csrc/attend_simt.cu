@@ -64,14 +64,19 @@ __global__ void __launch_bounds__(Simt<D, TR>::NT, Simt<D, TR>::CTAS)
   int64_t before = sp.before;
   for (int64_t at = sp.begin; at < sp.end;) {
     const AttendUnit U = attend_unit(A, P, sm.scan.lengths(A.c), u);
-    const int64_t last = before + U.pieces;
+    const int64_t last = before + U.cost;
     if (last <= at) {
       before = last;
       ++u;
       continue;
     }
     const int64_t stop = min(sp.end, last);
-    const int s0 = (int)(at - before), s1 = (int)(stop - before);
+    int s0, s1;
+    attend_pieces(P, U, at, stop, before, s0, s1);
+    if (s0 >= s1) {                                    // the unit's start alone
+      at = stop;
+      continue;
+    }
     const int32_t* table = J.table + ((size_t)U.b * J.Hkv + U.h) * J.max_pages;
 
     for (int i = tid; i < SM::RT * (D / 4); i += NT) {

@@ -27,11 +27,13 @@
 // The maxima are only raised when a value passes them by 8 (base 2), so the common
 // step has one vote and no reduction: weights then stay below 2^8.
 #include "attend.cuh"
+#include "umma.cuh"
 
 namespace mmshift {
 namespace {
 
 constexpr int NT = 128, NW = NT / 32;
+constexpr int kCluster = 8;
 constexpr float kRaise = 8.f;
 
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
@@ -103,7 +105,7 @@ struct Token {
 
   struct alignas(16) Smem {
     float o[NW][8 * NQ][SROW];
-    float2 ml[NW][8 * NQ];
+    float2 ml[NW][8 * NQ], part[8 * NQ];
     AttendScan<NT> scan;
   };
 
@@ -208,7 +210,11 @@ struct Token {
   }
 };
 
-template <int D, bool I8, int NQ>
+// CLUSTER: a cluster of kCluster CTAs has a unit, each an equal part of its pieces, and
+// merges the parts through distributed shared memory: one launch, no lengths to add up.
+// For calls of few units that can only be short (see launch_attend); others are
+// balanced over all SMs, and merged by a kernel of their own.
+template <int D, bool I8, int NQ, bool CLUSTER>
 __global__ void __launch_bounds__(NT, NQ == 1 ? 3 : 2) attend_token_kernel(const __grid_constant__ AttendJob A,
                                                                            const __grid_constant__ AttendPlan P) {
   using T = Token<D, I8, NQ>;
@@ -216,19 +222,29 @@ __global__ void __launch_bounds__(NT, NQ == 1 ? 3 : 2) attend_token_kernel(const
   attend_start();
   const CacheJob& J = A.c;
   const int lane = threadIdx.x % 32, w = threadIdx.x / 32, g = lane / 4, c = lane % 4;
-  const AttendSpan sp = attend_span(A, P, &sm.scan);
+  const int rank = CLUSTER ? blockIdx.x % kCluster : 0;
+  const AttendSpan sp = CLUSTER ? AttendSpan{0, 1, 0, (int)blockIdx.x / kCluster} : attend_span(A, P, &sm.scan);
   int u = sp.unit;
   int64_t before = sp.before;
   for (int64_t at = sp.begin; at < sp.end;) {
-    const AttendUnit U = attend_unit(A, P, sm.scan.lengths(A.c), u);
-    const int64_t last = before + U.pieces;
-    if (last <= at) {                                  // a unit without pieces
-      before = last;
-      ++u;
-      continue;
+    const AttendUnit U = attend_unit(A, P, CLUSTER ? nullptr : sm.scan.lengths(A.c), u);
+    const int64_t last = before + U.cost, stop = min(sp.end, last);
+    int s0, s1;
+    if constexpr (CLUSTER) {
+      s0 = U.pieces * rank / kCluster;
+      s1 = U.pieces * (rank + 1) / kCluster;
+    } else {
+      if (last <= at) {                                // a unit without pieces
+        before = last;
+        ++u;
+        continue;
+      }
+      attend_pieces(P, U, at, stop, before, s0, s1);
+      if (s0 >= s1) {                                  // the unit's start alone
+        at = stop;
+        continue;
+      }
     }
-    const int64_t stop = min(sp.end, last);
-    const int s0 = (int)(at - before), s1 = (int)(stop - before);
     const int32_t* table = J.table + ((size_t)U.b * J.Hkv + U.h) * J.max_pages;
 
     // row of the pool of each 16-key block, -1 behind the end and without a page
@@ -522,33 +538,72 @@ __global__ void __launch_bounds__(NT, NQ == 1 ? 3 : 2) attend_token_kernel(const
         acc.z += v.z * f;
         acc.w += v.w * f;
       }
-      if (whole) {
+      if constexpr (CLUSTER) {
+        *reinterpret_cast<float4*>(&sm.o[0][r][d0]) = acc;   // read by this thread alone
+        if (d0 == 0) sm.part[r] = make_float2(top, z);
+      } else if (whole) {
         attend_write<__nv_bfloat16, D>(A, U.b, U.h, r, d0, acc, top, z);
       } else {
         *reinterpret_cast<float4*>(P.po + (slot + r) * D + d0) = acc;
         if (d0 == 0) P.pml[slot + r] = make_float2(top, z);
       }
     }
-    __syncthreads();
-    at = stop;
-    if (stop == last) {
-      before = last;
-      ++u;
+    if constexpr (CLUSTER) {
+      umma::cluster_sync();
+      for (int i = rank * NT + threadIdx.x; i < U.rows * (D / 4); i += kCluster * NT) {
+        const int r = i / (D / 4), d0 = i % (D / 4) * 4;
+        const uint32_t po = umma::smem_u32(&sm.o[0][r][d0]), pm = umma::smem_u32(&sm.part[r]);
+        float2 ml[kCluster];
+        float top = -INFINITY, z = 0.f;
+#pragma unroll
+        for (int k = 0; k < kCluster; ++k) {
+          ml[k] = umma::ld_cluster_f2(umma::mapa(pm, k));
+          top = fmaxf(top, ml[k].x);
+        }
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int k = 0; k < kCluster; ++k) {
+          const float f = ml[k].x == -INFINITY ? 1.f : fast_exp2(ml[k].x - top);
+          const uint32_t p = umma::mapa(po, k);
+          const float2 a = umma::ld_cluster_f2(p), b = umma::ld_cluster_f2(p + 8);
+          z += ml[k].y * f;
+          acc.x += a.x * f;
+          acc.y += a.y * f;
+          acc.z += b.x * f;
+          acc.w += b.y * f;
+        }
+        attend_write<__nv_bfloat16, D>(A, U.b, U.h, r, d0, acc, top, z);
+      }
+      umma::cluster_sync();                            // the others have read this CTA's part
+      at = sp.end;
+    } else {
+      __syncthreads();
+      at = stop;
+      if (stop == last) {
+        before = last;
+        ++u;
+      }
     }
   }
 }
 
 }  // namespace
 
-cudaError_t launch_attend_token(const AttendJob& A, const AttendPlan& P, cudaStream_t st) {
-  auto go = [&](auto kernel) { return launch_kernel(kernel, dim3(P.workers), NT, 0, st, true, 0, A, P); };
+cudaError_t launch_attend_token(const AttendJob& A, const AttendPlan& P, bool cluster, cudaStream_t st) {
   const CacheJob& J = A.c;
+  auto go = [&](auto whole, auto parts) {
+    if (cluster)
+      return launch_kernel(parts, dim3(P.uoff[J.B] * kCluster), NT, 0, st, true, kCluster, A, P);
+    return launch_kernel(whole, dim3(P.workers), NT, 0, st, true, 0, A, P);
+  };
+#define MMSHIFT_TOKEN(D, I8, NQ) go(attend_token_kernel<D, I8, NQ, false>, attend_token_kernel<D, I8, NQ, true>)
   if (P.rows <= 8) {
-    if (J.d == 128) return J.i8 ? go(attend_token_kernel<128, true, 1>) : go(attend_token_kernel<128, false, 1>);
-    return J.i8 ? go(attend_token_kernel<64, true, 1>) : go(attend_token_kernel<64, false, 1>);
+    if (J.d == 128) return J.i8 ? MMSHIFT_TOKEN(128, true, 1) : MMSHIFT_TOKEN(128, false, 1);
+    return J.i8 ? MMSHIFT_TOKEN(64, true, 1) : MMSHIFT_TOKEN(64, false, 1);
   }
-  if (J.d == 128) return J.i8 ? go(attend_token_kernel<128, true, 2>) : go(attend_token_kernel<128, false, 2>);
-  return J.i8 ? go(attend_token_kernel<64, true, 2>) : go(attend_token_kernel<64, false, 2>);
+  if (J.d == 128) return J.i8 ? MMSHIFT_TOKEN(128, true, 2) : MMSHIFT_TOKEN(128, false, 2);
+  return J.i8 ? MMSHIFT_TOKEN(64, true, 2) : MMSHIFT_TOKEN(64, false, 2);
+#undef MMSHIFT_TOKEN
 }
 
 }  // namespace mmshift

@@ -175,7 +175,7 @@ __device__ __forceinline__ bool wait_bar(uint64_t* bar, uint32_t parity, volatil
 // A run: consecutive key tiles [s0, s1) of a unit that the CTA works on together.
 struct Run {
   AttendUnit U;
-  int64_t before;        // pieces before the unit
+  int64_t before;        // costs before the unit
   int s0, s1;
   bool two;              // the second block has rows
 };
@@ -184,7 +184,7 @@ struct Run {
 // lane a unit; a role itself those behind them (units of few keys).
 constexpr int RUNS = 16;
 struct Walk {
-  int k, unit;           // runs so far; behind the list, the next unit and the pieces before it
+  int k, unit;           // runs so far; behind the list, the next unit and the costs before it
   int64_t before;
 };
 struct RunList {
@@ -193,12 +193,11 @@ struct RunList {
   int n;
 };
 
-__device__ __forceinline__ Run run_of(const AttendSpan& sp, const AttendUnit& U, int64_t before) {
+__device__ __forceinline__ Run run_of(const AttendPlan& P, const AttendSpan& sp, const AttendUnit& U, int64_t before) {
   Run R;
   R.U = U;
   R.before = before;
-  R.s0 = (int)(max(sp.begin, before) - before);
-  R.s1 = (int)(min(sp.end, before + U.pieces) - before);
+  attend_pieces(P, U, sp.begin, sp.end, before, R.s0, R.s1);
   R.two = U.rows > BQ;
   return R;
 }
@@ -209,18 +208,19 @@ __device__ __forceinline__ void list_runs(const AttendJob& A, const AttendPlan& 
   const int u = sp.unit + lane;
   const bool in = sp.begin < sp.end && lane < RUNS && u < P.uoff[A.c.B];
   AttendUnit U;
-  U.pieces = 0;
+  U.pieces = U.cost = 0;
   if (in) U = attend_unit(A, P, nullptr, u);
-  int64_t x = U.pieces;
+  int64_t x = U.cost;
 #pragma unroll
   for (int d = 1; d < RUNS; d <<= 1) {
     const int64_t y = __shfl_up_sync(0xffffffffu, x, d);
     if (lane >= d) x += y;
   }
-  const int64_t before = sp.before + x - U.pieces;
-  const bool mine = in && U.pieces > 0 && before < sp.end;
+  const int64_t before = sp.before + x - U.cost;
+  const Run R = run_of(P, sp, U, before);
+  const bool mine = in && R.s0 < R.s1;
   const unsigned all = __ballot_sync(0xffffffffu, mine);
-  if (mine) list->run[__popc(all & ((1u << lane) - 1u))] = run_of(sp, U, before);
+  if (mine) list->run[__popc(all & ((1u << lane) - 1u))] = R;
   if (lane == RUNS - 1) {                              // where the walk goes on
     list->n = __popc(all);
     list->rest = Walk{0, u + 1, in ? sp.before + x : sp.end};
@@ -240,13 +240,10 @@ __device__ __forceinline__ bool next_run(const AttendJob& A, const AttendPlan& P
   }
   while (w.before < sp.end) {
     const AttendUnit U = attend_unit(A, P, nullptr, w.unit);
-    const int64_t before = w.before;
-    w.before += U.pieces;
+    R = run_of(P, sp, U, w.before);
+    w.before += U.cost;
     ++w.unit;
-    if (U.pieces) {
-      R = run_of(sp, U, before);
-      return true;
-    }
+    if (R.s0 < R.s1) return true;
   }
   return false;
 }

@@ -80,6 +80,23 @@ def test_long_sequence(dtype, kind, n):
 
 
 @pytest.mark.parametrize("dtype,kind", KINDS)
+@pytest.mark.parametrize("d", [64, 128])
+def test_long_chunk(dtype, kind, d):
+    """Several row tiles, rings of tiles gone round many times."""
+    _run([[4500, 300]], [150], 6, d, dtype, kind, 32)
+
+
+@pytest.mark.parametrize("dtype,kind", KINDS)
+@pytest.mark.parametrize("n,r", [(1, 2), (2, 9)])
+def test_more_sequences_than_any_list_holds(dtype, kind, n, r):
+    """1,088 and 2,816 sequences of a few rows: lengths that do not fit in shared memory, workers
+    with more units than are listed ahead."""
+    B, H = 64, 17 if n == 1 else 44
+    lens = [[(5 * b + 7 * h) % 23 for h in range(H)] for b in range(B)]
+    _run(lens, [n] * B, H * r, 64, dtype, kind, 16)
+
+
+@pytest.mark.parametrize("dtype,kind", KINDS)
 @pytest.mark.parametrize("n", [1, 20])
 def test_large_logits_and_scale(dtype, kind, n):
     """Logits of hundreds, the largest anywhere: the running maximum has to follow."""
