@@ -8,59 +8,41 @@
 namespace mmshift {
 namespace {
 
-// The partial sums of units that several workers share, and zeros for units
-// without keys. A block takes RPB rows: RPB = 1 with all its warps on the parts of
-// a row (few rows, many parts), else a warp a row.
-template <typename T, int D, int RPB>
-__global__ void __launch_bounds__(256) attend_merge_kernel(const __grid_constant__ AttendJob A,
-                                                           const __grid_constant__ AttendPlan P) {
-  constexpr int LV = D / 32;                           // values of a lane
-  __shared__ AttendScan<256> scan;
-  __shared__ int64_t place[2];
-  const int u = blockIdx.x, w = threadIdx.x / 32, lane = threadIdx.x % 32;
-  // Which workers share the unit follows from the lengths, which were there before the
-  // attention kernel began: worked out while that still runs.
-  {
-    const AttendSums x(A, P, &scan);
-    if (u >= x.u0 && u < x.u1) {
-      int64_t a = x.before;
-      for (int k = x.u0; k < u; ++k) a += attend_unit(A, P, scan.lengths(A.c), k).cost;
-      place[0] = a;
-      place[1] = x.W;
-    }
-    __syncthreads();
-  }
-  const AttendUnit U = attend_unit(A, P, scan.lengths(A.c), u);
-  const int64_t before = place[0], a = before + P.extra, b = a + U.pieces;   // where its pieces are
-  int i0 = 0, i1 = -1, first = 0;
-  bool whole = false;
-  if (a < b) {
-    const Shares sh = shares_of(place[1], P.workers, P.least);
+// Which workers have a unit's parts: workers [i0, i1], the first one's slot.
+struct Parts {
+  int i0, i1, first;
+  __device__ __forceinline__ Parts(const AttendPlan& P, const Shares& sh, const AttendUnit& U, int64_t before) {
+    const int64_t a = before + P.extra;                // its pieces are at [a, a + pieces)
     i0 = sh.of(a);
-    whole = b <= sh.begin(i0 + 1);                     // one worker had it all
-    i1 = sh.of(b - 1);
+    i1 = a + U.pieces <= sh.begin(i0 + 1) ? i0 : sh.of(a + U.pieces - 1);
     first = attend_slot(i0, sh.begin(i0), before);
   }
-  const int r = RPB == 1 ? blockIdx.y : blockIdx.y * RPB + w;
-  dependent_start();
-  if (whole || r >= U.rows) return;
-  const int parts = i1 - i0 + 1;
-  // a worker's first piece has an even slot; only the unit's first part can be a last piece
-  auto at = [&](int k) { return (size_t)(k ? 2 * (i0 + k) : first) * P.rows + r; };
-  float top = -INFINITY;
-  for (int k = lane; k < parts; k += 32) top = fmaxf(top, P.pml[at(k)].x);
+  // A worker's first part has an even slot; only the unit's first can be a worker's last.
+  __device__ __forceinline__ size_t slot(const AttendPlan& P, int k, int r) const {
+    return (size_t)(k ? 2 * (i0 + k) : first) * P.rows + r;
+  }
+};
+
+// A warp's sum over the parts k0, k0 + STEP, ... of row r: its lane's D / 32 values.
+template <int D, int STEP>
+__device__ __forceinline__ void add_parts(const AttendPlan& P, const Parts& x, int r, int lane, int k0, float& top,
+                                          float& z, float (&o)[D / 32]) {
+  const int parts = x.i1 - x.i0 + 1;
+  top = -INFINITY;
+  for (int k = lane; k < parts; k += 32) top = fmaxf(top, P.pml[x.slot(P, k, r)].x);
 #pragma unroll
   for (int s = 16; s; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
-  float z = 0.f, o[LV] = {};
-  constexpr int STEP = RPB == 1 ? 8 : 1;
+  z = 0.f;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) o[i] = 0.f;
 #pragma unroll 8
-  for (int k = RPB == 1 ? w : 0; k < parts; k += STEP) {
-    const size_t slot = at(k);
+  for (int k = k0; k < parts; k += STEP) {
+    const size_t slot = x.slot(P, k, r);
     const float2 ml = P.pml[slot];
     const float f = ml.x == -INFINITY ? 1.f : fast_exp2(ml.x - top);
     z += ml.y * f;
-    const float* p = P.po + slot * D + lane * LV;
-    if constexpr (LV == 4) {
+    const float* p = P.po + slot * D + lane * (D / 32);
+    if constexpr (D == 128) {
       const float4 v = *reinterpret_cast<const float4*>(p);
       o[0] += v.x * f;
       o[1] += v.y * f;
@@ -72,47 +54,111 @@ __global__ void __launch_bounds__(256) attend_merge_kernel(const __grid_constant
       o[1] += v.y * f;
     }
   }
-  if constexpr (RPB == 1) {
-    __shared__ alignas(16) float so[8][D];
-    __shared__ float sz[8];
-#pragma unroll
-    for (int i = 0; i < LV; ++i) so[w][lane * LV + i] = o[i];
-    if (lane == 0) sz[w] = z;
-    __syncthreads();
-    if (threadIdx.x >= D / 4) return;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    z = 0.f;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const float4 x = *reinterpret_cast<const float4*>(&so[k][threadIdx.x * 4]);
-      v.x += x.x;
-      v.y += x.y;
-      v.z += x.z;
-      v.w += x.w;
-      z += sz[k];
-    }
-    attend_write<T, D>(A, U.b, U.h, U.row0 + r, threadIdx.x * 4, v, top, z);
+}
+
+// The merge of few units of many parts each (4 units of 114): a block a row, its warps
+// on the row's parts. Zeros for units without keys. Which workers share the unit follows
+// from the lengths, which were there before the attention kernel began: worked out while
+// that still runs.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) attend_merge_row_kernel(const __grid_constant__ AttendJob A,
+                                                               const __grid_constant__ AttendPlan P) {
+  __shared__ AttendScan<256> scan;
+  __shared__ AttendStart place;
+  __shared__ alignas(16) float so[8][D];
+  __shared__ float sz[8];
+  const int u = blockIdx.x, r = blockIdx.y, w = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const AttendSums x(A, P, &scan);
+  if (u >= x.u0 && u < x.u1) {
+    place.before = x.before;
+    for (int k = x.u0; k < u; ++k) place.before += attend_unit(A, P, scan.lengths(A.c), k).cost;
+  }
+  __syncthreads();
+  const AttendUnit U = attend_unit(A, P, scan.lengths(A.c), u);
+  float top = -INFINITY, z = 0.f, o[D / 32] = {};
+  if (U.pieces) {
+    const Parts parts(P, shares_of(x.W, P.workers, P.least), U, place.before);
+    dependent_start();
+    if (parts.i0 == parts.i1 || r >= U.rows) return;   // one worker had it all
+    add_parts<D, 8>(P, parts, r, lane, w, top, z, o);
   } else {
-    // four neighbouring values to one lane
-    float4 v;
-    if constexpr (LV == 4) {
-      v = make_float4(o[0], o[1], o[2], o[3]);
-      attend_write<T, D>(A, U.b, U.h, U.row0 + r, lane * 4, v, top, z);
-    } else {
-      const float x = __shfl_down_sync(0xffffffffu, o[0], 1), y = __shfl_down_sync(0xffffffffu, o[1], 1);
-      v = make_float4(o[0], o[1], x, y);
-      if (lane % 2 == 0) attend_write<T, D>(A, U.b, U.h, U.row0 + r, lane * 2, v, top, z);
+    dependent_start();
+    if (r >= U.rows) return;
+  }
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) so[w][lane * (D / 32) + i] = o[i];
+  if (lane == 0) sz[w] = z;
+  __syncthreads();
+  if (threadIdx.x >= D / 4) return;
+  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+  z = 0.f;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const float4 y = *reinterpret_cast<const float4*>(&so[k][threadIdx.x * 4]);
+    v.x += y.x;
+    v.y += y.y;
+    v.z += y.z;
+    v.w += y.w;
+    z += sz[k];
+  }
+  attend_write<T, D>(A, U.b, U.h, U.row0 + r, threadIdx.x * 4, v, top, z);
+}
+
+// The merge of many units: only those across a border of two workers' shares have
+// parts, so a block takes a border (and 8 rows, a warp a row), the first inside its unit's
+// pieces. The blocks behind them write zeros for units without keys.
+constexpr int kEmptyBlocks = 16;
+
+template <typename T, int D>
+__global__ void __launch_bounds__(256) attend_merge_border_kernel(const __grid_constant__ AttendJob A,
+                                                                  const __grid_constant__ AttendPlan P) {
+  dependent_start();
+  const int w = threadIdx.x / 32, lane = threadIdx.x % 32, i = blockIdx.x + 1;
+  if (i >= P.workers) {
+    __shared__ int empty[256], n;
+    if (blockIdx.y) return;
+    const int units = P.uoff[A.c.B];
+    for (int u0 = (i - P.workers) * 256; u0 < units; u0 += kEmptyBlocks * 256) {
+      if (threadIdx.x == 0) n = 0;
+      __syncthreads();
+      const int u = u0 + threadIdx.x;
+      if (u < units && !attend_unit(A, P, nullptr, u).pieces) empty[atomicAdd(&n, 1)] = u;
+      __syncthreads();
+      for (int k = 0; k < n; ++k) {
+        const AttendUnit U = attend_unit(A, P, nullptr, empty[k]);
+        for (int e = threadIdx.x; e < U.rows * (D / 4); e += 256)
+          attend_write<T, D>(A, U.b, U.h, U.row0 + e / (D / 4), e % (D / 4) * 4, make_float4(0.f, 0.f, 0.f, 0.f),
+                             -INFINITY, 0.f);
+      }
+      __syncthreads();
     }
+    return;
+  }
+  const Shares sh = shares_of(P.start[P.workers].before, P.workers, P.least);
+  if (i >= sh.n) return;
+  const AttendStart s = P.start[i];
+  const AttendUnit U = attend_unit(A, P, nullptr, s.unit);
+  const Parts parts(P, sh, U, s.before);
+  const int r = blockIdx.y * 8 + w;
+  if (parts.i0 + 1 != i || parts.i0 == parts.i1 || r >= U.rows) return;
+  float top, z, o[D / 32];
+  add_parts<D, 1>(P, parts, r, lane, 0, top, z, o);
+  // four neighbouring values to one lane
+  if constexpr (D == 128) {
+    attend_write<T, D>(A, U.b, U.h, U.row0 + r, lane * 4, make_float4(o[0], o[1], o[2], o[3]), top, z);
+  } else {
+    const float a = __shfl_down_sync(0xffffffffu, o[0], 1), b = __shfl_down_sync(0xffffffffu, o[1], 1);
+    if (lane % 2 == 0) attend_write<T, D>(A, U.b, U.h, U.row0 + r, lane * 2, make_float4(o[0], o[1], a, b), top, z);
   }
 }
 
 template <typename T, int D>
 cudaError_t launch_merge_t(const AttendJob& A, const AttendPlan& P, cudaStream_t st) {
   const unsigned units = P.uoff[A.c.B];
-  // few units, then many parts each: 4 units of 114 parts
   if (8 * units <= (unsigned)P.workers)
-    return launch_kernel(attend_merge_kernel<T, D, 1>, dim3(units, P.rows), 256, 0, st, true, 0, A, P);
-  return launch_kernel(attend_merge_kernel<T, D, 8>, dim3(units, (P.rows + 7) / 8), 256, 0, st, true, 0, A, P);
+    return launch_kernel(attend_merge_row_kernel<T, D>, dim3(units, P.rows), 256, 0, st, true, 0, A, P);
+  return launch_kernel(attend_merge_border_kernel<T, D>, dim3(P.workers - 1 + kEmptyBlocks, (P.rows + 7) / 8), 256, 0, st,
+                       true, 0, A, P);
 }
 
 cudaError_t launch_merge(const AttendJob& A, const AttendPlan& P, cudaStream_t st) {
@@ -187,7 +233,9 @@ char* place(AttendPlan& P, const CacheJob& J, char* at) {
   P.po = reinterpret_cast<float*>(at);
   at += align256((size_t)2 * P.workers * P.rows * J.d * sizeof(float));
   P.pml = reinterpret_cast<float2*>(at);
-  return at + align256((size_t)2 * P.workers * P.rows * sizeof(float2));
+  at += align256((size_t)2 * P.workers * P.rows * sizeof(float2));
+  P.start = reinterpret_cast<AttendStart*>(at);
+  return at + align256((size_t)(P.workers + 1) * sizeof(AttendStart));
 }
 
 }  // namespace

@@ -15,6 +15,12 @@
 
 namespace mmshift {
 
+// Where a worker's share begins: the unit with its first piece, the costs before that.
+struct AttendStart {
+  int64_t before;
+  int32_t unit, unused;
+};
+
 struct AttendPlan {
   int32_t uoff[MMSHIFT_MAX_BATCH + 1];  // units, prefix over requests
   int32_t tiles[MMSHIFT_MAX_BATCH];     // a request's row tiles per KV head
@@ -24,6 +30,7 @@ struct AttendPlan {
   int32_t workers, least;               // workers at most; one has 2^least pieces where there are as many
   float* po;                            // [2 * workers][rows][d] sums of weights times values
   float2* pml;                          // [2 * workers][rows] their maximum (base 2) and sum of weights
+  AttendStart* start;                   // [workers], and one more whose `before` is all units' cost
 };
 
 struct AttendUnit {
@@ -118,6 +125,7 @@ __device__ __forceinline__ AttendSpan attend_span(const AttendJob& A, const Atte
   const Shares sh = shares_of(x.W, P.workers, P.least);
   const int i = blockIdx.x;
   const int64_t begin = i < sh.n ? sh.begin(i) : x.W, end = i < sh.n ? sh.begin(i + 1) : x.W;
+  if (i == 0 && threadIdx.x == 0) P.start[P.workers].before = x.W;
   if (begin >= end) return AttendSpan{begin, end, 0, 0};
   if (begin >= x.before && begin < x.before + x.sum) {
     int u = x.u0;
@@ -129,6 +137,7 @@ __device__ __forceinline__ AttendSpan attend_span(const AttendJob& A, const Atte
       ++u;
     }
     s->span = AttendSpan{begin, end, a, u};
+    P.start[i] = AttendStart{a, u, 0};
   }
   __syncthreads();
   return s->span;
