@@ -8,6 +8,11 @@
 namespace mmshift {
 namespace {
 
+// Start of a merge: everything before it is done. The next kernel is not let in early:
+// merges start early themselves, so it would come while the attention kernel still runs
+// (178 to 285 us instead of 68 for a call behind another).
+__device__ __forceinline__ void merge_start() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 // Which workers have a unit's parts: workers [i0, i1], the first one's slot.
 struct Parts {
   int i0, i1, first;
@@ -78,11 +83,11 @@ __global__ void __launch_bounds__(256) attend_merge_row_kernel(const __grid_cons
   float top = -INFINITY, z = 0.f, o[D / 32] = {};
   if (U.pieces) {
     const Parts parts(P, shares_of(x.W, P.workers, P.least), U, place.before);
-    dependent_start();
+    merge_start();
     if (parts.i0 == parts.i1 || r >= U.rows) return;   // one worker had it all
     add_parts<D, 8>(P, parts, r, lane, w, top, z, o);
   } else {
-    dependent_start();
+    merge_start();
     if (r >= U.rows) return;
   }
 #pragma unroll
@@ -112,7 +117,7 @@ constexpr int kEmptyBlocks = 16;
 template <typename T, int D>
 __global__ void __launch_bounds__(256) attend_merge_border_kernel(const __grid_constant__ AttendJob A,
                                                                   const __grid_constant__ AttendPlan P) {
-  dependent_start();
+  merge_start();
   const int w = threadIdx.x / 32, lane = threadIdx.x % 32, i = blockIdx.x + 1;
   if (i >= P.workers) {
     __shared__ int empty[256], n;

@@ -40,13 +40,6 @@ struct AttendUnit {
   int pieces, cost;    // cost: pieces and extra, 0 without keys
 };
 
-// Start of an attention kernel: everything before it in the stream is done, and the
-// merge kernel may start and read the lengths too.
-__device__ __forceinline__ void attend_start() {
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-}
-
 // lens: the sequences' lengths (AttendScan::lengths), or null to read them from the cache.
 __device__ __forceinline__ AttendUnit attend_unit(const AttendJob& A, const AttendPlan& P, const int32_t* lens, int u) {
   const CacheJob& J = A.c;

@@ -56,7 +56,7 @@ __global__ void __launch_bounds__(Simt<D, TR>::NT, Simt<D, TR>::CTAS)
   constexpr int NT = SM::NT, BK = SM::BK, NK = SM::NK;
   extern __shared__ __align__(16) unsigned char smraw[];
   typename SM::Smem& sm = *reinterpret_cast<typename SM::Smem*>(smraw);
-  attend_start();
+  cache_start();
   const CacheJob& J = A.c;
   const int tid = threadIdx.x, lane = tid % 32, tx = tid % 16, ty = tid / 16;
   const AttendSpan sp = attend_span(A, P, &sm.scan);
@@ -298,14 +298,10 @@ template <int D, bool I8, int TR>
 cudaError_t launch(const AttendJob& A, const AttendPlan& P, cudaStream_t st) {
   using SM = Simt<D, TR>;
   constexpr int bytes = (int)sizeof(typename SM::Smem);
-  // A call of many units is not launched as a programmatic dependent: behind another
-  // call's merge it then took 488 to 790 us for 64 requests of 8 heads (512 units) instead
-  // of 444. One of few saves 1 to 2 us by it.
-  const bool overlap = 2 * P.uoff[A.c.B] < P.workers;
   const cudaError_t e =
       cudaFuncSetAttribute(attend_simt_kernel<D, I8, TR>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
   if (e != cudaSuccess) return e;
-  return launch_kernel(attend_simt_kernel<D, I8, TR>, dim3(P.workers), SM::NT, bytes, st, overlap, 0, A, P);
+  return launch_kernel(attend_simt_kernel<D, I8, TR>, dim3(P.workers), SM::NT, bytes, st, true, 0, A, P);
 }
 
 template <int D, bool I8>

@@ -219,7 +219,7 @@ __global__ void __launch_bounds__(NT, NQ == 1 ? 3 : 2) attend_token_kernel(const
                                                                            const __grid_constant__ AttendPlan P) {
   using T = Token<D, I8, NQ>;
   __shared__ typename T::Smem sm;
-  attend_start();
+  cache_start();
   const CacheJob& J = A.c;
   const int lane = threadIdx.x % 32, w = threadIdx.x / 32, g = lane / 4, c = lane % 4;
   const int rank = CLUSTER ? blockIdx.x % kCluster : 0;

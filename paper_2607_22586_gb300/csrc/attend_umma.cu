@@ -331,7 +331,7 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
   __syncthreads();
   fence_after();
   const uint32_t tmem = tbase;
-  attend_start();
+  cache_start();
   const AttendSpan sp = attend_span(A, P, &scan);
   if (warp == 0) list_runs(A, P, sp, lane, &runs);
   __syncthreads();

@@ -57,7 +57,7 @@ __global__ void __launch_bounds__(256) cache_write_kernel(const __grid_constant_
                                                           const uint8_t* K, const uint8_t* V,
                                                           const int32_t* idx, const int32_t* count,
                                                           bool vec) {
-  dependent_start();
+  cache_start();
   constexpr int ROWB = D * (int)sizeof(T), LPR = ROWB / 16, G = 256 / LPR;
   const int l = blockIdx.y, part = threadIdx.x % LPR;
   const int rows = J.off[J.B] * J.Hkv;                    // at most 2^30
@@ -176,7 +176,7 @@ template <typename T, int D, bool I8, int N>
 __global__ void __launch_bounds__(256) cache_read_kernel(const __grid_constant__ CacheJob J,
                                                          const int32_t* first, uint8_t* oK,
                                                          uint8_t* oV, bool vec) {
-  dependent_start();
+  cache_start();
   constexpr int ROWB = D * (int)sizeof(T), LPR = ROWB / 16, G = 256 / LPR;
   const int l = blockIdx.y, part = threadIdx.x % LPR;
   const int rows = J.off[J.B] * J.Hkv;

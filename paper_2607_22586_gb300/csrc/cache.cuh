@@ -37,6 +37,13 @@ __device__ __forceinline__ int64_t cache_slot(const CacheJob& J, size_t u, int t
   return page_row(J.table[u * J.max_pages + (t >> J.page_shift)], J.n_pages, J.page_shift, t);
 }
 
+// Start of the cache's kernels (but the merges): everything before one in the stream is
+// done, and the next one may take its place on the SMs.
+__device__ __forceinline__ void cache_start() {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
 // 16 bytes by plain loads and stores; `vec`: the address allows one access, else
 // it is that of 16-bit or larger elements.
 __device__ __forceinline__ uint4 load_plain16(const uint8_t* p, bool vec) {
