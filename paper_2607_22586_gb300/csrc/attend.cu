@@ -17,7 +17,7 @@ __device__ __forceinline__ void merge_start() { asm volatile("griddepcontrol.wai
 struct Parts {
   int i0, i1, first;
   __device__ __forceinline__ Parts(const AttendPlan& P, const Shares& sh, const AttendUnit& U, int64_t before) {
-    const int64_t a = before + P.extra;                // its pieces are at [a, a + pieces)
+    const int64_t a = before + U.extra;                // its pieces are at [a, a + pieces)
     i0 = sh.of(a);
     i1 = a + U.pieces <= sh.begin(i0 + 1) ? i0 : sh.of(a + U.pieces - 1);
     first = attend_slot(i0, sh.begin(i0), before);
@@ -172,11 +172,17 @@ cudaError_t launch_merge(const AttendJob& A, const AttendPlan& P, cudaStream_t s
   return A.c.d == 128 ? launch_merge_t<float, 128>(A, P, st) : launch_merge_t<float, 64>(A, P, st);
 }
 
-// Requests whose rows of a KV head are at most this many have a plan of their own:
-// bfloat16 rows go to the token kernel, float32 rows to tiles of 8 or 16 rows (others to
-// tiles of 256 and of 64 or 128).
+// Requests of few rows of a KV head have a plan of their own, of tiles of at most this
+// many: bfloat16 rows go to the token kernel, float32 rows to tiles of 8 or 16 rows
+// (requests of more rows to tiles of 256, or 64 or 128).
 constexpr int kTokenRows = 16;
 constexpr int kClusterSteps = 4;
+
+// Rows of a request's KV head that go to the plan of tiles of kTokenRows. More than one
+// tile reads the keys again, from the L2, but starts sooner than the chunk kernel: 16
+// requests of 32 heads, 300 to 750 rows, 32 tokens: bfloat16 68 us (chunk kernel 92),
+// 8-bit 62 (95); 48 tokens: 96 (93), 87 (96); 64 tokens: 125 (95), 112 (98).
+int few_rows(const CacheJob& J) { return J.bf16 ? 32 : kTokenRows; }
 
 constexpr int kSMs = 152;              // the workspace is sized without asking the device
 
@@ -211,13 +217,13 @@ AttendPlan plan_of(const CacheJob& J, int most, Take take) {
 
 // Plans for `nsm` SMs; a CTA a worker, as many as fit.
 AttendPlan token_plan(const CacheJob& J, int nsm) {
-  AttendPlan P = plan_of(J, kTokenRows, [&](int rows) { return rows <= kTokenRows; });
+  AttendPlan P = plan_of(J, kTokenRows, [&](int rows) { return rows <= few_rows(J); });
   if (J.bf16) {
     const int row = J.i8 ? J.d : 2 * J.d;
     while ((row << P.step_shift) < 4096) ++P.step_shift;   // a warp's piece: 4 KB of K
     P.least = 2;
     P.workers = nsm * (P.rows <= 8 ? 3 : 2);
-    P.extra = 8;
+    P.extra = P.extra1 = 8;
   } else {
     P.step_shift = 5;
     P.workers = nsm * (P.rows <= 8 ? 4 : 3);
@@ -226,10 +232,11 @@ AttendPlan token_plan(const CacheJob& J, int nsm) {
 }
 
 AttendPlan chunk_plan(const CacheJob& J, int nsm) {
-  AttendPlan P = plan_of(J, J.bf16 ? 256 : 128, [&](int rows) { return rows > kTokenRows; });
+  AttendPlan P = plan_of(J, J.bf16 ? 256 : 128, [&](int rows) { return rows > few_rows(J); });
   P.step_shift = J.bf16 ? 7 : 6;
   P.workers = nsm;
   P.extra = !J.bf16 ? 0 : J.i8 ? 4 : 6;
+  P.extra1 = !J.bf16 ? 0 : 3;
   return P;
 }
 

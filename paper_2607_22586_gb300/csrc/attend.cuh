@@ -5,7 +5,7 @@
 // row's, are cut into pieces of 2^step_shift, and the pieces of all units in
 // their order are shared out evenly to the workers (CTAs), however long the
 // sequences are: their lengths are read on the device, so every CTA adds up
-// the pieces itself. A unit counts for `extra` pieces more, before its first: its
+// the pieces itself. A unit counts for some pieces more, before its first: its
 // start and end take a worker about as long. A worker's range covers whole units,
 // whose results it writes, and at most two parts of units, its first and its last,
 // whose partial sums it leaves for the merge kernel.
@@ -26,7 +26,7 @@ struct AttendPlan {
   int32_t tiles[MMSHIFT_MAX_BATCH];     // a request's row tiles per KV head
   Divisor by_tiles[MMSHIFT_MAX_BATCH];
   int32_t rows;                         // query rows of a tile
-  int32_t step_shift, extra;
+  int32_t step_shift, extra, extra1;    // extra1: of units of at most 128 rows
   int32_t workers, least;               // workers at most; one has 2^least pieces where there are as many
   float* po;                            // [2 * workers][rows][d] sums of weights times values
   float2* pml;                          // [2 * workers][rows] their maximum (base 2) and sum of weights
@@ -37,7 +37,8 @@ struct AttendUnit {
   int b, h, n;         // request, KV head, the request's tokens
   int row0, rows;      // the tile's first row, its rows
   int len, keys;       // rows of the sequence; keys that the tile's last row attends to
-  int pieces, cost;    // cost: pieces and extra, 0 without keys
+  int pieces, extra;   // its key pieces; what it counts for beside them
+  int cost;            // both together, 0 without keys
 };
 
 // lens: the sequences' lengths (AttendScan::lengths), or null to read them from the cache.
@@ -54,7 +55,8 @@ __device__ __forceinline__ AttendUnit attend_unit(const AttendJob& A, const Atte
   x.len = lens ? lens[seq] : cache_len(J, seq);
   x.keys = keys_of(A.causal, x.len, x.n, J.by_r(x.row0 + x.rows - 1));
   x.pieces = (x.keys + (1 << P.step_shift) - 1) >> P.step_shift;
-  x.cost = x.pieces ? x.pieces + P.extra : 0;
+  x.extra = x.rows <= 128 ? P.extra1 : P.extra;
+  x.cost = x.pieces ? x.pieces + x.extra : 0;
   return x;
 }
 
@@ -137,9 +139,9 @@ __device__ __forceinline__ AttendSpan attend_span(const AttendJob& A, const Atte
 }
 
 // The unit's pieces [s0, s1) among a worker's [begin, end), with `before` before the unit.
-__device__ __forceinline__ void attend_pieces(const AttendPlan& P, const AttendUnit& U, int64_t begin, int64_t end,
+__device__ __forceinline__ void attend_pieces(const AttendUnit& U, int64_t begin, int64_t end,
                                               int64_t before, int& s0, int& s1) {
-  const int64_t first = before + P.extra;
+  const int64_t first = before + U.extra;
   s0 = (int)(max(begin, first) - first);
   s1 = (int)max(min(end, first + U.pieces) - first, (int64_t)0);
 }

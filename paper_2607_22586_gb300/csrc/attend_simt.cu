@@ -72,7 +72,7 @@ __global__ void __launch_bounds__(Simt<D, TR>::NT, Simt<D, TR>::CTAS)
     }
     const int64_t stop = min(sp.end, last);
     int s0, s1;
-    attend_pieces(P, U, at, stop, before, s0, s1);
+    attend_pieces(U, at, stop, before, s0, s1);
     if (s0 >= s1) {                                    // the unit's start alone
       at = stop;
       continue;

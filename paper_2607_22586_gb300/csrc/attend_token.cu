@@ -239,7 +239,7 @@ __global__ void __launch_bounds__(NT, NQ == 1 ? 3 : 2) attend_token_kernel(const
         ++u;
         continue;
       }
-      attend_pieces(P, U, at, stop, before, s0, s1);
+      attend_pieces(U, at, stop, before, s0, s1);
       if (s0 >= s1) {                                  // the unit's start alone
         at = stop;
         continue;
@@ -283,7 +283,7 @@ __global__ void __launch_bounds__(NT, NQ == 1 ? 3 : 2) attend_token_kernel(const
     for (int nq = 0; nq < NQ; ++nq) {
       const int row = 8 * nq + g;
       const bool in = row < U.rows;
-      const int tok = in ? J.by_r(row) : 0, j = in ? row - tok * J.r : 0;
+      const int all = in ? U.row0 + row : 0, tok = J.by_r(all), j = all - tok * J.r;
       const uint8_t* p = A.q + ((size_t)(J.off[U.b] + tok) * J.stride + (size_t)(U.h * J.r + j) * D) * 2;
 #pragma unroll
       for (int i = 0; i < 2 * T::KS / 4; ++i) {
@@ -327,11 +327,11 @@ __global__ void __launch_bounds__(NT, NQ == 1 ? 3 : 2) attend_token_kernel(const
       for (int e = 0; e < 2; ++e) {
         m[nq][e] = -INFINITY;
         l[nq][e] = 0.f;
-        lim[nq][e] = keys_of(A.causal, U.len, U.n, J.by_r(min(8 * nq + 2 * c + e, U.rows - 1)));
+        lim[nq][e] = keys_of(A.causal, U.len, U.n, J.by_r(U.row0 + min(8 * nq + 2 * c + e, U.rows - 1)));
 #pragma unroll
         for (int mt = 0; mt < T::MT; ++mt) o[nq][mt][e] = o[nq][mt][2 + e] = 0.f;
       }
-    const int least = keys_of(A.causal, U.len, U.n, 0);   // keys that every row attends to
+    const int least = keys_of(A.causal, U.len, U.n, J.by_r(U.row0));   // keys that every row attends to
 
     for (; s < s1; s += NW) {
       const int t0 = s * T::KEYS;
@@ -542,7 +542,7 @@ __global__ void __launch_bounds__(NT, NQ == 1 ? 3 : 2) attend_token_kernel(const
         *reinterpret_cast<float4*>(&sm.o[0][r][d0]) = acc;   // read by this thread alone
         if (d0 == 0) sm.part[r] = make_float2(top, z);
       } else if (whole) {
-        attend_write<__nv_bfloat16, D>(A, U.b, U.h, r, d0, acc, top, z);
+        attend_write<__nv_bfloat16, D>(A, U.b, U.h, U.row0 + r, d0, acc, top, z);
       } else {
         *reinterpret_cast<float4*>(P.po + (slot + r) * D + d0) = acc;
         if (d0 == 0) P.pml[slot + r] = make_float2(top, z);
@@ -572,7 +572,7 @@ __global__ void __launch_bounds__(NT, NQ == 1 ? 3 : 2) attend_token_kernel(const
           acc.z += b.x * f;
           acc.w += b.y * f;
         }
-        attend_write<__nv_bfloat16, D>(A, U.b, U.h, r, d0, acc, top, z);
+        attend_write<__nv_bfloat16, D>(A, U.b, U.h, U.row0 + r, d0, acc, top, z);
       }
       umma::cluster_sync();                            // the others have read this CTA's part
       at = sp.end;

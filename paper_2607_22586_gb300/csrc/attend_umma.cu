@@ -16,7 +16,8 @@
 //   warp 9      MMA issuer;
 //   warps 12-15 (8-bit pages) make codes bfloat16.
 // The blocks alternate: while one block's softmax runs, the tensor cores have
-// the other block's products. A row's maximum is only raised when a logit passes it
+// the other block's products. Tiles of at most 128 rows take the blocks in turn, so
+// that one's results go out while the next one begins. A row's maximum is only raised when a logit passes it
 // by 8 (base 2); then the thread rescales its row of O itself, which is idle at
 // that point: S of a tile is complete only after the products of the tile before.
 // P is rounded to bfloat16 (the tensor cores' operand type), its sum is not.
@@ -178,13 +179,16 @@ struct Run {
   int64_t before;        // costs before the unit
   int s0, s1;
   bool two;              // the second block has rows
+  int x;                 // else: the block that has them, each in turn
+  __device__ __forceinline__ bool has(int b) const { return two || b == x; }
+  __device__ __forceinline__ int first_row(int b) const { return two ? b * BQ : 0; }   // of block b in the tile
 };
 
 // A role's walk over the CTA's runs. A warp works the first ones out for all roles, a
 // lane a unit; a role itself those behind them (units of few keys).
 constexpr int RUNS = 16;
 struct Walk {
-  int k, unit;           // runs so far; behind the list, the next unit and the costs before it
+  int runs, k, unit;     // runs so far, those of the list; behind it, the next unit and the costs before it
   int64_t before;
 };
 struct RunList {
@@ -193,11 +197,11 @@ struct RunList {
   int n;
 };
 
-__device__ __forceinline__ Run run_of(const AttendPlan& P, const AttendSpan& sp, const AttendUnit& U, int64_t before) {
+__device__ __forceinline__ Run run_of(const AttendSpan& sp, const AttendUnit& U, int64_t before) {
   Run R;
   R.U = U;
   R.before = before;
-  attend_pieces(P, U, sp.begin, sp.end, before, R.s0, R.s1);
+  attend_pieces(U, sp.begin, sp.end, before, R.s0, R.s1);
   R.two = U.rows > BQ;
   return R;
 }
@@ -208,7 +212,7 @@ __device__ __forceinline__ void list_runs(const AttendJob& A, const AttendPlan& 
   const int u = sp.unit + lane;
   const bool in = sp.begin < sp.end && lane < RUNS && u < P.uoff[A.c.B];
   AttendUnit U;
-  U.pieces = U.cost = 0;
+  U.pieces = U.extra = U.cost = 0;
   if (in) U = attend_unit(A, P, nullptr, u);
   int64_t x = U.cost;
 #pragma unroll
@@ -217,35 +221,37 @@ __device__ __forceinline__ void list_runs(const AttendJob& A, const AttendPlan& 
     if (lane >= d) x += y;
   }
   const int64_t before = sp.before + x - U.cost;
-  const Run R = run_of(P, sp, U, before);
+  const Run R = run_of(sp, U, before);
   const bool mine = in && R.s0 < R.s1;
   const unsigned all = __ballot_sync(0xffffffffu, mine);
   if (mine) list->run[__popc(all & ((1u << lane) - 1u))] = R;
   if (lane == RUNS - 1) {                              // where the walk goes on
     list->n = __popc(all);
-    list->rest = Walk{0, u + 1, in ? sp.before + x : sp.end};
+    list->rest = Walk{0, 0, u + 1, in ? sp.before + x : sp.end};
   }
 }
 
 __device__ __forceinline__ bool next_run(const AttendJob& A, const AttendPlan& P, const AttendSpan& sp,
                                          const RunList& list, Walk& w, Run& R) {
-  if (w.k < list.n) {
-    R = list.run[w.k];
-    ++w.k;
-    return true;
+  bool found = w.k < list.n;
+  if (found) {
+    R = list.run[w.k++];
+  } else {
+    if (w.k == list.n) {
+      w.k = RUNS + 1;
+      w.unit = list.rest.unit;
+      w.before = list.rest.before;
+    }
+    while (!found && w.before < sp.end) {
+      const AttendUnit U = attend_unit(A, P, nullptr, w.unit);
+      R = run_of(sp, U, w.before);
+      w.before += U.cost;
+      ++w.unit;
+      found = R.s0 < R.s1;
+    }
   }
-  if (w.k == list.n) {
-    w = list.rest;
-    w.k = RUNS + 1;
-  }
-  while (w.before < sp.end) {
-    const AttendUnit U = attend_unit(A, P, nullptr, w.unit);
-    R = run_of(P, sp, U, w.before);
-    w.before += U.cost;
-    ++w.unit;
-    if (R.s0 < R.s1) return true;
-  }
-  return false;
+  R.x = w.runs++ & 1;
+  return found;
 }
 
 // The part of a row's sums that comes from values that are not finite, of columns
@@ -335,7 +341,7 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
   const AttendSpan sp = attend_span(A, P, &scan);
   if (warp == 0) list_runs(A, P, sp, lane, &runs);
   __syncthreads();
-  Walk walk = {0, 0, 0};
+  Walk walk = {0, 0, 0, 0};
   Run R;
   if (warp == PRODUCER) {
     // bfloat16 rows go where the MMAs read them, codes to a ring of their own
@@ -422,9 +428,9 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
       __syncwarp();
     };
     while (ok && next_run(A, P, sp, runs, walk, R)) {
-      const int nx = R.two ? 2 : 1;
       if (!wait(&full[stage], phase)) break;
-      for (int x = 0; x < nx; ++x) {
+      for (int x = 0; x < 2; ++x) {
+        if (!R.has(x)) continue;
         if (!wait(&q_ready[x], qp >> x)) break;
         qp ^= 1u << x;
         fence_after();
@@ -434,7 +440,8 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
       if (!ok) break;
       commit(&empty[stage]);
       step();
-      for (int x = 0; x < nx; ++x) {                   // the last run's O has been read
+      for (int x = 0; x < 2; ++x) {                    // the block's last O has been read
+        if (!R.has(x)) continue;
         if (!wait(&o_free[x], (of >> x) ^ 1u)) break;
         of ^= 1u << x;
       }
@@ -445,14 +452,15 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
         const bool more = s + 1 < R.s1;
         if (!wait(&full[vst], phase)) break;
         step();
-        for (int x = 0; x < nx; ++x) {
+        for (int x = 0; x < 2; ++x) {
+          if (!R.has(x)) continue;
           if (!wait(&p_ready[x], pp >> x)) break;
           pp ^= 1u << x;
           fence_after();
           issue_o(x, vst, s > R.s0);
-          if (x == nx - 1) commit(&empty[vst]);
+          if (x == 1 || !R.two) commit(&empty[vst]);
           if (more) {
-            if (x == 0 && !wait(&full[stage], phase)) break;
+            if ((x == 0 || !R.two) && !wait(&full[stage], phase)) break;
             issue_s(x);
           } else {
             commit(&o_ready[x]);
@@ -544,7 +552,7 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
     while (ok && next_run(A, P, sp, runs, walk, R)) {
       const AttendUnit& U = R.U;
       const int ntiles = R.s1 - R.s0;
-      if (x == 1 && !R.two) {
+      if (!R.has(x)) {
         vstage += 2 * ntiles;
         vphase ^= (vstage / SM::STAGES) & 1;
         vstage %= SM::STAGES;
@@ -559,7 +567,7 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
         return lane < 8 && s < R.s1 && t < U.keys ? table[t >> J.page_shift] : 0;
       };
       int next = entry_of(R.s0);
-      const int brow = x * BQ + lrow, row = U.row0 + brow;
+      const int brow = R.first_row(x) + lrow, row = U.row0 + brow;
       const bool live = brow < U.rows;
       const int tok = J.by_r(row), j = row - tok * J.r;
       {
@@ -605,7 +613,7 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
       for (int i = 0; i < NR; ++i) {
         m[i] = -INFINITY;
         l[i] = 0.f;
-        const int r = U.row0 + x * BQ + (I8 ? warp % 4 * 32 + g + 8 * i : lrow);
+        const int r = U.row0 + R.first_row(x) + (I8 ? warp % 4 * 32 + g + 8 * i : lrow);
         lim[i] = r < U.row0 + U.rows ? keys_of(A.causal, U.len, U.n, J.by_r(r)) : 0;
       }
       // a value of the thread's row, of those that the quads hold
@@ -654,7 +662,7 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
         if (I8 && !wait_bar(&full[vs], vp, abort_)) { ok = false; break; }
         fence_after();
         const bool masked = special || gone;
-        if (gone && warp == 0 && lane == 0) set_status(J.status, kStatusBadPage);
+        if (gone && warp % 4 == 0 && lane == 0) set_status(J.status, kStatusBadPage);
         auto hidden = [&](int i, int r) { return k0 + i >= lim[r] || ((gone >> (i / 16)) & 1u); };
         // raises the maxima to `top` (base 2) where some row's passes them by enough
         auto raise = [&](float (&top)[NR]) {
