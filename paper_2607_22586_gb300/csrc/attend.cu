@@ -174,15 +174,17 @@ cudaError_t launch_merge(const AttendJob& A, const AttendPlan& P, cudaStream_t s
 
 // Requests of few rows of a KV head have a plan of their own, of tiles of at most this
 // many: bfloat16 rows go to the token kernel, float32 rows to tiles of 8 or 16 rows
-// (requests of more rows to tiles of 256, or 64 or 128).
+// (requests of more rows to tiles of 256, or 128).
 constexpr int kTokenRows = 16;
 constexpr int kClusterSteps = 4;
 
 // Rows of a request's KV head that go to the plan of tiles of kTokenRows. More than one
-// tile reads the keys again, from the L2, but starts sooner than the chunk kernel: 16
-// requests of 32 heads, 300 to 750 rows, 32 tokens: bfloat16 68 us (chunk kernel 92),
-// 8-bit 62 (95); 48 tokens: 96 (93), 87 (96); 64 tokens: 125 (95), 112 (98).
-int few_rows(const CacheJob& J) { return J.bf16 ? 32 : kTokenRows; }
+// tile reads the keys again, from the L2, but starts sooner than a chunk's tile and
+// computes fewer rows that are not there: 16 requests of 32 heads, 300 to 750 rows,
+// 32 tokens: bfloat16 68 us (chunk kernel 92), 8-bit 62 (95); 48 tokens: 96 (93), 87 (96);
+// 64 tokens: 125 (95), 112 (98). float32 rows: 32 tokens 209 (tiles of 128: 474), 64
+// tokens 407 (548), 96 tokens 616 (573); 8-bit pages 284 (463), 563 (537), 856 (560).
+int few_rows(const CacheJob& J) { return J.bf16 ? 32 : 64; }
 
 constexpr int kSMs = 152;              // the workspace is sized without asking the device
 
@@ -226,7 +228,7 @@ AttendPlan token_plan(const CacheJob& J, int nsm) {
     P.extra = P.extra1 = 8;
   } else {
     P.step_shift = 5;
-    P.workers = nsm * (P.rows <= 8 ? 4 : 3);
+    P.workers = nsm * (J.d == 64 ? 8 : P.rows <= 8 ? 5 : 4);
   }
   return P;
 }

@@ -5,10 +5,14 @@
 // threads are 16 lanes of one warp, so its weights change hands through shared memory
 // without a barrier of the CTA. K of the next tile arrives (asynchronous copies; 8-bit
 // codes through registers, to be converted) while this one's values are added up, V while
-// its logits are. Chunks (TR = 8, 128 rows by 64 keys) are bound by what shared memory
-// feeds the FMAs, 128 bytes a clock and SM: 8 x 4 sums take 1.5 bytes an FMA, the 8 x 8
-// (or 8 x 4, d = 64) of the second product 1 (1.5). Few rows (TR = 1, 2) are bound by the
-// bytes of K and V.
+// its logits are. The shape is bound by what shared memory feeds the FMAs, 128 bytes
+// a clock and SM. Chunks (NT = 256, TR = 8: 128 rows by 64 keys): 8 x 4 sums take 1.5 bytes
+// an FMA, the 8 x 8 (or 8 x 4, d = 64) of the second product 1 (1.5): 512 tokens of 28
+// heads over 4096 rows, d = 128, 607 us (46 TFLOP/s of 80). Few rows (TR = 2, two or four
+// warps, five or four CTAs an SM): 64 requests of one token, 64 heads, 500 to 6000 rows
+// 312 us (4.9 TB/s) over float32 pages, 350 over 8-bit ones; 445 and 451 with four warps
+// and TR = 1, which read a key four times, not twice; 334 and 452 with one warp and TR = 4, too
+// few to hide the loads.
 #include <type_traits>
 
 #include "attend.cuh"
@@ -17,7 +21,6 @@
 namespace mmshift {
 namespace {
 
-using umma::fadd2;
 using umma::ffma2;
 using umma::lds_2x64;
 using umma::pk2;
@@ -26,10 +29,9 @@ using umma::upk2;
 
 constexpr float kRaise = 8.f;
 
-template <int D, int TR>
+template <int D, int NT, int TR>
 struct Simt {
-  static constexpr int NT = TR >= 4 ? 256 : 128, BK = TR >= 4 ? 64 : 32, NK = BK / 16;
-  static constexpr int CTAS = TR >= 4 ? 1 : TR == 2 ? 3 : 4;   // of an SM
+  static constexpr int BK = NT == 256 ? 64 : 32, NK = BK / 16;
   static constexpr int RT = NT / 16 * TR;
   static constexpr int QS = D + 4, PS = RT + 4;        // floats between rows: no bank conflicts
   struct Smem {
@@ -38,7 +40,7 @@ struct Simt {
     alignas(16) float v[BK][D];
     alignas(16) float p[BK][PS];
     float ks[BK], vs[BK];
-    AttendScan<NT, 256> scan;
+    AttendScan<NT, 512> scan;
   };
 };
 
@@ -49,11 +51,22 @@ __device__ __forceinline__ void copy16(void* dst, const void* src, bool in) {
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group 0;" ::: "memory"); }
 
-template <int D, bool I8, int TR>
-__global__ void __launch_bounds__(Simt<D, TR>::NT, Simt<D, TR>::CTAS)
+// Four codes as floats: 2^23 + 128 + code has the code's bits, the sign's turned over, at its
+// end, so that no conversion is needed.
+__device__ __forceinline__ float4 codes4(uint32_t x) {
+  x ^= 0x80808080u;
+  constexpr float k = 8388736.f;
+  return make_float4(__uint_as_float(__byte_perm(x, 0x4b000000u, 0x7440)) - k,
+                     __uint_as_float(__byte_perm(x, 0x4b000000u, 0x7441)) - k,
+                     __uint_as_float(__byte_perm(x, 0x4b000000u, 0x7442)) - k,
+                     __uint_as_float(__byte_perm(x, 0x4b000000u, 0x7443)) - k);
+}
+
+template <int D, bool I8, int NT, int TR>
+__global__ void __launch_bounds__(NT, 1)
     attend_simt_kernel(const __grid_constant__ AttendJob A, const __grid_constant__ AttendPlan P) {
-  using SM = Simt<D, TR>;
-  constexpr int NT = SM::NT, BK = SM::BK, NK = SM::NK;
+  using SM = Simt<D, NT, TR>;
+  constexpr int BK = SM::BK, NK = SM::NK;
   extern __shared__ __align__(16) unsigned char smraw[];
   typename SM::Smem& sm = *reinterpret_cast<typename SM::Smem*>(smraw);
   cache_start();
@@ -111,12 +124,18 @@ __global__ void __launch_bounds__(Simt<D, TR>::NT, Simt<D, TR>::CTAS)
       return t < U.keys ? page_row(table[t >> J.page_shift], J.n_pages, J.page_shift, t) : -1;
     };
     auto fetch = [&](int s, const uint8_t* pages, const float* scales, float* dst, int pitch) {
+      const uint8_t* from = nullptr;                   // the row of key `lk` of its 16 keys, null without one
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const int key = lk + i * STEP, row = s < s1 ? row_of(s * BK + key) : -1;
-        const size_t src = (size_t)(row < 0 ? 0 : row) * ROWB + part * 16;
-        if constexpr (I8) codes[i] = row < 0 ? make_uint4(0, 0, 0, 0) : *reinterpret_cast<const uint4*>(pages + src);
-        else copy16(dst + key * pitch + part * 4, pages + src, row >= 0);
+        const int key = lk + i * STEP, t = s * BK + key;
+        if (i * STEP % 16 == 0) {
+          const int64_t row = s < s1 ? row_of(t) : -1;
+          from = row < 0 ? nullptr : pages + row * ROWB + part * 16;
+        }
+        const bool in = from && t < U.keys;
+        const uint8_t* src = in ? from + i * STEP % 16 * ROWB : pages;
+        if constexpr (I8) codes[i] = in ? *reinterpret_cast<const uint4*>(src) : make_uint4(0, 0, 0, 0);
+        else copy16(dst + key * pitch + part * 4, src, in);
       }
       if constexpr (I8) {
         if (tid < BK) {
@@ -131,12 +150,20 @@ __global__ void __launch_bounds__(Simt<D, TR>::NT, Simt<D, TR>::CTAS)
       if constexpr (I8) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-          const uint32_t x[4] = {codes[i].x, codes[i].y, codes[i].z, codes[i].w};
+          // Neighbours begin at other quarters of their 16 values: no bank conflicts.
+          const int turn = part / 2 % 4;
+          uint32_t x[4] = {codes[i].x, codes[i].y, codes[i].z, codes[i].w};
+          if (turn & 1) {
+            const uint32_t y = x[0];
+            x[0] = x[1], x[1] = x[2], x[2] = x[3], x[3] = y;
+          }
+          if (turn & 2) {
+            const uint32_t y = x[0], z = x[1];
+            x[0] = x[2], x[1] = x[3], x[2] = y, x[3] = z;
+          }
           float4* to = reinterpret_cast<float4*>(dst + (lk + i * STEP) * pitch + part * 16);
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            to[e] = make_float4((float)(int8_t)x[e], (float)(int8_t)(x[e] >> 8), (float)(int8_t)(x[e] >> 16),
-                                (float)(int8_t)(x[e] >> 24));
+          for (int e = 0; e < 4; ++e) to[(e + turn) % 4] = codes4(x[e]);
         }
         if (tid < BK) scales[tid] = scale * by;
       } else {
@@ -237,9 +264,14 @@ __global__ void __launch_bounds__(Simt<D, TR>::NT, Simt<D, TR>::CTAS)
         uint64_t vv[D / 64][2];
 #pragma unroll
         for (int c = 0; c < D / 64; ++c) lds_2x64(va + (key * D + 64 * c) * 4, vv[c][0], vv[c][1]);
+        float ww[TR];
+        using Some = std::conditional_t<TR == 2, float2, float4>;
+#pragma unroll
+        for (int i = 0; i < TR; i += sizeof(Some) / 4)
+          *reinterpret_cast<Some*>(ww + i) = *reinterpret_cast<const Some*>(pp + key * SM::PS + i);
 #pragma unroll
         for (int i = 0; i < TR; ++i) {
-          const float w = pp[key * SM::PS + i];
+          const float w = ww[i];
           if (decltype(mask)::value && w < 0.f) continue;
           const uint64_t w2 = pk2(w, w);
 #pragma unroll
@@ -249,13 +281,14 @@ __global__ void __launch_bounds__(Simt<D, TR>::NT, Simt<D, TR>::CTAS)
           }
         }
       };
+      const int end = min(U.keys - k0, BK);
       if (!masked) {
 #pragma unroll 4
         for (int key = 0; key < BK; ++key) add(key, std::false_type());
       } else {
         // a zero weight times a value that is not finite would be a NaN
 #pragma unroll 1
-        for (int key = 0; key < BK; ++key) add(key, std::true_type());
+        for (int key = 0; key < end; ++key) add(key, std::true_type());
       }
       __syncwarp();
     }
@@ -294,22 +327,20 @@ __global__ void __launch_bounds__(Simt<D, TR>::NT, Simt<D, TR>::CTAS)
   }
 }
 
-template <int D, bool I8, int TR>
+template <int D, bool I8, int NT, int TR>
 cudaError_t launch(const AttendJob& A, const AttendPlan& P, cudaStream_t st) {
-  using SM = Simt<D, TR>;
-  constexpr int bytes = (int)sizeof(typename SM::Smem);
-  const cudaError_t e =
-      cudaFuncSetAttribute(attend_simt_kernel<D, I8, TR>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  constexpr int bytes = (int)sizeof(typename Simt<D, NT, TR>::Smem);
+  const auto kernel = attend_simt_kernel<D, I8, NT, TR>;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
   if (e != cudaSuccess) return e;
-  return launch_kernel(attend_simt_kernel<D, I8, TR>, dim3(P.workers), SM::NT, bytes, st, true, 0, A, P);
+  return launch_kernel(kernel, dim3(P.workers), NT, bytes, st, true, 0, A, P);
 }
 
 template <int D, bool I8>
 cudaError_t launch_rows(const AttendJob& A, const AttendPlan& P, cudaStream_t st) {
-  if (P.rows <= 8) return launch<D, I8, 1>(A, P, st);
-  if (P.rows <= 16) return launch<D, I8, 2>(A, P, st);
-  if (P.rows <= 64) return launch<D, I8, 4>(A, P, st);
-  return launch<D, I8, 8>(A, P, st);
+  if (P.rows <= 8) return launch<D, I8, 64, 2>(A, P, st);
+  if (P.rows <= 16) return launch<D, I8, 128, 2>(A, P, st);
+  return launch<D, I8, 256, 8>(A, P, st);
 }
 
 }  // namespace
