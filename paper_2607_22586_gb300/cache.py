@@ -97,8 +97,9 @@ class PagedKVCache:
         for t in ts:
             if t.dtype != self.dtype or t.device != self.device or t.shape[-3:] != (total, heads, self.head_dim):
                 raise ValueError(f"rows must be [..., {total}, {heads}, {self.head_dim}] of {self.dtype} on {self.device}")
-            if t.stride(-1) != 1 or (heads > 1 and t.stride(-2) != self.head_dim) or t.stride(-3) != ts[0].stride(-3):
-                raise ValueError("a token's heads must be dense, and the tokens equally far apart")
+            if t.stride(-1) != 1 or (heads > 1 and t.stride(-2) != self.head_dim) or t.stride(-3) != ts[0].stride(-3) \
+                    or (total > 1 and t.stride(-3) < heads * self.head_dim):
+                raise ValueError("a token's heads must be dense, and the tokens equally far apart, without overlap")
             stride = t.stride(-3)
         return stride if total > 1 else heads * self.head_dim
 
@@ -110,6 +111,10 @@ class PagedKVCache:
         if (selector.n_layers, len(selector.budgets), selector.n_kv_heads, selector.head_dim, selector.dtype,
                 selector.device) != (self.n_layers, self.batch, self.n_kv_heads, self.head_dim, self.dtype, self.device):
             raise ValueError("the selector's shape is not the cache's")
+        for t, like in ((idx, selector.out_idx.shape), (counts, self.lens.shape)):
+            if t is not None and (t.dtype != torch.int32 or t.device != self.device or not t.is_contiguous()
+                                  or t.shape != like):
+                raise ValueError("idx [L, R, Hkv] and counts [L, B, Hkv] must be contiguous int32 tensors")
         if idx is None:
             idx, counts = selector.out_idx, selector.out_count
         with self._on_device():
@@ -135,6 +140,8 @@ class PagedKVCache:
         layers = self.n_layers if layer is None else 1
         shape, _, _, total = self._call(new, layers)
         stride = self._check(total, self.n_kv_heads, K, V)
+        if layer is not None and (K.dim() != 3 or V.dim() != 3):
+            raise ValueError("rows of one layer must be [T, Hkv, d]")
         if layer is None and (K.dim() != 4 or len(K) != layers or K.stride() != V.stride()):
             raise ValueError("rows of all layers must be [L, T, Hkv, d], K's and V's laid out alike")
         shape.layer_stride_kv = K.stride(0) if layer is None else 0
@@ -148,6 +155,8 @@ class PagedKVCache:
         [T, Hq, d]. ``lse`` [T, Hq] float32 receives the log-sum-exp where given."""
         shape, ws, n, total = self._call(new, 0)
         stride = self._check(total, self.n_q_heads, q)
+        if q.dim() != 3:
+            raise ValueError("queries must be [T, Hq, d]")
         with self._on_device():
             if out is None:
                 out = torch.empty((total, self.n_q_heads, self.head_dim), dtype=self.dtype, device=self.device)

@@ -146,3 +146,30 @@ def test_constructor_refusals():
     used = c.page_table[c.page_table >= 0]
     assert sorted(used.tolist()) == list(range(1 + 1 + 2 + 3 + 1 + 1 + 7 + 1)) and len(c.k_pages) == 17
     assert c.page_table[1, 1, 0].tolist() == list(range(9, 16)) and c.page_table[0, 0, 0].tolist() == [0] + [-1] * 6
+
+
+def test_rows_that_overlap_or_have_other_axes_are_refused():
+    """Before anything is launched: without a GPU."""
+    c = _cache(device="cpu")
+    q, k = torch.zeros((1, 6, 64), dtype=torch.bfloat16), torch.zeros((2, 1, 2, 64), dtype=torch.bfloat16)
+    flat = torch.zeros(3 * 384, dtype=torch.bfloat16)
+    for call in (lambda: c.attend(q.expand(3, 6, 64), [1, 2]),                       # one row for all tokens
+                 lambda: c.attend(flat.as_strided((3, 6, 64), (320, 64, 1)), [1, 2]),
+                 lambda: c.append(k.expand(2, 3, 2, 64), k.expand(2, 3, 2, 64), [1, 2]),
+                 lambda: c.attend(torch.zeros((2, 3, 6, 64), dtype=torch.bfloat16), [1, 2]),
+                 lambda: c.append(k.expand(2, 1, 2, 64), k, [1, 0], layer=1)):
+        with pytest.raises(ValueError):
+            call()
+
+
+def test_indices_of_another_shape_or_type_are_refused():
+    """Before anything is launched: without a GPU."""
+    c, sel = _cache(device="cpu", batch=1), KVSelector.__new__(KVSelector)
+    sel.__dict__.update(n_layers=2, budgets=[5], n_kv_heads=2, head_dim=64, dtype=torch.bfloat16, device=c.device,
+                        out_idx=torch.zeros((2, 5, 2), dtype=torch.int32), out_count=None, _check=lambda *a: None)
+    k = torch.zeros((2, 9, 2, 64), dtype=torch.bfloat16)
+    idx, counts = sel.out_idx, torch.zeros((2, 1, 2), dtype=torch.int32)
+    for i, n in ((idx.long(), None), (idx[:, :4], None), (idx.transpose(0, 2), None), (idx, counts.long()),
+                 (idx, counts[:1])):
+        with pytest.raises(ValueError):
+            c.fill(sel, k, k, i, n)
