@@ -41,6 +41,12 @@ struct AttendUnit {
   int cost;            // both together, 0 without keys
 };
 
+// A sequence's length, from the L2: a merge reads it before its griddepcontrol.wait, when the
+// L1 need not have what was written before the attention kernel began.
+__device__ __forceinline__ int attend_len(const CacheJob& J, size_t u) {
+  return min(max(__ldcg(J.lens + u), 0), J.cap);
+}
+
 // lens: the sequences' lengths (AttendScan::lengths), or null to read them from the cache.
 __device__ __forceinline__ AttendUnit attend_unit(const AttendJob& A, const AttendPlan& P, const int32_t* lens, int u) {
   const CacheJob& J = A.c;
@@ -52,7 +58,7 @@ __device__ __forceinline__ AttendUnit attend_unit(const AttendJob& A, const Atte
   x.row0 = (rem - x.h * tiles) * P.rows;
   x.rows = min(P.rows, all - x.row0);
   const int seq = x.b * J.Hkv + x.h;
-  x.len = lens ? lens[seq] : cache_len(J, seq);
+  x.len = lens ? lens[seq] : attend_len(J, seq);
   x.keys = keys_of(A.causal, x.len, x.n, J.by_r(x.row0 + x.rows - 1));
   x.pieces = (x.keys + (1 << P.step_shift) - 1) >> P.step_shift;
   x.extra = x.rows <= 128 ? P.extra1 : P.extra;
@@ -88,7 +94,7 @@ struct AttendSums {
     const CacheJob& J = A.c;
     const int tid = threadIdx.x, lane = tid % 32, w = tid / 32, U = P.uoff[J.B];
     if (s->lengths(J))
-      for (int i = tid; i < J.B * J.Hkv; i += NT) s->lens[i] = cache_len(J, i);
+      for (int i = tid; i < J.B * J.Hkv; i += NT) s->lens[i] = attend_len(J, i);
     __syncthreads();
     const int per = (U + NT - 1) / NT;
     u0 = min(tid * per, U);

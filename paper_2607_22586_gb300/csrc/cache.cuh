@@ -29,7 +29,7 @@ __device__ __forceinline__ int cache_request(const CacheJob& J, int tok) { retur
 
 // Rows of sequence u = (l * B + b) * Hkv + h.
 __device__ __forceinline__ int cache_len(const CacheJob& J, size_t u) {
-  return min(max(__ldcg(J.lens + u), 0), J.cap);
+  return min(max(J.lens[u], 0), J.cap);
 }
 
 // The pool's row of position t < cap of sequence u, -1 if it has no page.
