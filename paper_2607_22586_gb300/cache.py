@@ -1,6 +1,6 @@
 """Torch-facing convenience around the paged cache's entry points: owns the pages,
-their table and the lengths of a batch's sequences, and a workspace for each shape
-of call. PyTorch only provides device memory and streams here.
+their table and the lengths of a batch's sequences, and a workspace that does for
+every call. PyTorch only provides device memory and streams here.
 
     cache = PagedKVCache(28, 4, 128, torch.bfloat16, batch=1, rows=2048 + 512,
                          n_layers=28, cache_dtype=torch.int8)
@@ -20,6 +20,9 @@ import torch
 
 from . import _lib as L
 from .selector import _DT, KVSelector
+
+
+_KEPT = 256   # combinations of row counts whose shapes are kept
 
 
 class PagedKVCache:
@@ -58,34 +61,35 @@ class PagedKVCache:
             self.k_scales, self.v_scales = (make(total, page_size, dt=torch.float32) for _ in range(2))
         self._all = self._struct(self.page_table, self.lens)
         self._layers = [self._struct(self.page_table[i], self.lens[i]) for i in range(n_layers)]
-        self._calls, self._counts = {}, {}
-        # a device status word each, kept for as long as the cache: a captured call uses it again
-        self._status = make(256, dt=torch.uint8)
-        self._used = [self._status]
+        self._calls, self._counts, self._captured = {}, {}, []
+        # The largest call's: the plans' tiles are full from 256 rows of a KV head on, those
+        # of few rows from 17 to 32.
+        r = n_q_heads // max(n_kv_heads, 1) or 1
+        self._ws_bytes = sum(self._shape([n] * batch, 1)[1] for n in (256, max(32 // r, 1)))
+        self._workspace = make(self._ws_bytes, dt=torch.uint8)
 
     def _struct(self, table, lens):
         return L.make_cache(self.k_pages, self.v_pages, table, lens, self.k_scales, self.v_scales)
 
+    def _shape(self, new: Sequence[int], layers: int):
+        """Shape of a call with these numbers of rows, and the workspace that attention needs for it."""
+        cu = [0]
+        for n in new:
+            cu.append(cu[-1] + int(n))
+        shape = L.make_shape(self.n_q_heads, self.n_kv_heads, self.head_dim, 2, _DT[self.dtype], cu, [1] * self.batch,
+                             n_layers=layers, layer_stride_kv=cu[-1] * self.n_kv_heads * self.head_dim)
+        return shape, L.mmshift_cache_workspace_size(shape, self._all), cu[-1]
+
     def _call(self, new: Sequence[int], layers: int):
-        """Shape and workspace of calls with these numbers of rows."""
+        """Shape and rows of calls with these numbers of rows."""
         key = (tuple(new), layers)
         if key not in self._calls:
             if len(new) != self.batch:
                 raise ValueError(f"{len(new)} row counts for {self.batch} requests")
-            cu = [0]
-            for n in new:
-                cu.append(cu[-1] + int(n))
-            dense = cu[-1] * self.n_kv_heads * self.head_dim
-            shape = L.make_shape(self.n_q_heads, self.n_kv_heads, self.head_dim, 2, _DT[self.dtype], cu,
-                                 [1] * self.batch, n_layers=layers, layer_stride_kv=dense)
-            n, ws = 256, self._status
-            if layers == 0:                                # attention, over one layer
-                shape.n_layers = 1
-                n = L.mmshift_cache_workspace_size(shape, self._layers[0])
-                ws = torch.empty(n, dtype=torch.uint8, device=self.device)
-                ws[:256].zero_()
-                self._used.append(ws)
-            self._calls[key] = (shape, ws, n, cu[-1])
+            if len(self._calls) >= _KEPT:
+                self._calls.clear()
+            shape, _, total = self._shape(new, layers)
+            self._calls[key] = (shape, total)
         return self._calls[key]
 
     def _on_device(self):
@@ -118,7 +122,7 @@ class PagedKVCache:
         if idx is None:
             idx, counts = selector.out_idx, selector.out_count
         with self._on_device():
-            L.check(L.mmshift_cache_fill(selector.shape, self._all, K, V, idx, counts, self._status, 256,
+            L.check(L.mmshift_cache_fill(selector.shape, self._all, K, V, idx, counts, self._workspace, self._ws_bytes,
                                          torch.cuda.current_stream()), "mmshift_cache_fill")
 
     def advance(self, new: Sequence[int]) -> None:
@@ -131,14 +135,18 @@ class PagedKVCache:
             self.lens.add_(key[0])
             return
         if key not in self._counts:
+            if len(self._counts) >= _KEPT:
+                self._counts.clear()
             self._counts[key] = torch.tensor(key, dtype=torch.int32, device=self.device)[None, :, None]
+        if self.lens.is_cuda and torch.cuda.is_current_stream_capturing():
+            self._captured.append(self._counts[key])       # read by every replay
         self.lens.add_(self._counts[key])
 
     def append(self, K: torch.Tensor, V: torch.Tensor, new: Sequence[int], layer: Optional[int] = None) -> None:
         """The new tokens' rows (counted by advance() before): K, V [L, T, Hkv, d], or
         [T, Hkv, d] of one layer."""
         layers = self.n_layers if layer is None else 1
-        shape, _, _, total = self._call(new, layers)
+        shape, total = self._call(new, layers)
         stride = self._check(total, self.n_kv_heads, K, V)
         if layer is not None and (K.dim() != 3 or V.dim() != 3):
             raise ValueError("rows of one layer must be [T, Hkv, d]")
@@ -147,13 +155,13 @@ class PagedKVCache:
         shape.layer_stride_kv = K.stride(0) if layer is None else 0
         with self._on_device():
             L.check(L.mmshift_cache_append(shape, self._all if layer is None else self._layers[layer], K, V, stride,
-                                           self._status, 256, torch.cuda.current_stream()), "mmshift_cache_append")
+                                           self._workspace, self._ws_bytes, torch.cuda.current_stream()), "mmshift_cache_append")
 
     def attend(self, q: torch.Tensor, new: Sequence[int], layer: int = 0, causal: bool = True,
                softmax_scale: float = 0.0, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None):
         """Attention of the new tokens' queries q [T, Hq, d] over a layer's sequences:
         [T, Hq, d]. ``lse`` [T, Hq] float32 receives the log-sum-exp where given."""
-        shape, ws, n, total = self._call(new, 0)
+        shape, total = self._call(new, 1)
         stride = self._check(total, self.n_q_heads, q)
         if q.dim() != 3:
             raise ValueError("queries must be [T, Hq, d]")
@@ -166,26 +174,25 @@ class PagedKVCache:
                                     or lse.shape != q.shape[:2]):
                 raise ValueError("lse must be a contiguous float32 tensor [T, Hq]")
             L.check(L.mmshift_cache_attention(shape, self._layers[layer], q, stride, causal, softmax_scale, out, lse,
-                                              ws, n, torch.cuda.current_stream()), "mmshift_cache_attention")
+                                              self._workspace, self._ws_bytes, torch.cuda.current_stream()), "mmshift_cache_attention")
         return out
 
     def read(self, rows: Sequence[int], first: Optional[torch.Tensor] = None):
         """The first ``rows[b]`` rows of each sequence of request b (from ``first``
         [L, B, Hkv] int32 on, where given), zeros behind a sequence's end: K and V
         [L, T, Hkv, d]."""
-        shape, _, _, total = self._call(rows, self.n_layers)
+        shape, total = self._call(rows, self.n_layers)
         if first is not None and (first.dtype != torch.int32 or first.device != self.device
                                   or not first.is_contiguous() or first.shape != self.lens.shape):
             raise ValueError("first must be a contiguous int32 tensor [L, B, Hkv]")
         with self._on_device():
             k, v = (torch.empty((self.n_layers, total, self.n_kv_heads, self.head_dim), dtype=self.dtype,
                                 device=self.device) for _ in range(2))
-            L.check(L.mmshift_cache_read(shape, self._all, first, k, v, self._status, 256,
+            L.check(L.mmshift_cache_read(shape, self._all, first, k, v, self._workspace, self._ws_bytes,
                                          torch.cuda.current_stream()), "mmshift_cache_read")
         return k, v
 
     def poll(self) -> None:
         """Waits for the current stream and raises what a call on the cache reported."""
         with self._on_device():
-            for ws in self._used:
-                L.check(L.mmshift_poll_status(ws, torch.cuda.current_stream()), "mmshift_poll_status")
+            L.check(L.mmshift_poll_status(self._workspace, torch.cuda.current_stream()), "mmshift_poll_status")

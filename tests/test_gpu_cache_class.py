@@ -173,3 +173,20 @@ def test_indices_of_another_shape_or_type_are_refused():
                  (idx, counts[:1])):
         with pytest.raises(ValueError):
             c.fill(sel, k, k, i, n)
+
+
+@pytest.mark.parametrize("dtype,kind", [("bf16", "bf16"), ("bf16", "i8"), ("f32", "f32"), ("f32", "i8")])
+def test_the_workspace_does_for_every_call(dtype, kind):
+    """And what is kept for combinations of row counts does not grow without end."""
+    g = torch.Generator().manual_seed(11)
+    for r in (1, 3, 7, 9, 11, 16, 17, 31, 32, 33, 64, 65, 300):
+        for batch in (1, 3):
+            c = _cache(device="cpu", n_q_heads=2 * r, dtype=R.DT[dtype], batch=batch, head_dim=128 if r % 2 else 64,
+                       cache_dtype=torch.int8 if kind == "i8" else None)
+            calls = [[n] * batch for n in range(1, 70)] + [[n] + [1] * (batch - 1) for n in (256, 300, 1000)]
+            calls += [(2 ** torch.randint(0, 13, (batch,), generator=g)).tolist() for _ in range(40)]
+            assert max(c._shape(new, 1)[1] for new in calls) <= c._ws_bytes
+    for n in range(1000):
+        c._call([n, 1, 2], 1)
+        c.advance([n, 1, 2])
+    assert len(c._calls) <= 256 and len(c._counts) <= 256 and not c._captured
