@@ -1,9 +1,10 @@
-// Attention of few query rows (up to 16 of a request and KV head: single tokens
+// Attention of few query rows (tiles of up to 16 of a request and KV head: single tokens
 // under grouped heads, a few drafted tokens) over bfloat16 or 8-bit pages.
 //
 // Bound by the bytes of K and V, which pass once from global memory to the
 // registers of the warp that uses them: no shared memory, no barrier in
-// the loop. Each warp takes pieces of KEYS keys of its own and keeps its own
+// the loop. 64 requests of one token, 64 heads, 2 to 24 thousand rows: 260 us over 8-bit
+// pages (6.0 TB/s; 53 % of the issue slots), 446 over bfloat16 ones (6.8 TB/s). Each warp takes pieces of KEYS keys of its own and keeps its own
 // running maximum, sums and output. Both products are m16n8k16 MMAs with
 // the keys (and then the dimensions) as M and the query rows as N, so eight
 // rows cost one column block and no product is spent on padding beyond that:
@@ -25,7 +26,8 @@
 // taken of e^(z - m) as ever.
 //
 // The maxima are only raised when a value passes them by 8 (base 2), so the common
-// step has one vote and no reduction: weights then stay below 2^8.
+// step has one vote and no reduction: weights then stay below 2^8. bfloat16 rows: a weight
+// is rounded to bfloat16, the MMA's operand, its sum is not.
 #include "attend.cuh"
 #include "umma.cuh"
 
@@ -247,8 +249,7 @@ __global__ void __launch_bounds__(NT, NQ == 1 ? 3 : 2) attend_token_kernel(const
     }
     const int32_t* table = J.table + ((size_t)U.b * J.Hkv + U.h) * J.max_pages;
 
-    // row of the pool of each 16-key block, -1 behind the end and without a page
-    // raises a maximum to its row's of the step; what sums relative to it have to be multiplied by
+    // Raises a maximum to its row's of the step; what sums relative to it have to be multiplied by.
     auto raise_max = [&](float& m, auto&& value) {
       float top = m;
 #pragma unroll
