@@ -2,8 +2,8 @@
 
 The computation lives in libmmshift.so (CUDA kernels behind the C ABI of
 include/mmshift.h); ``_lib`` is its ctypes binding with the same entry-point
-names, ``selector.KVSelector`` a torch-facing convenience, ``synth`` the seeded
-synthetic workloads. Importing the package does not load the library; the first
+names, ``selector.KVSelector`` and ``cache.PagedKVCache`` (the kept rows in pages, and
+attention over them) torch-facing conveniences, ``synth`` the seeded synthetic workloads. Importing the package does not load the library; the first
 call does, and fails loudly if the library cannot be built or loaded.
 """
 from . import synth  # noqa: F401

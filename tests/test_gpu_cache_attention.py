@@ -336,3 +336,38 @@ def test_selection_then_decoding(dtype, kind, head_budgets):
         for layer in range(L_):
             R.check_attention(R.attend(cache, q[layer], new, layer=layer), R.reference(cache, q[layer], new, layer=layer))
     assert M.mmshift_poll_status(ws) == 0
+
+
+@pytest.mark.parametrize("dtype,kind", KINDS)
+def test_pages_past_32_bits_of_bytes(dtype, kind):
+    """The same pages behind the first 4 GB of a pool: same bits written, read and attended to."""
+    d, new, hq = 128, [1, 40, 100], 6
+    small = R.Cache([[300, 1], [90, 41], [700, 100]], d, kind, 64).fill_random()
+    row = d * small.kp.element_size()
+    shift = 2 ** 32 // (row * 64) + 5
+    big = R.Cache.__new__(R.Cache)
+    big.__dict__.update(small.__dict__, n_pages=shift + small.n_pages)
+    big.table = torch.where((small.table >= 0) & (small.table < small.n_pages), small.table + shift, -1).int()
+    for name in ("kp", "vp", "ks", "vs"):
+        pages = getattr(small, name)
+        if pages is not None:
+            far = torch.empty((big.n_pages, *pages.shape[1:]), dtype=pages.dtype, device="cuda")
+            far[shift:] = pages
+            setattr(big, name, far)
+    q = _q(new, hq, d, dtype)
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    k, v = (torch.randn((sum(new), 2, d), generator=gen, device="cuda").to(R.DT[dtype]) for _ in range(2))
+    shape, got = R.shape_of(small, new, hq, dtype), []
+    for c in (small, big):
+        struct = c.struct()
+        ws, n = R.workspace(shape, struct)
+        s = torch.cuda.current_stream()
+        M.check(M.mmshift_cache_append(shape, struct, k, v, 0, ws, n, s), "append")
+        out = [torch.empty_like(q)] + [torch.empty((sum(new), 2, d), dtype=R.DT[dtype], device="cuda") for _ in range(2)]
+        lse = torch.empty(q.shape[:2], device="cuda")
+        M.check(M.mmshift_cache_read(shape, struct, None, out[1], out[2], ws, n, s), "read")
+        M.check(M.mmshift_cache_attention(shape, struct, q, 0, 1, 0.0, out[0], lse, ws, n, s), "attention")
+        assert M.mmshift_poll_status(ws) == 0
+        got.append(out + [lse] + [t[-small.n_pages:] for t in (c.kp, c.vp, c.ks, c.vs) if t is not None])
+    for a, b in zip(*got):
+        assert R.same(a, b)
