@@ -21,8 +21,9 @@
 // when a logit passes it by 8 (base 2); then the thread rescales its row of O itself,
 // which is idle at that point: S of a tile is complete only after the products of the
 // tile before. 2048 tokens of 28 heads over 34816 rows: 635 us, 1.56 PFLOP/s (8-bit
-// pages 1080: a thread's exponentials and the converted tiles, not the products);
-// a run's start (lengths, Q) and end (O) take about 10 us, which is what short chunks
+// pages 1090: 2.3 times the instructions, for codes and scales; 54 % of the issue slots,
+// the tensor pipe at 37 %). S in halves, its maximum checked against the one there is
+// instead of read first, took 685 (1093). A run's start (lengths, Q) and end (O) take about 10 us, which is what short chunks
 // wait for. P is rounded to bfloat16 (the tensor cores' operand type), its sum is not.
 //
 // Tiles that hold keys which some row of the tile does not attend to (the chunk's
