@@ -20,7 +20,7 @@
 // that one's results go out while the next one begins. A row's maximum is only raised
 // when a logit passes it by 8 (base 2); then the thread rescales its row of O itself,
 // which is idle at that point: S of a tile is complete only after the products of the
-// tile before. 2048 tokens of 28 heads over 34816 rows: 635 us, 1.56 PFLOP/s (8-bit
+// tile before. 2048 tokens of 28 heads over 34816 rows: 616 us, 1.61 PFLOP/s (8-bit
 // pages 1090: 2.3 times the instructions, for codes and scales; 54 % of the issue slots,
 // the tensor pipe at 37 %). S in halves, its maximum checked against the one there is
 // instead of read first, took 685 (1093). A run's start (lengths, Q) and end (O) take about 10 us, which is what short chunks
@@ -715,19 +715,27 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
             }
           };
           if (!masked) {
-            float v[BK];
-#pragma unroll
-            for (int i = 0; i < BK; i += 32) ld32(scol + i, v + i);
-            tmem_wait_ld();
-#pragma unroll
-            for (int i = 0; i < BK; i += 32) pin32(v + i);
-            float top[1] = {max_of<BK>(v) * A.alpha};
+            // The second half is read again: 128 values and the rest do not fit in 168 registers
+            // (spilled, a long chunk took 636 us instead of 616).
+            float v[64];
+            auto half = [&](int i) {
+              ld32(scol + i, v);
+              ld32(scol + i + 32, v + 32);
+              tmem_wait_ld();
+              pin32(v);
+              pin32(v + 32);
+            };
+            half(64);
+            float top[1] = {max_of<64>(v)};
+            half(0);
+            top[0] = fmaxf(top[0], max_of<64>(v)) * A.alpha;
             raise(top);
             const float mu = m[0] == -INFINITY ? 0.f : m[0];
 #pragma unroll
             for (int i = 0; i < BK; i += 32) {
+              if (i == 64) half(64);
               uint32_t w[16];
-              weights(v + i, mu, w);
+              weights(v + i % 64, mu, w);
               st16(scol + i / 2, w);
             }
           } else {
