@@ -110,9 +110,11 @@ __global__ void __launch_bounds__(256) attend_merge_row_kernel(const __grid_cons
 }
 
 // The merge of many units: only those across a border of two workers' shares have
-// parts, so a block takes a border (and 8 rows, a warp a row), the first inside its unit's
-// pieces. The blocks behind them write zeros for units without keys.
-constexpr int kEmptyBlocks = 16;
+// parts, so a block takes a border (and 32 rows, kMergeRows a warp in turn), the first
+// inside its unit's pieces. The blocks behind them write zeros for units without keys. Most
+// blocks only find that they have nothing to do: with 8 rows each there are so many that
+// ragged turns take 150 us instead of 145, with 64 rows a warp has too much (150).
+constexpr int kEmptyBlocks = 16, kMergeRows = 4;
 
 template <typename T, int D>
 __global__ void __launch_bounds__(256) attend_merge_border_kernel(const __grid_constant__ AttendJob A,
@@ -144,16 +146,19 @@ __global__ void __launch_bounds__(256) attend_merge_border_kernel(const __grid_c
   const AttendStart s = P.start[i];
   const AttendUnit U = attend_unit(A, P, nullptr, s.unit);
   const Parts parts(P, sh, U, s.before);
-  const int r = blockIdx.y * 8 + w;
-  if (parts.i0 + 1 != i || parts.i0 == parts.i1 || r >= U.rows) return;
-  float top, z, o[D / 32];
-  add_parts<D, 1>(P, parts, r, lane, 0, top, z, o);
-  // four neighbouring values to one lane
-  if constexpr (D == 128) {
-    attend_write<T, D>(A, U.b, U.h, U.row0 + r, lane * 4, make_float4(o[0], o[1], o[2], o[3]), top, z);
-  } else {
-    const float a = __shfl_down_sync(0xffffffffu, o[0], 1), b = __shfl_down_sync(0xffffffffu, o[1], 1);
-    if (lane % 2 == 0) attend_write<T, D>(A, U.b, U.h, U.row0 + r, lane * 2, make_float4(o[0], o[1], a, b), top, z);
+  if (parts.i0 + 1 != i || parts.i0 == parts.i1) return;
+  const int r0 = blockIdx.y * 8 * kMergeRows + w, r1 = min(U.rows, (int)(blockIdx.y + 1) * 8 * kMergeRows);
+#pragma unroll 1
+  for (int r = r0; r < r1; r += 8) {
+    float top, z, o[D / 32];
+    add_parts<D, 1>(P, parts, r, lane, 0, top, z, o);
+    // four neighbouring values to one lane
+    if constexpr (D == 128) {
+      attend_write<T, D>(A, U.b, U.h, U.row0 + r, lane * 4, make_float4(o[0], o[1], o[2], o[3]), top, z);
+    } else {
+      const float a = __shfl_down_sync(0xffffffffu, o[0], 1), b = __shfl_down_sync(0xffffffffu, o[1], 1);
+      if (lane % 2 == 0) attend_write<T, D>(A, U.b, U.h, U.row0 + r, lane * 2, make_float4(o[0], o[1], a, b), top, z);
+    }
   }
 }
 
@@ -162,8 +167,9 @@ cudaError_t launch_merge_t(const AttendJob& A, const AttendPlan& P, cudaStream_t
   const unsigned units = P.uoff[A.c.B];
   if (8 * units <= (unsigned)P.workers)
     return launch_kernel(attend_merge_row_kernel<T, D>, dim3(units, P.rows), 256, 0, st, true, 0, A, P);
-  return launch_kernel(attend_merge_border_kernel<T, D>, dim3(P.workers - 1 + kEmptyBlocks, (P.rows + 7) / 8), 256, 0, st,
-                       true, 0, A, P);
+  constexpr int rows = 8 * kMergeRows;
+  return launch_kernel(attend_merge_border_kernel<T, D>, dim3(P.workers - 1 + kEmptyBlocks, (P.rows + rows - 1) / rows),
+                       256, 0, st, true, 0, A, P);
 }
 
 cudaError_t launch_merge(const AttendJob& A, const AttendPlan& P, cudaStream_t st) {
