@@ -17,34 +17,69 @@ namespace {
 
 constexpr float kLeastMost = 7.703719777548943e-34f;   // 2^-110: 127 / it is finite
 
-// The codes of 16 bytes of a row (8 bfloat16 or 4 float32 values) and the row's
-// scale. LPR lanes hold a row. The product x * (127 / most) is at most 127 (1 + 2^-23),
-// which rounds to 127.
-template <typename T, int LPR>
-__device__ __forceinline__ float quantise16(const uint4& w, uint32_t (&code)[2]) {
+// The largest magnitude's bit pattern of 16 bytes of a row (8 bfloat16 or 4 float32
+// values): the patterns' order is the values', and a NaN is the largest.
+template <typename T>
+__device__ __forceinline__ uint32_t most16(const uint4& w) {
+  if constexpr (sizeof(T) == 2) {
+    constexpr uint32_t k = 0x7fff7fffu;
+    const uint32_t m = __vmaxu2(__vmaxu2(w.x & k, w.y & k), __vmaxu2(w.z & k, w.w & k));
+    return max(m & 0xffffu, m >> 16);
+  } else {
+    constexpr uint32_t k = 0x7fffffffu;
+    return max(max(w.x & k, w.y & k), max(w.z & k, w.w & k));
+  }
+}
+
+// rint(x * inv), at most 127 (1 + 2^-23) before it is rounded: 1.5 * 2^23 added, the sum's
+// last byte is the code (no conversion: those go at a quarter of the rate).
+template <typename T>
+__device__ __forceinline__ void codes16(const uint4& w, float inv, uint32_t (&code)[2]) {
   constexpr int N = 16 / (int)sizeof(T);
   const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-  float x[N];
+  uint32_t c[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    if constexpr (sizeof(T) == 2) x[i] = (i & 1) ? bf16_hi(u[i / 2]) : bf16_lo(u[i / 2]);
-    else x[i] = __uint_as_float(u[i]);
+    float x;
+    if constexpr (sizeof(T) == 2) x = (i & 1) ? bf16_hi(u[i / 2]) : bf16_lo(u[i / 2]);
+    else x = __uint_as_float(u[i]);
+    c[i] = __float_as_uint(__fadd_rn(__fmul_rn(x, inv), 12582912.f));
   }
-  // magnitudes as bit patterns: their order is the values', and a NaN is the largest
-  uint32_t m = 0;
 #pragma unroll
-  for (int i = 0; i < N; ++i) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);
+  for (int i = 0; i < N; i += 4) {
+    const uint32_t lo = __byte_perm(c[i], c[i + 1], 0x0040), hi = __byte_perm(c[i + 2], c[i + 3], 0x0040);
+    code[i / 4] = inv != 0.f ? __byte_perm(lo, hi, 0x5410) : 0;   // x may be no number
+  }
+}
+
+// The codes of 16 bytes of a K and of a V row, by the LPR lanes that hold them, and
+// their scale: K's in lanes 2, 6, ..., V's in lanes 3, 7, ... Of a row pair's four quotients
+// every lane works out one: with all four, a reduction for each row and conversions,
+// filling 229,000 bfloat16 rows and reading them back took 73.5 us instead of 69.
+template <typename T, int LPR>
+__device__ __forceinline__ float quantise16(const uint4& k, const uint4& v, int part, uint32_t (&ck)[2],
+                                            uint32_t (&cv)[2]) {
+  uint32_t mk = most16<T>(k), mv = most16<T>(v);
+  if constexpr (sizeof(T) == 2) {
+    uint32_t m = mk | mv << 16;
 #pragma unroll
-  for (int s = LPR / 2; s; s >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, s));
-  const float most = __uint_as_float(m);
-  const bool fine = m < 0x7f800000u;
-  const float inv = fine && most >= kLeastMost ? __fdiv_rn(127.f, most) : 0.f;
-  code[0] = code[1] = 0;
+    for (int s = LPR / 2; s; s >>= 1) m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, s));
+    mk = m << 16;
+    mv = m & 0xffff0000u;
+  } else {
 #pragma unroll
-  for (int i = 0; i < N; ++i)
-    if (inv != 0.f)
-      code[i / 4] |= (uint32_t)(uint8_t)(int8_t)__float2int_rn(__fmul_rn(x[i], inv)) << (8 * (i & 3));
-  return fine ? __fdiv_rn(most, 127.f) : __uint_as_float(0x7fffffffu);
+    for (int s = LPR / 2; s; s >>= 1) {
+      mk = max(mk, __shfl_xor_sync(0xffffffffu, mk, s));
+      mv = max(mv, __shfl_xor_sync(0xffffffffu, mv, s));
+    }
+  }
+  const uint32_t m = part & 1 ? mv : mk;
+  const float most = __uint_as_float(m), q = __fdiv_rn(part & 2 ? most : 127.f, part & 2 ? 127.f : most);
+  auto usable = [](uint32_t x) { return x < 0x7f800000u && __uint_as_float(x) >= kLeastMost; };
+  const float ik = __shfl_sync(0xffffffffu, q, 0, LPR), iv = __shfl_sync(0xffffffffu, q, 1, LPR);
+  codes16<T>(k, usable(mk) ? ik : 0.f, ck);
+  codes16<T>(v, usable(mv) ? iv : 0.f, cv);
+  return m < 0x7f800000u ? q : __uint_as_float(0x7fffffffu);
 }
 
 // Rows into pages. FILL: the rows idx keeps of a prompt, to positions 0, 1, ...;
@@ -105,7 +140,7 @@ __global__ void __launch_bounds__(256) cache_write_kernel(const __grid_constant_
     }
     if constexpr (I8) {
       uint32_t ck[2], cv[2];
-      const float sk = quantise16<T, LPR>(kk[k], ck), sv = quantise16<T, LPR>(vv[k], cv);
+      const float scale = quantise16<T, LPR>(kk[k], vv[k], part, ck, cv);
       if (slot < 0) continue;
       constexpr int CB = 16 / (int)sizeof(T);             // code bytes of a lane
       const size_t dst = (size_t)slot * D + part * CB;
@@ -116,10 +151,8 @@ __global__ void __launch_bounds__(256) cache_write_kernel(const __grid_constant_
         *reinterpret_cast<uint32_t*>(J.kp + dst) = ck[0];
         *reinterpret_cast<uint32_t*>(J.vp + dst) = cv[0];
       }
-      if (part == 0) {
-        J.ks[slot] = sk;
-        J.vs[slot] = sv;
-      }
+      if (part == 2) J.ks[slot] = scale;
+      if (part == 3) J.vs[slot] = scale;
     } else {
       if (slot < 0) continue;
       const size_t dst = (size_t)slot * ROWB + part * 16;
@@ -294,10 +327,11 @@ mmshift_status check_workspace(const void* ws, size_t bytes, size_t scratch = 0)
   return ws && aligned(ws, 256) && bytes >= 256 + scratch ? MMSHIFT_OK : MMSHIFT_ERR_WORKSPACE;
 }
 
-// Calls of more rows (of all heads and layers) than this give each group of lanes four:
-// 609,000 8-bit rows are read in 74.2 us instead of 87.3 (6.4 TB/s), 229,000 written and
-// read back in 73.7 instead of 76.9; 17,800 take 15.9 instead of 9.7 us that way, and
-// 3,076 float32 rows 3.7 instead of 2.7.
+// Calls of more rows (of all heads and layers) than this give each group of lanes four to
+// read, or two to write: 609,000 8-bit rows are read in 74.2 us instead of 87.3 (6.4 TB/s);
+// 229,000 written, 8-bit from bfloat16, and read back in 65 (68 with one row written, 69
+// with four, 88 with eight), unquantised float32 in 72 (76, 73). 17,800 rows take 15.9
+// instead of 9.7 us with four, 3,076 float32 rows 3.7 instead of 2.7.
 constexpr int64_t kMany = 40000;
 
 template <bool FILL, int N>
@@ -327,7 +361,7 @@ cudaError_t launch_write(const CacheJob& J, const void* K, const void* V, const 
                          const int32_t* count, cudaStream_t st) {
   const int64_t rows = (int64_t)J.off[J.B] * J.Hkv * J.L;
   if (!rows) return cudaSuccess;
-  return rows > kMany ? launch_write_n<FILL, 4>(J, K, V, idx, count, st)
+  return rows > kMany ? launch_write_n<FILL, 2>(J, K, V, idx, count, st)
                       : launch_write_n<FILL, 1>(J, K, V, idx, count, st);
 }
 
