@@ -254,3 +254,64 @@ def test_append_and_read_report_missing_pages():
                 assert R.same(out[0, t], want)
             else:
                 assert (out[:, t] == 0).all()
+
+
+@pytest.mark.parametrize("dtype,kind", KINDS)
+@pytest.mark.parametrize("d", [64, 128])
+def test_long_calls(dtype, kind, d):
+    """More than 40,000 rows of all heads, of which a group of lanes takes some together: appended
+    (some before a sequence's start, some not finite), read from the middle on, and filled."""
+    H, new, lens = 3, [9001, 0, 5003], [[9001, 9500, 8000], [4, 5, 6], [5003, 1, 5100]]
+    T, cu = sum(new), R.cu_of(new)
+    K, V = _rows((1, T, H, d), dtype, 1), _rows((1, T, H, d), dtype, 2)
+    K[0, 70, :, 3] = math.inf
+    V[0, 71, 1, 5] = math.nan
+    cache, ref = R.Cache(lens, d, kind, 64, seed=d), R.Cache(lens, d, kind, 64, seed=d)
+    for b, n in enumerate(new):
+        for h in range(H):
+            pos = torch.arange(n) + lens[b][h] - n
+            keep = pos >= 0
+            ref.put(0, b, h, pos[keep], K[0, cu[b]:cu[b + 1], h][keep.cuda()], V[0, cu[b]:cu[b + 1], h][keep.cuda()])
+    shape, struct = R.shape_of(cache, new, 2 * H, dtype), cache.struct()
+    ws, n = R.workspace(shape, struct)
+    M.check(M.mmshift_cache_append(shape, struct, K, V, 0, ws, n), "append")
+
+    def check():
+        assert M.mmshift_poll_status(ws) == 0
+        for got, want in zip(cache.tensors(), ref.tensors()):
+            if got.is_floating_point():
+                assert torch.equal(torch.isnan(got), torch.isnan(want))
+                got, want = got.nan_to_num(0, 1, -1), want.nan_to_num(0, 1, -1)
+            assert R.same(got, want)
+
+    check()
+    first = torch.tensor([[[0, 400, 7999], [0, 0, 0], [3, 0, 100]]], dtype=torch.int32)
+    out = torch.full((2, T, H, d), 9.0, dtype=R.DT[dtype], device="cuda")
+    M.check(M.mmshift_cache_read(shape, struct, first.cuda(), out[0], out[1], ws, n), "read")
+    assert M.mmshift_poll_status(ws) == 0
+    for b, m in enumerate(new):
+        for h in range(H):
+            pos = torch.arange(m) + int(first[0, b, h])
+            pos = pos[pos < lens[b][h]]
+            want = cache.get(0, b, h, pos)
+            for x, w in zip(out[:, cu[b]:cu[b + 1], h], want):
+                w = w.float().to(R.DT[dtype])
+                assert torch.equal(torch.isnan(x[:len(pos)]), torch.isnan(w))
+                assert R.same(x[:len(pos)].nan_to_num(0, 1, -1).contiguous(), w.nan_to_num(0, 1, -1))
+                assert (x[len(pos):] == 0).all()
+
+    seq, budgets = [9001, 1, 5003], [8000, 1, 5003]
+    keep = [min(a, b) for a, b in zip(seq, budgets)]
+    K, V = _rows((1, sum(seq), H, d), dtype, 3), _rows((1, sum(seq), H, d), dtype, 4)
+    cache, ref = (R.Cache([[n] * H for n in keep], d, kind, 64, seed=1) for _ in range(2))
+    cache.lens.fill_(-77)
+    gen, at, cuk = torch.Generator().manual_seed(6), R.cu_of(seq), R.cu_of(keep)
+    idx = torch.zeros((1, sum(keep), H), dtype=torch.int32)
+    for b, m in enumerate(keep):
+        for h in range(H):
+            t = torch.randperm(seq[b], generator=gen)[:m].sort().values
+            idx[0, cuk[b]:cuk[b + 1], h] = t.int()
+            ref.put(0, b, h, torch.arange(m), K[0, at[b] + t.cuda(), h], V[0, at[b] + t.cuda(), h])
+    shape, struct = M.make_shape(H, H, d, 2, 0 if dtype == "bf16" else 1, at, budgets), cache.struct()
+    M.check(M.mmshift_cache_fill(shape, struct, K, V, idx.cuda(), None, ws, 256), "fill")
+    check()
