@@ -56,6 +56,7 @@ struct ChunkSmem {
   static constexpr int HALF = BK * 128;              // 64 columns of 128 rows
   static constexpr int TILE = HALVES * HALF;         // a block of Q, a tile of K or V
   static constexpr int STAGES = D == 64 ? 8 : I8 ? 3 : 5;
+  static_assert(STAGES >= 3, "v_before_s(): a tile's V is three positions behind the K of the tile before");
   static constexpr int RAW = BK * D;                 // a tile of codes
   // Tiles whose scales are kept: those of tile j + SCALES are written when its K has a
   // stage, which is after the V of tile j was freed, and so read by all.
@@ -301,6 +302,9 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
   unsigned char* raw = ring + SM::STAGES * SM::TILE;
   __shared__ uint64_t rfull[I8 ? SM::RAWS : 1], rempty[I8 ? SM::RAWS : 1];
   __shared__ alignas(16) float scales[I8 ? SM::SCALES : 1][2][I8 ? BK : 1];   // K's (times alpha) and V's
+  // Every wait is for the next fill of its stage that the waiting warp does not know to be complete,
+  // or for one that is: producer, converters and issuer pass all positions of the ring, the softmax
+  // blocks see v_before_s().
   __shared__ uint64_t full[SM::STAGES], empty[SM::STAGES], q_ready[2], s_ready[2], o_ready[2], o_free[2];
   __shared__ uint64_t p_ready[2], drain;
   __shared__ uint32_t tbase;
@@ -640,10 +644,14 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
         int vs = vstage + 1;
         uint32_t vp = vphase;
         if (vs == SM::STAGES) { vs = 0; vp ^= 1u; }
-        if (!I8 && special) {
+        // V is cleaned while S is computed where the block is in step with the ring. (8-bit pages:
+        // nothing to clean, but the tile's scales were written before its V was.)
+        const bool clean = !I8 && special, early = clean && v_before_s(s, R.s0);
+        if (!early && !wait_bar(&s_ready[x], sph, abort_)) { ok = false; break; }
+        if ((I8 || clean) && !wait_bar(&full[vs], vp, abort_)) { ok = false; break; }
+        if (clean) {
           // Both blocks clean V, each before it reports its P: what one finds clean the
           // other has cleaned, after it set the flag.
-          if (!wait_bar(&full[vs], vp, abort_)) { ok = false; break; }
           unsigned char* vt = ring + vs * SM::TILE;
           constexpr int CH = SM::HALVES * 8;             // 16-byte chunks of a row
 #pragma unroll 4
@@ -660,10 +668,8 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
           }
           fence_async();
         }
-        if (!wait_bar(&s_ready[x], sph, abort_)) { ok = false; break; }
+        if (early && !wait_bar(&s_ready[x], sph, abort_)) { ok = false; break; }
         sph ^= 1u;
-        // 8-bit pages: the tile's scales were written before its V was
-        if (I8 && !wait_bar(&full[vs], vp, abort_)) { ok = false; break; }
         fence_after();
         const bool masked = special || gone;
         if (gone && warp % 4 == 0 && lane == 0) set_status(J.status, kStatusBadPage);

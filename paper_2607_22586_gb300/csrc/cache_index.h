@@ -36,6 +36,14 @@ MMSHIFT_HD int keys_of(int causal, int len, int n, int i) {
   return e > 0 ? e : 0;
 }
 
+// Whether a block of the chunk kernel may wait for the V of key tile `s` of a run that
+// begins at tile `s0` before it has waited for the tile's S. A wait by parity tells
+// neighbouring fills of a stage apart and no others, so the fill before the wanted one has to be
+// known to be complete. Behind a run's first tile it is: S of the tile before says that all
+// fills up to that tile's K are. At the first tile the block may come from a run that it took no
+// part in, many rounds ahead of the ring; then S of the tile itself says so.
+MMSHIFT_HD bool v_before_s(int s, int s0) { return s > s0; }
+
 // Division of 0 <= x < 2^31 by a number d >= 1 known on the host, as one high product:
 // with L the least L such that d <= 2^L, m = ceil(2^(31 + L) / d) < 2^32 gives
 // floor(x / d) = floor(x m / 2^(31 + L)) (Granlund and Montgomery, 1994).
