@@ -1,5 +1,6 @@
 """Attention calls in which a CTA has many units in turn (runs): chunks of at most 128 rows
-of a KV head, whose blocks take the runs in turn, beside longer ones. Against the formula in float64, with garbage behind every sequence's end."""
+of a KV head, whose blocks take the runs in turn, beside longer ones, and more runs than are
+listed ahead. Against the formula in float64, with garbage behind every sequence's end."""
 import math
 import random
 
@@ -9,6 +10,7 @@ import torch
 from tests import cache_ref as R
 
 pytestmark = pytest.mark.gpu
+KINDS = [("bf16", "bf16"), ("bf16", "i8"), ("f32", "f32"), ("f32", "i8")]
 
 
 def _reference(cache, q, new):
@@ -97,3 +99,13 @@ def test_short_chunks_beside_long_ones(kind, d):
     new = [40, 300, 17, 1000, 128, 129] * 4
     lens = [[n + (37 * i + 211 * h) % 900 * (i % 3 > 0) for h in range(3)] for i, n in enumerate(new)]
     _run(lens, new, 6, d, "bf16", kind, 16)
+
+
+@pytest.mark.parametrize("dtype,kind", KINDS)
+@pytest.mark.parametrize("d", [64, 128])
+def test_more_runs_than_are_listed(dtype, kind, d):
+    """2,816 units of 45 rows (float32: 72, more than the few rows' kernels take) over at most 22
+    keys: 18 runs a CTA, where 16 are listed ahead."""
+    B, H, n = 64, 44, 5 if dtype == "bf16" else 8
+    lens = [[(5 * b + 7 * h) % 23 for h in range(H)] for b in range(B)]
+    _run(lens, [n] * B, H * 9, d, dtype, kind, 16)
