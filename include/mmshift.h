@@ -381,10 +381,11 @@ mmshift_status mmshift_coverage(const mmshift_shape* s, const void* K, const voi
  * lens counts the rows that a call appends or queries for too: a decode step
  * first adds each request's number of new tokens to lens, then appends and
  * attends for every layer. lens and page_table are read on the device, so a
- * captured step can be replayed as the sequences grow. lens outside
- * [0, max_pages * page_size] is clamped; a position there whose table entry is
+ * captured step can be replayed as the sequences grow. read and attention clamp
+ * lens to [0, max_pages * page_size]; a position there whose table entry is
  * outside [0, n_pages) has no page: a write to it is dropped, it reads as zeros,
- * attention leaves its key out, and mmshift_poll_status reports it.
+ * attention leaves its key out, and mmshift_poll_status reports it. So are rows
+ * appended behind the table dropped and reported: see mmshift_cache_append.
  *
  * The shape of append, read and attention lists the rows of the call, not a
  * prompt: request b has T_b = cu_seqlens[b+1] - cu_seqlens[b] >= 0 rows
@@ -423,8 +424,11 @@ mmshift_status mmshift_cache_fill(const mmshift_shape* s, const mmshift_cache* c
                                   void* workspace, size_t workspace_bytes,
                                   mmshift_stream_t stream);
 
-/* New tokens' rows: K[l][cu_b + i][h] becomes position lens[l][b][h] - n_b + i
- * (dropped where that is negative). K, V: [L][T, Hkv, d] in the shape's
+/* New tokens' rows: K[l][cu_b + i][h] becomes position lens[l][b][h] - n_b + i.
+ * Dropped where that is negative, and where it is max_pages * page_size or more, which
+ * mmshift_poll_status reports: the rows of a full sequence stay as they are (attention
+ * that follows sees them all, and takes the new tokens for its last ones). lens above 2^30,
+ * which no table holds, counts as max_pages * page_size. K, V: [L][T, Hkv, d] in the shape's
  * dtype, tokens row_stride elements apart (0 = Hkv * d), layers
  * layer_stride_kv apart. */
 mmshift_status mmshift_cache_append(const mmshift_shape* s, const mmshift_cache* c, const void* K,

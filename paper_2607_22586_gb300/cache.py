@@ -27,8 +27,9 @@ _KEPT = 256   # combinations of row counts whose shapes are kept
 
 class PagedKVCache:
     """Sequences of ``rows`` rows at most (an int, or one for each layer, request
-    and KV head: [L, B, Hkv]), each with its pages from the start. Calls run on the
-    current stream; a cache is used on one stream at a time."""
+    and KV head: [L, B, Hkv]), each with its pages from the start. Rows appended to a full
+    sequence are left out, and poll() reports it (``capacity``: rows that every sequence
+    holds). Calls run on the current stream; a cache is used on one stream at a time."""
 
     def __init__(self, n_q_heads: int, n_kv_heads: int, head_dim: int, dtype: torch.dtype, batch: int,
                  rows: Union[int, Sequence, torch.Tensor], n_layers: int = 1, page_size: int = 64,

@@ -116,7 +116,7 @@ __global__ void __launch_bounds__(256) cache_write_kernel(const __grid_constant_
       bad[k] = there[k] && (t < 0 || t >= J.src[b + 1] - J.src[b]);
       src[k] = ((size_t)l * J.ls + (((size_t)J.src[b] + (bad[k] ? 0 : t)) * J.Hkv + h) * D) * sizeof(T);
     } else {
-      pos[k] = live ? cache_len(J, u) - n + i : 0;
+      pos[k] = live ? append_end(J.lens[u], J.cap) - n + i : 0;
       there[k] = live && pos[k] >= 0;
       src[k] = ((size_t)l * J.ls + (size_t)c * J.stride + (size_t)h * D) * sizeof(T);
     }

@@ -30,6 +30,11 @@ MMSHIFT_HD int32_t page_row(int32_t page, int32_t n_pages, int page_shift, int t
   return (page << page_shift) + (t & ((1 << page_shift) - 1));   // the pool's rows are below 2^31
 }
 
+// Where the rows of a call end in a sequence of which the device was told `len` rows: positions
+// from the table's end on exist for no row, so a full sequence's rows stay what they are. A number
+// that is no length (no table holds more than 2^30 rows) counts as the table's end.
+MMSHIFT_HD int append_end(int len, int cap) { return len > 1 << 30 ? cap : len > 0 ? len : 0; }
+
 // Keys that token i of a request's n tokens attends to in a sequence of len rows.
 MMSHIFT_HD int keys_of(int causal, int len, int n, int i) {
   const int e = causal ? len - n + i + 1 : len;
