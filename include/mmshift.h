@@ -453,9 +453,10 @@ mmshift_status mmshift_cache_read(const mmshift_shape* s, const mmshift_cache* c
  * have no part in its result whatever they hold, NaN included.
  * Q [T, Hq, d], tokens row_stride elements apart (0 = Hq * d); out [T, Hq, d],
  * dense; lse (nullable) [T, Hq] float32; scale 0 = 1/sqrt(d). bfloat16
- * weights e^(z - max) are rounded to bfloat16 before the product with v (few rows
- * over 8-bit pages: to float16); an 8-bit row's scale is multiplied into them
- * before that. */
+ * weights e^(z - max) are rounded to bfloat16 before the product with v; an 8-bit
+ * row's scale is multiplied into them before that. Few rows (up to 32 of a KV head) over 8-bit
+ * pages: to float16, off by at most 2^-11 of such a weight or, where that is more, by
+ * 2^-32 of the row's largest one. */
 mmshift_status mmshift_cache_attention(const mmshift_shape* s, const mmshift_cache* c,
                                        const void* Q, int64_t row_stride, int32_t causal,
                                        float softmax_scale, void* out, float* lse,

@@ -22,11 +22,15 @@
 // thousand rows.) A query row is scaled by a power of two that brings its largest
 // value to 2^14, so what float16 cannot hold of it is below 2^-39 of that. K's scale
 // goes to the logit. V's goes into the weight, whose float16 form is relative to the
-// row's largest such product: w = e^(z + ln vs - M), while the sum of weights is
-// taken of e^(z - m) as ever.
+// row's largest such product: w = 2^7 e^(z + ln vs - M), while the sum of weights is
+// taken of e^(z - m) as ever. With 2^7, weights reach 2^15 (the maximum is only raised by steps,
+// below), the last power of two that float16 holds; its lower end, where a half step is 2^-25,
+// then lies at 2^-32 of the largest product: rounding is off by at most 2^-11 of a weight or
+// by that. (Without it, 3,000 weights of e^-18 beside one of 1 were all rounded to zero.)
 //
 // The maxima are only raised when a value passes them by 8 (base 2), so the common
-// step has one vote and no reduction: weights then stay below 2^8. bfloat16 rows: a weight
+// step has one vote and no reduction: weights then stay below 2^8 (2^15 in the
+// form above). bfloat16 rows: a weight
 // is rounded to bfloat16, the MMA's operand, its sum is not.
 #include "attend.cuh"
 #include "umma.cuh"
@@ -36,7 +40,7 @@ namespace {
 
 constexpr int NT = 128, NW = NT / 32;
 constexpr int kCluster = 8;
-constexpr float kRaise = 8.f;
+constexpr float kRaise = 8.f, kUp = 7.f;   // kRaise + kUp: the exponent of float16's last power of two
 
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
                                          uint32_t b0, uint32_t b1) {
@@ -418,8 +422,8 @@ __global__ void __launch_bounds__(NT, NQ == 1 ? 3 : 2) attend_token_kernel(const
         const float m0 = m[nq][0] == -INFINITY ? 0.f : m[nq][0], m1 = m[nq][1] == -INFINITY ? 0.f : m[nq][1];
         float w0 = 0.f, w1 = 0.f;
         if constexpr (I8) {
-          w0 = mw[nq][0] == -INFINITY ? 0.f : mw[nq][0];
-          w1 = mw[nq][1] == -INFINITY ? 0.f : mw[nq][1];
+          w0 = mw[nq][0] == -INFINITY ? 0.f : mw[nq][0] - kUp;
+          w1 = mw[nq][1] == -INFINITY ? 0.f : mw[nq][1] - kUp;
         }
 #pragma unroll
         for (int nb = 0; nb < T::NB; ++nb) {
@@ -505,7 +509,7 @@ __global__ void __launch_bounds__(NT, NQ == 1 ? 3 : 2) attend_token_kernel(const
         for (int d = 4; d < 32; d <<= 1) z += __shfl_xor_sync(0xffffffffu, z, d);
         const int r = 8 * nq + 2 * c + e;
         if constexpr (I8) {                            // O relative to m
-          const float f = mw[nq][e] == -INFINITY ? 1.f : exp2f(mw[nq][e] - m[nq][e]);
+          const float f = mw[nq][e] == -INFINITY ? 1.f : exp2f(mw[nq][e] - kUp - m[nq][e]);
 #pragma unroll
           for (int mt = 0; mt < T::MT; ++mt) {
             o[nq][mt][e] *= f;
