@@ -111,7 +111,8 @@ class PagedKVCache:
     def fill(self, selector: KVSelector, K: torch.Tensor, V: torch.Tensor,
              idx: Optional[torch.Tensor] = None, counts: Optional[torch.Tensor] = None) -> None:
         """Starts the sequences with the rows that a selection kept (default: the
-        selector's last one): K, V [L, T, Hkv, d] as the selector took them."""
+        selector's last one): K, V [L, T, Hkv, d] as the selector took them; the first
+        ``counts`` [L, B, Hkv] int32 rows of each head's where given."""
         selector._check(K, V)
         if (selector.n_layers, len(selector.budgets), selector.n_kv_heads, selector.head_dim, selector.dtype,
                 selector.device) != (self.n_layers, self.batch, self.n_kv_heads, self.head_dim, self.dtype, self.device):
@@ -121,7 +122,7 @@ class PagedKVCache:
                                   or t.shape != like):
                 raise ValueError("idx [L, R, Hkv] and counts [L, B, Hkv] must be contiguous int32 tensors")
         if idx is None:
-            idx, counts = selector.out_idx, selector.out_count
+            idx, counts = selector.out_idx, selector.out_count if counts is None else counts
         with self._on_device():
             L.check(L.mmshift_cache_fill(selector.shape, self._all, K, V, idx, counts, self._workspace, self._ws_bytes,
                                          torch.cuda.current_stream()), "mmshift_cache_fill")
