@@ -122,7 +122,7 @@ class PagedKVCache:
                                   or t.shape != like):
                 raise ValueError("idx [L, R, Hkv] and counts [L, B, Hkv] must be contiguous int32 tensors")
         if idx is None:
-            idx, counts = selector.out_idx, selector.out_count if counts is None else counts
+            idx, counts = selector.out_idx, selector.kept_count if counts is None else counts
         with self._on_device():
             L.check(L.mmshift_cache_fill(selector.shape, self._all, K, V, idx, counts, self._workspace, self._ws_bytes,
                                          torch.cuda.current_stream()), "mmshift_cache_fill")

@@ -30,6 +30,7 @@ class KVSelector:
         self.n_q_heads = n_q_heads
         self.budgets = list(budgets)
         self.out_count = None
+        self.kept_count = None    # the last call's counts: out_count, or None where heads keep their budgets
         self.shape = L.make_shape(n_q_heads, n_kv_heads, head_dim, window, _DT[dtype], cu_seqlens,
                                   budgets, n_layers=n_layers,
                                   layer_stride_kv=total * n_kv_heads * head_dim,
@@ -99,6 +100,7 @@ class KVSelector:
             L.check(L.mmshift_select(self.shape, K, V, qwin, proxies_in, self.params, self.out_idx,
                                      self.out_k, self.out_v, debug, self.workspace, self.ws_bytes,
                                      stream), "mmshift_select")
+        self.kept_count = self.out_count if head_budgets is not None else None
         return self.out_idx, self.out_k, self.out_v
 
     def prefill_stats(self, qfull: torch.Tensor, layer_stride: int = 0, stream=None) -> torch.Tensor:

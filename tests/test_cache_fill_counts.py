@@ -54,3 +54,18 @@ def test_indices_come_without_the_selection_s_counts(filled):
     assert seen["got"][0] is idx and seen["got"][1] is counts
     cache.fill(sel, K, K)
     assert seen["got"][0] is sel.out_idx and seen["got"][1] is sel.out_count
+
+
+def test_counts_of_an_earlier_selection_are_not_used(filled):
+    """A selection without budgets per head keeps every head's budget, whatever one before it kept."""
+    sel, cache, K, Q, seen = filled
+    budgets = torch.ones((2, 1, 2), dtype=torch.int32)
+    stats = torch.zeros((2, 1, 2, 6 * 64))
+    for again in ({}, {"stats": stats}):
+        sel(K, K, Q, head_budgets=budgets)
+        cache.fill(sel, K, K)
+        assert seen["got"][1] is sel.out_count
+        kept = sel.out_count
+        sel(K, K, Q, **again)
+        cache.fill(sel, K, K)
+        assert seen["got"][1] is None and sel.out_count is kept
