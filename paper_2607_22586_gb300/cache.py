@@ -102,8 +102,8 @@ class PagedKVCache:
         for t in ts:
             if t.dtype != self.dtype or t.device != self.device or t.shape[-3:] != (total, heads, self.head_dim):
                 raise ValueError(f"rows must be [..., {total}, {heads}, {self.head_dim}] of {self.dtype} on {self.device}")
-            if t.stride(-1) != 1 or (heads > 1 and t.stride(-2) != self.head_dim) or t.stride(-3) != ts[0].stride(-3) \
-                    or (total > 1 and t.stride(-3) < heads * self.head_dim):
+            if t.stride(-1) != 1 or (heads > 1 and t.stride(-2) != self.head_dim) \
+                    or (total > 1 and (t.stride(-3) != ts[0].stride(-3) or t.stride(-3) < heads * self.head_dim)):
                 raise ValueError("a token's heads must be dense, and the tokens equally far apart, without overlap")
             stride = t.stride(-3)
         return stride if total > 1 else heads * self.head_dim
@@ -152,7 +152,8 @@ class PagedKVCache:
         stride = self._check(total, self.n_kv_heads, K, V)
         if layer is not None and (K.dim() != 3 or V.dim() != 3):
             raise ValueError("rows of one layer must be [T, Hkv, d]")
-        if layer is None and (K.dim() != 4 or len(K) != layers or K.stride() != V.stride()):
+        if layer is None and (K.dim() != 4 or V.dim() != 4 or len(K) != layers or len(V) != layers
+                              or (layers > 1 and K.stride(0) != V.stride(0))):
             raise ValueError("rows of all layers must be [L, T, Hkv, d], K's and V's laid out alike")
         shape.layer_stride_kv = K.stride(0) if layer is None else 0
         with self._on_device():
