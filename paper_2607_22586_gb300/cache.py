@@ -140,9 +140,14 @@ class PagedKVCache:
             if len(self._counts) >= _KEPT:
                 self._counts.clear()
             self._counts[key] = torch.tensor(key, dtype=torch.int32, device=self.device)[None, :, None]
-        if self.lens.is_cuda and torch.cuda.is_current_stream_capturing():
-            self._captured.append(self._counts[key])       # read by every replay
-        self.lens.add_(self._counts[key])
+        counts = self._counts[key]
+        if self.lens.is_cuda:
+            with self._on_device():                        # whichever is current for the caller
+                if torch.cuda.is_current_stream_capturing():
+                    self._captured.append(counts)          # read by every replay
+                else:                                      # may be dropped while another stream than its own reads it
+                    counts.record_stream(torch.cuda.current_stream())
+        self.lens.add_(counts)
 
     def append(self, K: torch.Tensor, V: torch.Tensor, new: Sequence[int], layer: Optional[int] = None) -> None:
         """The new tokens' rows (counted by advance() before): K, V [L, T, Hkv, d], or
