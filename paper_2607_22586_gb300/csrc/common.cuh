@@ -232,8 +232,10 @@ __device__ __forceinline__ void dependent_start() {
 
 // Launches a kernel, with cluster > 1 in clusters along x. `overlap`: as a
 // programmatic dependent of the kernel before it in the stream, whose
-// launch latency then overlaps that kernel (both start with dependent_start,
-// so a kernel still begins its work after the one before it has finished).
+// launch latency then overlaps that kernel (every such kernel starts with dependent_start,
+// the paged cache's with cache_start or merge_start, so it still begins its work after the
+// one before it has finished; attend_merge_row_kernel alone reads lengths ahead of its wait,
+// which the attention kernel before it has waited for before it let the merge in).
 // Short calls use it: about 1 us per kernel of a ten-kernel call. Long ones do
 // not: waiting CTAs take places and issue slots from kernels that fill the SMs.
 template <class... KP, class... A>
