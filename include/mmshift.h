@@ -389,7 +389,8 @@ mmshift_status mmshift_coverage(const mmshift_shape* s, const void* K, const voi
  *
  * The shape of append, read and attention lists the rows of the call, not a
  * prompt: request b has T_b = cu_seqlens[b+1] - cu_seqlens[b] >= 0 rows
- * (n_b below); window and budgets are not read. Pages that a call writes belong to
+ * (n_b below), at most 2^30 / n_q_heads in all, and batch * n_kv_heads is at most
+ * 2^30; window and budgets are not read. Pages that a call writes belong to
  * one sequence; pages that it only reads may be shared. Workspace (and status
  * word, zero at first): mmshift_cache_workspace_size() bytes for attention with
  * that shape, 256 for the other calls, 256-byte aligned; what it holds besides

@@ -283,7 +283,8 @@ mmshift_status check_rows(const mmshift_shape* s) {
   if (s->cu_seqlens[0] != 0) return MMSHIFT_ERR_INVALID_ARG;
   for (int b = 0; b < s->batch; ++b)
     if (s->cu_seqlens[b + 1] < s->cu_seqlens[b]) return MMSHIFT_ERR_INVALID_ARG;
-  // rows of all heads are counted in 31 bits of blocks and of indices
+  // a layer's sequences, and rows of all heads, are counted in 31 bits of blocks and of indices
+  if ((int64_t)s->batch * s->n_kv_heads > (int64_t)1 << 30) return MMSHIFT_ERR_UNSUPPORTED;
   if ((int64_t)s->cu_seqlens[s->batch] * s->n_q_heads > (int64_t)1 << 30) return MMSHIFT_ERR_UNSUPPORTED;
   return MMSHIFT_OK;
 }
