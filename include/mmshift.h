@@ -453,7 +453,7 @@ mmshift_status mmshift_cache_read(const mmshift_shape* s, const mmshift_cache* c
  * NaN in both. Keys that a token does not attend to
  * have no part in its result whatever they hold, NaN included.
  * Q [T, Hq, d], tokens row_stride elements apart (0 = Hq * d); out [T, Hq, d],
- * dense; lse (nullable) [T, Hq] float32; scale 0 = 1/sqrt(d). bfloat16
+ * dense; lse (nullable) [T, Hq] float32; scale 0 = 1/sqrt(d), at most 2^127. bfloat16
  * weights e^(z - max) are rounded to bfloat16 before the product with v; an 8-bit
  * row's scale is multiplied into them before that. Few rows (up to 32 of a KV head) over 8-bit
  * pages: to float16, off by at most 2^-11 of such a weight or, where that is more, by

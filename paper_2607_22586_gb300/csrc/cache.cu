@@ -480,7 +480,7 @@ mmshift_status mmshift_cache_attention(const mmshift_shape* s, const mmshift_cac
   const int64_t dense = (int64_t)J.Hq * J.d;
   if (row_stride && row_stride < dense) return MMSHIFT_ERR_INVALID_ARG;
   if (causal != 0 && causal != 1) return MMSHIFT_ERR_INVALID_ARG;
-  if (!(softmax_scale >= 0.f) || !std::isfinite(softmax_scale)) return MMSHIFT_ERR_INVALID_ARG;
+  if (!(softmax_scale >= 0.f) || !std::isfinite(softmax_scale * kLog2e)) return MMSHIFT_ERR_INVALID_ARG;
   if (J.off[J.B] && (!Q || !out)) return MMSHIFT_ERR_INVALID_ARG;
   if (!aligned(Q, esz) || !aligned(out, esz) || !aligned(lse, 4)) return MMSHIFT_ERR_INVALID_ARG;
   if ((st = check_workspace(workspace, workspace_bytes, attend_scratch_bytes(J))) != MMSHIFT_OK) return st;
