@@ -644,14 +644,12 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
         int vs = vstage + 1;
         uint32_t vp = vphase;
         if (vs == SM::STAGES) { vs = 0; vp ^= 1u; }
-        // V is cleaned while S is computed where the block is in step with the ring. (8-bit pages:
-        // nothing to clean, but the tile's scales were written before its V was.)
-        const bool clean = !I8 && special, early = clean && v_before_s(s, R.s0);
-        if (!early && !wait_bar(&s_ready[x], sph, abort_)) { ok = false; break; }
-        if ((I8 || clean) && !wait_bar(&full[vs], vp, abort_)) { ok = false; break; }
-        if (clean) {
+        if (!I8 && special) {
           // Both blocks clean V, each before it reports its P: what one finds clean the
-          // other has cleaned, after it set the flag.
+          // other has cleaned, after it set the flag. While S is computed, where the block is
+          // known to be in step with the ring; else it waits for S here (and passes below).
+          if (!v_before_s(s, R.s0) && !wait_bar(&s_ready[x], sph, abort_)) { ok = false; break; }
+          if (!wait_bar(&full[vs], vp, abort_)) { ok = false; break; }
           unsigned char* vt = ring + vs * SM::TILE;
           constexpr int CH = SM::HALVES * 8;             // 16-byte chunks of a row
 #pragma unroll 4
@@ -668,8 +666,10 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
           }
           fence_async();
         }
-        if (early && !wait_bar(&s_ready[x], sph, abort_)) { ok = false; break; }
+        if (!wait_bar(&s_ready[x], sph, abort_)) { ok = false; break; }
         sph ^= 1u;
+        // 8-bit pages: the tile's scales were written before its V was
+        if (I8 && !wait_bar(&full[vs], vp, abort_)) { ok = false; break; }
         fence_after();
         const bool masked = special || gone;
         if (gone && warp % 4 == 0 && lane == 0) set_status(J.status, kStatusBadPage);
