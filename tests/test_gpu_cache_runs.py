@@ -109,3 +109,39 @@ def test_more_runs_than_are_listed(dtype, kind, d):
     B, H, n = 64, 44, 5 if dtype == "bf16" else 8
     lens = [[(5 * b + 7 * h) % 23 for h in range(H)] for b in range(B)]
     _run(lens, [n] * B, H * 9, d, dtype, kind, 16)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("new,lens,hq,hkv", [
+    ([1000] * 16, [[1000] * 4] * 16, 28, 4),
+    ([64] * 64, [[2300] * 8, [64] * 8] * 32, 8, 8),
+    ([10] * 64, [[1500] * 4, [60] * 4] * 32, 28, 4)])
+def test_not_finite_values_reach_only_their_own_readers(d, new, lens, hq, hkv):
+    """Values of the last tokens that are not finite: the tokens before them do not attend to
+    them, so not a bit of their results may differ."""
+    cache = R.Cache(lens, d, "bf16", 64).fill_random(7)
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    q = torch.randn((sum(new), hq, d), generator=gen, device="cuda").bfloat16()
+    want = R.attend(cache, q, new)
+    for b in range(len(new)):
+        for h in range(hkv):
+            last = cache.slots(0, b, h, [lens[b][h] - 1])
+            cache.vp.view(-1, d)[last, (7 * b + h) % d] = math.nan if b % 2 else math.inf
+    out, lse = R.attend(cache, q, new)
+    cu = R.cu_of(new)
+    last = torch.zeros(sum(new), dtype=torch.bool, device="cuda")
+    last[torch.tensor(cu[1:], device="cuda") - 1] = True
+    assert R.same(out[~last], want[0][~last]) and R.same(lse, want[1])
+    for b in range(len(new)):
+        for h in range(hkv):
+            x = out[cu[b + 1] - 1, h * (hq // hkv):(h + 1) * (hq // hkv)]
+            bad = ~torch.isfinite(x)
+            assert bad[:, (7 * b + h) % d].all() and int(bad.sum()) == hq // hkv
+
+
+@pytest.mark.parametrize("dtype,kind", KINDS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("r", [17, 32, 33, 71, 128, 300])
+def test_many_query_heads_of_one_kv_head(dtype, kind, d, r):
+    """One token's rows are more than a tile of the few rows' kernels, or than a block's."""
+    _run([[700], [1], [0], [129]], [1, 1, 1, 2], r, d, dtype, kind, 32)
