@@ -5,10 +5,12 @@
 // threads are 16 lanes of one warp, so its weights change hands through shared memory
 // without a barrier of the CTA. K of the next tile arrives (asynchronous copies; 8-bit
 // codes through registers, to be converted) while this one's values are added up, V while
-// its logits are. The shape is bound by what shared memory feeds the FMAs, 128 bytes
+// its logits are. The shape follows from what shared memory feeds the FMAs, 128 bytes
 // a clock and SM. Chunks (NT = 256, TR = 8: 128 rows by 64 keys): 8 x 4 sums take 1.5 bytes
 // an FMA, the 8 x 8 (or 8 x 4, d = 64) of the second product 1 (1.5): 512 tokens of 28
-// heads over 4096 rows, d = 128, 607 us (46 TFLOP/s of 80). Few rows (TR = 2, two or four
+// heads over 4096 rows, d = 128, 607 us (46 TFLOP/s of 80). Counters there: FMA pipe 65 % of
+// cycles, shared memory 53 %, issue slots 45 % (d = 64, 257 tokens: 52, 40, 41 %): 250 registers
+// leave two warps a scheduler, which mostly wait out an instruction's latency. Few rows (TR = 2, two or four
 // warps, five or four CTAs an SM): 64 requests of one token, 64 heads, 500 to 6000 rows
 // 312 us (4.9 TB/s) over float32 pages, 350 over 8-bit ones; 445 and 451 with four warps
 // and TR = 1, which read a key four times, not twice; 334 and 452 with one warp and TR = 4, too

@@ -20,11 +20,12 @@
 // that one's results go out while the next one begins. A row's maximum is only raised
 // when a logit passes it by 8 (base 2); then the thread rescales its row of O itself,
 // which is idle at that point: S of a tile is complete only after the products of the
-// tile before. 2048 tokens of 28 heads over 34816 rows: 616 us, 1.61 PFLOP/s (8-bit
-// pages 1090: 2.3 times the instructions, for codes and scales; 54 % of the issue slots,
-// the tensor pipe at 37 %). S in halves, its maximum checked against the one there is
-// instead of read first, took 685 (1093). A run's start (lengths, Q) and end (O) take about 10 us, which is what short chunks
-// wait for. P is rounded to bfloat16 (the tensor cores' operand type), its sum is not.
+// tile before. 2048 tokens of 28 heads over 34816 rows: 620 us in short runs, 640 to 660 in long
+// ones, 1.50 to 1.60 PFLOP/s (8-bit pages 1080: 2.3 times the instructions, for codes and scales;
+// 54 % of the issue slots, the tensor pipe at 37 %). S in halves, its maximum checked against the
+// one there is instead of read first, took 685 (1093). A run's start (lengths, Q) and end (O) take
+// about 10 us, which is what short chunks wait for: 16 prompts of 1000 tokens on their own rows
+// 273 us. P is rounded to bfloat16 (the tensor cores' operand type), its sum is not.
 //
 // Tiles that hold keys which some row of the tile does not attend to (the chunk's
 // own keys under the causal mask, the last tile) are masked, and their V rows are
@@ -722,7 +723,7 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
           };
           if (!masked) {
             // The second half is read again: 128 values and the rest do not fit in 168 registers
-            // (spilled, a long chunk took 636 us instead of 616).
+            // (spilled, a long chunk took 636 us instead of 616 on one GPU).
             float v[64];
             auto half = [&](int i) {
               ld32(scol + i, v);
