@@ -23,7 +23,10 @@
  *   - the attention-mass coverage of a kept set for given decode queries
  *     (mmshift_coverage; Section 1, Fig. 1b);
  *   - a paged cache for the kept rows, 8-bit if wanted: filled from a
- *     selection, appended to, read back and attended to (mmshift_cache_*).
+ *     selection, appended to, read back and attended to (mmshift_cache_*), its
+ *     pages shared by forked sequences, trimmed and given back;
+ *   - what comes before the selection: rotary positions (mmshift_rope) and
+ *     attention over whole prompts (mmshift_prompt_attention).
  *
  * Conventions shared by every entry point:
  *   - All pointers except the ones marked "host" are device pointers. The
@@ -463,6 +466,138 @@ mmshift_status mmshift_cache_attention(const mmshift_shape* s, const mmshift_cac
                                        float softmax_scale, void* out, float* lse,
                                        void* workspace, size_t workspace_bytes,
                                        mmshift_stream_t stream);
+
+/* Attention of new tokens over one layer's sequences, as mmshift_cache_attention and with
+ * its results, where sequences share pages: forked answers to one prompt. Requests
+ * cu_groups[g] .. cu_groups[g+1]-1 form a group (host array, cu_groups[0] = 0,
+ * cu_groups[n_groups] = batch, each of at least one request). The pages that all sequences of a
+ * group's KV head have in common from position 0 on, as their table entries say, are read and multiplied
+ * once for all rows of the group; each row's two parts are joined in float32. Where a group's
+ * sequences have nothing in common, its rows just attend to their own. Workspace:
+ * mmshift_cache_shared_workspace_size() bytes for that shape. */
+mmshift_status mmshift_cache_shared_workspace_size(const mmshift_shape* s, const mmshift_cache* c,
+                                                   int32_t n_groups, const int32_t* cu_groups,
+                                                   size_t* bytes);
+mmshift_status mmshift_cache_attention_shared(const mmshift_shape* s, const mmshift_cache* c,
+                                              int32_t n_groups, const int32_t* cu_groups,
+                                              const void* Q, int64_t row_stride, int32_t causal,
+                                              float softmax_scale, void* out, float* lse,
+                                              void* workspace, size_t workspace_bytes,
+                                              mmshift_stream_t stream);
+
+/* ---- Pages held by several sequences, and pages that are free ----
+ *
+ * refs: device [n_pages] int32, how many sequences hold each page (entries of the
+ * page table, of all layers, that name it), kept by the calls below from a pool of which
+ * all pages are free (refs zero, table entries -1). They write refs, page_table and lens. A
+ * page is free where its refs is 0. Free pages are taken lowest first, by sequences in
+ * their order [L][batch][Hkv] and by their positions: the same calls give the same pages.
+ * Calls on one cache, these and the ones above, follow one another on a stream. Workspace of all:
+ * mmshift_cache_pages_workspace_size() bytes for the shape of the call, 256-byte aligned,
+ * status word zero at first (mmshift_cache_fork and _free need 256 bytes of it). */
+mmshift_status mmshift_cache_pages_workspace_size(const mmshift_shape* s, const mmshift_cache* c,
+                                                  size_t* bytes);
+
+/* Pages for the rows that an append (or fill) with this shape writes, positions
+ * lens - n_b .. lens - 1 of every sequence of request b: where there is no page a free one is taken,
+ * and a page that other sequences hold too is replaced by a free one, into which its
+ * rows before those positions are copied. With no page free an entry becomes -1, its sequence
+ * loses what it held there, other sequences nothing; mmshift_poll_status reports it. */
+mmshift_status mmshift_cache_reserve(const mmshift_shape* s, const mmshift_cache* c, int32_t* refs,
+                                     void* workspace, size_t workspace_bytes,
+                                     mmshift_stream_t stream);
+
+/* Every sequence of request dst[i] becomes a copy of request src[i]'s, for n pairs (host
+ * arrays): what dst held is given back, src's pages up to its length are held by both, and
+ * its length is copied. Nothing is moved; what either writes later goes to a page of
+ * its own (mmshift_cache_reserve). A request may be the source of many; a dst appears once
+ * and is no src. Of the shape, cu_seqlens counts for nothing here. */
+mmshift_status mmshift_cache_fork(const mmshift_shape* s, const mmshift_cache* c, int32_t* refs,
+                                  int32_t n, const int32_t* src, const int32_t* dst,
+                                  void* workspace, size_t workspace_bytes, mmshift_stream_t stream);
+
+/* The n requests `which` (host array, each once) give all pages back; their lengths
+ * become 0. */
+mmshift_status mmshift_cache_free(const mmshift_shape* s, const mmshift_cache* c, int32_t* refs,
+                                  int32_t n, const int32_t* which, void* workspace,
+                                  size_t workspace_bytes, mmshift_stream_t stream);
+
+/* Keeps some rows of sequences, in order: for request b with n_b = cu_seqlens[b+1] -
+ * cu_seqlens[b] > 0, position i < m of its sequence becomes what position idx[l][cu_b + i][h] was,
+ * m = min(n_b, lens), with count (nullable: device [L][batch][Hkv]) min(n_b, lens, count);
+ * lens becomes m, and pages behind the rows are given back. idx: device [L, T, Hkv] int32,
+ * idx >= i and below lens (ascending indices are), as mmshift_topk writes them; other ones
+ * give a zero row and are reported by mmshift_poll_status. 8-bit rows keep their codes
+ * and scales. Rows move in place; pages that other sequences hold too stay as they are, the
+ * rows go to free ones (none free: reported, rows lost, as in mmshift_cache_reserve).
+ * Requests without rows stay as they are. */
+mmshift_status mmshift_cache_compact(const mmshift_shape* s, const mmshift_cache* c, int32_t* refs,
+                                     const int32_t* idx, const int32_t* count, void* workspace,
+                                     size_t workspace_bytes, mmshift_stream_t stream);
+
+/* ---- Rotary positions ----
+ *
+ * Pair j < rot_dims / 2 of a head turns by w = positions * inv_freq[j]:
+ *   x' = amplitude (x cos w - y sin w),  y' = amplitude (y cos w + x sin w)
+ * with (x, y) dimensions (j, j + rot_dims / 2), or (2j, 2j + 1) interleaved; dimensions from
+ * rot_dims on stay. Angles are exact to 2^-29 turns and float32's rounding at any position;
+ * sums are float32, rounded once. */
+enum { MMSHIFT_ROPE_HALF = 0, MMSHIFT_ROPE_INTERLEAVED = 1 };
+typedef struct {
+  int32_t layout;           /* MMSHIFT_ROPE_HALF or MMSHIFT_ROPE_INTERLEAVED */
+  int32_t rot_dims;         /* even, 2..head_dim; 0 = head_dim */
+  int32_t inverse;          /* 1 turns by -w: takes a rotation back (with amplitude 1; the
+                               gradient of the rotation with the same amplitude) */
+  int32_t n_axes;           /* position axes, 1..3 (text, or time / row / column); 0 = 1 */
+  int32_t sections[3];      /* n_axes > 1: consecutive pairs of each axis, rot_dims / 2 in all */
+  float amplitude;          /* 0 = 1 */
+  const double* inv_freq;   /* host [rot_dims / 2], radians a position */
+  const int32_t* positions; /* device [n_axes][T], of any sign */
+} mmshift_rotary;
+
+/* Frequencies theta^(-2j / rot_dims), and for contexts `factor` times as long as trained:
+ * LINEAR divides all by factor; BASE takes theta * factor^(rot_dims / (rot_dims - 2)); PARTS
+ * keeps those of at least high_turns turns within original_length, divides those of at most
+ * low_turns, and goes linearly by turns between (its amplitude is 0.1 ln(factor) + 1, else
+ * 1). scaling NULL = NONE; factor >= 1. inv_freq: host [rot_dims / 2]; amplitude nullable. */
+enum { MMSHIFT_ROPE_SCALE_NONE = 0, MMSHIFT_ROPE_SCALE_LINEAR = 1, MMSHIFT_ROPE_SCALE_BASE = 2,
+       MMSHIFT_ROPE_SCALE_PARTS = 3 };
+typedef struct {
+  int32_t kind;
+  double factor, original_length, low_turns, high_turns;
+} mmshift_rope_scaling;
+mmshift_status mmshift_rope_frequencies(int32_t rot_dims, double theta,
+                                        const mmshift_rope_scaling* scaling, double* inv_freq,
+                                        float* amplitude);
+
+/* Q [L][T, Hq, d] and K [L][T, Hkv, d] (either nullable, with its output) rotated; all layers
+ * at the same positions. Tokens row_stride elements apart (0 = dense), layers layer_stride
+ * (0 = T * row_stride). An output is its input (in place, with its strides) or a dense [L][T, heads, d]
+ * buffer that does not overlap it. T = cu_seqlens[batch], requests may be empty, T * Hq at most 2^30;
+ * window and budgets are not read. */
+mmshift_status mmshift_rope(const mmshift_shape* s, const mmshift_rotary* r, const void* Q,
+                            int64_t q_row_stride, int64_t q_layer_stride, const void* K,
+                            int64_t k_row_stride, int64_t k_layer_stride, void* out_Q, void* out_K,
+                            mmshift_stream_t stream);
+
+/* ---- Attention over whole prompts ----
+ *
+ * For token i of request b and query head hq, h = hq / r, over the keys of its request:
+ *   z_t = scale * q . k_t,  lse = ln sum_t e^(z_t),  out = sum_t e^(z_t - lse) v_t
+ * over t <= i if causal, all t < T_b if not: what the prefill of one layer (n_layers = 1)
+ * needs before mmshift_select takes its K, V and last queries. Masked keys, NaN and infinite
+ * logits, roundings and `scale` as in mmshift_cache_attention; requests may be empty, T * Hq is
+ * at most 2^30, window and budgets are not read. Q [T, Hq, d], K and V [T, Hkv, d], tokens
+ * q_row_stride and kv_row_stride elements apart (0 = dense); K and V start at multiples of
+ * 16 bytes, kv_row_stride is a multiple of 16 bytes. out [T, Hq, d] dense; lse (nullable)
+ * [T, Hq] float32. Workspace: mmshift_prompt_workspace_size() bytes, 256-byte aligned, status
+ * word zero at first; what it holds besides that need not outlive the call. */
+mmshift_status mmshift_prompt_workspace_size(const mmshift_shape* s, size_t* bytes);
+mmshift_status mmshift_prompt_attention(const mmshift_shape* s, const void* Q, int64_t q_row_stride,
+                                        const void* K, const void* V, int64_t kv_row_stride,
+                                        int32_t causal, float softmax_scale, void* out, float* lse,
+                                        void* workspace, size_t workspace_bytes,
+                                        mmshift_stream_t stream);
 
 /* Allocation-free variant of mmshift_scores_topk.
  *

@@ -3,7 +3,8 @@
 The computation lives in libmmshift.so (CUDA kernels behind the C ABI of
 include/mmshift.h); ``_lib`` is its ctypes binding with the same entry-point
 names, ``selector.KVSelector`` and ``cache.PagedKVCache`` (the kept rows in pages, and
-attention over them) torch-facing conveniences, ``synth`` the seeded synthetic workloads. Importing the package does not load the library; the first
+attention over them), ``prompt.Rotary`` and ``prompt.PromptAttention`` (what comes before
+a selection) torch-facing conveniences, ``synth`` the seeded synthetic workloads. Importing the package does not load the library; the first
 call does, and fails loudly if the library cannot be built or loaded.
 """
 from . import synth  # noqa: F401
@@ -18,4 +19,8 @@ from ._lib import (MMShiftError, Params, Shape, Debug, Cache, check, default_par
                    mmshift_coverage_workspace_size, mmshift_coverage,
                    mmshift_select_head_budgets, mmshift_topk_head_budgets,
                    make_cache, mmshift_cache_workspace_size, mmshift_cache_fill,
-                   mmshift_cache_append, mmshift_cache_read, mmshift_cache_attention)
+                   mmshift_cache_append, mmshift_cache_read, mmshift_cache_attention,
+                   mmshift_cache_shared_workspace_size, mmshift_cache_attention_shared,
+                   mmshift_cache_pages_workspace_size, mmshift_cache_reserve, mmshift_cache_fork,
+                   mmshift_cache_free, mmshift_cache_compact, Rotary, make_rotary, rope_frequencies,
+                   mmshift_rope, mmshift_prompt_workspace_size, mmshift_prompt_attention)

@@ -27,6 +27,9 @@ MMSHIFT_I8 = 2
 MMSHIFT_SCORE_VOTE = 0
 MMSHIFT_SCORE_MASS = 1
 MMSHIFT_MAX_BATCH = 64
+MMSHIFT_ROPE_HALF = 0
+MMSHIFT_ROPE_INTERLEAVED = 1
+ROPE_SCALINGS = ("none", "linear", "base", "parts")   # MMSHIFT_ROPE_SCALE_*, in their order
 
 EXPORTED = [
     "mmshift_default_params", "mmshift_output_rows", "mmshift_workspace_size",
@@ -41,6 +44,11 @@ EXPORTED = [
     "mmshift_select_head_budgets", "mmshift_topk_head_budgets",
     "mmshift_cache_workspace_size", "mmshift_cache_fill", "mmshift_cache_append",
     "mmshift_cache_read", "mmshift_cache_attention",
+    "mmshift_cache_shared_workspace_size", "mmshift_cache_attention_shared",
+    "mmshift_cache_pages_workspace_size", "mmshift_cache_reserve", "mmshift_cache_fork",
+    "mmshift_cache_free", "mmshift_cache_compact",
+    "mmshift_rope_frequencies", "mmshift_rope",
+    "mmshift_prompt_workspace_size", "mmshift_prompt_attention",
 ]
 MMSHIFT_NOALLOC_SCRATCH_BYTES = 8 << 20
 
@@ -85,6 +93,21 @@ class Cache(ctypes.Structure):
         ("max_pages", ctypes.c_int32), ("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p),
         ("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p),
         ("page_table", ctypes.c_void_p), ("lens", ctypes.c_void_p),
+    ]
+
+
+class Rotary(ctypes.Structure):
+    _fields_ = [
+        ("layout", ctypes.c_int32), ("rot_dims", ctypes.c_int32), ("inverse", ctypes.c_int32),
+        ("n_axes", ctypes.c_int32), ("sections", ctypes.c_int32 * 3), ("amplitude", ctypes.c_float),
+        ("inv_freq", ctypes.POINTER(ctypes.c_double)), ("positions", ctypes.c_void_p),
+    ]
+
+
+class RopeScaling(ctypes.Structure):
+    _fields_ = [
+        ("kind", ctypes.c_int32), ("factor", ctypes.c_double), ("original_length", ctypes.c_double),
+        ("low_turns", ctypes.c_double), ("high_turns", ctypes.c_double),
     ]
 
 
@@ -166,6 +189,31 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.mmshift_cache_attention.argtypes = [_SP, _CP, _VP, ctypes.c_int64, ctypes.c_int32, ctypes.c_float,
                                             _VP, _VP, _VP, ctypes.c_size_t, _VP]
     lib.mmshift_cache_attention.restype = st
+    ip, sz, i32, i64 = ctypes.POINTER(ctypes.c_int32), ctypes.c_size_t, ctypes.c_int32, ctypes.c_int64
+    lib.mmshift_cache_shared_workspace_size.argtypes = [_SP, _CP, i32, ip, ctypes.POINTER(sz)]
+    lib.mmshift_cache_shared_workspace_size.restype = st
+    lib.mmshift_cache_attention_shared.argtypes = [_SP, _CP, i32, ip, _VP, i64, i32, ctypes.c_float, _VP, _VP,
+                                                   _VP, sz, _VP]
+    lib.mmshift_cache_attention_shared.restype = st
+    lib.mmshift_cache_pages_workspace_size.argtypes = [_SP, _CP, ctypes.POINTER(sz)]
+    lib.mmshift_cache_pages_workspace_size.restype = st
+    lib.mmshift_cache_reserve.argtypes = [_SP, _CP, _VP, _VP, sz, _VP]
+    lib.mmshift_cache_reserve.restype = st
+    lib.mmshift_cache_fork.argtypes = [_SP, _CP, _VP, i32, ip, ip, _VP, sz, _VP]
+    lib.mmshift_cache_fork.restype = st
+    lib.mmshift_cache_free.argtypes = [_SP, _CP, _VP, i32, ip, _VP, sz, _VP]
+    lib.mmshift_cache_free.restype = st
+    lib.mmshift_cache_compact.argtypes = [_SP, _CP, _VP, _VP, _VP, _VP, sz, _VP]
+    lib.mmshift_cache_compact.restype = st
+    lib.mmshift_rope_frequencies.argtypes = [i32, ctypes.c_double, ctypes.POINTER(RopeScaling),
+                                             ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_float)]
+    lib.mmshift_rope_frequencies.restype = st
+    lib.mmshift_rope.argtypes = [_SP, ctypes.POINTER(Rotary), _VP, i64, i64, _VP, i64, i64, _VP, _VP, _VP]
+    lib.mmshift_rope.restype = st
+    lib.mmshift_prompt_workspace_size.argtypes = [_SP, ctypes.POINTER(sz)]
+    lib.mmshift_prompt_workspace_size.restype = st
+    lib.mmshift_prompt_attention.argtypes = [_SP, _VP, i64, _VP, _VP, i64, i32, ctypes.c_float, _VP, _VP, _VP, sz, _VP]
+    lib.mmshift_prompt_attention.restype = st
     lib.mmshift_scores_topk_noalloc.argtypes = [_SP, _PP, _VP, _VP, _VP, _VP, _VP]
     lib.mmshift_scores_topk_noalloc.restype = st
     lib.mmshift_poll_status.argtypes = [_VP, _VP]
@@ -442,6 +490,114 @@ def mmshift_cache_attention(shape, cache, Q, row_stride, causal, softmax_scale, 
                             workspace_bytes, stream=None) -> int:
     return load_library().mmshift_cache_attention(
         ctypes.byref(shape), ctypes.byref(cache), _ptr(Q), int(row_stride), int(causal),
+        float(softmax_scale), _ptr(out), _ptr(lse), _ptr(workspace), workspace_bytes, _ptr(stream))
+
+
+def _ints(values) -> ctypes.Array:
+    values = [int(x) for x in values]
+    return (ctypes.c_int32 * max(len(values), 1))(*values)
+
+
+def mmshift_cache_shared_workspace_size(shape: Shape, cache: Cache, cu_groups: Sequence[int]) -> int:
+    n = ctypes.c_size_t()
+    check(load_library().mmshift_cache_shared_workspace_size(
+        ctypes.byref(shape), ctypes.byref(cache), len(cu_groups) - 1, _ints(cu_groups), ctypes.byref(n)),
+        "mmshift_cache_shared_workspace_size")
+    return n.value
+
+
+def mmshift_cache_attention_shared(shape, cache, cu_groups, Q, row_stride, causal, softmax_scale, out, lse,
+                                   workspace, workspace_bytes, stream=None) -> int:
+    """cu_groups: prefix offsets of the groups over the requests."""
+    return load_library().mmshift_cache_attention_shared(
+        ctypes.byref(shape), ctypes.byref(cache), len(cu_groups) - 1, _ints(cu_groups), _ptr(Q), int(row_stride),
+        int(causal), float(softmax_scale), _ptr(out), _ptr(lse), _ptr(workspace), workspace_bytes, _ptr(stream))
+
+
+def mmshift_cache_pages_workspace_size(shape: Shape, cache: Cache) -> int:
+    n = ctypes.c_size_t()
+    check(load_library().mmshift_cache_pages_workspace_size(ctypes.byref(shape), ctypes.byref(cache),
+                                                            ctypes.byref(n)), "mmshift_cache_pages_workspace_size")
+    return n.value
+
+
+def mmshift_cache_reserve(shape, cache, refs, workspace, workspace_bytes, stream=None) -> int:
+    return load_library().mmshift_cache_reserve(ctypes.byref(shape), ctypes.byref(cache), _ptr(refs),
+                                                _ptr(workspace), workspace_bytes, _ptr(stream))
+
+
+def mmshift_cache_fork(shape, cache, refs, src, dst, workspace, workspace_bytes, stream=None) -> int:
+    """src, dst: request numbers, as many of each."""
+    if len(src) != len(dst):
+        raise ValueError(f"{len(src)} sources for {len(dst)} copies")
+    return load_library().mmshift_cache_fork(ctypes.byref(shape), ctypes.byref(cache), _ptr(refs), len(dst),
+                                             _ints(src), _ints(dst), _ptr(workspace), workspace_bytes, _ptr(stream))
+
+
+def mmshift_cache_free(shape, cache, refs, which, workspace, workspace_bytes, stream=None) -> int:
+    return load_library().mmshift_cache_free(ctypes.byref(shape), ctypes.byref(cache), _ptr(refs), len(which),
+                                             _ints(which), _ptr(workspace), workspace_bytes, _ptr(stream))
+
+
+def mmshift_cache_compact(shape, cache, refs, idx, count, workspace, workspace_bytes, stream=None) -> int:
+    return load_library().mmshift_cache_compact(ctypes.byref(shape), ctypes.byref(cache), _ptr(refs), _ptr(idx),
+                                                _ptr(count), _ptr(workspace), workspace_bytes, _ptr(stream))
+
+
+def rope_frequencies(rot_dims: int, theta: float, scaling: str = "none", factor: float = 1.0,
+                     original_length: float = 0.0, low_turns: float = 1.0, high_turns: float = 32.0):
+    """Radians a position of each pair [rot_dims / 2], and the amplitude that goes with them
+    (mmshift_rope_frequencies; ``scaling``: one of ROPE_SCALINGS)."""
+    if scaling not in ROPE_SCALINGS:
+        raise ValueError(f"scaling must be one of {ROPE_SCALINGS}")
+    kind = RopeScaling(ROPE_SCALINGS.index(scaling), factor, original_length, low_turns, high_turns)
+    freq, amplitude = (ctypes.c_double * max(rot_dims // 2, 1))(), ctypes.c_float()
+    check(load_library().mmshift_rope_frequencies(rot_dims, theta, ctypes.byref(kind), freq, ctypes.byref(amplitude)),
+          "mmshift_rope_frequencies")
+    return list(freq), amplitude.value
+
+
+def make_rotary(inv_freq: Sequence[float], positions, layout: str = "half", sections: Optional[Sequence[int]] = None,
+                amplitude: float = 1.0, inverse: bool = False) -> Rotary:
+    """Rotation by positions [T] or [n_axes, T] (int32, on the device), with the pairs of
+    ``inv_freq``; ``sections``: consecutive pairs of each axis."""
+    import torch
+
+    layouts = {"half": MMSHIFT_ROPE_HALF, "interleaved": MMSHIFT_ROPE_INTERLEAVED}
+    if layout not in layouts:
+        raise ValueError(f"layout must be one of {tuple(layouts)}")
+    if positions is not None and (positions.dtype != torch.int32 or not positions.is_contiguous()
+                                  or positions.dim() not in (1, 2)):
+        raise ValueError("positions must be a contiguous int32 tensor [T] or [n_axes, T]")
+    axes = 1 if positions is None or positions.dim() == 1 else positions.shape[0]
+    sections = list(sections) if sections is not None else [len(inv_freq)]
+    if len(sections) != axes or not 1 <= axes <= 3:
+        raise ValueError(f"{len(sections)} sections for {axes} axes of positions")
+    freq = (ctypes.c_double * max(len(inv_freq), 1))(*inv_freq)
+    r = Rotary(layout=layouts[layout], rot_dims=2 * len(inv_freq), inverse=int(inverse), n_axes=axes,
+               sections=(ctypes.c_int32 * 3)(*sections), amplitude=amplitude, inv_freq=freq, positions=_ptr(positions))
+    r._keep = (freq, positions)
+    return r
+
+
+def mmshift_rope(shape, rotary, Q, q_row_stride, q_layer_stride, K, k_row_stride, k_layer_stride, out_Q, out_K,
+                 stream=None) -> int:
+    return load_library().mmshift_rope(
+        ctypes.byref(shape), ctypes.byref(rotary), _ptr(Q), int(q_row_stride), int(q_layer_stride), _ptr(K),
+        int(k_row_stride), int(k_layer_stride), _ptr(out_Q), _ptr(out_K), _ptr(stream))
+
+
+def mmshift_prompt_workspace_size(shape: Shape) -> int:
+    n = ctypes.c_size_t()
+    check(load_library().mmshift_prompt_workspace_size(ctypes.byref(shape), ctypes.byref(n)),
+          "mmshift_prompt_workspace_size")
+    return n.value
+
+
+def mmshift_prompt_attention(shape, Q, q_row_stride, K, V, kv_row_stride, causal, softmax_scale, out, lse,
+                             workspace, workspace_bytes, stream=None) -> int:
+    return load_library().mmshift_prompt_attention(
+        ctypes.byref(shape), _ptr(Q), int(q_row_stride), _ptr(K), _ptr(V), int(kv_row_stride), int(causal),
         float(softmax_scale), _ptr(out), _ptr(lse), _ptr(workspace), workspace_bytes, _ptr(stream))
 
 

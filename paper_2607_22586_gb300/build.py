@@ -21,7 +21,7 @@ LIB = os.path.join(BUILD, "libmmshift.so")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 SOURCES = ["api.cu", "proxy.cu", "score_simt.cu", "score_umma.cu", "select.cu", "stats.cu",
            "hidden.cu", "coverage.cu", "noalloc.cu", "cache.cu", "attend.cu", "attend_token.cu", "attend_umma.cu",
-           "attend_simt.cu"]
+           "attend_simt.cu", "pages.cu", "shared.cu", "rope.cu", "prompt.cu", "prompt_umma.cu"]
 
 
 def _nvcc() -> str:

@@ -10,6 +10,17 @@ every call. PyTorch only provides device memory and streams here.
         cache.append(k, v, new)
         for layer in range(28):
             out = cache.attend(q[layer], new, layer)
+
+With ``pages`` the sequences take their pages from a pool as they grow, share them and give
+them back: eight answers to one prompt are
+
+    cache = PagedKVCache(28, 4, 128, torch.bfloat16, batch=8, rows=4096, n_layers=28, pages=20000)
+    ...                                      # the prompt's rows into request 0
+    cache.fork([0] * 7, range(1, 8))
+    ...                                      # advance, append
+    out = cache.attend(q, [1] * 8, layer, groups=[8])
+    cache.compact(idx, rows)                 # keeps some rows of each
+    cache.free([3])
 """
 from __future__ import annotations
 
@@ -29,11 +40,12 @@ class PagedKVCache:
     """Sequences of ``rows`` rows at most (an int, or one for each layer, request
     and KV head: [L, B, Hkv]), each with its pages from the start. Rows appended to a full
     sequence are left out, and poll() reports it (``capacity``: rows that every sequence
-    holds). Calls run on the current stream; a cache is used on one stream at a time."""
+    holds). With ``pages``, a pool of so many pages: sequences have none at first, advance() and
+    fill() take them, poll() reports when none was free. Calls run on the current stream; a cache is used on one stream at a time."""
 
     def __init__(self, n_q_heads: int, n_kv_heads: int, head_dim: int, dtype: torch.dtype, batch: int,
                  rows: Union[int, Sequence, torch.Tensor], n_layers: int = 1, page_size: int = 64,
-                 cache_dtype: Optional[torch.dtype] = None, device="cuda"):
+                 cache_dtype: Optional[torch.dtype] = None, device="cuda", pages: Optional[int] = None):
         cache_dtype = dtype if cache_dtype is None else cache_dtype
         if dtype not in _DT or cache_dtype not in (dtype, torch.int8):
             raise ValueError(f"unsupported dtypes {dtype} with a cache of {cache_dtype}")
@@ -46,15 +58,21 @@ class PagedKVCache:
         need = torch.as_tensor(rows, dtype=torch.int64).cpu().expand(n_layers, batch, n_kv_heads)
         if int(need.min()) < 1:
             raise ValueError("every sequence needs room for a row")
-        pages = (need + page_size - 1) // page_size
-        ends = pages.flatten().cumsum(0).view(pages.shape)
-        total, most = int(ends.flatten()[-1]), int(pages.max())
+        if pages is not None and (pages < 1 or bool((need != need.flatten()[0]).any())):
+            raise ValueError("a pool has at least a page, and its sequences as many rows at most")
+        have = (need + page_size - 1) // page_size
+        ends = have.flatten().cumsum(0).view(have.shape)
+        total, most = int(ends.flatten()[-1]) if pages is None else pages, int(have.max())
         # a sequence's pages follow one another; entries behind them are no pages
-        entry = torch.arange(most).expand(*pages.shape, most)
-        table = torch.where(entry < pages[..., None], entry + (ends - pages)[..., None], -1)
+        entry = torch.arange(most).expand(*have.shape, most)
+        table = torch.where(entry < have[..., None], entry + (ends - have)[..., None], -1)
+        if pages is not None:
+            table = torch.full_like(table, -1)
         self.page_table = table.to(torch.int32).to(self.device)
-        self.capacity = (pages * page_size).amin().item()
-        self.lens = torch.zeros(pages.shape, dtype=torch.int32, device=self.device)
+        self.capacity = (have * page_size).amin().item()
+        self.lens = torch.zeros(have.shape, dtype=torch.int32, device=self.device)
+        # how many sequences hold each page of a pool
+        self.refs = None if pages is None else torch.zeros(pages, dtype=torch.int32, device=self.device)
         make = lambda *s, dt: torch.zeros(s, dtype=dt, device=self.device)  # noqa: E731
         self.k_pages, self.v_pages = (make(total, page_size, head_dim, dt=cache_dtype) for _ in range(2))
         self.k_scales = self.v_scales = None
@@ -62,12 +80,16 @@ class PagedKVCache:
             self.k_scales, self.v_scales = (make(total, page_size, dt=torch.float32) for _ in range(2))
         self._all = self._struct(self.page_table, self.lens)
         self._layers = [self._struct(self.page_table[i], self.lens[i]) for i in range(n_layers)]
-        self._calls, self._counts, self._captured = {}, {}, []
+        self._calls, self._counts, self._captured, self._groups = {}, {}, [], {}
         # The largest call's: the plans' tiles are full from 256 rows of a KV head on, those
         # of few rows from 17 to 32.
         r = n_q_heads // max(n_kv_heads, 1) or 1
         self._ws_bytes = sum(self._shape([n] * batch, 1)[1] for n in (256, max(32 // r, 1)))
+        if pages is not None:                          # the calls on pages of full sequences
+            full, _, _ = self._shape([min(self.capacity, (1 << 30) // (n_q_heads * batch))] * batch, n_layers)
+            self._ws_bytes = max(self._ws_bytes, L.mmshift_cache_pages_workspace_size(full, self._all))
         self._workspace = make(self._ws_bytes, dt=torch.uint8)
+        self._shared = None                            # workspace of attention in groups
 
     def _struct(self, table, lens):
         return L.make_cache(self.k_pages, self.v_pages, table, lens, self.k_scales, self.v_scales)
@@ -123,6 +145,14 @@ class PagedKVCache:
                 raise ValueError("idx [L, R, Hkv] and counts [L, B, Hkv] must be contiguous int32 tensors")
         if idx is None:
             idx, counts = selector.out_idx, selector.kept_count if counts is None else counts
+        if self.refs is not None:                      # pages for the rows
+            rows = [min(c, b - a) for c, a, b in zip(selector.budgets, selector.shape.cu_seqlens[:self.batch],
+                                                     selector.shape.cu_seqlens[1:self.batch + 1])]
+            most = self._row_counts(rows)
+            self.free(range(self.batch))
+            self.lens.copy_(most.expand(self.lens.shape) if counts is None
+                            else torch.minimum(counts.clamp(min=0), most))
+            self._reserve(rows)
         with self._on_device():
             L.check(L.mmshift_cache_fill(selector.shape, self._all, K, V, idx, counts, self._workspace, self._ws_bytes,
                                          torch.cuda.current_stream()), "mmshift_cache_fill")
@@ -133,9 +163,13 @@ class PagedKVCache:
         if len(new) != self.batch:
             raise ValueError(f"{len(new)} row counts for {self.batch} requests")
         key = tuple(int(n) for n in new)
-        if len(set(key)) == 1:
-            self.lens.add_(key[0])
-            return
+        self.lens.add_(key[0] if len(set(key)) == 1 else self._row_counts(key))
+        if self.refs is not None:
+            self._reserve([max(n, 0) for n in key])
+
+    def _row_counts(self, rows: Sequence[int]) -> torch.Tensor:
+        """[1, B, 1] int32 on the device."""
+        key = tuple(int(n) for n in rows)
         if key not in self._counts:
             if len(self._counts) >= _KEPT:
                 self._counts.clear()
@@ -147,7 +181,56 @@ class PagedKVCache:
                     self._captured.append(counts)          # read by every replay
                 else:                                      # may be dropped while another stream than its own reads it
                     counts.record_stream(torch.cuda.current_stream())
-        self.lens.add_(counts)
+        return counts
+
+    def _pool(self) -> torch.Tensor:
+        if self.refs is None:
+            raise ValueError("the cache has no pool of pages (``pages``)")
+        return self.refs
+
+    def _requests(self, which: Sequence[int]) -> list:
+        which = [int(b) for b in which]
+        if any(not 0 <= b < self.batch for b in which):
+            raise ValueError(f"requests are numbered from 0 to {self.batch - 1}")
+        return which
+
+    def _reserve(self, new: Sequence[int]) -> None:
+        """Pages of their own for the last ``new[b]`` rows of each sequence of request b."""
+        shape, total = self._call(new, self.n_layers)
+        if total:
+            with self._on_device():
+                L.check(L.mmshift_cache_reserve(shape, self._all, self._pool(), self._workspace, self._ws_bytes,
+                                                torch.cuda.current_stream()), "mmshift_cache_reserve")
+
+    def fork(self, src: Sequence[int], dst: Sequence[int]) -> None:
+        """Request dst[i] becomes a copy of request src[i] that shares its pages, for every i;
+        what it held before is given back."""
+        src, dst = self._requests(src), self._requests(dst)
+        shape, _ = self._call([0] * self.batch, self.n_layers)
+        with self._on_device():
+            L.check(L.mmshift_cache_fork(shape, self._all, self._pool(), src, dst, self._workspace, self._ws_bytes,
+                                         torch.cuda.current_stream()), "mmshift_cache_fork")
+
+    def free(self, requests: Sequence[int]) -> None:
+        """The requests give their pages back and have no rows."""
+        which = self._requests(requests)
+        shape, _ = self._call([0] * self.batch, self.n_layers)
+        with self._on_device():
+            L.check(L.mmshift_cache_free(shape, self._all, self._pool(), which, self._workspace, self._ws_bytes,
+                                         torch.cuda.current_stream()), "mmshift_cache_free")
+
+    def compact(self, idx: torch.Tensor, rows: Sequence[int], counts: Optional[torch.Tensor] = None) -> None:
+        """Keeps the rows ``idx`` [L, T, Hkv] int32 of the sequences, ascending, ``rows[b]`` of
+        request b (of each head the first ``counts`` [L, B, Hkv] where given); requests
+        without rows stay as they are. Pages behind the rows are given back."""
+        shape, total = self._call(rows, self.n_layers)
+        for t, like in ((idx, (self.n_layers, total, self.n_kv_heads)), (counts, tuple(self.lens.shape))):
+            if t is not None and (t.dtype != torch.int32 or t.device != self.device or not t.is_contiguous()
+                                  or tuple(t.shape) != like):
+                raise ValueError("idx [L, T, Hkv] and counts [L, B, Hkv] must be contiguous int32 tensors")
+        with self._on_device():
+            L.check(L.mmshift_cache_compact(shape, self._all, self._pool(), idx, counts, self._workspace,
+                                            self._ws_bytes, torch.cuda.current_stream()), "mmshift_cache_compact")
 
     def append(self, K: torch.Tensor, V: torch.Tensor, new: Sequence[int], layer: Optional[int] = None) -> None:
         """The new tokens' rows (counted by advance() before): K, V [L, T, Hkv, d], or
@@ -166,9 +249,12 @@ class PagedKVCache:
                                            self._workspace, self._ws_bytes, torch.cuda.current_stream()), "mmshift_cache_append")
 
     def attend(self, q: torch.Tensor, new: Sequence[int], layer: int = 0, causal: bool = True,
-               softmax_scale: float = 0.0, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None):
+               softmax_scale: float = 0.0, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+               groups: Optional[Sequence[int]] = None):
         """Attention of the new tokens' queries q [T, Hq, d] over a layer's sequences:
-        [T, Hq, d]. ``lse`` [T, Hq] float32 receives the log-sum-exp where given."""
+        [T, Hq, d]. ``lse`` [T, Hq] float32 receives the log-sum-exp where given. ``groups``:
+        numbers of requests, in order, that share pages; what they share is read once. (To be
+        captured, such a call of as many tokens has to have been made once before.)"""
         shape, total = self._call(new, 1)
         stride = self._check(total, self.n_q_heads, q)
         if q.dim() != 3:
@@ -181,9 +267,40 @@ class PagedKVCache:
             if lse is not None and (lse.dtype != torch.float32 or lse.device != self.device or not lse.is_contiguous()
                                     or lse.shape != q.shape[:2]):
                 raise ValueError("lse must be a contiguous float32 tensor [T, Hq]")
+            if groups is not None:
+                cu, ws, n = self._shared_call(shape, layer, tuple(new), tuple(groups))
+                L.check(L.mmshift_cache_attention_shared(shape, self._layers[layer], cu, q, stride, causal, softmax_scale,
+                                                         out, lse, ws, n, torch.cuda.current_stream()),
+                        "mmshift_cache_attention_shared")
+                return out
             L.check(L.mmshift_cache_attention(shape, self._layers[layer], q, stride, causal, softmax_scale, out, lse,
                                               self._workspace, self._ws_bytes, torch.cuda.current_stream()), "mmshift_cache_attention")
         return out
+
+    def _shared_call(self, shape, layer: int, new: tuple, groups: tuple):
+        """Offsets of the groups, and a workspace that does for the call."""
+        key = (new, groups)
+        if key not in self._groups:
+            if sum(groups) != self.batch or min(groups) < 1:
+                raise ValueError(f"groups of {self.batch} requests in all, of at least one each")
+            cu = [0]
+            for g in groups:
+                cu.append(cu[-1] + g)
+            if len(self._groups) >= _KEPT:
+                self._groups.clear()
+            self._groups[key] = (cu, L.mmshift_cache_shared_workspace_size(shape, self._layers[layer], cu))
+        cu, n = self._groups[key]
+        capturing = torch.cuda.is_current_stream_capturing()
+        if self._shared is None or self._shared.numel() < n:
+            grown = torch.zeros(n, dtype=torch.uint8, device=self.device)
+            if self._shared is not None:               # what calls have reported
+                grown[:256].copy_(self._shared[:256])
+                if not capturing:
+                    self._shared.record_stream(torch.cuda.current_stream())
+            self._shared = grown
+        if capturing and not any(t is self._shared for t in self._captured):
+            self._captured.append(self._shared)        # used by every replay
+        return cu, self._shared, self._shared.numel()
 
     def read(self, rows: Sequence[int], first: Optional[torch.Tensor] = None):
         """The first ``rows[b]`` rows of each sequence of request b (from ``first``
@@ -203,4 +320,6 @@ class PagedKVCache:
     def poll(self) -> None:
         """Waits for the current stream and raises what a call on the cache reported."""
         with self._on_device():
-            L.check(L.mmshift_poll_status(self._workspace, torch.cuda.current_stream()), "mmshift_poll_status")
+            stream, used = torch.cuda.current_stream(), [w for w in (self._workspace, self._shared) if w is not None]
+            for status in [L.mmshift_poll_status(w, stream) for w in used]:    # all are read and cleared
+                L.check(status, "mmshift_poll_status")

@@ -248,6 +248,16 @@ AttendPlan chunk_plan(const CacheJob& J, int nsm) {
   return P;
 }
 
+// Whole prompts: all requests go to the chunks' tiles.
+AttendPlan prompt_plan(const CacheJob& J, int nsm) {
+  AttendPlan P = plan_of(J, J.bf16 ? 256 : 128, [](int) { return true; });
+  P.step_shift = J.bf16 ? 7 : 6;
+  P.workers = nsm;
+  P.extra = J.bf16 ? 2 : 0;
+  P.extra1 = J.bf16 ? 1 : 0;
+  return P;
+}
+
 // The plan's buffers from `at` on; where they end.
 char* place(AttendPlan& P, const CacheJob& J, char* at) {
   P.po = reinterpret_cast<float*>(at);
@@ -264,6 +274,21 @@ size_t attend_scratch_bytes(const CacheJob& J) {
   AttendPlan t = token_plan(J, kSMs), c = chunk_plan(J, kSMs);
   char* const base = reinterpret_cast<char*>(uintptr_t(256));
   return place(c, J, place(t, J, base)) - base;
+}
+
+size_t prompt_scratch_bytes(const CacheJob& J) {
+  AttendPlan P = prompt_plan(J, kSMs);
+  char* const base = reinterpret_cast<char*>(uintptr_t(256));
+  return place(P, J, base) - base;
+}
+
+cudaError_t launch_prompt(const AttendJob& A, void* scratch, cudaStream_t st) {
+  const int nsm = sm_count();
+  if (nsm <= 0) return cudaErrorInvalidDevice;
+  AttendPlan P = prompt_plan(A.c, nsm);
+  place(P, A.c, static_cast<char*>(scratch));
+  const cudaError_t e = A.c.bf16 ? launch_prompt_umma(A, P, st) : launch_prompt_simt(A, P, st);
+  return e == cudaSuccess ? launch_merge(A, P, st) : e;
 }
 
 cudaError_t launch_attend(const AttendJob& A, void* scratch, cudaStream_t st) {

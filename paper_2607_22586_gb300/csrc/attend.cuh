@@ -42,9 +42,10 @@ struct AttendUnit {
 };
 
 // A sequence's length, from the L2: a merge reads it before its griddepcontrol.wait, when the
-// L1 need not have what was written before the attention kernel began.
-__device__ __forceinline__ int attend_len(const CacheJob& J, size_t u) {
-  return min(max(__ldcg(J.lens + u), 0), J.cap);
+// L1 need not have what was written before the attention kernel began. A prompt's is in the call.
+__device__ __forceinline__ int attend_len(const CacheJob& J, int u) {
+  const int b = J.lens ? 0 : J.by_heads(u);
+  return J.lens ? min(max(__ldcg(J.lens + u), 0), J.cap) : J.off[b + 1] - J.off[b];
 }
 
 // lens: the sequences' lengths (AttendScan::lengths), or null to read them from the cache.
@@ -80,7 +81,7 @@ struct AttendScan {
   AttendSpan span;
   int32_t lens[LENS];
   __device__ __forceinline__ const int32_t* lengths(const CacheJob& J) const {
-    return J.B * J.Hkv <= LENS ? lens : nullptr;
+    return J.lens && J.B * J.Hkv <= LENS ? lens : nullptr;
   }
 };
 
@@ -168,6 +169,11 @@ __device__ __forceinline__ void attend_write(const AttendJob& A, int b, int h, i
   const float f = z == 0.f ? 0.f : 1.f / z;
   T* out = reinterpret_cast<T*>(A.out) + at * D + d0;
   if (z == 0.f) v = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (A.part) {
+    *reinterpret_cast<float4*>(A.part + at * D + d0) = v;
+    if (d0 == 0) A.part_ml[at] = make_float2(top, z);
+    return;
+  }
   if constexpr (sizeof(T) == 2) {
     if (A.ovec) {
       *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(v.x * f, v.y * f), pack_bf16(v.z * f, v.w * f));
@@ -193,5 +199,7 @@ __device__ __forceinline__ void attend_write(const AttendJob& A, int b, int h, i
 cudaError_t launch_attend_token(const AttendJob& A, const AttendPlan& P, bool cluster, cudaStream_t st);
 cudaError_t launch_attend_simt(const AttendJob& A, const AttendPlan& P, cudaStream_t st);
 cudaError_t launch_attend_chunk(const AttendJob& A, const AttendPlan& P, cudaStream_t st);
+cudaError_t launch_prompt_umma(const AttendJob& A, const AttendPlan& P, cudaStream_t st);
+cudaError_t launch_prompt_simt(const AttendJob& A, const AttendPlan& P, cudaStream_t st);
 
 }  // namespace mmshift

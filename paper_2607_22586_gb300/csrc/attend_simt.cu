@@ -64,7 +64,7 @@ __device__ __forceinline__ float4 codes4(uint32_t x) {
                      __uint_as_float(__byte_perm(x, 0x4b000000u, 0x7443)) - k);
 }
 
-template <int D, bool I8, int NT, int TR>
+template <int D, bool I8, int NT, int TR, bool PROMPT>
 __global__ void __launch_bounds__(NT, 1)
     attend_simt_kernel(const __grid_constant__ AttendJob A, const __grid_constant__ AttendPlan P) {
   using SM = Simt<D, NT, TR>;
@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(NT, 1)
       at = stop;
       continue;
     }
-    const int32_t* table = J.table + ((size_t)U.b * J.Hkv + U.h) * J.max_pages;
+    const int32_t* table = PROMPT ? nullptr : cache_table(J, (size_t)U.b * J.Hkv + U.h);
 
     for (int i = tid; i < SM::RT * (D / 4); i += NT) {
       const int r = i / (D / 4), d0 = i % (D / 4) * 4;
@@ -122,7 +122,10 @@ __global__ void __launch_bounds__(NT, 1)
     const int lk = tid / LPR, part = tid % LPR;
     uint4 codes[I8 ? N : 1];
     float scale = 0.f;
+    // a prompt's rows are K's and V's own, tokens apart
+    const int64_t pitch_in = PROMPT ? A.kv_stride * 4 : ROWB;
     auto row_of = [&](int t) {
+      if constexpr (PROMPT) return t < U.keys ? J.off[U.b] + t : -1;
       return t < U.keys ? page_row(table[t >> J.page_shift], J.n_pages, J.page_shift, t) : -1;
     };
     auto fetch = [&](int s, const uint8_t* pages, const float* scales, float* dst, int pitch) {
@@ -132,10 +135,10 @@ __global__ void __launch_bounds__(NT, 1)
         const int key = lk + i * STEP, t = s * BK + key;
         if (i * STEP % 16 == 0) {
           const int64_t row = s < s1 ? row_of(t) : -1;
-          from = row < 0 ? nullptr : pages + row * ROWB + part * 16;
+          from = row < 0 ? nullptr : pages + row * pitch_in + part * 16 + (PROMPT ? U.h * ROWB : 0);
         }
         const bool in = from && t < U.keys;
-        const uint8_t* src = in ? from + i * STEP % 16 * ROWB : pages;
+        const uint8_t* src = in ? from + i * STEP % 16 * pitch_in : pages;
         if constexpr (I8) codes[i] = in ? *reinterpret_cast<const uint4*>(src) : make_uint4(0, 0, 0, 0);
         else copy16(dst + key * pitch + part * 4, src, in);
       }
@@ -329,10 +332,10 @@ __global__ void __launch_bounds__(NT, 1)
   }
 }
 
-template <int D, bool I8, int NT, int TR>
+template <int D, bool I8, int NT, int TR, bool PROMPT = false>
 cudaError_t launch(const AttendJob& A, const AttendPlan& P, cudaStream_t st) {
   constexpr int bytes = (int)sizeof(typename Simt<D, NT, TR>::Smem);
-  const auto kernel = attend_simt_kernel<D, I8, NT, TR>;
+  const auto kernel = attend_simt_kernel<D, I8, NT, TR, PROMPT>;
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
   if (e != cudaSuccess) return e;
   return launch_kernel(kernel, dim3(P.workers), NT, bytes, st, true, 0, A, P);
@@ -346,6 +349,10 @@ cudaError_t launch_rows(const AttendJob& A, const AttendPlan& P, cudaStream_t st
 }
 
 }  // namespace
+
+cudaError_t launch_prompt_simt(const AttendJob& A, const AttendPlan& P, cudaStream_t st) {
+  return A.c.d == 128 ? launch<128, false, 256, 8, true>(A, P, st) : launch<64, false, 256, 8, true>(A, P, st);
+}
 
 cudaError_t launch_attend_simt(const AttendJob& A, const AttendPlan& P, cudaStream_t st) {
   if (A.c.d == 128) return A.c.i8 ? launch_rows<128, true>(A, P, st) : launch_rows<128, false>(A, P, st);

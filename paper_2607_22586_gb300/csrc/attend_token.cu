@@ -251,7 +251,7 @@ __global__ void __launch_bounds__(NT, NQ == 1 ? 3 : 2) attend_token_kernel(const
         continue;
       }
     }
-    const int32_t* table = J.table + ((size_t)U.b * J.Hkv + U.h) * J.max_pages;
+    const int32_t* table = cache_table(J, (size_t)U.b * J.Hkv + U.h);
 
     // Raises a maximum to its row's of the step; what sums relative to it have to be multiplied by.
     auto raise_max = [&](float& m, auto&& value) {

@@ -253,6 +253,8 @@ __global__ void __launch_bounds__(256) cache_read_kernel(const __grid_constant__
 
 bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
+}  // namespace
+
 mmshift_status check_cache(const mmshift_shape* s, const mmshift_cache* c) {
   if (!c) return MMSHIFT_ERR_INVALID_ARG;
   if (c->dtype != s->dtype && c->dtype != MMSHIFT_I8) return MMSHIFT_ERR_UNSUPPORTED;
@@ -289,7 +291,7 @@ mmshift_status check_rows(const mmshift_shape* s) {
   return MMSHIFT_OK;
 }
 
-void fill_job(const mmshift_shape* s, const mmshift_cache* c, void* ws, CacheJob* J) {
+static void fill_job(const mmshift_shape* s, const mmshift_cache* c, void* ws, CacheJob* J) {
   std::memset(J, 0, sizeof(*J));
   J->B = s->batch;
   J->L = s->n_layers;
@@ -323,10 +325,32 @@ mmshift_status rows_job(const mmshift_shape* s, const mmshift_cache* c, void* ws
   return MMSHIFT_OK;
 }
 
+mmshift_status attend_args(const CacheJob& J, const void* Q, int64_t row_stride, int32_t causal, float softmax_scale,
+                           const void* out, const float* lse) {
+  const size_t esz = J.bf16 ? 2 : 4;
+  if (row_stride && row_stride < (int64_t)J.Hq * J.d) return MMSHIFT_ERR_INVALID_ARG;
+  if (causal != 0 && causal != 1) return MMSHIFT_ERR_INVALID_ARG;
+  if (!(softmax_scale >= 0.f) || !std::isfinite(softmax_scale * kLog2e)) return MMSHIFT_ERR_INVALID_ARG;
+  if (J.off[J.B] && (!Q || !out)) return MMSHIFT_ERR_INVALID_ARG;
+  if (!aligned(Q, esz) || !aligned(out, esz) || !aligned(lse, 4)) return MMSHIFT_ERR_INVALID_ARG;
+  return MMSHIFT_OK;
+}
+
+void attend_set(AttendJob& A, const void* Q, int64_t row_stride, int32_t causal, float softmax_scale) {
+  CacheJob& J = A.c;
+  J.stride = row_stride ? row_stride : (int64_t)J.Hq * J.d;
+  A.q = static_cast<const uint8_t*>(Q);
+  A.causal = causal;
+  A.qvec = aligned(Q, 16) && J.stride * (J.bf16 ? 2 : 4) % 16 == 0;
+  A.alpha = (softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt((float)J.d)) * kLog2e;
+}
+
 // Rows are moved with the status word alone, attention takes `scratch` bytes more.
-mmshift_status check_workspace(const void* ws, size_t bytes, size_t scratch = 0) {
+mmshift_status check_workspace(const void* ws, size_t bytes, size_t scratch) {
   return ws && aligned(ws, 256) && bytes >= 256 + scratch ? MMSHIFT_OK : MMSHIFT_ERR_WORKSPACE;
 }
+
+namespace {
 
 // Calls of more rows (of all heads and layers) than this give each group of lanes four to
 // read, or two to write: 609,000 8-bit rows are read in 74.2 us instead of 87.3 (6.4 TB/s);
@@ -476,22 +500,12 @@ mmshift_status mmshift_cache_attention(const mmshift_shape* s, const mmshift_cac
   mmshift_status st = rows_job(s, c, workspace, &J);
   if (st != MMSHIFT_OK) return st;
   if (J.L != 1) return MMSHIFT_ERR_UNSUPPORTED;
-  const size_t esz = J.bf16 ? 2 : 4;
-  const int64_t dense = (int64_t)J.Hq * J.d;
-  if (row_stride && row_stride < dense) return MMSHIFT_ERR_INVALID_ARG;
-  if (causal != 0 && causal != 1) return MMSHIFT_ERR_INVALID_ARG;
-  if (!(softmax_scale >= 0.f) || !std::isfinite(softmax_scale * kLog2e)) return MMSHIFT_ERR_INVALID_ARG;
-  if (J.off[J.B] && (!Q || !out)) return MMSHIFT_ERR_INVALID_ARG;
-  if (!aligned(Q, esz) || !aligned(out, esz) || !aligned(lse, 4)) return MMSHIFT_ERR_INVALID_ARG;
+  if ((st = attend_args(J, Q, row_stride, causal, softmax_scale, out, lse)) != MMSHIFT_OK) return st;
   if ((st = check_workspace(workspace, workspace_bytes, attend_scratch_bytes(J))) != MMSHIFT_OK) return st;
-  J.stride = row_stride ? row_stride : dense;
-  A.q = static_cast<const uint8_t*>(Q);
+  attend_set(A, Q, row_stride, causal, softmax_scale);
   A.out = static_cast<uint8_t*>(out);
-  A.lse = lse;
-  A.causal = causal;
-  A.qvec = aligned(Q, 16) && J.stride * esz % 16 == 0;
   A.ovec = aligned(out, 16);
-  A.alpha = (softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt((float)J.d)) * kLog2e;
+  A.lse = lse;
   if (!J.off[J.B]) return MMSHIFT_OK;
   return done(launch_attend(A, static_cast<char*>(workspace) + 256, (cudaStream_t)stream));
 }

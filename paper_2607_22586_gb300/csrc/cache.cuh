@@ -19,7 +19,8 @@ struct CacheJob {
   uint8_t *kp, *vp;
   float *ks, *vs;
   const int32_t* table;
-  int32_t* lens;
+  const int64_t* at;             // where a sequence's entries begin in the table, or null: max_pages apart
+  int32_t* lens;                 // or null: whole prompts, as many rows as the call's
   int* status;
   int32_t off[MMSHIFT_MAX_BATCH + 1];
   int32_t src[MMSHIFT_MAX_BATCH + 1];   // fill: the prompts' token offsets
@@ -32,9 +33,14 @@ __device__ __forceinline__ int cache_len(const CacheJob& J, size_t u) {
   return min(max(J.lens[u], 0), J.cap);
 }
 
+// The page table of sequence u.
+__device__ __forceinline__ const int32_t* cache_table(const CacheJob& J, size_t u) {
+  return J.table + (J.at ? (size_t)J.at[u] : u * J.max_pages);
+}
+
 // The pool's row of position t < cap of sequence u, -1 if it has no page.
 __device__ __forceinline__ int64_t cache_slot(const CacheJob& J, size_t u, int t) {
-  return page_row(J.table[u * J.max_pages + (t >> J.page_shift)], J.n_pages, J.page_shift, t);
+  return page_row(cache_table(J, u)[t >> J.page_shift], J.n_pages, J.page_shift, t);
 }
 
 // Start of the cache's kernels (but the merges): everything before one in the stream is
@@ -67,12 +73,29 @@ struct AttendJob {
   const uint8_t* q;
   uint8_t* out;
   float* lse;                    // or null
+  float* part;                   // or null: rows [T * Hq][d] of sums instead of out and lse, with their
+  float2* part_ml;               // [T * Hq] maximum (base 2) and sum of weights, to be joined with others
+  int64_t kv_stride;             // prompts: elements between two tokens' rows of K and V
   int32_t causal;
   int32_t qvec, ovec;            // rows of q / out allow 16-byte accesses
   float alpha;                   // scale * log2(e)
 };
 
+// Checks that the entry points share: of a call's rows, of a cache; the job of both; and of a
+// workspace of a status word and `scratch` bytes more.
+mmshift_status check_rows(const mmshift_shape* s);
+mmshift_status check_cache(const mmshift_shape* s, const mmshift_cache* c);
+mmshift_status rows_job(const mmshift_shape* s, const mmshift_cache* c, void* ws, CacheJob* J);
+mmshift_status check_workspace(const void* ws, size_t bytes, size_t scratch = 0);
+
+// What entries of attention check of their arguments, and what they make of them.
+mmshift_status attend_args(const CacheJob& J, const void* Q, int64_t row_stride, int32_t causal, float softmax_scale,
+                           const void* out, const float* lse);
+void attend_set(AttendJob& A, const void* Q, int64_t row_stride, int32_t causal, float softmax_scale);
+
 size_t attend_scratch_bytes(const CacheJob& J);
 cudaError_t launch_attend(const AttendJob& A, void* scratch, cudaStream_t st);
+size_t prompt_scratch_bytes(const CacheJob& J);
+cudaError_t launch_prompt(const AttendJob& A, void* scratch, cudaStream_t st);
 
 }  // namespace mmshift

@@ -29,6 +29,7 @@ enum : int {
   kStatusBadIndex = 2,  // gather saw an index outside [0, T_b)
   kStatusBadBudget = 4, // a per-head budget outside [1, C_b] (clamped)
   kStatusBadPage = 8,   // a cache position without a page
+  kStatusNoPage = 16,   // no page of the pool was free
 };
 
 struct ReqInfo {

@@ -1,0 +1,162 @@
+"""Refusals of rotary positions and of attention over prompts: before anything is enqueued, so
+without a GPU. No pointer here is dereferenced but the frequencies', which lie on the host."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+import paper_2607_22586_gb300 as M
+from paper_2607_22586_gb300 import _lib as L
+from paper_2607_22586_gb300.prompt import PromptAttention, Rotary
+
+FAKE = 1 << 40
+BAD, UNSUPPORTED, WORKSPACE = L.MMSHIFT_ERR_INVALID_ARG, L.MMSHIFT_ERR_UNSUPPORTED, L.MMSHIFT_ERR_WORKSPACE
+
+
+def _shape(**kw):
+    base = dict(n_q_heads=8, n_kv_heads=2, head_dim=128, window=2, dtype=0, cu_seqlens=[0, 3, 3, 10], budgets=[4, 1, 2])
+    base.update(kw)
+    return M.make_shape(**base)
+
+
+BAD_ROWS = [
+    (dict(n_q_heads=7), BAD), (dict(n_kv_heads=0), BAD), (dict(head_dim=96), UNSUPPORTED), (dict(dtype=2), UNSUPPORTED),
+    (dict(cu_seqlens=[0, 3, 2, 10]), BAD), (dict(cu_seqlens=[1, 3, 3, 10]), BAD),
+    (dict(cu_seqlens=[0, 1, 1, 2 ** 27 + 1]), UNSUPPORTED),            # rows of all heads past 2^30
+]
+
+
+def _prompt(s=None, q=FAKE, k=FAKE, v=FAKE, out=FAKE, lse=None, ws=FAKE, n=1 << 40, qs=0, ks=0, causal=1, scale=0.0):
+    return M.mmshift_prompt_attention(s or _shape(), q, qs, k, v, ks, causal, scale, out, lse, ws, n)
+
+
+@pytest.mark.parametrize("bad,code", BAD_ROWS + [(dict(n_layers=2), UNSUPPORTED)])
+def test_bad_shapes(bad, code):
+    s = _shape(**bad)
+    assert _prompt(s) == code
+    with pytest.raises(M.MMShiftError) as e:
+        M.mmshift_prompt_workspace_size(s)
+    assert e.value.code == code
+
+
+@pytest.mark.parametrize("bad,code", [
+    (dict(q=None), BAD), (dict(k=None), BAD), (dict(v=None), BAD), (dict(out=None), BAD), (dict(ws=None), WORKSPACE),
+    (dict(q=FAKE + 1), BAD), (dict(k=FAKE + 8), BAD), (dict(v=FAKE + 2), BAD), (dict(out=FAKE + 1), BAD),
+    (dict(lse=FAKE + 2), BAD), (dict(qs=8 * 128 - 8), BAD), (dict(ks=2 * 128 - 8), BAD), (dict(ks=2 * 128 + 4), BAD),
+    (dict(ks=1 << 38), BAD), (dict(causal=2), BAD), (dict(scale=-1.0), BAD), (dict(scale=math.nan), BAD),
+    (dict(scale=2.0 ** 128 / 1.2), BAD), (dict(ws=FAKE + 128), WORKSPACE), (dict(n=255), WORKSPACE),
+    (dict(n=M.mmshift_prompt_workspace_size(_shape()) - 1), WORKSPACE),
+])
+def test_bad_prompt_arguments(bad, code):
+    assert _prompt(**bad) == code
+
+
+def test_prompts_without_rows_are_no_error():
+    s = _shape(cu_seqlens=[0, 0, 0, 0])
+    n = M.mmshift_prompt_workspace_size(s)
+    assert _prompt(s, n=n) == L.MMSHIFT_OK
+    assert _prompt(s, q=None, k=None, v=None, out=None, n=n) == L.MMSHIFT_OK
+
+
+def _rotary(n=64, positions=FAKE, **kw):
+    freq = (ctypes.c_double * n)(*kw.pop("freq", [1.0 / (j + 1) for j in range(n)]))
+    sections = (ctypes.c_int32 * 3)(*kw.pop("sections", (0, 0, 0)))
+    r = L.Rotary(inv_freq=freq, positions=positions, sections=sections, **kw)
+    r._freq = freq
+    return r
+
+
+def _rope(r, s=None, q=FAKE, k=FAKE + (1 << 36), oq=FAKE + (2 << 36), ok=FAKE + (3 << 36), qs=0, ql=0, ks=0, kl=0):
+    return M.mmshift_rope(s or _shape(), r, q, qs, ql, k, ks, kl, oq, ok)
+
+
+@pytest.mark.parametrize("bad,code", BAD_ROWS)
+def test_bad_rope_shapes(bad, code):
+    assert _rope(_rotary(), _shape(**bad)) == code
+
+
+@pytest.mark.parametrize("bad", [
+    dict(layout=2), dict(layout=-1), dict(rot_dims=1), dict(rot_dims=3), dict(rot_dims=130), dict(rot_dims=-2),
+    dict(inverse=2), dict(n_axes=4), dict(n_axes=-1), dict(n_axes=2, sections=(32, 31, 0)),
+    dict(n_axes=2, sections=(65, -1, 0)), dict(n_axes=3, sections=(2 ** 31 - 1, 2 ** 31 - 1, 66)),
+    dict(amplitude=-1.0), dict(amplitude=math.nan), dict(amplitude=math.inf), dict(positions=None), dict(positions=FAKE + 2),
+    dict(freq=[math.nan] * 64), dict(freq=[1.0] * 63 + [math.inf]),
+])
+def test_bad_rotations(bad):
+    assert _rope(_rotary(**bad)) == BAD
+
+
+@pytest.mark.parametrize("bad", [
+    dict(q=None), dict(oq=None), dict(k=None), dict(ok=None), dict(q=FAKE + 1), dict(ok=FAKE + (3 << 36) + 1),
+    dict(qs=8 * 128 - 1), dict(ks=2 * 128 - 1), dict(q=None, oq=None, k=None, ok=None),
+    dict(oq=FAKE + 2), dict(oq=FAKE - 10 * 8 * 128 * 2 + 2), dict(oq=FAKE + 10 * 8 * 128 * 2 - 2),   # overlaps what is read
+    dict(s=_shape(n_layers=2), ql=10 * 8 * 128 - 1), dict(s=_shape(n_layers=2), kl=-1),
+])
+def test_bad_rope_arguments(bad):
+    assert _rope(_rotary(), **bad) == BAD
+
+
+def test_nothing_to_rotate_is_no_error():
+    s = _shape(cu_seqlens=[0, 0, 0, 0])
+    assert _rope(_rotary(positions=None), s, q=None, k=None, oq=None, ok=None) == L.MMSHIFT_OK
+    assert M.mmshift_rope(s, None_rotary(), None, 0, 0, None, 0, 0, None, None) == BAD
+
+
+def None_rotary():
+    return L.Rotary()                              # no frequencies
+
+
+@pytest.mark.parametrize("a", [
+    dict(rot_dims=0), dict(rot_dims=3), dict(rot_dims=130), dict(theta=0.0), dict(theta=-1.0), dict(theta=math.inf),
+    dict(scaling="linear", factor=0.5), dict(scaling="linear", factor=math.nan), dict(scaling="base", rot_dims=2, factor=2.0),
+    dict(scaling="parts", factor=2.0), dict(scaling="parts", factor=2.0, original_length=-1.0),
+    dict(scaling="parts", factor=2.0, original_length=100.0, low_turns=3.0, high_turns=3.0),
+])
+def test_bad_frequencies(a):
+    base = dict(rot_dims=64, theta=1e4)
+    base.update(a)
+    with pytest.raises(M.MMShiftError) as e:
+        M.rope_frequencies(**base)
+    assert e.value.code == BAD
+
+
+def test_frequencies():
+    f, a = M.rope_frequencies(64, 1e4)
+    assert a == 1.0 and max(abs(x - 1e4 ** (-j / 32)) / x for j, x in enumerate(f)) < 1e-14
+    f, a = M.rope_frequencies(64, 1e4, "parts", 4.0, 2048, 1.0, 4.0)
+    for j, x in enumerate(f):
+        y = 1e4 ** (-j / 32)
+        keep = min(max((2048 * y / (2 * math.pi) - 1) / 3, 0), 1)
+        assert abs(x - (y * keep + y / 4 * (1 - keep))) < 1e-14 * y
+    assert abs(a - (0.1 * math.log(4) + 1)) < 1e-6
+
+
+def test_classes_refuse():
+    with pytest.raises(ValueError):
+        Rotary(64, layout="both")(torch.zeros(1, 1, 64), None, torch.zeros(1, dtype=torch.int32))
+    with pytest.raises(ValueError):
+        Rotary(64, rot_dims=32, inv_freq=[1.0])
+    with pytest.raises(ValueError):
+        Rotary(64, scaling="other")
+    r = Rotary(64)
+    x, p = torch.zeros(3, 2, 64), torch.zeros(3, dtype=torch.int32)
+    for bad in (lambda: r(None, None, p), lambda: r(x, None, p), lambda: r(x[0], None, p)):   # no rows of a GPU
+        with pytest.raises(ValueError):
+            bad()
+    with pytest.raises(ValueError):
+        M.make_rotary([1.0], p.long())
+    with pytest.raises(ValueError):
+        M.make_rotary([1.0], p, sections=[1, 0])
+    with pytest.raises(ValueError):
+        M.make_rotary([1.0] * 4, p.view(3, 1), sections=[2, 2])
+    with pytest.raises(ValueError):
+        PromptAttention(4, 2, 64, torch.float16, [0, 3], device="cpu")
+    with pytest.raises(M.MMShiftError):
+        PromptAttention(4, 3, 64, torch.bfloat16, [0, 3], device="cpu")
+    at = PromptAttention(4, 2, 64, torch.bfloat16, [0, 3], device="cpu")
+    rows = lambda h, dt=torch.bfloat16: torch.zeros(3, h, 64, dtype=dt)  # noqa: E731
+    for q, k, v in ((rows(4), rows(4), rows(2)), (rows(4)[:2], rows(2), rows(2)), (rows(4, torch.float32), rows(2), rows(2)),
+                    (rows(4), rows(2), rows(4)[:, ::2]), (rows(4), rows(4)[:, :2], rows(2))):
+        with pytest.raises(ValueError):
+            at(q, k, v)
