@@ -149,7 +149,7 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
   __shared__ uint32_t tbase;
   __shared__ int abort_flag, odd_flag;
   __shared__ AttendScan<NT, 1> scan;
-  __shared__ RunList runs;
+  __shared__ RunList<16> runs;
   volatile int* abort_ = &abort_flag;
   const CacheJob& J = A.c;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;

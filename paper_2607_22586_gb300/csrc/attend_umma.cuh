@@ -105,11 +105,11 @@ struct Run {
 
 // A role's walk over the CTA's runs. A warp works the first ones out for all roles, a
 // lane a unit; a role itself those behind them (units of few keys).
-constexpr int RUNS = 16;
 struct Walk {
   int runs, k, unit;     // runs so far, those of the list; behind it, the next unit and the costs before it
   int64_t before;
 };
+template <int RUNS>
 struct RunList {
   Run run[RUNS];
   Walk rest;
@@ -126,8 +126,9 @@ __device__ __forceinline__ Run run_of(const AttendSpan& sp, const AttendUnit& U,
 }
 
 // By a whole warp: the first runs of the CTA.
+template <int RUNS>
 __device__ __forceinline__ void list_runs(const AttendJob& A, const AttendPlan& P, const AttendSpan& sp, int lane,
-                                          RunList* list) {
+                                          RunList<RUNS>* list) {
   const int u = sp.unit + lane;
   const bool in = sp.begin < sp.end && lane < RUNS && u < P.uoff[A.c.B];
   AttendUnit U;
@@ -150,8 +151,9 @@ __device__ __forceinline__ void list_runs(const AttendJob& A, const AttendPlan& 
   }
 }
 
+template <int RUNS>
 __device__ __forceinline__ bool next_run(const AttendJob& A, const AttendPlan& P, const AttendSpan& sp,
-                                         const RunList& list, Walk& w, Run& R) {
+                                         const RunList<RUNS>& list, Walk& w, Run& R) {
   bool found = w.k < list.n;
   if (found) {
     R = list.run[w.k++];

@@ -67,7 +67,7 @@ mmshift_status mmshift_prompt_attention(const mmshift_shape* s, const void* Q, i
   J.kp = static_cast<uint8_t*>(const_cast<void*>(K));
   J.vp = static_cast<uint8_t*>(const_cast<void*>(V));
   A.out = static_cast<uint8_t*>(out);
-  A.ovec = aligned(out, 16);
+  A.ovec = aligned(out, 32) ? 2 : aligned(out, 16);   // 2: 32 bytes at once
   A.lse = lse;
   const cudaError_t e = launch_prompt(A, static_cast<char*>(workspace) + 256, (cudaStream_t)stream);
   return e == cudaSuccess ? MMSHIFT_OK : noalloc_cuda_fail(e);
