@@ -32,33 +32,6 @@ constexpr int PRODUCER = 8, ISSUER = 9, LOADER = 10, FINISHER = 12;   // first w
 // Registers a thread of the softmax warpgroups and of the others: in all as many as at the launch.
 constexpr int SOFTMAX_REGS = 152, OTHER_REGS = 104;
 
-template <int D>
-struct PromptSmem {
-  static constexpr int NT = 512;
-  static_assert(256 * (SOFTMAX_REGS + OTHER_REGS) <= 512 * 128, "more registers than the launch has");
-  static constexpr int HALVES = D / 64;
-  static constexpr int HALF = BK * 128;              // 64 columns of 128 rows
-  static constexpr int TILE = HALVES * HALF;         // a block of Q, a tile of K or V
-  static constexpr int QS = 3;                       // blocks of Q
-  static constexpr int STAGES = D == 64 ? 8 : 4;
-  // Before the tiles: barriers and what roles tell one another. All of the CTA's shared memory is
-  // asked for, and none declared besides, so the tiles' alignment costs nothing.
-  struct Head {
-    uint64_t full[STAGES], empty[STAGES], q_full[QS], q_empty[QS];
-    uint64_t s_ready[2], p_ready[2], o_ready[2], o_free[2], l_ready[2], v_ask, v_clean, drain;
-    union {
-      AttendScan<NT, 1> scan;          // before the roles begin
-      float2 ml[2][BQ];                // a block's rows: maximum (base 2) and sum of weights
-    };
-    RunList<8> runs;
-    uint32_t tbase;
-    int abort_flag, odd_flag;
-  };
-  static constexpr int BYTES = 227 * 1024;
-  static_assert((QS + STAGES) * TILE + 3 * 1024 <= BYTES && sizeof(Head) <= 3 * 1024, "shared memory");
-  static constexpr uint32_t O_COL = 256, O_STRIDE = D;
-};
-
 // Start: everything before in the stream is done, and the next kernel may take its place.
 __device__ __forceinline__ void prompt_start() {
   asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -70,39 +43,79 @@ __device__ __forceinline__ void copy_async16(uint32_t dst, const void* src, bool
 }
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
+// A run, as the roles need it: key tiles [s0, s1) of a unit. The producer works it out once for all.
+struct PromptRun {
+  int64_t slot;          // its first row's place for partial sums, -1 if the run has all of the unit's keys
+  int tok0, h;           // the request's first token; KV head
+  int n, row0, rows;     // the request's tokens; the tile's first row, its rows
+  int s0, s1;
+  int end[2];            // tiles [s0, end) are the block's: rows in front may see fewer keys
+  int least;             // keys that every row sees
+  int blocks, use;       // bit b: block b has rows; its Q is use + (blocks == 3 ? b : 0)
+};
+__device__ __forceinline__ bool has(const PromptRun& r, int b) { return r.blocks >> b & 1; }
+__device__ __forceinline__ int first_row(const PromptRun& r, int b) { return r.blocks == 3 ? b * BQ : 0; }
+__device__ __forceinline__ int q_use(const PromptRun& r, int b) { return r.use + (r.blocks == 3 ? b : 0); }
+// Keys of the prompt's token tok.
+__device__ __forceinline__ int keys_at(const AttendJob& A, const PromptRun& r, int tok) { return A.causal ? tok + 1 : r.n; }
+
+template <int D>
+struct PromptSmem {
+  static constexpr int NT = 512;
+  static_assert(256 * (SOFTMAX_REGS + OTHER_REGS) <= 512 * 128, "more registers than the launch has");
+  static constexpr int HALVES = D / 64;
+  static constexpr int HALF = BK * 128;              // 64 columns of 128 rows
+  static constexpr int TILE = HALVES * HALF;         // a block of Q, a tile of K or V
+  static constexpr int QS = 3;                       // blocks of Q
+  static constexpr int RUNS = 4;                     // of the ring of runs
+  static constexpr int READERS = 15;                 // warps that read it: all but the producer
+  static constexpr int STAGES = D == 64 ? 8 : 4;
+  // Before the tiles: barriers and what roles tell one another. All of the CTA's shared memory is
+  // asked for, and none declared besides, so the tiles' alignment costs nothing.
+  struct Head {
+    uint64_t full[STAGES], empty[STAGES], q_full[QS], q_empty[QS];
+    uint64_t s_ready[2], p_ready[2], o_ready[2], o_free[2], l_ready[2], v_ask, v_clean, drain;
+    uint64_t run_full[RUNS], run_empty[RUNS];
+    PromptRun run[RUNS];
+    union {
+      AttendScan<NT, 1> scan;          // before the roles begin
+      float2 ml[2][BQ];                // a block's rows: maximum (base 2) and sum of weights
+    };
+    uint32_t tbase;
+    int abort_flag, odd_flag;
+  };
+  static constexpr int BYTES = 227 * 1024;
+  static_assert((QS + STAGES) * TILE + 3 * 1024 <= BYTES && sizeof(Head) <= 3 * 1024, "shared memory");
+  static constexpr uint32_t O_COL = 256, O_STRIDE = D;
+};
+
 // The part of a row's sums that comes from values that are not finite, of columns
 // [d0, d0 + 32): added with the row's weights, key by key. Rare, so slow.
 template <int D>
-__device__ __forceinline__ void add_not_finite(const AttendJob& A, const Run& R, int row, int lim, float m, int d0,
-                                                   float* o) {
+__device__ __forceinline__ void add_not_finite(const AttendJob& A, const PromptRun& r, int tok, int j, float m, int d0,
+                                               float* o) {
   const CacheJob& J = A.c;
-  const int tok = J.by_r(row), j = row - tok * J.r;
-  const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(A.q) +
-                           (size_t)(J.off[R.U.b] + tok) * J.stride + (size_t)(R.U.h * J.r + j) * D;
-  const int first = keys_of(A.causal, R.U.len, R.U.n, J.by_r(R.U.row0));
-  for (int t = max(R.s0 * BK, first / BK * BK); t < min(R.s1 * BK, lim); ++t) {
-    const size_t at = (size_t)(J.off[R.U.b] + t) * A.kv_stride + (size_t)R.U.h * D;
+  const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(A.q) + (size_t)(r.tok0 + tok) * J.stride +
+                           (size_t)(r.h * J.r + j) * D;
+#pragma unroll 1
+  for (int t = max(r.s0, r.least / BK) * BK; t < min(r.s1 * BK, keys_at(A, r, tok)); ++t) {
+    const size_t at = (size_t)(r.tok0 + t) * A.kv_stride + (size_t)r.h * D;
     const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(J.vp) + at + d0;
     bool any = false;
+#pragma unroll 1
     for (int i = 0; i < 32; ++i) any |= !isfinite(to_f32(v[i]));
     if (!any) continue;
     const __nv_bfloat16* k = reinterpret_cast<const __nv_bfloat16*>(J.kp) + at;
     float s = 0.f;
+#pragma unroll 1
     for (int i = 0; i < D; ++i) s = fmaf(to_f32(q[i]), to_f32(k[i]), s);
     const float p = fast_exp2(fmaf(s, A.alpha, -m));
+#pragma unroll
     for (int i = 0; i < 32; ++i) {
       const float x = to_f32(v[i]);
       if (!isfinite(x)) o[i] += p * x;
     }
   }
-}
-
-// Key tiles [s0, end) of a run that block b works on: rows in front may see fewer keys than the
-// tile's last one. One at least, so that the block has sums.
-__device__ __forceinline__ int block_end(const AttendJob& A, const Run& R, int b) {
-  const int last = min(R.U.rows, R.first_row(b) + BQ) - 1;
-  const int keys = keys_of(A.causal, R.U.len, R.U.n, A.c.by_r(R.U.row0 + last));
-  return max(min(R.s1, (keys + BK - 1) / BK), R.s0 + 1);
 }
 
 __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS)); }
@@ -129,12 +142,6 @@ __device__ __forceinline__ bool wait_all(uint64_t* bar, uint32_t parity, volatil
 // A value that is the same in all lanes, where the compiler knows that it is.
 __device__ __forceinline__ int uniform(int x) { return (int)__reduce_max_sync(0xffffffffu, (unsigned)x); }
 
-// What the issuer has to know of a run.
-struct IssueRun {
-  int s0, s1, end0, end1, masked;      // masked: the first tile whose V is cleaned
-  int blocks, use;                     // bit b: block b has rows; its Q is use + (blocks == 3 ? b : 0)
-};
-
 // 32 bytes of a row at once where the address allows.
 __device__ __forceinline__ void store32(uint8_t* p, const uint32_t* w) {
   asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]),
@@ -156,7 +163,6 @@ __global__ void __launch_bounds__(PromptSmem<D>::NT, 1) attend_prompt_kernel(con
   uint64_t *const full = hd.full, *const empty = hd.empty, *const q_full = hd.q_full, *const q_empty = hd.q_empty;
   uint64_t *const s_ready = hd.s_ready, *const p_ready = hd.p_ready, *const o_ready = hd.o_ready;
   uint64_t *const o_free = hd.o_free, *const l_ready = hd.l_ready;
-  auto& runs = hd.runs;
   if (sm + (SM::QS + SM::STAGES) * SM::TILE > smraw + SM::BYTES) {   // the base is not where it always is
     if (threadIdx.x == 0) set_status(A.c.status, kStatusTimeout);
     return;
@@ -184,6 +190,10 @@ __global__ void __launch_bounds__(PromptSmem<D>::NT, 1) attend_prompt_kernel(con
       mbar_init(&o_free[i], 4);
       mbar_init(&l_ready[i], 4);
     }
+    for (int s = 0; s < SM::RUNS; ++s) {
+      mbar_init(&hd.run_full[s], 1);
+      mbar_init(&hd.run_empty[s], SM::READERS);
+    }
     mbar_init(&hd.v_ask, 1);
     mbar_init(&hd.v_clean, 4);
     mbar_init(&hd.drain, 1);
@@ -201,23 +211,71 @@ __global__ void __launch_bounds__(PromptSmem<D>::NT, 1) attend_prompt_kernel(con
   const uint32_t tmem = hd.tbase;
   prompt_start();
   const AttendSpan sp = attend_span(A, P, &hd.scan);
-  if (warp == 0) list_runs(A, P, sp, lane, &runs);
-  __syncthreads();
-  Walk walk = {0, 0, 0, 0};
-  Run R;
+  __syncthreads();                     // the scan's place is ml's from here on
+  // A warp's walk over the runs. A run without blocks ends it.
+  int at = 0;
+  uint32_t at_phase = 0;
+  auto next = [&](PromptRun& r) {
+    if (!wait_all(&hd.run_full[at], at_phase, abort_)) return false;
+    r = hd.run[at];
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&hd.run_empty[at]);
+    if (++at == SM::RUNS) { at = 0; at_phase ^= 1u; }
+    return r.blocks != 0;
+  };
   // Blocks of Q are used in the order of the runs, a run's first block first: use n lies in
   // place n % QS.
   if (warp == PRODUCER) {
     fewer_registers();
     if (lane == 0) {
-      int stage = 0;
-      uint32_t phase = 0;
+      int stage = 0, unit = sp.unit, out = 0, use = 0, singles = 0;
+      uint32_t phase = 0, out_phase = 0;
+      int64_t before = sp.before;
       ArmedStages armed;
       bool ok = true;
-      while (ok && next_run(A, P, sp, runs, walk, R)) {
-        const int row0 = J.off[R.U.b], col0 = R.U.h * D;
-        for (int s = R.s0; ok && s < R.s1; ++s) {
-#pragma unroll
+      // The CTA's next run, into the ring; false where the ring's readers have given up.
+      auto publish = [&](PromptRun& r) {
+        r.blocks = 0;
+        while (before < sp.end) {
+          const AttendUnit U = attend_unit(A, P, nullptr, unit);
+          const int64_t first = before;
+          int s0, s1;
+          attend_pieces(U, sp.begin, sp.end, first, s0, s1);
+          before += U.cost;
+          ++unit;
+          if (s0 >= s1) continue;
+          r.tok0 = J.off[U.b];
+          r.h = U.h;
+          r.n = U.n;
+          r.row0 = U.row0;
+          r.rows = U.rows;
+          r.s0 = s0;
+          r.s1 = s1;
+          r.slot = s0 == 0 && s1 == U.pieces ? -1 : (int64_t)attend_slot(blockIdx.x, sp.begin, first) * P.rows;
+          r.least = keys_of(A.causal, U.len, U.n, J.by_r(U.row0));
+          r.blocks = U.rows > BQ ? 3 : 1 << (singles++ & 1);   // one block's rows: each in turn
+          r.use = use;
+          use += r.blocks == 3 ? 2 : 1;
+          // at least a tile, so that the block has sums
+          const int keys = keys_of(A.causal, U.len, U.n, J.by_r(U.row0 + min(U.rows, BQ) - 1));
+          const int end = max(min(s1, (keys + BK - 1) / BK), s0 + 1);
+          r.end[0] = r.blocks == 3 ? end : has(r, 0) ? s1 : s0;
+          r.end[1] = has(r, 1) ? s1 : s0;
+          break;
+        }
+        if (!wait_one(&hd.run_empty[out], out_phase ^ 1u, abort_)) return false;
+        hd.run[out] = r;
+        mbar_arrive(&hd.run_full[out]);
+        if (++out == SM::RUNS) { out = 0; out_phase ^= 1u; }
+        return true;
+      };
+      PromptRun r, n;
+      ok = publish(r);
+      while (ok && r.blocks) {
+        ok = publish(n);                               // a run ahead, so that Q can be loaded
+        const int row0 = r.tok0, col0 = r.h * D;
+        for (int s = r.s0; ok && s < r.s1; ++s) {
+#pragma unroll 1
           for (int kv = 0; kv < 2; ++kv) {
             if (!wait_one(&empty[stage], phase ^ 1u, abort_)) { ok = false; break; }
             mbar_expect_tx(&full[stage], SM::TILE);
@@ -229,141 +287,128 @@ __global__ void __launch_bounds__(PromptSmem<D>::NT, 1) attend_prompt_kernel(con
             if (++stage == SM::STAGES) { stage = 0; phase ^= 1u; }
           }
         }
+        r = n;
       }
       if (!armed.drain(full)) *abort_ = 1;
     }
     __syncwarp();
   } else if (warp == ISSUER) {
     fewer_registers();
-    {
-      const uint32_t id_s = idesc_bf16_f32(BQ, BK), id_o = idesc_bf16_f32(BQ, D) | (1u << 16);   // V: MN-major
-      const uint64_t qd = sdesc_k_sw128(smem_u32(sm)), kd = sdesc_k_sw128(smem_u32(ring));
-      const uint64_t vd = sdesc_mn_sw128(smem_u32(ring), SM::HALF);
-      int stage = 0, use = 0;
-      uint32_t phase = 0, pp = 0, of = 0, vc = 0;      // of the ring, of block i's barriers (bit i), of v_clean
-      bool ok = true, issued = false;
-      auto wait = [&](uint64_t* bar, uint32_t parity) {
-        ok = ok && wait_all(bar, parity & 1u, abort_);
-        return ok;
-      };
-      auto step = [&] {
-        if (++stage == SM::STAGES) { stage = 0; phase ^= 1u; }
-      };
-      auto next = [&](IssueRun& r) {
-        if (!__all_sync(0xffffffffu, next_run(A, P, sp, runs, walk, R))) return false;
-        r.s0 = uniform(R.s0);
-        r.s1 = uniform(R.s1);
-        r.end0 = uniform(R.has(0) ? block_end(A, R, 0) : R.s0);
-        r.end1 = uniform(R.has(1) ? block_end(A, R, 1) : R.s0);
-        r.masked = uniform(keys_of(A.causal, R.U.len, R.U.n, J.by_r(R.U.row0)) / BK);
-        r.blocks = uniform(R.two ? 3 : 1 << R.x);
-        r.use = use;
-        use += r.blocks == 3 ? 2 : 1;
-        return true;
-      };
-      auto commit = [&](uint64_t* bar) {
-        if (elect_one()) mma_commit(bar);
-        __syncwarp();
-      };
-      // S of block x, whose Q is in a place, with the K tile of the stage
-      auto issue_s = [&](int x, int place) {
-        const uint64_t k = kd + (uint64_t)(stage * (SM::TILE >> 4)), q = qd + (uint64_t)(place * (SM::TILE >> 4));
-        if (elect_one()) {
+    const uint32_t id_s = idesc_bf16_f32(BQ, BK), id_o = idesc_bf16_f32(BQ, D) | (1u << 16);   // V: MN-major
+    const uint64_t qd = sdesc_k_sw128(smem_u32(sm)), kd = sdesc_k_sw128(smem_u32(ring));
+    const uint64_t vd = sdesc_mn_sw128(smem_u32(ring), SM::HALF);
+    int stage = 0;
+    uint32_t phase = 0, pp = 0, of = 0, vc = 0;        // of the ring, of block i's barriers (bit i), of v_clean
+    bool ok = true, issued = false;
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      ok = ok && wait_all(bar, parity & 1u, abort_);
+      return ok;
+    };
+    auto step = [&] {
+      if (++stage == SM::STAGES) { stage = 0; phase ^= 1u; }
+    };
+    auto commit = [&](uint64_t* bar) {
+      if (elect_one()) mma_commit(bar);
+      __syncwarp();
+    };
+    auto next_uniform = [&](PromptRun& r) {
+      const bool any = __all_sync(0xffffffffu, next(r));
+      r.s0 = uniform(r.s0);
+      r.s1 = uniform(r.s1);
+      r.end[0] = uniform(r.end[0]);
+      r.end[1] = uniform(r.end[1]);
+      r.least = uniform(r.least);
+      r.blocks = uniform(r.blocks);
+      r.use = uniform(r.use);
+      return any;
+    };
+    // S of block x, whose Q is use q, with the K tile of the stage
+    auto issue_s = [&](int x, int q, bool first, bool last) {
+      const int place = q % SM::QS;
+      if (first && !wait(&q_full[place], (uint32_t)(q / SM::QS))) return;
+      fence_after();
+      const uint64_t k = kd + (uint64_t)(stage * (SM::TILE >> 4)), at = qd + (uint64_t)(place * (SM::TILE >> 4));
+      if (elect_one()) {
 #pragma unroll
-          for (int ks = 0; ks < D / 16; ++ks) {
-            const uint64_t o = (uint64_t)(((ks / 4) * SM::HALF + (ks % 4) * 32) >> 4);
-            mma_bf16(tmem + x * BK, q + o, k + o, id_s, ks > 0 ? 1u : 0u);
-          }
-          mma_commit(&s_ready[x]);
+        for (int ks = 0; ks < D / 16; ++ks) {
+          const uint64_t o = (uint64_t)(((ks / 4) * SM::HALF + (ks % 4) * 32) >> 4);
+          mma_bf16(tmem + x * BK, at + o, k + o, id_s, ks > 0 ? 1u : 0u);
         }
+        mma_commit(&s_ready[x]);
+        if (last) mma_commit(&q_empty[place]);
+      }
+      __syncwarp();
+      issued = true;
+    };
+    PromptRun r, n;
+    bool have = next_uniform(r);
+    if (have && wait(&full[stage], phase)) {
+#pragma unroll 1
+      for (int x = 0; ok && x < 2; ++x)
+        if (has(r, x)) issue_s(x, q_use(r, x), true, r.end[x] == r.s0 + 1);
+      commit(&empty[stage]);
+      step();
+    }
+    while (ok && have) {
+      const bool more = next_uniform(n);
+      const int masked = r.least / BK;                 // the first tile whose V is cleaned
+      for (int s = r.s0; ok && s < r.s1; ++s) {
+        // In order: P V of a tile reads P before S of the next tile (of this run or the next) takes
+        // its place. While one block's products run, the other's softmax does.
+        const int vst = stage;
+        const bool last = s + 1 == r.s1;
+        bool k_there = false, v_there = s < masked;
+        if (!wait(&full[vst], phase)) break;
+        if (!v_there && elect_one()) mbar_arrive(&hd.v_ask);
         __syncwarp();
-        issued = true;
-      };
-      // the first S of a run
-      auto first_s = [&](const IssueRun& r, int x) {
-        const int n = r.use + (r.blocks == 3 ? x : 0), place = n % SM::QS;
-        if (!wait(&q_full[place], (uint32_t)(n / SM::QS))) return;
-        fence_after();
-        issue_s(x, place);
-        if ((x ? r.end1 : r.end0) == r.s0 + 1) commit(&q_empty[place]);
-      };
-      auto issue_o = [&](int x, int st, bool add) {
-        const uint64_t v = vd + (uint64_t)(st * (SM::TILE >> 4));
-        if (elect_one()) {
-#pragma unroll
-          for (int ks = 0; ks < BK / 16; ++ks)
-            mma_p(tmem + SM::O_COL + x * SM::O_STRIDE, tmem + x * BK + ks * 8, v + (uint64_t)((ks * 2048) >> 4), id_o,
-                  add || ks > 0 ? 1u : 0u);
-        }
-        __syncwarp();
-      };
-      IssueRun r, n;
-      bool have = next(r);
-      if (have && wait(&full[stage], phase)) {
-        for (int x = 0; ok && x < 2; ++x)
-          if (r.blocks >> x & 1) first_s(r, x);
-        commit(&empty[stage]);
         step();
-      }
-      while (ok && have) {
-        const bool more = next(n);
-        const int place0 = r.use % SM::QS, place1 = (r.use + 1) % SM::QS;
-        for (int s = r.s0; ok && s < r.s1; ++s) {
-          // In order: P V of a tile reads P before S of the next tile (of this run or the next) takes
-          // its place. While one block's products run, the other's softmax does.
-          const int vst = stage;
-          const bool last = s + 1 == r.s1;
-          bool k_there = false, v_there = s < r.masked;
-          if (!wait(&full[vst], phase)) break;
-          if (!v_there) {
-            if (lane == 0) mbar_arrive(&hd.v_ask);
-          }
-          step();
+#pragma unroll 1
+        for (int x = 0; x < 2; ++x) {
+          const int end = x ? r.end[1] : r.end[0];
+          if (s < end) {
+            if (s == r.s0) {                           // the block's last O has been read
+              if (!wait(&o_free[x], (of >> x) ^ 1u)) break;
+              of ^= 1u << x;
+            }
+            if (!wait(&p_ready[x], pp >> x)) break;
+            pp ^= 1u << x;
+            if (!v_there) {
+              if (!wait(&hd.v_clean, vc)) break;
+              vc ^= 1u;
+              v_there = true;
+            }
+            fence_after();
+            const uint64_t v = vd + (uint64_t)(vst * (SM::TILE >> 4));
+            if (elect_one()) {
 #pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            const int end = x ? r.end1 : r.end0;
-            if (s < end) {
-              if (s == r.s0) {                         // the block's last O has been read
-                if (!wait(&o_free[x], (of >> x) ^ 1u)) break;
-                of ^= 1u << x;
-              }
-              if (!wait(&p_ready[x], pp >> x)) break;
-              pp ^= 1u << x;
-              if (!v_there) {
-                if (!wait(&hd.v_clean, vc)) break;
-                vc ^= 1u;
-                v_there = true;
-              }
-              fence_after();
-              issue_o(x, vst, s > r.s0);
-              if (s + 1 == end) commit(&o_ready[x]);
+              for (int ks = 0; ks < BK / 16; ++ks)
+                mma_p(tmem + SM::O_COL + x * SM::O_STRIDE, tmem + x * BK + ks * 8, v + (uint64_t)((ks * 2048) >> 4), id_o,
+                      s > r.s0 || ks > 0 ? 1u : 0u);
+              if (s + 1 == end) mma_commit(&o_ready[x]);
+              if (x || s >= r.end[1]) mma_commit(&empty[vst]);   // the run's last block has had the tile's V
             }
-            if (x == (s < r.end1 ? 1 : 0)) commit(&empty[vst]);   // the run's last block has had the tile's V
-            if (last ? more && (n.blocks >> x & 1) : s + 1 < end) {
-              if (!k_there && !wait(&full[stage], phase)) break;
-              k_there = true;
-              if (last) {
-                first_s(n, x);
-              } else {
-                const int place = x && r.blocks == 3 ? place1 : place0;
-                issue_s(x, place);
-                if (s + 2 == end) commit(&q_empty[place]);
-              }
-            }
+            __syncwarp();
           }
-          if (!ok) break;
-          if (!last || more) {
-            commit(&empty[stage]);
-            step();
+          if (last ? more && has(n, x) : s + 1 < end) {
+            if (!k_there && !wait(&full[stage], phase)) break;
+            k_there = true;
+            const int next_end = x ? n.end[1] : n.end[0];
+            issue_s(x, last ? q_use(n, x) : q_use(r, x), last, last ? next_end == n.s0 + 1 : s + 2 == end);
+            if (!ok) break;
           }
         }
-        r = n;
-        have = more;
+        if (!ok) break;
+        if (!last || more) {
+          commit(&empty[stage]);
+          step();
+        }
       }
-      if (issued) {
-        commit(&hd.drain);
-        if (!mbar_wait_drain(&hd.drain, 0)) *abort_ = 1;
-      }
+      r = n;
+      have = more;
+    }
+    if (issued) {
+      commit(&hd.drain);
+      if (!mbar_wait_drain(&hd.drain, 0)) *abort_ = 1;
     }
   } else if (warp >= FINISHER) {
     fewer_registers();
@@ -372,50 +417,47 @@ __global__ void __launch_bounds__(PromptSmem<D>::NT, 1) attend_prompt_kernel(con
     uint32_t ask = 0, oph = 0;                           // phase of v_ask; bit x: of block x's o_ready
     int stage = 1;                                       // of the next tile's V
     bool ok = true;
-    while (ok && next_run(A, P, sp, runs, walk, R)) {
-      const AttendUnit& U = R.U;
-      const int least = keys_of(A.causal, U.len, U.n, J.by_r(U.row0));   // keys that every row attends to
-      for (int s = R.s0; s < R.s1; ++s) {
-        const int vs = stage;
+    PromptRun r;
+    while (ok && next(r)) {
+      for (int s = r.s0; s < r.s1; ++s) {
+        const int vs = stage, k0 = s * BK;
         stage = (stage + 2) % SM::STAGES;
-        const int k0 = s * BK;
-        if (k0 + BK <= least) continue;
+        if (k0 + BK <= r.least) continue;
         if (!wait_all(&hd.v_ask, ask, abort_)) { ok = false; break; }
         ask ^= 1u;
         unsigned char* vt = ring + vs * SM::TILE;
         constexpr int CH = SM::HALVES * 8;               // 16-byte chunks of a row
-        const int i0 = max(least - k0, 0) * CH;
+        const int i0 = max(r.least - k0, 0) * CH, keys = keys_at(A, r, J.by_r(r.row0 + r.rows - 1));
 #pragma unroll 4
         for (int i = i0 + fw * 32 + lane; i < BK * CH; i += 128) {
           const int key = i / CH, ch = i % CH;
           uint4* p = reinterpret_cast<uint4*>(vt + (ch / 8) * SM::HALF + key * 128 + (ch % 8) * 16);
-          const uint4 w = k0 + key < U.keys ? *p : make_uint4(0, 0, 0, 0);
+          const uint4 w = k0 + key < keys ? *p : make_uint4(0, 0, 0, 0);
           const bool bad = not_finite2(w.x) || not_finite2(w.y) || not_finite2(w.z) || not_finite2(w.w);
           if (bad) *reinterpret_cast<volatile int*>(&hd.odd_flag) = 1;
-          if (bad || k0 + key >= U.keys) *p = make_uint4(finite2(w.x), finite2(w.y), finite2(w.z), finite2(w.w));
+          if (bad || k0 + key >= keys) *p = make_uint4(finite2(w.x), finite2(w.y), finite2(w.z), finite2(w.w));
         }
         fence_async();
         __syncwarp();
         if (lane == 0) mbar_arrive(&hd.v_clean);
       }
+#pragma unroll 1
       for (int x = 0; ok && x < 2; ++x) {
-        if (!R.has(x)) continue;
+        if (!has(r, x)) continue;
         const uint32_t ph = oph >> x & 1u;
         if (!wait_all(&l_ready[x], ph, abort_) || !wait_all(&o_ready[x], ph, abort_)) { ok = false; break; }
         oph ^= 1u << x;
         fence_after();
-        const int lrow = fw * 32 + lane, brow = R.first_row(x) + lrow, row = U.row0 + brow;
-        const bool live = brow < U.rows;
+        const int lrow = fw * 32 + lane, brow = first_row(r, x) + lrow, row = r.row0 + brow;
+        const bool live = brow < r.rows, whole = r.slot < 0;
         const int tok = J.by_r(row), j = row - tok * J.r;
         const float2 t = hd.ml[x][lrow];
         const float m = t.x, l = t.y;
         // set by this warp's lanes or those beside it, before they reported a tile clean whose product
         // is in O by now
         const bool fix = *reinterpret_cast<volatile int*>(&hd.odd_flag) != 0;
-        const bool whole = R.s0 == 0 && R.s1 == U.pieces;
         const float f = l == 0.f ? 0.f : 1.f / l;
-        const int64_t orow = (int64_t)(J.off[U.b] + tok) * J.Hq + U.h * J.r + j;
-        const int64_t slot = (int64_t)attend_slot(blockIdx.x, sp.begin, R.before) * P.rows + brow;
+        const int64_t orow = (int64_t)(r.tok0 + tok) * J.Hq + r.h * J.r + j, slot = r.slot + brow;
         const uint32_t ocol = tmem + lanes + SM::O_COL + x * SM::O_STRIDE;
 #pragma unroll 1
         for (int i = 0; i < D; i += 32) {
@@ -433,7 +475,7 @@ __global__ void __launch_bounds__(PromptSmem<D>::NT, 1) attend_prompt_kernel(con
             float y[32];
 #pragma unroll
             for (int c = 0; c < 32; ++c) y[c] = o[c];
-            add_not_finite<D>(A, R, row, keys_of(A.causal, U.len, U.n, tok), m == -INFINITY ? 0.f : m, i, y);
+            add_not_finite<D>(A, r, tok, j, m == -INFINITY ? 0.f : m, i, y);
 #pragma unroll
             for (int c = 0; c < 32; ++c) o[c] = y[c];
           }
@@ -467,23 +509,23 @@ __global__ void __launch_bounds__(PromptSmem<D>::NT, 1) attend_prompt_kernel(con
     // Rows [64 w, 64 w + 64) of each block, LPR lanes a row, 16 bytes a lane.
     constexpr int LPR = D / 8, PER = 32 / LPR;
     const int r0 = (warp - LOADER) * 64 + lane / LPR, ch = lane % LPR;
-    int use = 0;
     bool ok = true;
-    while (ok && next_run(A, P, sp, runs, walk, R)) {
-      const AttendUnit& U = R.U;
+    PromptRun r;
+    while (ok && next(r)) {
+#pragma unroll 1
       for (int x = 0; ok && x < 2; ++x) {
-        if (!R.has(x)) continue;
-        const int place = use % SM::QS;
+        if (!has(r, x)) continue;
+        const int use = q_use(r, x), place = use % SM::QS;
         if (!wait_all(&q_empty[place], (uint32_t)(use / SM::QS) & 1u ^ 1u, abort_)) { ok = false; break; }
         const uint32_t dst = smem_u32(sm + place * SM::TILE + (ch / 8) * SM::HALF);
 #pragma unroll 4
         for (int i = 0; i < 64; i += PER) {
-          const int r = r0 + i, brow = R.first_row(x) + r, row = U.row0 + brow;
-          const bool in = brow < U.rows;
+          const int at = r0 + i, brow = first_row(r, x) + at, row = r.row0 + brow;
+          const bool in = brow < r.rows;
           const int tok = J.by_r(row), j = row - tok * J.r;
           const uint8_t* src =
-              A.q + (in ? ((int64_t)(J.off[U.b] + tok) * J.stride + (int64_t)(U.h * J.r + j) * D) * 2 + ch * 16 : 0);
-          const uint32_t to = dst + r * 128 + ((ch % 8) ^ (r % 8)) * 16;
+              A.q + (in ? ((int64_t)(r.tok0 + tok) * J.stride + (int64_t)(r.h * J.r + j) * D) * 2 + ch * 16 : 0);
+          const uint32_t to = dst + at * 128 + ((ch % 8) ^ (at % 8)) * 16;
           if (A.qvec) {
             copy_async16(to, src, in);
           } else {
@@ -496,7 +538,6 @@ __global__ void __launch_bounds__(PromptSmem<D>::NT, 1) attend_prompt_kernel(con
         fence_async();
         __syncwarp();
         if (lane == 0) mbar_arrive(&q_full[place]);
-        ++use;
       }
     }
   } else {
@@ -507,37 +548,43 @@ __global__ void __launch_bounds__(PromptSmem<D>::NT, 1) attend_prompt_kernel(con
     const uint64_t al2 = pk2(A.alpha, A.alpha);
     uint32_t sph = 0, fph = 1;                           // phases of s_ready, and of the o_free before
     bool ok = true;
-    while (ok && next_run(A, P, sp, runs, walk, R)) {
-      if (!R.has(x)) continue;
-      const int end = block_end(A, R, x), s0 = R.s0;
-      const int brow = R.first_row(x) + lrow;
-      const int lim = brow < R.U.rows ? keys_of(A.causal, R.U.len, R.U.n, J.by_r(R.U.row0 + brow)) : 0;
+    PromptRun r;
+    while (ok && next(r)) {
+      if (!has(r, x)) continue;
+      const int s0 = r.s0, end = x ? r.end[1] : r.end[0], brow = first_row(r, x) + lrow;
+      const int lim = brow < r.rows ? keys_at(A, r, J.by_r(r.row0 + brow)) : 0;
       const int all = __reduce_min_sync(0xffffffffu, lim);   // keys that every row of the warp sees
       float m = -INFINITY, l = 0.f;
       for (int s = s0; s < end; ++s) {
         if (!wait_all(&s_ready[x], sph, abort_)) { ok = false; break; }
         sph ^= 1u;
         fence_after();
+        if (s * BK + BK > all) {                         // keys that some row of the warp does not see
+#pragma unroll 1
+          for (int i = max(all - s * BK, 0) / 32 * 32; i < BK; i += 32) {
+            float y[32];
+            uint32_t w[32];
+            ld32(scol + i, y);
+            tmem_wait_ld();
+            pin32(y);
+            const int n = lim - (s * BK + i);
+            const uint32_t seen = n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u;
+#pragma unroll
+            for (int k = 0; k < 32; ++k) w[k] = seen >> k & 1u ? __float_as_uint(y[k]) : 0xff800000u;
+            st16(scol + i, w);
+            st16(scol + i + 16, w + 16);
+          }
+          wait_st();
+        }
         // Half a row at a time; the second half is read again: 128 values and the rest do not fit
         // in the registers.
         float v[64];
-        const bool cut = s * BK + BK > all;              // keys that some row of the warp does not see
         auto half = [&](int i) {
           ld32(scol + i, v);
           ld32(scol + i + 32, v + 32);
           tmem_wait_ld();
           pin32(v);
           pin32(v + 32);
-          if (cut) {
-#pragma unroll
-            for (int j = 0; j < 64; j += 32) {
-              const int n = lim - (s * BK + i + j);
-              const uint32_t seen = n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u;
-#pragma unroll
-              for (int k = 0; k < 32; ++k)
-                if (!(seen >> k & 1u)) v[j + k] = -INFINITY;
-            }
-          }
         };
         half(64);
         float top = max_of<64>(v);
