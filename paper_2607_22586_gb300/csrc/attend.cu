@@ -248,13 +248,16 @@ AttendPlan chunk_plan(const CacheJob& J, int nsm) {
   return P;
 }
 
+// Rows of a block of a prompt's tile: whole tokens, if a token's heads fit.
+int prompt_block(const CacheJob& J) { return J.r <= 128 ? 128 / J.r * J.r : 128; }
+
 // Whole prompts: all requests go to the chunks' tiles.
 AttendPlan prompt_plan(const CacheJob& J, int nsm) {
-  AttendPlan P = plan_of(J, J.bf16 ? 256 : 128, [](int) { return true; });
+  AttendPlan P = plan_of(J, J.bf16 ? 2 * prompt_block(J) : 128, [](int) { return true; });
   P.step_shift = J.bf16 ? 7 : 6;
   P.workers = nsm;
-  P.extra = J.bf16 ? 2 : 0;
-  P.extra1 = J.bf16 ? 1 : 0;
+  P.extra = J.bf16 ? 3 : 0;
+  P.extra1 = J.bf16 ? 2 : 0;
   return P;
 }
 
@@ -282,10 +285,11 @@ size_t prompt_scratch_bytes(const CacheJob& J) {
   return place(P, J, base) - base;
 }
 
-cudaError_t launch_prompt(const AttendJob& A, void* scratch, cudaStream_t st) {
+cudaError_t launch_prompt(AttendJob& A, void* scratch, cudaStream_t st) {
   const int nsm = sm_count();
   if (nsm <= 0) return cudaErrorInvalidDevice;
   AttendPlan P = prompt_plan(A.c, nsm);
+  A.block_rows = prompt_block(A.c);
   place(P, A.c, static_cast<char*>(scratch));
   const cudaError_t e = A.c.bf16 ? launch_prompt_umma(A, P, st) : launch_prompt_simt(A, P, st);
   return e == cudaSuccess ? launch_merge(A, P, st) : e;

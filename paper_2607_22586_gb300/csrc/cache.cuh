@@ -76,6 +76,7 @@ struct AttendJob {
   float* part;                   // or null: rows [T * Hq][d] of sums instead of out and lse, with their
   float2* part_ml;               // [T * Hq] maximum (base 2) and sum of weights, to be joined with others
   int64_t kv_stride;             // prompts: elements between two tokens' rows of K and V
+  int32_t block_rows;            // prompts: rows of a block, whole tokens where a token's heads fit
   int32_t causal;
   int32_t qvec, ovec;            // rows of q / out allow 16-byte accesses
   float alpha;                   // scale * log2(e)
@@ -96,6 +97,6 @@ void attend_set(AttendJob& A, const void* Q, int64_t row_stride, int32_t causal,
 size_t attend_scratch_bytes(const CacheJob& J);
 cudaError_t launch_attend(const AttendJob& A, void* scratch, cudaStream_t st);
 size_t prompt_scratch_bytes(const CacheJob& J);
-cudaError_t launch_prompt(const AttendJob& A, void* scratch, cudaStream_t st);
+cudaError_t launch_prompt(AttendJob& A, void* scratch, cudaStream_t st);
 
 }  // namespace mmshift

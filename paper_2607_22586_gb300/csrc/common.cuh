@@ -304,6 +304,9 @@ cudaError_t launch_hidden_proxies(HiddenJob J, void* scratch, const void* W, int
 // unavailable or rejects the layout.
 bool make_tmap_bf16_3d(CUtensorMap* m, const void* base, uint64_t d0, uint64_t d1, uint64_t d2,
                        uint64_t stride1_bytes, uint64_t stride2_bytes, uint32_t box1);
+// The same with boxes of 64 x box1 x box2 elements.
+bool make_tmap_bf16_box(CUtensorMap* m, const void* base, uint64_t d0, uint64_t d1, uint64_t d2,
+                        uint64_t stride1_bytes, uint64_t stride2_bytes, uint32_t box1, uint32_t box2);
 // The same of rows of bytes (row_bytes a multiple of 16, at most 256), whole rows a box, not swizzled.
 bool make_tmap_u8_rows(CUtensorMap* m, const void* base, uint32_t row_bytes, uint64_t rows, uint32_t box_rows);
 bool tmap_encoder_available();

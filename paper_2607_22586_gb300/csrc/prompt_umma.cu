@@ -7,19 +7,24 @@
 // 1000 tokens and seven heads a KV head has 28 tiles, of 5 key tiles on average), so a
 // run's start and end are other warps' work, and the products go on from run to run:
 //   warps 0-7   softmax, a warpgroup a block;
-//   warp 8      TMA producer of K and V tiles;
-//   warp 9      MMA issuer, one thread: a block's first S of the next run follows its last P V;
-//   warps 10-11 load Q of the next blocks into a ring of three places;
-//   warps 12-15 clean V where a tile is masked, and take O out: 104 registers a thread.
-// The issuer is alone in its warp, and what it asks for is in registers: while the products read
-// shared memory at its full rate, an access there takes hundreds of cycles, and the issuer's
-// own path is what the tensor cores wait for.
+//   warp 8      TMA producer of K and V tiles, which works the runs out for all;
+//   warp 9      MMA issuer: a block's first S of the next run follows its last P V;
+//   warp 10     Q of the next blocks into a ring of three places;
+//   warp 11     cleans V where a tile is masked;
+//   warps 12-15 take O out: 104 registers a thread.
+// A block has as many whole tokens as fit in 128 rows (126 rows of seven heads each), so that one
+// TMA box of their heads fills it; rows behind them are computed and dropped.
+// The issuer's loop has conditions and bounds that the compiler knows to be the same in all lanes, or
+// descriptors would go from vector to uniform registers one by one: the tensor cores would wait for
+// instructions (32,768 tokens of 28 heads: 6.33 instead of 4.8 to 5.0 ms). What all roles need of a run
+// is in shared memory, and their code is kept short: it is fetched again and again.
 // K's and V's rows are tokens apart: a tile is one box of 128 rows. Rows behind a prompt's last
 // are the next prompt's: a zero weight times a NaN there would be a NaN, so in tiles that hold
 // keys which some row does not attend to, values that are not finite are set to zero
 // for the product and added to the rows that do attend to them at the end.
 // Every wait is bounded; a role that gives up ends the CTA as score_umma.cu says.
 #include <algorithm>
+#include <climits>
 
 #include "attend_umma.cuh"
 
@@ -28,7 +33,7 @@ namespace {
 
 using namespace umma;
 
-constexpr int PRODUCER = 8, ISSUER = 9, LOADER = 10, FINISHER = 12;   // first warps of the roles
+constexpr int PRODUCER = 8, ISSUER = 9, LOADER = 10, CLEANER = 11, FINISHER = 12;   // first warps of the roles
 // Registers a thread of the softmax warpgroups and of the others: in all as many as at the launch.
 constexpr int SOFTMAX_REGS = 152, OTHER_REGS = 104;
 
@@ -37,11 +42,6 @@ __device__ __forceinline__ void prompt_start() {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
-
-__device__ __forceinline__ void copy_async16(uint32_t dst, const void* src, bool in) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
 // A run, as the roles need it: key tiles [s0, s1) of a unit. The producer works it out once for all.
 struct PromptRun {
@@ -54,7 +54,10 @@ struct PromptRun {
   int blocks, use;       // bit b: block b has rows; its Q is use + (blocks == 3 ? b : 0)
 };
 __device__ __forceinline__ bool has(const PromptRun& r, int b) { return r.blocks >> b & 1; }
-__device__ __forceinline__ int first_row(const PromptRun& r, int b) { return r.blocks == 3 ? b * BQ : 0; }
+// The first row of block b in the tile; blocks have A.block_rows rows.
+__device__ __forceinline__ int first_row(const AttendJob& A, const PromptRun& r, int b) {
+  return r.blocks == 3 ? b * A.block_rows : 0;
+}
 __device__ __forceinline__ int q_use(const PromptRun& r, int b) { return r.use + (r.blocks == 3 ? b : 0); }
 // Keys of the prompt's token tok.
 __device__ __forceinline__ int keys_at(const AttendJob& A, const PromptRun& r, int tok) { return A.causal ? tok + 1 : r.n; }
@@ -150,7 +153,8 @@ __device__ __forceinline__ void store32(uint8_t* p, const uint32_t* w) {
 }
 
 template <int D>
-__global__ void __launch_bounds__(PromptSmem<D>::NT, 1) attend_prompt_kernel(const __grid_constant__ CUtensorMap kmap,
+__global__ void __launch_bounds__(PromptSmem<D>::NT, 1) attend_prompt_kernel(const __grid_constant__ CUtensorMap qmap,
+                                                              const __grid_constant__ CUtensorMap kmap,
                                                               const __grid_constant__ CUtensorMap vmap,
                                                               const __grid_constant__ AttendJob A,
                                                               const __grid_constant__ AttendPlan P) {
@@ -180,7 +184,7 @@ __global__ void __launch_bounds__(PromptSmem<D>::NT, 1) attend_prompt_kernel(con
       mbar_init(&empty[s], 1);
     }
     for (int s = 0; s < SM::QS; ++s) {
-      mbar_init(&q_full[s], 2);      // both loaders
+      mbar_init(&q_full[s], 1);
       mbar_init(&q_empty[s], 1);
     }
     for (int i = 0; i < 2; ++i) {
@@ -195,9 +199,10 @@ __global__ void __launch_bounds__(PromptSmem<D>::NT, 1) attend_prompt_kernel(con
       mbar_init(&hd.run_empty[s], SM::READERS);
     }
     mbar_init(&hd.v_ask, 1);
-    mbar_init(&hd.v_clean, 4);
+    mbar_init(&hd.v_clean, 1);
     mbar_init(&hd.drain, 1);
     fence_barrier_init();
+    prefetch_tmap(&qmap);
     prefetch_tmap(&kmap);
     prefetch_tmap(&vmap);
   }
@@ -253,11 +258,11 @@ __global__ void __launch_bounds__(PromptSmem<D>::NT, 1) attend_prompt_kernel(con
           r.s1 = s1;
           r.slot = s0 == 0 && s1 == U.pieces ? -1 : (int64_t)attend_slot(blockIdx.x, sp.begin, first) * P.rows;
           r.least = keys_of(A.causal, U.len, U.n, J.by_r(U.row0));
-          r.blocks = U.rows > BQ ? 3 : 1 << (singles++ & 1);   // one block's rows: each in turn
+          r.blocks = U.rows > A.block_rows ? 3 : 1 << (singles++ & 1);   // one block's rows: each in turn
           r.use = use;
           use += r.blocks == 3 ? 2 : 1;
           // at least a tile, so that the block has sums
-          const int keys = keys_of(A.causal, U.len, U.n, J.by_r(U.row0 + min(U.rows, BQ) - 1));
+          const int keys = keys_of(A.causal, U.len, U.n, J.by_r(U.row0 + min(U.rows, A.block_rows) - 1));
           const int end = max(min(s1, (keys + BK - 1) / BK), s0 + 1);
           r.end[0] = r.blocks == 3 ? end : has(r, 0) ? s1 : s0;
           r.end[1] = has(r, 1) ? s1 : s0;
@@ -414,51 +419,28 @@ __global__ void __launch_bounds__(PromptSmem<D>::NT, 1) attend_prompt_kernel(con
     fewer_registers();
     const int fw = warp - FINISHER;
     const uint32_t lanes = (uint32_t)(fw * 32) << 16;
-    uint32_t ask = 0, oph = 0;                           // phase of v_ask; bit x: of block x's o_ready
-    int stage = 1;                                       // of the next tile's V
+    uint32_t oph = 0;                                    // bit x: phase of block x's o_ready
     bool ok = true;
     PromptRun r;
     while (ok && next(r)) {
-      for (int s = r.s0; s < r.s1; ++s) {
-        const int vs = stage, k0 = s * BK;
-        stage = (stage + 2) % SM::STAGES;
-        if (k0 + BK <= r.least) continue;
-        if (!wait_all(&hd.v_ask, ask, abort_)) { ok = false; break; }
-        ask ^= 1u;
-        unsigned char* vt = ring + vs * SM::TILE;
-        constexpr int CH = SM::HALVES * 8;               // 16-byte chunks of a row
-        const int i0 = max(r.least - k0, 0) * CH, keys = keys_at(A, r, J.by_r(r.row0 + r.rows - 1));
-#pragma unroll 4
-        for (int i = i0 + fw * 32 + lane; i < BK * CH; i += 128) {
-          const int key = i / CH, ch = i % CH;
-          uint4* p = reinterpret_cast<uint4*>(vt + (ch / 8) * SM::HALF + key * 128 + (ch % 8) * 16);
-          const uint4 w = k0 + key < keys ? *p : make_uint4(0, 0, 0, 0);
-          const bool bad = not_finite2(w.x) || not_finite2(w.y) || not_finite2(w.z) || not_finite2(w.w);
-          if (bad) *reinterpret_cast<volatile int*>(&hd.odd_flag) = 1;
-          if (bad || k0 + key >= keys) *p = make_uint4(finite2(w.x), finite2(w.y), finite2(w.z), finite2(w.w));
-        }
-        fence_async();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&hd.v_clean);
-      }
 #pragma unroll 1
       for (int x = 0; ok && x < 2; ++x) {
         if (!has(r, x)) continue;
         const uint32_t ph = oph >> x & 1u;
+        const int lrow = fw * 32 + lane, brow = first_row(A, r, x) + lrow, row = r.row0 + brow;
+        const bool live = lrow < A.block_rows && brow < r.rows, whole = r.slot < 0;
+        const int tok = J.by_r(row), j = row - tok * J.r;
+        const int64_t orow = (int64_t)(r.tok0 + tok) * J.Hq + r.h * J.r + j, slot = r.slot + brow;
+        const uint32_t ocol = tmem + lanes + SM::O_COL + x * SM::O_STRIDE;
         if (!wait_all(&l_ready[x], ph, abort_) || !wait_all(&o_ready[x], ph, abort_)) { ok = false; break; }
         oph ^= 1u << x;
         fence_after();
-        const int lrow = fw * 32 + lane, brow = first_row(r, x) + lrow, row = r.row0 + brow;
-        const bool live = brow < r.rows, whole = r.slot < 0;
-        const int tok = J.by_r(row), j = row - tok * J.r;
         const float2 t = hd.ml[x][lrow];
         const float m = t.x, l = t.y;
         // set by this warp's lanes or those beside it, before they reported a tile clean whose product
         // is in O by now
         const bool fix = *reinterpret_cast<volatile int*>(&hd.odd_flag) != 0;
         const float f = l == 0.f ? 0.f : 1.f / l;
-        const int64_t orow = (int64_t)(r.tok0 + tok) * J.Hq + r.h * J.r + j, slot = r.slot + brow;
-        const uint32_t ocol = tmem + lanes + SM::O_COL + x * SM::O_STRIDE;
 #pragma unroll 1
         for (int i = 0; i < D; i += 32) {
           float o[32];
@@ -471,31 +453,25 @@ __global__ void __launch_bounds__(PromptSmem<D>::NT, 1) attend_prompt_kernel(con
             if (lane == 0) mbar_arrive(&o_free[x]);
           }
           if (!live) continue;
-          if (fix) {
-            float y[32];
-#pragma unroll
-            for (int c = 0; c < 32; ++c) y[c] = o[c];
-            add_not_finite<D>(A, r, tok, j, m == -INFINITY ? 0.f : m, i, y);
-#pragma unroll
-            for (int c = 0; c < 32; ++c) o[c] = y[c];
-          }
+          if (fix) add_not_finite<D>(A, r, tok, j, m == -INFINITY ? 0.f : m, i, o);
           if (whole) {
-            uint32_t w[16];
-#pragma unroll
-            for (int c = 0; c < 16; ++c) w[c] = l == 0.f ? 0u : pack_bf16(o[2 * c] * f, o[2 * c + 1] * f);
             uint8_t* const to = A.out + (orow * D + i) * 2;
-            if (A.ovec == 2) {
-              store32(to, w);
-              store32(to + 32, w + 8);
-            } else {
 #pragma unroll
-              for (int c = 0; c < 4; ++c)
-                store_row16(to + c * 16, make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]), A.ovec);
+            for (int c = 0; c < 32; c += 16) {
+              uint32_t w[8];
+#pragma unroll
+              for (int e = 0; e < 8; ++e) w[e] = l == 0.f ? 0u : pack_bf16(o[c + 2 * e] * f, o[c + 2 * e + 1] * f);
+              if (A.ovec == 2) {
+                store32(to + 2 * c, w);
+              } else {
+                store_row16(to + 2 * c, make_uint4(w[0], w[1], w[2], w[3]), A.ovec);
+                store_row16(to + 2 * c + 16, make_uint4(w[4], w[5], w[6], w[7]), A.ovec);
+              }
             }
           } else {
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
-              store32(reinterpret_cast<uint8_t*>(P.po + slot * D + i + 8 * c), reinterpret_cast<const uint32_t*>(o + 8 * c));
+            for (int c = 0; c < 32; c += 8)
+              store32(reinterpret_cast<uint8_t*>(P.po + slot * D + i + c), reinterpret_cast<const uint32_t*>(o + c));
           }
         }
         if (live) {
@@ -504,42 +480,100 @@ __global__ void __launch_bounds__(PromptSmem<D>::NT, 1) attend_prompt_kernel(con
         }
       }
     }
-  } else if (warp >= LOADER) {
+  } else if (warp == CLEANER) {
     fewer_registers();
-    // Rows [64 w, 64 w + 64) of each block, LPR lanes a row, 16 bytes a lane.
-    constexpr int LPR = D / 8, PER = 32 / LPR;
-    const int r0 = (warp - LOADER) * 64 + lane / LPR, ch = lane % LPR;
+    uint32_t ask = 0;                                    // phase of v_ask
+    int stage = 1;                                       // of the next tile's V
     bool ok = true;
     PromptRun r;
+    while (ok && next(r)) {
+      for (int s = r.s0; s < r.s1; ++s) {
+        const int vs = stage, k0 = s * BK;
+        stage = (stage + 2) % SM::STAGES;
+        if (k0 + BK <= r.least) continue;
+        if (!wait_all(&hd.v_ask, ask, abort_)) { ok = false; break; }
+        ask ^= 1u;
+        unsigned char* vt = ring + vs * SM::TILE;
+        // Few tiles hold such values, so all of it is looked through before any is changed. A lane
+        // has every 32nd of the tile's 16-byte chunks.
+        constexpr int CH = SM::HALVES * 8, N = BK * CH / 32;    // chunks of a row, of a lane
+        const int i0 = max(r.least - k0, 0) * CH;
+        auto chunk = [&](int e) {
+          const int i = e * 32 + lane, key = i / CH, ch = i % CH;
+          return reinterpret_cast<uint4*>(vt + (ch / 8) * SM::HALF + key * 128 + (ch % 8) * 16);
+        };
+        uint32_t worst = 0;
+#pragma unroll 1
+        for (int e0 = i0 / 32 / 8 * 8; e0 < N; e0 += 8) {
+          uint4 w[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            w[e] = make_uint4(0, 0, 0, 0);
+            if ((e0 + e) * 32 + lane >= i0) w[e] = *chunk(e0 + e);
+          }
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            constexpr uint32_t k = 0x7fff7fffu;
+            worst = __vmaxu2(worst, __vmaxu2(__vmaxu2(w[e].x & k, w[e].y & k), __vmaxu2(w[e].z & k, w[e].w & k)));
+          }
+        }
+        if (__any_sync(0xffffffffu, not_finite2(worst))) {
+          const int keys = keys_at(A, r, J.by_r(r.row0 + r.rows - 1));
+#pragma unroll 1
+          for (int e = 0; e < N; ++e) {
+            const int i = e * 32 + lane;
+            if (i < i0) continue;
+            const uint4 w = *chunk(e);
+            if (!(not_finite2(w.x) || not_finite2(w.y) || not_finite2(w.z) || not_finite2(w.w))) continue;
+            if (k0 + i / CH < keys) *reinterpret_cast<volatile int*>(&hd.odd_flag) = 1;
+            *chunk(e) = make_uint4(finite2(w.x), finite2(w.y), finite2(w.z), finite2(w.w));
+          }
+        }
+        fence_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&hd.v_clean);
+      }
+    }
+  } else if (warp == LOADER) {
+    fewer_registers();
+    bool ok = true;
+    PromptRun r;
+    ArmedStages armed;
     while (ok && next(r)) {
 #pragma unroll 1
       for (int x = 0; ok && x < 2; ++x) {
         if (!has(r, x)) continue;
-        const int use = q_use(r, x), place = use % SM::QS;
-        if (!wait_all(&q_empty[place], (uint32_t)(use / SM::QS) & 1u ^ 1u, abort_)) { ok = false; break; }
-        const uint32_t dst = smem_u32(sm + place * SM::TILE + (ch / 8) * SM::HALF);
-#pragma unroll 4
-        for (int i = 0; i < 64; i += PER) {
-          const int at = r0 + i, brow = first_row(r, x) + at, row = r.row0 + brow;
-          const bool in = brow < r.rows;
-          const int tok = J.by_r(row), j = row - tok * J.r;
-          const uint8_t* src =
-              A.q + (in ? ((int64_t)(r.tok0 + tok) * J.stride + (int64_t)(r.h * J.r + j) * D) * 2 + ch * 16 : 0);
-          const uint32_t to = dst + at * 128 + ((ch % 8) ^ (at % 8)) * 16;
-          if (A.qvec) {
-            copy_async16(to, src, in);
-          } else {
-            const uint4 w = in ? load_plain16(src, false) : make_uint4(0, 0, 0, 0);
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w)
-                         : "memory");
+        const int use = q_use(r, x), place = use % SM::QS, row0 = r.row0 + first_row(A, r, x);
+        const uint32_t phase = (uint32_t)(use / SM::QS) & 1u;
+        if (!wait_all(&q_empty[place], phase ^ 1u, abort_)) { ok = false; break; }
+        unsigned char* const to = sm + place * SM::TILE;
+        if (A.qvec && J.r <= BQ) {                       // the block begins with a token's first head
+          if (lane == 0) {
+            mbar_expect_tx(&q_full[place], A.block_rows * D * 2);
+#pragma unroll
+            for (int c = 0; c < SM::HALVES; ++c)
+              tma_load_3d(to + c * SM::HALF, &qmap, &q_full[place], c * 64, r.h * J.r, r.tok0 + J.by_r(row0));
           }
+          armed.arm(place, phase);
+        } else {                                         // rows that start anywhere, or a token's heads in several blocks
+          constexpr int LPR = D / 8;                     // lanes of a row
+#pragma unroll 1
+          for (int i = lane / LPR; i < BQ; i += 32 / LPR) {
+            const int row = row0 + i, tok = J.by_r(row), ch = lane % LPR;
+            const bool in = i < A.block_rows && row < r.row0 + r.rows;
+            const uint8_t* src =
+                A.q + (in ? ((int64_t)(r.tok0 + tok) * J.stride + (int64_t)(r.h * J.r + row - tok * J.r) * D) * 2 + ch * 16 : 0);
+            const uint4 w = in ? load_plain16(src, A.qvec) : make_uint4(0, 0, 0, 0);
+            *reinterpret_cast<uint4*>(to + (ch / 8) * SM::HALF + i * 128 + ((ch % 8) ^ (i % 8)) * 16) = w;
+          }
+          fence_async();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&q_full[place]);
         }
-        copies_wait();
-        fence_async();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&q_full[place]);
       }
     }
+    if (!armed.drain(q_full)) *abort_ = 1;
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SOFTMAX_REGS));
     const int x = warp / 4, lrow = threadIdx.x % 128;   // block, its row
@@ -551,8 +585,11 @@ __global__ void __launch_bounds__(PromptSmem<D>::NT, 1) attend_prompt_kernel(con
     PromptRun r;
     while (ok && next(r)) {
       if (!has(r, x)) continue;
-      const int s0 = r.s0, end = x ? r.end[1] : r.end[0], brow = first_row(r, x) + lrow;
-      const int lim = brow < r.rows ? keys_at(A, r, J.by_r(r.row0 + brow)) : 0;
+      const int s0 = r.s0, end = x ? r.end[1] : r.end[0], brow = first_row(A, r, x) + lrow;
+      // rows that are none see everything, so that their warps need no mask, and raise no maximum: what
+      // they hold is whatever lies behind the block's Q
+      const bool live = lrow < A.block_rows && brow < r.rows;
+      const int lim = live ? keys_at(A, r, J.by_r(r.row0 + brow)) : INT_MAX;
       const int all = __reduce_min_sync(0xffffffffu, lim);   // keys that every row of the warp sees
       float m = -INFINITY, l = 0.f;
       for (int s = s0; s < end; ++s) {
@@ -591,7 +628,7 @@ __global__ void __launch_bounds__(PromptSmem<D>::NT, 1) attend_prompt_kernel(con
         half(0);
         top = fmaxf(top, max_of<64>(v)) * A.alpha;
         // raises the maximum where some row's passes it by enough
-        if (__any_sync(0xffffffffu, top > m + kRaise)) {
+        if (__any_sync(0xffffffffu, live && top > m + kRaise)) {
           const float mn = fmaxf(m, top), f = m == -INFINITY ? 0.f : fast_exp2(m - mn);
           m = mn;
           l *= f;
@@ -654,15 +691,19 @@ template <int D>
 cudaError_t launch(const AttendJob& A, const AttendPlan& P, cudaStream_t st) {
   using SM = PromptSmem<D>;
   const CacheJob& J = A.c;
-  CUtensorMap kmap, vmap;
+  CUtensorMap qmap, kmap, vmap;
   const uint64_t rows = J.off[J.B], cols = (uint64_t)J.Hkv * D, pitch = A.kv_stride * 2;
   if (!make_tmap_bf16_3d(&kmap, J.kp, cols, rows, 1, pitch, rows * pitch, BK) ||
       !make_tmap_bf16_3d(&vmap, J.vp, cols, rows, 1, pitch, rows * pitch, BK))
     return cudaErrorInvalidValue;
+  qmap = kmap;                                           // not used where Q's rows are copied
+  if (A.qvec && J.r <= BQ &&
+      !make_tmap_bf16_box(&qmap, A.q, D, J.Hq, rows, D * 2, J.stride * 2, J.r, A.block_rows / J.r))
+    return cudaErrorInvalidValue;
   const cudaError_t e =
       cudaFuncSetAttribute(attend_prompt_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, SM::BYTES);
   if (e != cudaSuccess) return e;
-  return launch_kernel(attend_prompt_kernel<D>, dim3(P.workers), SM::NT, SM::BYTES, st, true, 0, kmap, vmap, A, P);
+  return launch_kernel(attend_prompt_kernel<D>, dim3(P.workers), SM::NT, SM::BYTES, st, true, 0, qmap, kmap, vmap, A, P);
 }
 
 }  // namespace
