@@ -13,54 +13,6 @@ namespace {
 // (178 to 285 us instead of 68 for a call behind another).
 __device__ __forceinline__ void merge_start() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
-// Which workers have a unit's parts: workers [i0, i1], the first one's slot.
-struct Parts {
-  int i0, i1, first;
-  __device__ __forceinline__ Parts(const AttendPlan& P, const Shares& sh, const AttendUnit& U, int64_t before) {
-    const int64_t a = before + U.extra;                // its pieces are at [a, a + pieces)
-    i0 = sh.of(a);
-    i1 = a + U.pieces <= sh.begin(i0 + 1) ? i0 : sh.of(a + U.pieces - 1);
-    first = attend_slot(i0, sh.begin(i0), before);
-  }
-  // A worker's first part has an even slot; only the unit's first can be a worker's last.
-  __device__ __forceinline__ size_t slot(const AttendPlan& P, int k, int r) const {
-    return (size_t)(k ? 2 * (i0 + k) : first) * P.rows + r;
-  }
-};
-
-// A warp's sum over the parts k0, k0 + STEP, ... of row r: its lane's D / 32 values.
-template <int D, int STEP>
-__device__ __forceinline__ void add_parts(const AttendPlan& P, const Parts& x, int r, int lane, int k0, float& top,
-                                          float& z, float (&o)[D / 32]) {
-  const int parts = x.i1 - x.i0 + 1;
-  top = -INFINITY;
-  for (int k = lane; k < parts; k += 32) top = fmaxf(top, P.pml[x.slot(P, k, r)].x);
-#pragma unroll
-  for (int s = 16; s; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
-  z = 0.f;
-#pragma unroll
-  for (int i = 0; i < D / 32; ++i) o[i] = 0.f;
-#pragma unroll 8
-  for (int k = k0; k < parts; k += STEP) {
-    const size_t slot = x.slot(P, k, r);
-    const float2 ml = P.pml[slot];
-    const float f = ml.x == -INFINITY ? 1.f : fast_exp2(ml.x - top);
-    z += ml.y * f;
-    const float* p = P.po + slot * D + lane * (D / 32);
-    if constexpr (D == 128) {
-      const float4 v = *reinterpret_cast<const float4*>(p);
-      o[0] += v.x * f;
-      o[1] += v.y * f;
-      o[2] += v.z * f;
-      o[3] += v.w * f;
-    } else {
-      const float2 v = *reinterpret_cast<const float2*>(p);
-      o[0] += v.x * f;
-      o[1] += v.y * f;
-    }
-  }
-}
-
 // The merge of few units of many parts each (4 units of 114): a block a row, its warps
 // on the row's parts. Zeros for units without keys. Which workers share the unit follows
 // from the lengths, which were there before the attention kernel began: worked out while
@@ -256,8 +208,8 @@ AttendPlan prompt_plan(const CacheJob& J, int nsm) {
   AttendPlan P = plan_of(J, J.bf16 ? 2 * prompt_block(J) : 128, [](int) { return true; });
   P.step_shift = J.bf16 ? 7 : 6;
   P.workers = nsm;
-  P.extra = J.bf16 ? 3 : 0;
-  P.extra1 = J.bf16 ? 2 : 0;
+  P.extra = J.bf16 ? 2 : 0;
+  P.extra1 = J.bf16 ? 1 : 0;
   return P;
 }
 
@@ -291,20 +243,31 @@ cudaError_t launch_prompt(AttendJob& A, void* scratch, cudaStream_t st) {
   AttendPlan P = prompt_plan(A.c, nsm);
   A.block_rows = prompt_block(A.c);
   place(P, A.c, static_cast<char*>(scratch));
-  const cudaError_t e = A.c.bf16 ? launch_prompt_umma(A, P, st) : launch_prompt_simt(A, P, st);
-  return e == cudaSuccess ? launch_merge(A, P, st) : e;
+  if (!A.c.bf16) {
+    const cudaError_t e = launch_prompt_simt(A, P, st);
+    return e == cudaSuccess ? launch_merge(A, P, st) : e;
+  }
+  // Whole units where the workers' last ones differ by less than the merge of shared ones takes, about
+  // as long as six key tiles: 16 ragged prompts of 28 heads, 8 units a worker, 94 us (112 with shares);
+  // images of 16 heads, 2 units a worker, 43 (56).
+  PromptOrder O = prompt_order(A.c.B, A.c.off, A.c.r, P.rows, A.c.Hkv, A.causal);
+  O.whole = prompt_whole(O, A.c.off, A.c.r, P.rows, A.c.Hkv, A.causal, P.workers, P.extra, 6);
+  const cudaError_t e = launch_prompt_umma(A, P, O, st);
+  return e == cudaSuccess && !O.whole ? launch_merge(A, P, st) : e;
 }
 
-cudaError_t launch_attend(const AttendJob& A, void* scratch, cudaStream_t st) {
+// parts: where the plans go if sums are left as they are, else null: merged.
+cudaError_t launch_attend(const AttendJob& A, void* scratch, cudaStream_t st, AttendParts* parts) {
   const CacheJob& J = A.c;
   const int nsm = sm_count();
   if (nsm <= 0) return cudaErrorInvalidDevice;
   AttendPlan t = token_plan(J, nsm), c = chunk_plan(J, nsm);
   place(c, J, place(t, J, static_cast<char*>(scratch)));
+  if (parts) *parts = AttendParts{A, t, c, few_rows(J), 0};
   cudaError_t e = cudaSuccess;
   if (c.uoff[J.B]) {
     e = J.bf16 ? launch_attend_chunk(A, c, st) : launch_attend_simt(A, c, st);
-    if (e == cudaSuccess) e = launch_merge(A, c, st);
+    if (e == cudaSuccess && !parts) e = launch_merge(A, c, st);
   }
   if (e == cudaSuccess && t.uoff[J.B]) {
     if (J.bf16) {
@@ -315,13 +278,18 @@ cudaError_t launch_attend(const AttendJob& A, void* scratch, cudaStream_t st) {
       // 8-bit rows: 2049 8.1 (8.9), 4097 (4 steps) 10.3 (10.1).
       const bool cluster = J.cap >> t.step_shift <= 32 * kClusterSteps && 8 * t.uoff[J.B] <= t.workers;
       e = launch_attend_token(A, t, cluster, st);
+      if (parts) parts->whole = cluster;
       if (cluster) return e;
     } else {
       e = launch_attend_simt(A, t, st);
     }
-    if (e == cudaSuccess) e = launch_merge(A, t, st);
+    if (e == cudaSuccess && !parts) e = launch_merge(A, t, st);
   }
   return e;
+}
+
+cudaError_t launch_attend(const AttendJob& A, void* scratch, cudaStream_t st) {
+  return launch_attend(A, scratch, st, nullptr);
 }
 
 }  // namespace mmshift

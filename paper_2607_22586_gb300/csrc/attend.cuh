@@ -12,6 +12,7 @@
 #pragma once
 
 #include "cache.cuh"
+#include "prompt_index.h"
 
 namespace mmshift {
 
@@ -196,10 +197,112 @@ __device__ __forceinline__ void attend_write(const AttendJob& A, int b, int h, i
   if (d0 == 0 && A.lse) A.lse[at] = z == 0.f ? -INFINITY : (top + log2f(z)) * 0.6931471805599453f;
 }
 
+// Which workers have a unit's parts: workers [i0, i1], the first one's slot.
+struct Parts {
+  int i0, i1, first;
+  __device__ __forceinline__ Parts(const AttendPlan& P, const Shares& sh, const AttendUnit& U, int64_t before) {
+    const int64_t a = before + U.extra;                // its pieces are at [a, a + pieces)
+    i0 = sh.of(a);
+    i1 = a + U.pieces <= sh.begin(i0 + 1) ? i0 : sh.of(a + U.pieces - 1);
+    first = attend_slot(i0, sh.begin(i0), before);
+  }
+  // A worker's first part has an even slot; only the unit's first can be a worker's last.
+  __device__ __forceinline__ size_t slot(const AttendPlan& P, int k, int r) const {
+    return (size_t)(k ? 2 * (i0 + k) : first) * P.rows + r;
+  }
+};
+
+// A warp's sum over the parts k0, k0 + STEP, ... of row r: its lane's D / 32 values.
+template <int D, int STEP>
+__device__ __forceinline__ void add_parts(const AttendPlan& P, const Parts& x, int r, int lane, int k0, float& top,
+                                          float& z, float (&o)[D / 32]) {
+  const int parts = x.i1 - x.i0 + 1;
+  top = -INFINITY;
+  for (int k = lane; k < parts; k += 32) top = fmaxf(top, P.pml[x.slot(P, k, r)].x);
+#pragma unroll
+  for (int s = 16; s; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+  z = 0.f;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) o[i] = 0.f;
+#pragma unroll 8
+  for (int k = k0; k < parts; k += STEP) {
+    const size_t slot = x.slot(P, k, r);
+    const float2 ml = P.pml[slot];
+    const float f = ml.x == -INFINITY ? 1.f : fast_exp2(ml.x - top);
+    z += ml.y * f;
+    const float* p = P.po + slot * D + lane * (D / 32);
+    if constexpr (D == 128) {
+      const float4 v = *reinterpret_cast<const float4*>(p);
+      o[0] += v.x * f;
+      o[1] += v.y * f;
+      o[2] += v.z * f;
+      o[3] += v.w * f;
+    } else {
+      const float2 v = *reinterpret_cast<const float2*>(p);
+      o[0] += v.x * f;
+      o[1] += v.y * f;
+    }
+  }
+}
+
+// Attention whose sums are not merged yet: the plans of its few-row and of its other requests.
+struct AttendParts {
+  AttendJob A;
+  AttendPlan t, c;
+  int32_t few;         // rows of a request's KV head up to which it is in t
+  int32_t whole;       // t's units are all in A.part
+};
+cudaError_t launch_attend(const AttendJob& A, void* scratch, cudaStream_t st, AttendParts* parts);
+
+// A warp's: the sum of query row rho of a request's KV head, its lane's D / 32 values.
+template <int D>
+__device__ __forceinline__ void sum_of_row(const AttendParts& S, int b, int h, int rho, int lane, float& top, float& z,
+                                           float (&o)[D / 32]) {
+  const CacheJob& J = S.A.c;
+  const bool few = (J.off[b + 1] - J.off[b]) * J.r <= S.few;
+  const AttendPlan& P = few ? S.t : S.c;
+  const int tile = rho / P.rows, row = rho - tile * P.rows, u = P.uoff[b] + h * P.tiles[b] + tile;
+  top = -INFINITY;
+  z = 0.f;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) o[i] = 0.f;
+  if (!(few && S.whole)) {
+    const AttendUnit U = attend_unit(S.A, P, nullptr, u);
+    if (!U.pieces) return;
+    // If a worker's share begins in the unit, it says what is before the unit; else one worker had
+    // all of it.
+    const Shares sh = shares_of(P.start[P.workers].before, P.workers, P.least);
+    int lo = 0, hi = sh.n;                             // the first worker whose first unit is not before u
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (P.start[mid].unit < u) lo = mid + 1; else hi = mid;
+    }
+    if (lo < sh.n && P.start[lo].unit == u) {
+      const Parts parts(P, sh, U, P.start[lo].before);
+      if (parts.i0 < parts.i1) {
+        add_parts<D, 1>(P, parts, row, lane, 0, top, z, o);
+        return;
+      }
+    }
+  }
+  const int tok = J.by_r(rho);
+  const size_t at = (size_t)(J.off[b] + tok) * J.Hq + h * J.r + rho - tok * J.r;
+  const float2 ml = S.A.part_ml[at];
+  top = ml.x;
+  z = ml.y;
+  const float* p = S.A.part + at * D + lane * (D / 32);
+#pragma unroll
+  for (int i = 0; i < D / 32; i += 2) {
+    const float2 v = *reinterpret_cast<const float2*>(p + i);
+    o[i] = v.x;
+    o[i + 1] = v.y;
+  }
+}
+
 cudaError_t launch_attend_token(const AttendJob& A, const AttendPlan& P, bool cluster, cudaStream_t st);
 cudaError_t launch_attend_simt(const AttendJob& A, const AttendPlan& P, cudaStream_t st);
 cudaError_t launch_attend_chunk(const AttendJob& A, const AttendPlan& P, cudaStream_t st);
-cudaError_t launch_prompt_umma(const AttendJob& A, const AttendPlan& P, cudaStream_t st);
+cudaError_t launch_prompt_umma(const AttendJob& A, const AttendPlan& P, const PromptOrder& O, cudaStream_t st);
 cudaError_t launch_prompt_simt(const AttendJob& A, const AttendPlan& P, cudaStream_t st);
 
 }  // namespace mmshift

@@ -274,7 +274,13 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
       }
       __syncwarp();
     };
-    while (ok && next_run(A, P, sp, runs, walk, R)) {
+    // What the loop goes by is the same in all lanes, and known to be: with descriptors that go from
+    // vector to uniform registers one by one, the tensor cores wait for instructions.
+    while (ok && __all_sync(0xffffffffu, next_run(A, P, sp, runs, walk, R))) {
+      R.s0 = uniform(R.s0);
+      R.s1 = uniform(R.s1);
+      R.x = uniform(R.x);
+      R.two = uniform(R.two) != 0;
       if (!wait(&full[stage], phase)) break;
       for (int x = 0; x < 2; ++x) {
         if (!R.has(x)) continue;

@@ -142,9 +142,6 @@ __device__ __forceinline__ bool wait_all(uint64_t* bar, uint32_t parity, volatil
   return __all_sync(0xffffffffu, wait_one(bar, parity, abort));
 }
 
-// A value that is the same in all lanes, where the compiler knows that it is.
-__device__ __forceinline__ int uniform(int x) { return (int)__reduce_max_sync(0xffffffffu, (unsigned)x); }
-
 // 32 bytes of a row at once where the address allows.
 __device__ __forceinline__ void store32(uint8_t* p, const uint32_t* w) {
   asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]),
@@ -157,7 +154,8 @@ __global__ void __launch_bounds__(PromptSmem<D>::NT, 1) attend_prompt_kernel(con
                                                               const __grid_constant__ CUtensorMap kmap,
                                                               const __grid_constant__ CUtensorMap vmap,
                                                               const __grid_constant__ AttendJob A,
-                                                              const __grid_constant__ AttendPlan P) {
+                                                              const __grid_constant__ AttendPlan P,
+                                                              const __grid_constant__ PromptOrder O) {
   using SM = PromptSmem<D>;
   extern __shared__ __align__(16) unsigned char smraw[];
   typename SM::Head& hd = *reinterpret_cast<typename SM::Head*>(smraw);
@@ -215,7 +213,8 @@ __global__ void __launch_bounds__(PromptSmem<D>::NT, 1) attend_prompt_kernel(con
   fence_after();
   const uint32_t tmem = hd.tbase;
   prompt_start();
-  const AttendSpan sp = attend_span(A, P, &hd.scan);
+  AttendSpan sp = {0, 0, 0, 0};
+  if (!O.whole) sp = attend_span(A, P, &hd.scan);
   __syncthreads();                     // the scan's place is ml's from here on
   // A warp's walk over the runs. A run without blocks ends it.
   int at = 0;
@@ -233,7 +232,7 @@ __global__ void __launch_bounds__(PromptSmem<D>::NT, 1) attend_prompt_kernel(con
   if (warp == PRODUCER) {
     fewer_registers();
     if (lane == 0) {
-      int stage = 0, unit = sp.unit, out = 0, use = 0, singles = 0;
+      int stage = 0, unit = sp.unit, out = 0, use = 0, singles = 0, round = 0;
       uint32_t phase = 0, out_phase = 0;
       int64_t before = sp.before;
       ArmedStages armed;
@@ -241,32 +240,46 @@ __global__ void __launch_bounds__(PromptSmem<D>::NT, 1) attend_prompt_kernel(con
       // The CTA's next run, into the ring; false where the ring's readers have given up.
       auto publish = [&](PromptRun& r) {
         r.blocks = 0;
-        while (before < sp.end) {
+        bool any = false;
+        if (O.whole) {
+          const int u = prompt_turn(O, gridDim.x, blockIdx.x, round++);
+          any = u >= 0;
+          if (any) {
+            const PromptUnit x = prompt_unit(O, J.Hkv, A.causal, u);
+            r.tok0 = J.off[x.b];
+            r.h = x.h;
+            r.n = J.off[x.b + 1] - r.tok0;
+            r.row0 = x.tile * P.rows;
+            r.rows = min(P.rows, r.n * J.r - r.row0);
+            r.s0 = 0;
+            r.s1 = (keys_at(A, r, J.by_r(r.row0 + r.rows - 1)) + BK - 1) / BK;
+            r.slot = -1;
+          }
+        }
+        while (!any && before < sp.end) {
           const AttendUnit U = attend_unit(A, P, nullptr, unit);
           const int64_t first = before;
-          int s0, s1;
-          attend_pieces(U, sp.begin, sp.end, first, s0, s1);
+          attend_pieces(U, sp.begin, sp.end, first, r.s0, r.s1);
           before += U.cost;
           ++unit;
-          if (s0 >= s1) continue;
+          any = r.s0 < r.s1;
           r.tok0 = J.off[U.b];
           r.h = U.h;
           r.n = U.n;
           r.row0 = U.row0;
           r.rows = U.rows;
-          r.s0 = s0;
-          r.s1 = s1;
-          r.slot = s0 == 0 && s1 == U.pieces ? -1 : (int64_t)attend_slot(blockIdx.x, sp.begin, first) * P.rows;
-          r.least = keys_of(A.causal, U.len, U.n, J.by_r(U.row0));
-          r.blocks = U.rows > A.block_rows ? 3 : 1 << (singles++ & 1);   // one block's rows: each in turn
+          r.slot = r.s0 == 0 && r.s1 == U.pieces ? -1 : (int64_t)attend_slot(blockIdx.x, sp.begin, first) * P.rows;
+        }
+        if (any) {
+          r.least = keys_at(A, r, J.by_r(r.row0));
+          r.blocks = r.rows > A.block_rows ? 3 : 1 << (singles++ & 1);   // one block's rows: each in turn
           r.use = use;
           use += r.blocks == 3 ? 2 : 1;
           // at least a tile, so that the block has sums
-          const int keys = keys_of(A.causal, U.len, U.n, J.by_r(U.row0 + min(U.rows, A.block_rows) - 1));
-          const int end = max(min(s1, (keys + BK - 1) / BK), s0 + 1);
-          r.end[0] = r.blocks == 3 ? end : has(r, 0) ? s1 : s0;
-          r.end[1] = has(r, 1) ? s1 : s0;
-          break;
+          const int keys = keys_at(A, r, J.by_r(r.row0 + min(r.rows, A.block_rows) - 1));
+          const int end = max(min(r.s1, (keys + BK - 1) / BK), r.s0 + 1);
+          r.end[0] = r.blocks == 3 ? end : has(r, 0) ? r.s1 : r.s0;
+          r.end[1] = has(r, 1) ? r.s1 : r.s0;
         }
         if (!wait_one(&hd.run_empty[out], out_phase ^ 1u, abort_)) return false;
         hd.run[out] = r;
@@ -688,7 +701,7 @@ __global__ void __launch_bounds__(PromptSmem<D>::NT, 1) attend_prompt_kernel(con
 }
 
 template <int D>
-cudaError_t launch(const AttendJob& A, const AttendPlan& P, cudaStream_t st) {
+cudaError_t launch(const AttendJob& A, const AttendPlan& P, const PromptOrder& O, cudaStream_t st) {
   using SM = PromptSmem<D>;
   const CacheJob& J = A.c;
   CUtensorMap qmap, kmap, vmap;
@@ -703,13 +716,13 @@ cudaError_t launch(const AttendJob& A, const AttendPlan& P, cudaStream_t st) {
   const cudaError_t e =
       cudaFuncSetAttribute(attend_prompt_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, SM::BYTES);
   if (e != cudaSuccess) return e;
-  return launch_kernel(attend_prompt_kernel<D>, dim3(P.workers), SM::NT, SM::BYTES, st, true, 0, qmap, kmap, vmap, A, P);
+  return launch_kernel(attend_prompt_kernel<D>, dim3(P.workers), SM::NT, SM::BYTES, st, true, 0, qmap, kmap, vmap, A, P, O);
 }
 
 }  // namespace
 
-cudaError_t launch_prompt_umma(const AttendJob& A, const AttendPlan& P, cudaStream_t st) {
-  return A.c.d == 128 ? launch<128>(A, P, st) : launch<64>(A, P, st);
+cudaError_t launch_prompt_umma(const AttendJob& A, const AttendPlan& P, const PromptOrder& O, cudaStream_t st) {
+  return A.c.d == 128 ? launch<128>(A, P, O, st) : launch<64>(A, P, O, st);
 }
 
 }  // namespace mmshift

@@ -3,9 +3,9 @@
 // A group's rows attend twice: all of them to the pages that its sequences have in common, as if
 // they were one request's, and each to the pages behind those. Both are the attention that
 // the cache has anyway (attend.cu), over other lengths and beginnings of the page table, which
-// common_pages_kernel works out on the device; both leave sums with their maxima, in
-// float32, and join_parts_kernel adds them up:
-//   m = max(m0, m1), z = z0 2^(m0 - m) + z1 2^(m1 - m), out = (o0 2^(m0 - m) + o1 2^(m1 - m)) / z.
+// common_pages_kernel works out on the device; both leave sums of weights times values with their
+// maxima, in float32, as the workers left them, and join_kernel adds a row's up:
+//   m = max m_k, z = sum z_k 2^(m_k - m), out = sum o_k 2^(m_k - m) / z.
 // What the group has in common is read once instead of once a request, and its rows fill the
 // tensor cores' tiles together.
 #include <algorithm>
@@ -13,7 +13,7 @@
 #include <cmath>
 #include <cstring>
 
-#include "cache.cuh"
+#include "attend.cuh"
 
 namespace mmshift {
 mmshift_status noalloc_cuda_fail(cudaError_t e);
@@ -27,12 +27,15 @@ struct SharedJob {
   int32_t causal, n_groups;
   int64_t* at[2];                      // of the groups' common pages, of the requests' own
   int32_t* lens[2];                    // [n_groups][Hkv], [batch][Hkv]
-  const float* part[2];
-  const float2* ml[2];
+  int32_t group[MMSHIFT_MAX_BATCH + 1];   // first requests
+};
+
+struct JoinJob {
+  AttendParts part[2];                 // of the common pages, of the requests' own
   uint8_t* out;
   float* lse;
   int32_t ovec;
-  int32_t group[MMSHIFT_MAX_BATCH + 1];   // first requests
+  int32_t group[MMSHIFT_MAX_BATCH + 1], n_groups;
 };
 
 // Start: everything before in the stream is done, and the next kernel may take its place.
@@ -44,23 +47,29 @@ __device__ __forceinline__ void shared_start() {
 // A block a group and KV head: how many pages all its sequences with rows in the call have
 // in common. Only keys that every row attends to count, and requests alone have none.
 __global__ void __launch_bounds__(kCommon) common_pages_kernel(const __grid_constant__ SharedJob S) {
-  __shared__ int32_t common;
+  __shared__ int32_t common, first_, keys, members;
   const CacheJob& J = S.c;
   shared_start();
   const int g = blockIdx.x, h = blockIdx.y, b0 = S.group[g], b1 = S.group[g + 1], tid = threadIdx.x;
-  int first = -1, keys = INT_MAX, members = 0;
-  for (int b = b0; b < b1; ++b) {
-    const int n = J.off[b + 1] - J.off[b];
-    if (!n) continue;
-    if (first < 0) first = b;
-    ++members;
-    keys = min(keys, keys_of(S.causal, cache_len(J, (size_t)b * J.Hkv + h), n, 0));
+  if (tid == 0) {
+    first_ = keys = INT_MAX;
+    members = 0;
   }
-  const int most = members > 1 ? keys >> J.page_shift : 0;
+  __syncthreads();
+  if (b0 + tid < b1) {
+    const int b = b0 + tid, n = J.off[b + 1] - J.off[b];
+    if (n) {
+      atomicMin(&first_, b);
+      atomicMin(&keys, keys_of(S.causal, cache_len(J, (size_t)b * J.Hkv + h), n, 0));
+      atomicAdd(&members, 1);
+    }
+  }
+  __syncthreads();
+  const int first = members ? first_ : b0, most = members > 1 ? keys >> J.page_shift : 0;
   if (tid == 0) common = most;
   __syncthreads();
   // places in order, 256 at a time, the requests behind the first shared out to four threads a place
-  const int32_t* const lead = J.table + ((size_t)max(first, b0) * J.Hkv + h) * J.max_pages;
+  const int32_t* const lead = J.table + ((size_t)first * J.Hkv + h) * J.max_pages;
   for (int e0 = 0; e0 < most; e0 += 256) {
     const int e = e0 + tid % 256;
     bool same = true;
@@ -78,7 +87,7 @@ __global__ void __launch_bounds__(kCommon) common_pages_kernel(const __grid_cons
   __syncthreads();
   const int pages = common;
   if (tid == 0) {
-    S.at[0][g * J.Hkv + h] = ((int64_t)max(first, b0) * J.Hkv + h) * J.max_pages;
+    S.at[0][g * J.Hkv + h] = ((int64_t)first * J.Hkv + h) * J.max_pages;
     S.lens[0][g * J.Hkv + h] = pages << J.page_shift;
   }
   for (int b = b0 + tid; b < b1; b += kCommon) {
@@ -89,36 +98,33 @@ __global__ void __launch_bounds__(kCommon) common_pages_kernel(const __grid_cons
   }
 }
 
-// A row by D / 4 lanes, four values each.
+// A warp a row.
 template <typename T, int D>
-__global__ void __launch_bounds__(256) join_parts_kernel(const __grid_constant__ SharedJob S) {
-  const CacheJob& J = S.c;
+__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ JoinJob S) {
+  const CacheJob& J = S.part[1].A.c;
   shared_start();
-  const int64_t rows = (int64_t)J.off[J.B] * J.Hq;
-  const int64_t row = (int64_t)blockIdx.x * (256 / (D / 4)) + threadIdx.x / (D / 4);
-  const int d0 = threadIdx.x % (D / 4) * 4;
-  if (row >= rows) return;
-  const float2 a = S.ml[0][row], b = S.ml[1][row];
-  const float4 x = *reinterpret_cast<const float4*>(S.part[0] + row * D + d0);
-  const float4 y = *reinterpret_cast<const float4*>(S.part[1] + row * D + d0);
-  const float top = fmaxf(a.x, b.x);
-  const float fa = a.x == -INFINITY ? 1.f : fast_exp2(a.x - top), fb = b.x == -INFINITY ? 1.f : fast_exp2(b.x - top);
-  const float z = a.y * fa + b.y * fb, f = z == 0.f ? 0.f : 1.f / z;
-  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (z != 0.f)
-    v = make_float4((x.x * fa + y.x * fb) * f, (x.y * fa + y.y * fb) * f, (x.z * fa + y.z * fb) * f,
-                    (x.w * fa + y.w * fb) * f);
-  T* const out = reinterpret_cast<T*>(S.out) + row * D + d0;
-  if (S.ovec) {
-    if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
-    else *reinterpret_cast<float4*>(out) = v;
+  const int row = blockIdx.x * 8 + threadIdx.x / 32, lane = threadIdx.x % 32;
+  if (row >= J.off[J.B] * J.Hq) return;
+  const int tok = row / J.Hq, hq = row - tok * J.Hq, h = J.by_r(hq), j = hq - h * J.r;
+  const int b = range_of(J.off, J.B, tok), g = range_of(S.group, S.n_groups, b);
+  float ta, za, oa[D / 32], tb, zb, ob[D / 32];
+  sum_of_row<D>(S.part[0], g, h, (tok - S.part[0].A.c.off[g]) * J.r + j, lane, ta, za, oa);
+  sum_of_row<D>(S.part[1], b, h, (tok - J.off[b]) * J.r + j, lane, tb, zb, ob);
+  const float top = fmaxf(ta, tb);
+  const float fa = ta == -INFINITY ? 1.f : fast_exp2(ta - top), fb = tb == -INFINITY ? 1.f : fast_exp2(tb - top);
+  const float z = za * fa + zb * fb, f = z == 0.f ? 0.f : 1.f / z;
+  T* const out = reinterpret_cast<T*>(S.out) + (size_t)row * D + lane * (D / 32);
+  float v[D / 32];
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) v[i] = z == 0.f ? 0.f : (oa[i] * fa + ob[i] * fb) * f;
+  if (S.ovec && D == 128) {
+    if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[D / 64], v[D / 32 - 1]));
+    else *reinterpret_cast<float4*>(out) = make_float4(v[0], v[1], v[D / 64], v[D / 32 - 1]);
   } else {
-    out[0] = from_f32<T>(v.x);
-    out[1] = from_f32<T>(v.y);
-    out[2] = from_f32<T>(v.z);
-    out[3] = from_f32<T>(v.w);
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) out[i] = from_f32<T>(v[i]);
   }
-  if (d0 == 0 && S.lse) S.lse[row] = z == 0.f ? -INFINITY : (top + log2f(z)) * 0.6931471805599453f;
+  if (lane == 0 && S.lse) S.lse[row] = z == 0.f ? -INFINITY : (top + log2f(z)) * 0.6931471805599453f;
 }
 
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
@@ -138,7 +144,7 @@ struct SharedParts {
   int32_t* lens[2];
   float* part[2];
   float2* ml[2];
-  char* scratch;
+  char* scratch[2];
 };
 char* place(const CacheJob& J, const CacheJob& G, char* at, SharedParts* P) {
   const size_t rows = (size_t)J.off[J.B] * J.Hq;
@@ -153,8 +159,9 @@ char* place(const CacheJob& J, const CacheJob& G, char* at, SharedParts* P) {
     P->ml[i] = reinterpret_cast<float2*>(at);
     at += align256(rows * sizeof(float2));
   }
-  P->scratch = at;
-  return at + std::max(attend_scratch_bytes(J), attend_scratch_bytes(G));
+  P->scratch[0] = at;
+  P->scratch[1] = at + attend_scratch_bytes(G);
+  return P->scratch[1] + attend_scratch_bytes(J);
 }
 
 mmshift_status shared_job(const mmshift_shape* s, const mmshift_cache* c, int32_t n_groups, const int32_t* cu_groups,
@@ -170,13 +177,12 @@ mmshift_status shared_job(const mmshift_shape* s, const mmshift_cache* c, int32_
   return MMSHIFT_OK;
 }
 
-cudaError_t launch_join(const SharedJob& S, cudaStream_t st) {
-  const int per = 256 / (S.c.d / 4);
-  const int64_t rows = (int64_t)S.c.off[S.c.B] * S.c.Hq;
-  const dim3 grid((unsigned)((rows + per - 1) / per));
-  auto go = [&](auto kernel) { return launch_kernel(kernel, grid, 256, 0, st, true, 0, S); };
-  if (S.c.bf16) return S.c.d == 128 ? go(join_parts_kernel<__nv_bfloat16, 128>) : go(join_parts_kernel<__nv_bfloat16, 64>);
-  return S.c.d == 128 ? go(join_parts_kernel<float, 128>) : go(join_parts_kernel<float, 64>);
+cudaError_t launch_join(const JoinJob& S, cudaStream_t st) {
+  const CacheJob& J = S.part[1].A.c;
+  const unsigned rows = (unsigned)J.off[J.B] * J.Hq;
+  auto go = [&](auto kernel) { return launch_kernel(kernel, dim3((rows + 7) / 8), 256, 0, st, true, 0, S); };
+  if (J.bf16) return J.d == 128 ? go(join_kernel<__nv_bfloat16, 128>) : go(join_kernel<__nv_bfloat16, 64>);
+  return J.d == 128 ? go(join_kernel<float, 128>) : go(join_kernel<float, 64>);
 }
 
 }  // namespace
@@ -218,14 +224,16 @@ mmshift_status mmshift_cache_attention_shared(const mmshift_shape* s, const mmsh
   S.causal = causal;
   S.n_groups = n_groups;
   std::memcpy(S.group, cu_groups, (n_groups + 1) * sizeof(int32_t));
-  S.out = static_cast<uint8_t*>(out);
-  S.lse = lse;
-  S.ovec = aligned(out, 16);
+  JoinJob N;
+  std::memset(&N, 0, sizeof(N));
+  N.out = static_cast<uint8_t*>(out);
+  N.lse = lse;
+  N.ovec = aligned(out, 16);
+  N.n_groups = n_groups;
+  std::memcpy(N.group, S.group, sizeof(N.group));
   for (int i = 0; i < 2; ++i) {
     S.at[i] = P.at[i];
     S.lens[i] = P.lens[i];
-    S.part[i] = P.part[i];
-    S.ml[i] = P.ml[i];
     attend_set(A[i], Q, row_stride, i ? causal : 0, softmax_scale);
     A[i].part = P.part[i];
     A[i].part_ml = P.ml[i];
@@ -234,8 +242,8 @@ mmshift_status mmshift_cache_attention_shared(const mmshift_shape* s, const mmsh
   }
   const cudaStream_t cs = (cudaStream_t)stream;
   cudaError_t e = launch_kernel(common_pages_kernel, dim3(n_groups, J.Hkv), kCommon, 0, cs, true, 0, S);
-  for (int i = 0; e == cudaSuccess && i < 2; ++i) e = launch_attend(A[i], P.scratch, cs);
-  if (e == cudaSuccess) e = launch_join(S, cs);
+  for (int i = 0; e == cudaSuccess && i < 2; ++i) e = launch_attend(A[i], P.scratch[i], cs, &N.part[i]);
+  if (e == cudaSuccess) e = launch_join(N, cs);
   return e == cudaSuccess ? MMSHIFT_OK : noalloc_cuda_fail(e);
 }
 

@@ -16,7 +16,7 @@ def test_every_kernel_waits_before_it_reads():
         for kernel, body in kernels:
             assert body.count(start + "();") == 1, (name, kernel)
             ahead = body[:body.index(start + "();")]
-            for bad in ("J.lens", "J.table", "G.refs", "G.table", "J.pos", "S.part", "S.ml", "load", "attend_span"):
+            for bad in ("J.lens", "J.table", "G.refs", "G.table", "J.pos", "sum_of_row", "cache_len", "load", "attend_span"):
                 assert bad not in ahead, (name, kernel, bad)
         wait = code[code.index(f"void {start}()"):]
         wait = wait[:wait.index("\n}")]
