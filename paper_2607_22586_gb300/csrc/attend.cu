@@ -175,9 +175,10 @@ AttendPlan plan_of(const CacheJob& J, int most, Take take) {
   return P;
 }
 
-// Plans for `nsm` SMs; a CTA a worker, as many as fit.
-AttendPlan token_plan(const CacheJob& J, int nsm) {
-  AttendPlan P = plan_of(J, kTokenRows, [&](int rows) { return rows <= few_rows(J); });
+// Plans for `nsm` SMs; a CTA a worker, as many as fit. few: rows of a request's KV head up to which
+// it goes to the first.
+AttendPlan token_plan(const CacheJob& J, int nsm, int few) {
+  AttendPlan P = plan_of(J, kTokenRows, [&](int rows) { return rows <= few; });
   if (J.bf16) {
     const int row = J.i8 ? J.d : 2 * J.d;
     while ((row << P.step_shift) < 4096) ++P.step_shift;   // a warp's piece: 4 KB of K
@@ -191,8 +192,8 @@ AttendPlan token_plan(const CacheJob& J, int nsm) {
   return P;
 }
 
-AttendPlan chunk_plan(const CacheJob& J, int nsm) {
-  AttendPlan P = plan_of(J, J.bf16 ? 256 : 128, [&](int rows) { return rows > few_rows(J); });
+AttendPlan chunk_plan(const CacheJob& J, int nsm, int few) {
+  AttendPlan P = plan_of(J, J.bf16 ? 256 : 128, [&](int rows) { return rows > few; });
   P.step_shift = J.bf16 ? 7 : 6;
   P.workers = nsm;
   P.extra = !J.bf16 ? 0 : J.i8 ? 4 : 6;
@@ -225,8 +226,9 @@ char* place(AttendPlan& P, const CacheJob& J, char* at) {
 
 }  // namespace
 
-size_t attend_scratch_bytes(const CacheJob& J) {
-  AttendPlan t = token_plan(J, kSMs), c = chunk_plan(J, kSMs);
+size_t attend_scratch_bytes(const CacheJob& J, int few) {
+  if (!few) few = few_rows(J);
+  AttendPlan t = token_plan(J, kSMs, few), c = chunk_plan(J, kSMs, few);
   char* const base = reinterpret_cast<char*>(uintptr_t(256));
   return place(c, J, place(t, J, base)) - base;
 }
@@ -256,40 +258,42 @@ cudaError_t launch_prompt(AttendJob& A, void* scratch, cudaStream_t st) {
   return e == cudaSuccess && !O.whole ? launch_merge(A, P, st) : e;
 }
 
-// parts: where the plans go if sums are left as they are, else null: merged.
-cudaError_t launch_attend(const AttendJob& A, void* scratch, cudaStream_t st, AttendParts* parts) {
+cudaError_t attend_parts(const AttendJob& A, void* scratch, int few, AttendParts* S) {
   const CacheJob& J = A.c;
   const int nsm = sm_count();
   if (nsm <= 0) return cudaErrorInvalidDevice;
-  AttendPlan t = token_plan(J, nsm), c = chunk_plan(J, nsm);
-  place(c, J, place(t, J, static_cast<char*>(scratch)));
-  if (parts) *parts = AttendParts{A, t, c, few_rows(J), 0};
+  if (!few) few = few_rows(J);
+  *S = AttendParts{A, token_plan(J, nsm, few), chunk_plan(J, nsm, few), few, 0};
+  place(S->c, J, place(S->t, J, static_cast<char*>(scratch)));
+  // Clusters of eight CTAs where a warp has at most kClusterSteps steps even of a full
+  // table, and all clusters fit at once: longer steps then cost less than another launch
+  // and the reading of lengths. One token, 4 heads, bfloat16 rows: 513 rows 5.8 us (7.3
+  // by the balanced form and its merge), 2049 (4 steps) 8.7 (8.9), 4097 13.0 (10.3);
+  // 8-bit rows: 2049 8.1 (8.9), 4097 (4 steps) 10.3 (10.1).
+  const AttendPlan& t = S->t;
+  S->whole = J.bf16 && J.cap >> t.step_shift <= 32 * kClusterSteps && 8 * t.uoff[J.B] <= t.workers;
+  return cudaSuccess;
+}
+
+cudaError_t launch_attend(const AttendParts& S, bool merge, cudaStream_t st) {
+  const AttendJob& A = S.A;
+  const CacheJob& J = A.c;
   cudaError_t e = cudaSuccess;
-  if (c.uoff[J.B]) {
-    e = J.bf16 ? launch_attend_chunk(A, c, st) : launch_attend_simt(A, c, st);
-    if (e == cudaSuccess && !parts) e = launch_merge(A, c, st);
+  if (S.c.uoff[J.B]) {
+    e = J.bf16 ? launch_attend_chunk(A, S.c, st) : launch_attend_simt(A, S.c, st);
+    if (e == cudaSuccess && merge) e = launch_merge(A, S.c, st);
   }
-  if (e == cudaSuccess && t.uoff[J.B]) {
-    if (J.bf16) {
-      // Clusters of eight CTAs where a warp has at most kClusterSteps steps even of a full
-      // table, and all clusters fit at once: longer steps then cost less than another launch
-      // and the reading of lengths. One token, 4 heads, bfloat16 rows: 513 rows 5.8 us (7.3
-      // by the balanced form and its merge), 2049 (4 steps) 8.7 (8.9), 4097 13.0 (10.3);
-      // 8-bit rows: 2049 8.1 (8.9), 4097 (4 steps) 10.3 (10.1).
-      const bool cluster = J.cap >> t.step_shift <= 32 * kClusterSteps && 8 * t.uoff[J.B] <= t.workers;
-      e = launch_attend_token(A, t, cluster, st);
-      if (parts) parts->whole = cluster;
-      if (cluster) return e;
-    } else {
-      e = launch_attend_simt(A, t, st);
-    }
-    if (e == cudaSuccess && !parts) e = launch_merge(A, t, st);
+  if (e == cudaSuccess && S.t.uoff[J.B]) {
+    e = J.bf16 ? launch_attend_token(A, S.t, S.whole, st) : launch_attend_simt(A, S.t, st);
+    if (e == cudaSuccess && merge && !S.whole) e = launch_merge(A, S.t, st);
   }
   return e;
 }
 
 cudaError_t launch_attend(const AttendJob& A, void* scratch, cudaStream_t st) {
-  return launch_attend(A, scratch, st, nullptr);
+  AttendParts S;
+  const cudaError_t e = attend_parts(A, scratch, 0, &S);
+  return e == cudaSuccess ? launch_attend(S, true, st) : e;
 }
 
 }  // namespace mmshift

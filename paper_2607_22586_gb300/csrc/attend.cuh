@@ -49,15 +49,17 @@ __device__ __forceinline__ int attend_len(const CacheJob& J, int u) {
   return J.lens ? min(max(__ldcg(J.lens + u), 0), J.cap) : J.off[b + 1] - J.off[b];
 }
 
-// lens: the sequences' lengths (AttendScan::lengths), or null to read them from the cache.
-__device__ __forceinline__ AttendUnit attend_unit(const AttendJob& A, const AttendPlan& P, const int32_t* lens, int u) {
+// The unit of a request's KV head and row tile. lens: the sequences' lengths (AttendScan::lengths), or
+// null to read them from the cache.
+__device__ __forceinline__ AttendUnit attend_unit(const AttendJob& A, const AttendPlan& P, const int32_t* lens, int b,
+                                                  int h, int tile) {
   const CacheJob& J = A.c;
   AttendUnit x;
-  x.b = range_of(P.uoff, J.B, u);
-  x.n = J.off[x.b + 1] - J.off[x.b];
-  const int all = x.n * J.r, tiles = P.tiles[x.b], rem = u - P.uoff[x.b];
-  x.h = P.by_tiles[x.b](rem);
-  x.row0 = (rem - x.h * tiles) * P.rows;
+  x.b = b;
+  x.h = h;
+  x.n = J.off[b + 1] - J.off[b];
+  const int all = x.n * J.r;
+  x.row0 = tile * P.rows;
   x.rows = min(P.rows, all - x.row0);
   const int seq = x.b * J.Hkv + x.h;
   x.len = lens ? lens[seq] : attend_len(J, seq);
@@ -66,6 +68,10 @@ __device__ __forceinline__ AttendUnit attend_unit(const AttendJob& A, const Atte
   x.extra = x.rows <= 128 ? P.extra1 : P.extra;
   x.cost = x.pieces ? x.pieces + x.extra : 0;
   return x;
+}
+__device__ __forceinline__ AttendUnit attend_unit(const AttendJob& A, const AttendPlan& P, const int32_t* lens, int u) {
+  const int b = range_of(P.uoff, A.c.B, u), rem = u - P.uoff[b], h = P.by_tiles[b](rem);
+  return attend_unit(A, P, lens, b, h, rem - h * P.tiles[b]);
 }
 
 // A worker's place in the work: [begin, end) of all units' costs, the unit that
@@ -252,41 +258,69 @@ struct AttendParts {
   int32_t few;         // rows of a request's KV head up to which it is in t
   int32_t whole;       // t's units are all in A.part
 };
-cudaError_t launch_attend(const AttendJob& A, void* scratch, cudaStream_t st, AttendParts* parts);
+// The plans of a call (few: 0 for what attention itself takes), and the call with or without its merges.
+cudaError_t attend_parts(const AttendJob& A, void* scratch, int few, AttendParts* S);
+cudaError_t launch_attend(const AttendParts& S, bool merge, cudaStream_t st);
 
-// A warp's: the sum of query row rho of a request's KV head, its lane's D / 32 values.
-template <int D>
-__device__ __forceinline__ void sum_of_row(const AttendParts& S, int b, int h, int rho, int lane, float& top, float& z,
-                                           float (&o)[D / 32]) {
+// What a row's sum is found by: its request's first token and rows of a KV head, and of its plan.
+struct AttendRows {
+  int32_t tok0, rows, few, tile, units, tiles, unused[2];
+};
+inline AttendRows attend_rows(const AttendParts& S, int b) {
   const CacheJob& J = S.A.c;
-  const bool few = (J.off[b + 1] - J.off[b]) * J.r <= S.few;
+  const int rows = (J.off[b + 1] - J.off[b]) * J.r, few = rows <= S.few;
   const AttendPlan& P = few ? S.t : S.c;
-  const int tile = rho / P.rows, row = rho - tile * P.rows, u = P.uoff[b] + h * P.tiles[b] + tile;
+  return AttendRows{J.off[b], rows, few, P.rows, P.uoff[b], P.tiles[b], {0, 0}};
+}
+
+// A warp's: the sum of query row rho of KV head h of the request with rows R; its lane's D / 32 values.
+template <int D>
+__device__ __forceinline__ void sum_of_row(const AttendParts& S, const AttendRows& R, int b, int h, int rho, int lane,
+                                           float& top, float& z, float (&o)[D / 32]) {
+  const CacheJob& J = S.A.c;
+  const AttendPlan& P = R.few ? S.t : S.c;
+  const int tile = rho / R.tile, row = rho - tile * R.tile, u = R.units + h * R.tiles + tile;
+  const int tok = J.by_r(rho);
+  const size_t at = (size_t)(R.tok0 + tok) * J.Hq + h * J.r + rho - tok * J.r;
   top = -INFINITY;
   z = 0.f;
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) o[i] = 0.f;
-  if (!(few && S.whole)) {
-    const AttendUnit U = attend_unit(S.A, P, nullptr, u);
+  if (!(R.few && S.whole)) {
+    const int64_t W = P.start[P.workers].before;
+    const int len = attend_len(J, b * J.Hkv + h), rows = min(R.tile, R.rows - tile * R.tile);
+    AttendUnit U;
+    U.rows = rows;
+    U.keys = keys_of(S.A.causal, len, J.by_r(R.rows), J.by_r(tile * R.tile + rows - 1));
+    U.pieces = (U.keys + (1 << P.step_shift) - 1) >> P.step_shift;
+    U.extra = rows <= 128 ? P.extra1 : P.extra;
     if (!U.pieces) return;
     // If a worker's share begins in the unit, it says what is before the unit; else one worker had
     // all of it.
-    const Shares sh = shares_of(P.start[P.workers].before, P.workers, P.least);
+    const Shares sh = shares_of(W, P.workers, P.least);
     int lo = 0, hi = sh.n;                             // the first worker whose first unit is not before u
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (P.start[mid].unit < u) lo = mid + 1; else hi = mid;
+    while (lo < hi) {                                  // a lane a place in turn: a load's latency for 32
+      const int step = (hi - lo + 31) / 32, i = lo + lane * step;
+      const int less = __popc(__ballot_sync(0xffffffffu, i < hi && P.start[i].unit < u));
+      if (less) {
+        const int last = lo + (less - 1) * step;       // the last of them that is before u
+        hi = min(hi, last + step);
+        lo = last + 1;
+      } else {
+        hi = lo;
+      }
     }
-    if (lo < sh.n && P.start[lo].unit == u) {
-      const Parts parts(P, sh, U, P.start[lo].before);
-      if (parts.i0 < parts.i1) {
-        add_parts<D, 1>(P, parts, row, lane, 0, top, z, o);
-        return;
+    if (lo < sh.n) {
+      const AttendStart s = P.start[lo];
+      if (s.unit == u) {
+        const Parts parts(P, sh, U, s.before);
+        if (parts.i0 < parts.i1) {
+          add_parts<D, 1>(P, parts, row, lane, 0, top, z, o);
+          return;
+        }
       }
     }
   }
-  const int tok = J.by_r(rho);
-  const size_t at = (size_t)(J.off[b] + tok) * J.Hq + h * J.r + rho - tok * J.r;
   const float2 ml = S.A.part_ml[at];
   top = ml.x;
   z = ml.y;

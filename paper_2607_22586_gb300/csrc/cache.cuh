@@ -94,7 +94,7 @@ mmshift_status attend_args(const CacheJob& J, const void* Q, int64_t row_stride,
                            const void* out, const float* lse);
 void attend_set(AttendJob& A, const void* Q, int64_t row_stride, int32_t causal, float softmax_scale);
 
-size_t attend_scratch_bytes(const CacheJob& J);
+size_t attend_scratch_bytes(const CacheJob& J, int few = 0);
 cudaError_t launch_attend(const AttendJob& A, void* scratch, cudaStream_t st);
 size_t prompt_scratch_bytes(const CacheJob& J);
 cudaError_t launch_prompt(AttendJob& A, void* scratch, cudaStream_t st);

@@ -22,6 +22,7 @@ namespace {
 
 using umma::cluster_rank;
 using umma::cluster_sync;
+using umma::ld_cluster_int;
 using umma::mapa;
 using umma::smem_u32;
 
@@ -70,12 +71,6 @@ __device__ __forceinline__ Written written(const PagesJob& G, int u) {
     const int end = append_end(J.lens[u], J.cap);
     return Written{max(end - n, 0), min(end, J.cap)};
   }
-}
-
-__device__ __forceinline__ int ld_cluster_int(uint32_t caddr) {
-  int v;
-  asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(caddr) : "memory");
-  return v;
 }
 
 // The sum over all threads of the cluster before this one, and over all.

@@ -14,13 +14,20 @@
 #include <cstring>
 
 #include "attend.cuh"
+#include "umma.cuh"
 
 namespace mmshift {
 mmshift_status noalloc_cuda_fail(cudaError_t e);
 
 namespace {
 
-constexpr int kCommon = 1024;
+using umma::cluster_rank;
+using umma::cluster_sync;
+using umma::ld_cluster_int;
+using umma::mapa;
+using umma::smem_u32;
+
+constexpr int kCluster = 8;            // CTAs that compare a group's tables
 
 struct SharedJob {
   CacheJob c;
@@ -28,6 +35,9 @@ struct SharedJob {
   int64_t* at[2];                      // of the groups' common pages, of the requests' own
   int32_t* lens[2];                    // [n_groups][Hkv], [batch][Hkv]
   int32_t group[MMSHIFT_MAX_BATCH + 1];   // first requests
+  AttendRows row[2][MMSHIFT_MAX_BATCH];   // of the groups, of the requests
+  AttendRows* rows;                    // the same, in device memory
+  int32_t* place;                      // [T] of each token: group << 16 | request
 };
 
 struct JoinJob {
@@ -35,7 +45,8 @@ struct JoinJob {
   uint8_t* out;
   float* lse;
   int32_t ovec;
-  int32_t group[MMSHIFT_MAX_BATCH + 1], n_groups;
+  const AttendRows* rows;
+  const int32_t* place;
 };
 
 // Start: everything before in the stream is done, and the next kernel may take its place.
@@ -44,16 +55,25 @@ __device__ __forceinline__ void shared_start() {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
-// A block a group and KV head: how many pages all its sequences with rows in the call have
-// in common. Only keys that every row attends to count, and requests alone have none.
-__global__ void __launch_bounds__(kCommon) common_pages_kernel(const __grid_constant__ SharedJob S) {
+// A cluster a group and KV head: how many pages all its sequences with rows in the call have
+// in common. Only keys that every row attends to count, and requests alone have none. Warps
+// compare 32 places of the table at a time, eight requests at once (64 requests of 375 pages, 8 heads:
+// 15 us by one CTA each).
+__global__ void __launch_bounds__(256) common_pages_kernel(const __grid_constant__ SharedJob S) {
   __shared__ int32_t common, first_, keys, members;
   const CacheJob& J = S.c;
   shared_start();
-  const int g = blockIdx.x, h = blockIdx.y, b0 = S.group[g], b1 = S.group[g + 1], tid = threadIdx.x;
+  const int rank = cluster_rank(), g = blockIdx.x / kCluster, h = blockIdx.y, b0 = S.group[g], b1 = S.group[g + 1];
+  const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
   if (tid == 0) {
     first_ = keys = INT_MAX;
     members = 0;
+  }
+  // what join_kernel would look up step by step
+  if (h == 0) {
+    for (int t = J.off[b0] + rank * 256 + tid; t < J.off[b1]; t += kCluster * 256) S.place[t] = g << 16 | range_of(J.off, J.B, t);
+    if (g == 0 && rank == 0 && tid < 2 * MMSHIFT_MAX_BATCH)
+      S.rows[tid] = S.row[tid / MMSHIFT_MAX_BATCH][tid % MMSHIFT_MAX_BATCH];
   }
   __syncthreads();
   if (b0 + tid < b1) {
@@ -68,29 +88,31 @@ __global__ void __launch_bounds__(kCommon) common_pages_kernel(const __grid_cons
   const int first = members ? first_ : b0, most = members > 1 ? keys >> J.page_shift : 0;
   if (tid == 0) common = most;
   __syncthreads();
-  // places in order, 256 at a time, the requests behind the first shared out to four threads a place
   const int32_t* const lead = J.table + ((size_t)first * J.Hkv + h) * J.max_pages;
-  for (int e0 = 0; e0 < most; e0 += 256) {
-    const int e = e0 + tid % 256;
+  for (int e = rank * 32 + lane; e - lane < most; e += kCluster * 32) {
+    if (e >= most) continue;
+    const int32_t is = lead[e];
     bool same = true;
-    if (e < most) {
-      const int32_t is = lead[e];
 #pragma unroll 8
-      for (int b = first + 1 + tid / 256; b < b1; b += 4)
-        same &= J.off[b + 1] == J.off[b] || J.table[((size_t)b * J.Hkv + h) * J.max_pages + e] == is;
+    for (int b = first + 1 + warp; b < b1; b += 8)
+      same &= J.off[b + 1] == J.off[b] || J.table[((size_t)b * J.Hkv + h) * J.max_pages + e] == is;
+    if (!same) {
+      atomicMin(&common, e);
+      break;                                           // what lies behind cannot be less
     }
-    if (!same) atomicMin(&common, e);
-    __syncthreads();
-    if (common < e0 + 256) break;                      // the same for all threads
-    __syncthreads();
   }
   __syncthreads();
-  const int pages = common;
+  cluster_sync();
+  int pages = common;
+#pragma unroll
+  for (int r = 0; r < kCluster; ++r) pages = min(pages, ld_cluster_int(mapa(smem_u32(&common), r)));
+  cluster_sync();                                      // no CTA leaves while its result is read
+  if (rank) return;
   if (tid == 0) {
     S.at[0][g * J.Hkv + h] = ((int64_t)first * J.Hkv + h) * J.max_pages;
     S.lens[0][g * J.Hkv + h] = pages << J.page_shift;
   }
-  for (int b = b0 + tid; b < b1; b += kCommon) {
+  for (int b = b0 + tid; b < b1; b += 256) {
     const size_t u = (size_t)b * J.Hkv + h;
     const bool rows = J.off[b + 1] > J.off[b];
     S.at[1][u] = (int64_t)u * J.max_pages + (rows ? pages : 0);
@@ -98,33 +120,47 @@ __global__ void __launch_bounds__(kCommon) common_pages_kernel(const __grid_cons
   }
 }
 
-// A warp a row.
+// Two warps a row: one adds up the common pages' sums, one the request's own.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ JoinJob S) {
+  constexpr int N = D / 32;                            // values of a lane
+  __shared__ float2 ml[4];
+  __shared__ alignas(16) float sum[4][D];
   const CacheJob& J = S.part[1].A.c;
   shared_start();
-  const int row = blockIdx.x * 8 + threadIdx.x / 32, lane = threadIdx.x % 32;
-  if (row >= J.off[J.B] * J.Hq) return;
-  const int tok = row / J.Hq, hq = row - tok * J.Hq, h = J.by_r(hq), j = hq - h * J.r;
-  const int b = range_of(J.off, J.B, tok), g = range_of(S.group, S.n_groups, b);
-  float ta, za, oa[D / 32], tb, zb, ob[D / 32];
-  sum_of_row<D>(S.part[0], g, h, (tok - S.part[0].A.c.off[g]) * J.r + j, lane, ta, za, oa);
-  sum_of_row<D>(S.part[1], b, h, (tok - J.off[b]) * J.r + j, lane, tb, zb, ob);
-  const float top = fmaxf(ta, tb);
-  const float fa = ta == -INFINITY ? 1.f : fast_exp2(ta - top), fb = tb == -INFINITY ? 1.f : fast_exp2(tb - top);
-  const float z = za * fa + zb * fb, f = z == 0.f ? 0.f : 1.f / z;
-  T* const out = reinterpret_cast<T*>(S.out) + (size_t)row * D + lane * (D / 32);
-  float v[D / 32];
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, own = warp & 1;
+  const int row = blockIdx.x * 4 + warp / 2;
+  const bool in = row < J.off[J.B] * J.Hq;
+  const int tok = in ? row / J.Hq : 0, hq = in ? row - tok * J.Hq : 0, h = J.by_r(hq), j = hq - h * J.r;
+  const int at = S.place[tok], i = own ? at & 0xffff : at >> 16;
+  const AttendRows R = S.rows[own * MMSHIFT_MAX_BATCH + i];
+  float top, z, o[N];
+  sum_of_row<D>(S.part[own], R, i, h, (tok - R.tok0) * J.r + j, lane, top, z, o);
+  if (!own) {
 #pragma unroll
-  for (int i = 0; i < D / 32; ++i) v[i] = z == 0.f ? 0.f : (oa[i] * fa + ob[i] * fb) * f;
-  if (S.ovec && D == 128) {
-    if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[D / 64], v[D / 32 - 1]));
-    else *reinterpret_cast<float4*>(out) = make_float4(v[0], v[1], v[D / 64], v[D / 32 - 1]);
+    for (int k = 0; k < N; ++k) sum[warp / 2][lane * N + k] = o[k];
+    if (lane == 0) ml[warp / 2] = make_float2(top, z);
+  }
+  __syncthreads();
+  if (!own || !in) return;
+  const float2 x = ml[warp / 2];
+  const float most = fmaxf(top, x.x);
+  const float fa = x.x == -INFINITY ? 1.f : fast_exp2(x.x - most), fb = top == -INFINITY ? 1.f : fast_exp2(top - most);
+  const float all = x.y * fa + z * fb, f = all == 0.f ? 0.f : 1.f / all;
+  float v[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) v[k] = all == 0.f ? 0.f : (sum[warp / 2][lane * N + k] * fa + o[k] * fb) * f;
+  T* const out = reinterpret_cast<T*>(S.out) + (size_t)row * D + lane * N;
+  if (S.ovec && N == 4) {
+    if constexpr (sizeof(T) == 2)
+      *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[N / 2], v[N - 1]));
+    else
+      *reinterpret_cast<float4*>(out) = make_float4(v[0], v[1], v[N / 2], v[N - 1]);
   } else {
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) out[i] = from_f32<T>(v[i]);
+    for (int k = 0; k < N; ++k) out[k] = from_f32<T>(v[k]);
   }
-  if (lane == 0 && S.lse) S.lse[row] = z == 0.f ? -INFINITY : (top + log2f(z)) * 0.6931471805599453f;
+  if (lane == 0 && S.lse) S.lse[row] = all == 0.f ? -INFINITY : (most + log2f(all)) * 0.6931471805599453f;
 }
 
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
@@ -144,8 +180,15 @@ struct SharedParts {
   int32_t* lens[2];
   float* part[2];
   float2* ml[2];
+  AttendRows* rows;
+  int32_t* place;
   char* scratch[2];
 };
+
+// A request's own keys are few, so that one more tile of few rows costs less than a chunk's launch:
+// up to this many rows of a KV head go to the tiles of few rows.
+constexpr int kOwnRows = 64;
+
 char* place(const CacheJob& J, const CacheJob& G, char* at, SharedParts* P) {
   const size_t rows = (size_t)J.off[J.B] * J.Hq;
   for (int i = 0; i < 2; ++i) {
@@ -159,9 +202,13 @@ char* place(const CacheJob& J, const CacheJob& G, char* at, SharedParts* P) {
     P->ml[i] = reinterpret_cast<float2*>(at);
     at += align256(rows * sizeof(float2));
   }
+  P->rows = reinterpret_cast<AttendRows*>(at);
+  at += align256(2 * MMSHIFT_MAX_BATCH * sizeof(AttendRows));
+  P->place = reinterpret_cast<int32_t*>(at);
+  at += align256(J.off[J.B] * sizeof(int32_t));
   P->scratch[0] = at;
   P->scratch[1] = at + attend_scratch_bytes(G);
-  return P->scratch[1] + attend_scratch_bytes(J);
+  return P->scratch[1] + attend_scratch_bytes(J, kOwnRows);
 }
 
 mmshift_status shared_job(const mmshift_shape* s, const mmshift_cache* c, int32_t n_groups, const int32_t* cu_groups,
@@ -180,7 +227,7 @@ mmshift_status shared_job(const mmshift_shape* s, const mmshift_cache* c, int32_
 cudaError_t launch_join(const JoinJob& S, cudaStream_t st) {
   const CacheJob& J = S.part[1].A.c;
   const unsigned rows = (unsigned)J.off[J.B] * J.Hq;
-  auto go = [&](auto kernel) { return launch_kernel(kernel, dim3((rows + 7) / 8), 256, 0, st, true, 0, S); };
+  auto go = [&](auto kernel) { return launch_kernel(kernel, dim3((rows + 3) / 4), 256, 0, st, true, 0, S); };
   if (J.bf16) return J.d == 128 ? go(join_kernel<__nv_bfloat16, 128>) : go(join_kernel<__nv_bfloat16, 64>);
   return J.d == 128 ? go(join_kernel<float, 128>) : go(join_kernel<float, 64>);
 }
@@ -229,8 +276,8 @@ mmshift_status mmshift_cache_attention_shared(const mmshift_shape* s, const mmsh
   N.out = static_cast<uint8_t*>(out);
   N.lse = lse;
   N.ovec = aligned(out, 16);
-  N.n_groups = n_groups;
-  std::memcpy(N.group, S.group, sizeof(N.group));
+  N.rows = S.rows = P.rows;
+  N.place = S.place = P.place;
   for (int i = 0; i < 2; ++i) {
     S.at[i] = P.at[i];
     S.lens[i] = P.lens[i];
@@ -239,10 +286,13 @@ mmshift_status mmshift_cache_attention_shared(const mmshift_shape* s, const mmsh
     A[i].part_ml = P.ml[i];
     A[i].c.at = P.at[i];
     A[i].c.lens = P.lens[i];
+    const cudaError_t e = attend_parts(A[i], P.scratch[i], i ? kOwnRows : 0, &N.part[i]);
+    if (e != cudaSuccess) return noalloc_cuda_fail(e);
+    for (int b = 0; b < A[i].c.B; ++b) S.row[i][b] = attend_rows(N.part[i], b);
   }
   const cudaStream_t cs = (cudaStream_t)stream;
-  cudaError_t e = launch_kernel(common_pages_kernel, dim3(n_groups, J.Hkv), kCommon, 0, cs, true, 0, S);
-  for (int i = 0; e == cudaSuccess && i < 2; ++i) e = launch_attend(A[i], P.scratch[i], cs, &N.part[i]);
+  cudaError_t e = launch_kernel(common_pages_kernel, dim3(n_groups * kCluster, J.Hkv), 256, 0, cs, true, kCluster, S);
+  for (int i = 0; e == cudaSuccess && i < 2; ++i) e = launch_attend(N.part[i], false, cs);
   if (e == cudaSuccess) e = launch_join(N, cs);
   return e == cudaSuccess ? MMSHIFT_OK : noalloc_cuda_fail(e);
 }

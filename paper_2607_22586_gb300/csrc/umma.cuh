@@ -260,6 +260,11 @@ __device__ __forceinline__ float2 ld_cluster_f2(uint32_t caddr) {
   asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(caddr) : "memory");
   return v;
 }
+__device__ __forceinline__ int ld_cluster_int(uint32_t caddr) {
+  int v;
+  asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(caddr) : "memory");
+  return v;
+}
 // Relaxed arrival on an mbarrier of either CTA of the cluster: orders no
 // memory accesses, for releases whose data dependence is already complete
 // (e.g. tensor-memory reads finished by tcgen05.wait::ld).
