@@ -42,7 +42,8 @@ struct PagesJob {
   int32_t* list;                       // [most] free pages, lowest first
   PageJob* jobs;                       // [most]
   int32_t most;
-  int32_t group;                       // lanes of a sequence
+  int32_t vec;                         // refs allow 16-byte loads
+  int32_t group, once;                 // lanes of a sequence; they have all its pages at one go
   int32_t* old_table;                  // compact: the table and lengths before
   int32_t* old_lens;
 };
@@ -73,11 +74,17 @@ __device__ __forceinline__ Written written(const PagesJob& G, int u) {
   }
 }
 
-// The sum over all threads of the cluster before this one, and over all.
+// The barrier of the kernel's CTAs, and the sums over all their threads before one, and over all.
+template <int C>
+__device__ __forceinline__ void sync_all() {
+  if constexpr (C == 1) __syncthreads();
+  else cluster_sync();
+}
 struct ClusterScan {
   int32_t warp[kTake / 32];
   int32_t total;
 };
+template <int C>
 __device__ __forceinline__ void cluster_scan(ClusterScan& s, int x, int& before, int& all) {
   const int lane = threadIdx.x % 32, w = threadIdx.x / 32;
   int sum = x;
@@ -98,29 +105,33 @@ __device__ __forceinline__ void cluster_scan(ClusterScan& s, int x, int& before,
     s.warp[lane] = t;
     if (lane == 31) s.total = t;
   }
-  cluster_sync();
+  sync_all<C>();
   before = sum - x + (w ? s.warp[w - 1] : 0);
-  all = 0;
-  const int rank = cluster_rank();
+  if constexpr (C == 1) {
+    all = s.total;
+  } else {
+    all = 0;
+    const int rank = cluster_rank();
 #pragma unroll
-  for (int r = 0; r < kCluster; ++r) {
-    const int t = ld_cluster_int(mapa(smem_u32(&s.total), r));
-    if (r < rank) before += t;
-    all += t;
+    for (int r = 0; r < C; ++r) {
+      const int t = ld_cluster_int(mapa(smem_u32(&s.total), r));
+      if (r < rank) before += t;
+      all += t;
+    }
   }
 }
 
 // Every sequence's missing and shared pages among those that the call writes are replaced
 // by free ones. COMPACT: of the first pages, which will hold the kept rows; the pages behind them
 // are given back, and the lengths set.
-template <bool COMPACT>
+template <bool COMPACT, int C>
 __global__ void __launch_bounds__(kTake) take_pages_kernel(const __grid_constant__ PagesJob G) {
   __shared__ ClusterScan scan[2];
   const CacheJob& J = G.c;
-  const int rank = cluster_rank(), tid = rank * kTake + threadIdx.x, lane = threadIdx.x % 32;
+  const int rank = C == 1 ? 0 : cluster_rank(), tid = rank * kTake + threadIdx.x, lane = threadIdx.x % 32;
   pages_start();
   // A sequence's lanes take its pages in turn; a group of lanes has a run of sequences.
-  const int U = J.L * J.B * J.Hkv, groups = kCluster * kTake / G.group, per = (U + groups - 1) / groups;
+  const int U = J.L * J.B * J.Hkv, groups = C * kTake / G.group, per = (U + groups - 1) / groups;
   const int g = tid / G.group, part = tid % G.group;
   const unsigned mine = (G.group == 32 ? 0xffffffffu : (1u << G.group) - 1u) << (lane / G.group * G.group);
   const int64_t u_first = (int64_t)g * per;
@@ -128,67 +139,101 @@ __global__ void __launch_bounds__(kTake) take_pages_kernel(const __grid_constant
   const int page = 1 << J.page_shift;
 
   // Walks the pages that the group's sequences write: f(sequence, page's place in it, its entry
-  // or -1, whether it has to be replaced, how many before it of the walk have to be).
-  auto walk = [&](auto f) {
+  // or -1, whether it has to be replaced, how many before it of the walk have to be). Warps stay
+  // together: lanes that vote in groups of their own would go on one by one. Four pages a lane are
+  // asked for at once; a walk of no more than those (`once`) is not read again.
+  constexpr int K = 4;
+  const bool once = per == 1 && G.once;
+  Written w = {0, 0};
+  int32_t e[K];
+  bool need[K];
+  auto walk = [&](bool read, auto f) {
     int n = 0;
-    for (int u = u0; u < u1; ++u) {
-      const Written w = written<COMPACT>(G, u);
-      if (w.start >= w.stop) continue;                 // the same for all lanes of the group
-      const int first = w.start >> J.page_shift, end = (w.stop + page - 1) >> J.page_shift;
-      for (int i0 = first; i0 < end; i0 += G.group) {
-        const int i = i0 + part;
-        bool need = false;
-        int32_t e = -1;
-        if (i < end) {
-          e = G.table[(size_t)u * J.max_pages + i];
-          if (!is_page(J, e)) e = -1;
-          need = e < 0 || G.refs[e] > 1;
+    for (int k = 0; k < per; ++k) {
+      const int u = u0 + k;
+      if (read) w = u < u1 ? written<COMPACT>(G, u) : Written{0, 0};
+      const int first = w.start >> J.page_shift, end = w.start < w.stop ? (w.stop + page - 1) >> J.page_shift : first;
+      for (int i0 = first + part; __any_sync(0xffffffffu, i0 - part < end); i0 += K * G.group) {
+        if (read) {
+#pragma unroll
+          for (int x = 0; x < K; ++x) {
+            const int i = i0 + x * G.group;
+            e[x] = i < end ? G.table[(size_t)u * J.max_pages + i] : -1;
+            if (!is_page(J, e[x])) e[x] = -1;
+          }
+#pragma unroll
+          for (int x = 0; x < K; ++x) need[x] = i0 + x * G.group < end && (e[x] < 0 || G.refs[e[x]] > 1);
         }
-        const unsigned all = __ballot_sync(mine, need) & mine;
-        f(u, w, i, e, need, n + __popc(all & ((1u << lane) - 1u)));
-        n += __popc(all);
+#pragma unroll
+        for (int x = 0; x < K; ++x) {
+          const unsigned all = __ballot_sync(0xffffffffu, need[x]) & mine;
+          f(u, w, i0 + x * G.group, e[x], need[x], n + __popc(all & ((1u << lane) - 1u)));
+          n += __popc(all);
+        }
       }
     }
     return n;
   };
+  const int warp = tid / 32, warps = C * kTake / 32;
   if constexpr (COMPACT) {                             // what is moved is found by way of the table before
-    const int warp = tid / 32;
-    for (int64_t u = warp; u < U; u += kCluster * kTake / 32) {
+    for (int64_t u = warp; u < U; u += warps) {
       const int b = J.by_heads((int)u) % J.B;
       if (J.off[b + 1] == J.off[b]) continue;
       const int held = cache_len(J, u), pages = (held + page - 1) >> J.page_shift;
+#pragma unroll 4
       for (int i = lane; i < pages; i += 32) G.old_table[u * J.max_pages + i] = G.table[u * J.max_pages + i];
       if (lane == 0) G.old_lens[u] = held;
     }
   }
-  const int needed = walk([](int, Written, int, int32_t, bool, int) {});
+  const int needed = walk(true, [](int, Written, int, int32_t, bool, int) {});
   int before, all;
-  cluster_scan(scan[0], part ? 0 : needed, before, all);
+  cluster_scan<C>(scan[0], part ? 0 : needed, before, all);
   before = __shfl_sync(0xffffffffu, before, lane / G.group * G.group);
   if (all) {
-    // Warps have a run of pages each, and count them before they number the free ones.
-    const int warp = tid / 32, warps = kCluster * kTake / 32;
-    const int run = ((J.n_pages + warps - 1) / warps + 31) / 32 * 32;
+    // Warps have a run of pages each, and count them before they number the free ones; a lane has
+    // four in a row.
+    const int run = ((J.n_pages + warps - 1) / warps + 127) / 128 * 128;
     const int64_t p_first = (int64_t)warp * run;
     const int p0 = (int)min(p_first, (int64_t)J.n_pages), p1 = (int)min(p_first + run, (int64_t)J.n_pages);
+    auto free_of = [&](int p) {                        // bit i: page p + i is free
+      int32_t r[4] = {1, 1, 1, 1};
+      if (G.vec && p + 4 <= p1) {
+        const int4 x = *reinterpret_cast<const int4*>(G.refs + p);
+        r[0] = x.x, r[1] = x.y, r[2] = x.z, r[3] = x.w;
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (p + i < p1) r[i] = G.refs[p + i];
+      }
+      return (r[0] == 0) | (r[1] == 0) << 1 | (r[2] == 0) << 2 | (r[3] == 0) << 3;
+    };
     int free = 0;
-#pragma unroll 4
-    for (int p = p0 + lane; p < p1; p += 32) free += G.refs[p] == 0;
+#pragma unroll 8
+    for (int p = p0 + 4 * lane; p < p1; p += 128) free += __popc(free_of(p));
 #pragma unroll
     for (int s = 16; s; s >>= 1) free += __shfl_xor_sync(0xffffffffu, free, s);
     int at, found;
-    cluster_scan(scan[1], lane ? 0 : free, at, found);
+    cluster_scan<C>(scan[1], lane ? 0 : free, at, found);
     at = __shfl_sync(0xffffffffu, at, 0);
     const int end = min(all, G.most);
-    for (int p = p0; p < p1 && at < end; p += 32) {
-      const bool is = p + lane < p1 && G.refs[p + lane] == 0;
-      const unsigned is_free = __ballot_sync(0xffffffffu, is);
-      const int k = at + __popc(is_free & ((1u << lane) - 1u));
-      if (is && k < end) G.list[k] = p + lane;
-      at += __popc(is_free);
+    for (int p = p0; p < p1 && at < end; p += 128) {
+      const unsigned is = free_of(p + 4 * lane);
+      int before_lane = 0, here = 0;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const unsigned lanes = __ballot_sync(0xffffffffu, is >> x & 1u);
+        before_lane += __popc(lanes & ((1u << lane) - 1u));
+        here += __popc(lanes);
+      }
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const int k = at + before_lane + __popc(is & ((1u << x) - 1u));
+        if ((is >> x & 1u) && k < end) G.list[k] = p + 4 * lane + x;
+      }
+      at += here;
     }
-    cluster_sync();                                    // the list is there, and all counts have been read
-    walk([&](int u, Written w, int i, int32_t e, bool need, int n) {
+    sync_all<C>();                                     // the list is there, and all counts have been read
+    walk(!once, [&](int u, Written w, int i, int32_t e, bool need, int n) {
       if (!need) return;
       const int k = before + n;
       const int32_t to = k < min(found, G.most) ? G.list[k] : -1;
@@ -200,19 +245,19 @@ __global__ void __launch_bounds__(kTake) take_pages_kernel(const __grid_constant
       }
       G.table[(size_t)u * J.max_pages + i] = to;
     });
-    cluster_sync();                                    // the counts are no longer asked for
-    for (int k = tid; k < min(all, G.most); k += kCluster * kTake) {
+    sync_all<C>();                                     // the counts are no longer asked for
+    for (int k = tid; k < min(all, G.most); k += C * kTake) {
       const int32_t e = G.jobs[k].from;
       if (e >= 0) atomicSub(G.refs + e, 1);
     }
   }
   if (tid == 0) *G.taken = min(all, G.most);
   if constexpr (COMPACT) {
-    const int warp = tid / 32;
-    for (int64_t u = warp; u < U; u += kCluster * kTake / 32) {
+    for (int64_t u = warp; u < U; u += warps) {
       const int b = J.by_heads((int)u) % J.B;
       if (J.off[b + 1] == J.off[b]) continue;
       const int kept = written<true>(G, (int)u).stop;
+#pragma unroll 4
       for (int i = ((kept + page - 1) >> J.page_shift) + lane; i < J.max_pages; i += 32) {
         const int32_t e = G.table[u * J.max_pages + i];
         if (is_page(J, e)) atomicSub(G.refs + e, 1);
@@ -222,7 +267,7 @@ __global__ void __launch_bounds__(kTake) take_pages_kernel(const __grid_constant
       if (lane == 0) J.lens[u] = kept;
     }
   }
-  cluster_sync();                                      // no CTA leaves while its sums are read
+  if constexpr (C > 1) cluster_sync();                 // no CTA leaves while its sums are read
 }
 
 // The rows that were there already, into the pages that replace shared ones: a block a
@@ -419,7 +464,8 @@ size_t place(PagesJob* G, char* at) {
   const int64_t most = most_pages(G->c, &one), U = (int64_t)G->c.L * G->c.B * G->c.Hkv;
   G->most = (int32_t)most;
   G->group = 1;
-  while (G->group < 32 && G->group < one) G->group *= 2;
+  while (G->group < 32 && 4 * G->group < one) G->group *= 2;   // a lane asks for four pages at once
+  G->once = one <= 4 * G->group;
   G->taken = reinterpret_cast<int32_t*>(at);
   at += 256;
   G->list = reinterpret_cast<int32_t*>(at);
@@ -441,13 +487,19 @@ mmshift_status pages_job(const mmshift_shape* s, const mmshift_cache* c, int32_t
   if (!refs || !aligned(refs, 4)) return MMSHIFT_ERR_INVALID_ARG;
   G->table = const_cast<int32_t*>(c->page_table);
   G->refs = refs;
+  G->vec = aligned(refs, 16);
   const size_t need = place(G, static_cast<char*>(ws) + 256);
   return check_workspace(ws, bytes, need);
 }
 
 template <bool COMPACT>
 cudaError_t launch_take(const PagesJob& G, cudaStream_t st) {
-  return launch_kernel(take_pages_kernel<COMPACT>, dim3(kCluster), kTake, 0, st, true, kCluster, G);
+  // One CTA where its threads see two sequences at most and a few pages: a cluster's barriers take
+  // 1 to 2 us each.
+  const int64_t U = (int64_t)G.c.L * G.c.B * G.c.Hkv;
+  if (U * G.group <= 2 * kTake && G.c.n_pages <= 64 * kTake)
+    return launch_kernel(take_pages_kernel<COMPACT, 1>, dim3(1), kTake, 0, st, true, 0, G);
+  return launch_kernel(take_pages_kernel<COMPACT, kCluster>, dim3(kCluster), kTake, 0, st, true, kCluster, G);
 }
 
 template <int ROWB, bool I8>
