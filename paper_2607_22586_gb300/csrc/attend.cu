@@ -209,8 +209,8 @@ AttendPlan prompt_plan(const CacheJob& J, int nsm) {
   AttendPlan P = plan_of(J, J.bf16 ? 2 * prompt_block(J) : 128, [](int) { return true; });
   P.step_shift = J.bf16 ? 7 : 6;
   P.workers = nsm;
-  P.extra = J.bf16 ? 2 : 0;
-  P.extra1 = J.bf16 ? 1 : 0;
+  P.extra = J.bf16 ? 2 : 1;
+  P.extra1 = 1;
   return P;
 }
 
