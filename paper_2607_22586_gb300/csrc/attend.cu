@@ -205,12 +205,15 @@ AttendPlan chunk_plan(const CacheJob& J, int nsm, int few) {
 int prompt_block(const CacheJob& J) { return J.r <= 128 ? 128 / J.r * J.r : 128; }
 
 // Whole prompts: all requests go to the chunks' tiles.
+void prompt_costs(const CacheJob& J, int nsm, AttendPlan* P) {
+  P->step_shift = J.bf16 ? 7 : 6;
+  P->workers = nsm;
+  P->extra = J.bf16 ? 2 : 1;
+  P->extra1 = 1;
+}
 AttendPlan prompt_plan(const CacheJob& J, int nsm) {
   AttendPlan P = plan_of(J, J.bf16 ? 2 * prompt_block(J) : 128, [](int) { return true; });
-  P.step_shift = J.bf16 ? 7 : 6;
-  P.workers = nsm;
-  P.extra = J.bf16 ? 2 : 1;
-  P.extra1 = 1;
+  prompt_costs(J, nsm, &P);
   return P;
 }
 
@@ -258,12 +261,17 @@ cudaError_t launch_prompt(AttendJob& A, void* scratch, cudaStream_t st) {
   return e == cudaSuccess && !O.whole ? launch_merge(A, P, st) : e;
 }
 
-cudaError_t attend_parts(const AttendJob& A, void* scratch, int few, AttendParts* S) {
+cudaError_t attend_parts(const AttendJob& A, void* scratch, int few, bool common, AttendParts* S) {
   const CacheJob& J = A.c;
   const int nsm = sm_count();
   if (nsm <= 0) return cudaErrorInvalidDevice;
   if (!few) few = few_rows(J);
-  *S = AttendParts{A, token_plan(J, nsm, few), chunk_plan(J, nsm, few), few, 0};
+  *S = AttendParts{A, token_plan(J, nsm, few), chunk_plan(J, nsm, few), few, 0, common && J.bf16 && !J.i8};
+  if (S->common) {                                     // the prompts' kernel, its tiles and costs
+    S->c = plan_of(J, 2 * prompt_block(J), [&](int rows) { return rows > few; });
+    prompt_costs(J, nsm, &S->c);
+    S->A.block_rows = prompt_block(J);
+  }
   place(S->c, J, place(S->t, J, static_cast<char*>(scratch)));
   // Clusters of eight CTAs where a warp has at most kClusterSteps steps even of a full
   // table, and all clusters fit at once: longer steps then cost less than another launch
@@ -280,7 +288,9 @@ cudaError_t launch_attend(const AttendParts& S, bool merge, cudaStream_t st) {
   const CacheJob& J = A.c;
   cudaError_t e = cudaSuccess;
   if (S.c.uoff[J.B]) {
-    e = J.bf16 ? launch_attend_chunk(A, S.c, st) : launch_attend_simt(A, S.c, st);
+    e = S.common ? launch_common_umma(A, S.c, st)
+        : J.bf16 ? launch_attend_chunk(A, S.c, st)
+                 : launch_attend_simt(A, S.c, st);
     if (e == cudaSuccess && merge) e = launch_merge(A, S.c, st);
   }
   if (e == cudaSuccess && S.t.uoff[J.B]) {
@@ -292,7 +302,7 @@ cudaError_t launch_attend(const AttendParts& S, bool merge, cudaStream_t st) {
 
 cudaError_t launch_attend(const AttendJob& A, void* scratch, cudaStream_t st) {
   AttendParts S;
-  const cudaError_t e = attend_parts(A, scratch, 0, &S);
+  const cudaError_t e = attend_parts(A, scratch, 0, false, &S);
   return e == cudaSuccess ? launch_attend(S, true, st) : e;
 }
 

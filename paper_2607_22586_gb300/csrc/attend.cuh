@@ -257,9 +257,11 @@ struct AttendParts {
   AttendPlan t, c;
   int32_t few;         // rows of a request's KV head up to which it is in t
   int32_t whole;       // t's units are all in A.part
+  int32_t common;      // c's keys are whole pages that all rows see
 };
-// The plans of a call (few: 0 for what attention itself takes), and the call with or without its merges.
-cudaError_t attend_parts(const AttendJob& A, void* scratch, int few, AttendParts* S);
+// The plans of a call (few: 0 for what attention itself takes; common: of pages that a group's sequences
+// share), and the call with or without its merges.
+cudaError_t attend_parts(const AttendJob& A, void* scratch, int few, bool common, AttendParts* S);
 cudaError_t launch_attend(const AttendParts& S, bool merge, cudaStream_t st);
 
 // What a row's sum is found by: its request's first token and rows of a KV head, and of its plan.
@@ -337,6 +339,7 @@ cudaError_t launch_attend_token(const AttendJob& A, const AttendPlan& P, bool cl
 cudaError_t launch_attend_simt(const AttendJob& A, const AttendPlan& P, cudaStream_t st);
 cudaError_t launch_attend_chunk(const AttendJob& A, const AttendPlan& P, cudaStream_t st);
 cudaError_t launch_prompt_umma(const AttendJob& A, const AttendPlan& P, const PromptOrder& O, cudaStream_t st);
+cudaError_t launch_common_umma(const AttendJob& A, const AttendPlan& P, cudaStream_t st);
 cudaError_t launch_prompt_simt(const AttendJob& A, const AttendPlan& P, cudaStream_t st);
 
 }  // namespace mmshift

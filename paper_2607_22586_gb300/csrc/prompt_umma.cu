@@ -51,6 +51,7 @@ struct PromptRun {
   int s0, s1;
   int end[2];            // tiles [s0, end) are the block's: rows in front may see fewer keys
   int least;             // keys that every row sees
+  int seq;               // pages: the group's sequence
   int blocks, use;       // bit b: block b has rows; its Q is use + (blocks == 3 ? b : 0)
 };
 __device__ __forceinline__ bool has(const PromptRun& r, int b) { return r.blocks >> b & 1; }
@@ -149,7 +150,10 @@ __device__ __forceinline__ void store32(uint8_t* p, const uint32_t* w) {
                : "memory");
 }
 
-template <int D>
+// PAGED: K and V are pages of a cache, which every row of a group of requests sees as a whole (the
+// keys are whole pages, all in the pool): nothing is masked but what a box of no page fills with
+// zeros, and results are sums.
+template <int D, bool PAGED>
 __global__ void __launch_bounds__(PromptSmem<D>::NT, 1) attend_prompt_kernel(const __grid_constant__ CUtensorMap qmap,
                                                               const __grid_constant__ CUtensorMap kmap,
                                                               const __grid_constant__ CUtensorMap vmap,
@@ -256,6 +260,7 @@ __global__ void __launch_bounds__(PromptSmem<D>::NT, 1) attend_prompt_kernel(con
             r.slot = -1;
           }
         }
+        int seq = 0;
         while (!any && before < sp.end) {
           const AttendUnit U = attend_unit(A, P, nullptr, unit);
           const int64_t first = before;
@@ -265,13 +270,15 @@ __global__ void __launch_bounds__(PromptSmem<D>::NT, 1) attend_prompt_kernel(con
           any = r.s0 < r.s1;
           r.tok0 = J.off[U.b];
           r.h = U.h;
-          r.n = U.n;
+          r.n = PAGED ? U.keys : U.n;
+          seq = U.b * J.Hkv + U.h;
           r.row0 = U.row0;
           r.rows = U.rows;
           r.slot = r.s0 == 0 && r.s1 == U.pieces ? -1 : (int64_t)attend_slot(blockIdx.x, sp.begin, first) * P.rows;
         }
         if (any) {
-          r.least = keys_at(A, r, J.by_r(r.row0));
+          r.least = PAGED ? INT_MAX / 2 : keys_at(A, r, J.by_r(r.row0));
+          r.seq = seq;
           r.blocks = r.rows > A.block_rows ? 3 : 1 << (singles++ & 1);   // one block's rows: each in turn
           r.use = use;
           use += r.blocks == 3 ? 2 : 1;
@@ -292,18 +299,44 @@ __global__ void __launch_bounds__(PromptSmem<D>::NT, 1) attend_prompt_kernel(con
       while (ok && r.blocks) {
         ok = publish(n);                               // a run ahead, so that Q can be loaded
         const int row0 = r.tok0, col0 = r.h * D;
+        const int32_t* const table = PAGED ? cache_table(J, r.seq) : nullptr;
+        const int shift = PAGED ? min(J.page_shift, 7) : 7, boxes = BK >> shift;
+        const int outside = J.n_pages << J.page_shift;   // a box from there on reads zeros
+        // pages: a tile's boxes, asked for a tile ahead
+        int32_t entry[PAGED ? 8 : 1];
+        auto look_up = [&](int s) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int t = s * BK + (i << shift);
+            if (i < boxes) entry[PAGED ? i : 0] = s < r.s1 && t < r.n ? table[t >> J.page_shift] : -1;
+          }
+        };
+        if (PAGED && ok) look_up(r.s0);
         for (int s = r.s0; ok && s < r.s1; ++s) {
 #pragma unroll 1
           for (int kv = 0; kv < 2; ++kv) {
             if (!wait_one(&empty[stage], phase ^ 1u, abort_)) { ok = false; break; }
             mbar_expect_tx(&full[stage], SM::TILE);
+            const CUtensorMap* const map = kv ? &vmap : &kmap;
+            unsigned char* const to = ring + stage * SM::TILE;
+            if constexpr (PAGED) {
 #pragma unroll
-            for (int c = 0; c < SM::HALVES; ++c)
-              tma_load_3d(ring + stage * SM::TILE + c * SM::HALF, kv ? &vmap : &kmap, &full[stage], col0 + c * 64,
-                          row0 + s * BK, 0);
+              for (int i = 0; i < 8; ++i) {
+                if (i >= boxes) break;
+                const int got = page_row(entry[i], J.n_pages, J.page_shift, s * BK + (i << shift));
+#pragma unroll
+                for (int c = 0; c < SM::HALVES; ++c)
+                  tma_load_3d(to + c * SM::HALF + (i << shift) * 128, map, &full[stage], c * 64, got < 0 ? outside : got, 0);
+              }
+            } else {
+#pragma unroll
+              for (int c = 0; c < SM::HALVES; ++c)
+                tma_load_3d(to + c * SM::HALF, map, &full[stage], col0 + c * 64, row0 + s * BK, 0);
+            }
             armed.arm(stage, phase);
             if (++stage == SM::STAGES) { stage = 0; phase ^= 1u; }
           }
+          if (PAGED) look_up(s + 1);
         }
         r = n;
       }
@@ -441,9 +474,10 @@ __global__ void __launch_bounds__(PromptSmem<D>::NT, 1) attend_prompt_kernel(con
         if (!has(r, x)) continue;
         const uint32_t ph = oph >> x & 1u;
         const int lrow = fw * 32 + lane, brow = first_row(A, r, x) + lrow, row = r.row0 + brow;
-        const bool live = lrow < A.block_rows && brow < r.rows, whole = r.slot < 0;
+        const bool live = lrow < A.block_rows && brow < r.rows, whole = r.slot < 0, sums = PAGED || !whole;
         const int tok = J.by_r(row), j = row - tok * J.r;
-        const int64_t orow = (int64_t)(r.tok0 + tok) * J.Hq + r.h * J.r + j, slot = r.slot + brow;
+        const int64_t orow = (int64_t)(r.tok0 + tok) * J.Hq + r.h * J.r + j, slot = whole ? orow : r.slot + brow;
+        float* const po = PAGED && whole ? A.part : P.po;
         const uint32_t ocol = tmem + lanes + SM::O_COL + x * SM::O_STRIDE;
         if (!wait_all(&l_ready[x], ph, abort_) || !wait_all(&o_ready[x], ph, abort_)) { ok = false; break; }
         oph ^= 1u << x;
@@ -452,7 +486,7 @@ __global__ void __launch_bounds__(PromptSmem<D>::NT, 1) attend_prompt_kernel(con
         const float m = t.x, l = t.y;
         // set by this warp's lanes or those beside it, before they reported a tile clean whose product
         // is in O by now
-        const bool fix = *reinterpret_cast<volatile int*>(&hd.odd_flag) != 0;
+        const bool fix = !PAGED && *reinterpret_cast<volatile int*>(&hd.odd_flag) != 0;
         const float f = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll 1
         for (int i = 0; i < D; i += 32) {
@@ -466,8 +500,8 @@ __global__ void __launch_bounds__(PromptSmem<D>::NT, 1) attend_prompt_kernel(con
             if (lane == 0) mbar_arrive(&o_free[x]);
           }
           if (!live) continue;
-          if (fix) add_not_finite<D>(A, r, tok, j, m == -INFINITY ? 0.f : m, i, o);
-          if (whole) {
+          if (!PAGED && fix) add_not_finite<D>(A, r, tok, j, m == -INFINITY ? 0.f : m, i, o);
+          if (!sums) {
             uint8_t* const to = A.out + (orow * D + i) * 2;
 #pragma unroll
             for (int c = 0; c < 32; c += 16) {
@@ -484,11 +518,11 @@ __global__ void __launch_bounds__(PromptSmem<D>::NT, 1) attend_prompt_kernel(con
           } else {
 #pragma unroll
             for (int c = 0; c < 32; c += 8)
-              store32(reinterpret_cast<uint8_t*>(P.po + slot * D + i + c), reinterpret_cast<const uint32_t*>(o + c));
+              store32(reinterpret_cast<uint8_t*>(po + slot * D + i + c), reinterpret_cast<const uint32_t*>(o + c));
           }
         }
         if (live) {
-          if (!whole) P.pml[slot] = t;
+          if (sums) (PAGED && whole ? A.part_ml : P.pml)[slot] = t;
           else if (A.lse) A.lse[orow] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
         }
       }
@@ -700,29 +734,40 @@ __global__ void __launch_bounds__(PromptSmem<D>::NT, 1) attend_prompt_kernel(con
   if (threadIdx.x == 0 && hd.abort_flag) set_status(J.status, kStatusTimeout);
 }
 
-template <int D>
+template <int D, bool PAGED>
 cudaError_t launch(const AttendJob& A, const AttendPlan& P, const PromptOrder& O, cudaStream_t st) {
   using SM = PromptSmem<D>;
   const CacheJob& J = A.c;
   CUtensorMap qmap, kmap, vmap;
-  const uint64_t rows = J.off[J.B], cols = (uint64_t)J.Hkv * D, pitch = A.kv_stride * 2;
-  if (!make_tmap_bf16_3d(&kmap, J.kp, cols, rows, 1, pitch, rows * pitch, BK) ||
-      !make_tmap_bf16_3d(&vmap, J.vp, cols, rows, 1, pitch, rows * pitch, BK))
-    return cudaErrorInvalidValue;
+  auto make = [&](CUtensorMap* m, const void* base) {
+    if (PAGED) {
+      const uint64_t rows = (uint64_t)J.n_pages << J.page_shift;
+      return make_tmap_bf16_3d(m, base, D, rows, 1, D * 2, rows * D * 2, std::min(1 << J.page_shift, BK));
+    }
+    const uint64_t rows = J.off[J.B], cols = (uint64_t)J.Hkv * D, pitch = A.kv_stride * 2;
+    return make_tmap_bf16_3d(m, base, cols, rows, 1, pitch, rows * pitch, BK);
+  };
+  if (!make(&kmap, J.kp) || !make(&vmap, J.vp)) return cudaErrorInvalidValue;
   qmap = kmap;                                           // not used where Q's rows are copied
   if (A.qvec && J.r <= BQ &&
-      !make_tmap_bf16_box(&qmap, A.q, D, J.Hq, rows, D * 2, J.stride * 2, J.r, A.block_rows / J.r))
+      !make_tmap_bf16_box(&qmap, A.q, D, J.Hq, J.off[J.B], D * 2, J.stride * 2, J.r, A.block_rows / J.r))
     return cudaErrorInvalidValue;
   const cudaError_t e =
-      cudaFuncSetAttribute(attend_prompt_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, SM::BYTES);
+      cudaFuncSetAttribute(attend_prompt_kernel<D, PAGED>, cudaFuncAttributeMaxDynamicSharedMemorySize, SM::BYTES);
   if (e != cudaSuccess) return e;
-  return launch_kernel(attend_prompt_kernel<D>, dim3(P.workers), SM::NT, SM::BYTES, st, true, 0, qmap, kmap, vmap, A, P, O);
+  return launch_kernel(attend_prompt_kernel<D, PAGED>, dim3(P.workers), SM::NT, SM::BYTES, st, true, 0, qmap, kmap, vmap, A, P,
+                       O);
 }
 
 }  // namespace
 
 cudaError_t launch_prompt_umma(const AttendJob& A, const AttendPlan& P, const PromptOrder& O, cudaStream_t st) {
-  return A.c.d == 128 ? launch<128>(A, P, O, st) : launch<64>(A, P, O, st);
+  return A.c.d == 128 ? launch<128, false>(A, P, O, st) : launch<64, false>(A, P, O, st);
+}
+
+cudaError_t launch_common_umma(const AttendJob& A, const AttendPlan& P, cudaStream_t st) {
+  const PromptOrder O = {};
+  return A.c.d == 128 ? launch<128, true>(A, P, O, st) : launch<64, true>(A, P, O, st);
 }
 
 }  // namespace mmshift

@@ -56,7 +56,8 @@ __device__ __forceinline__ void shared_start() {
 }
 
 // A cluster a group and KV head: how many pages all its sequences with rows in the call have
-// in common. Only keys that every row attends to count, and requests alone have none. Warps
+// in common, up to an entry that is no page. Only keys that every row attends to count, and requests
+// alone have none. Warps
 // compare 32 places of the table at a time, eight requests at once (64 requests of 375 pages, 8 heads:
 // 15 us by one CTA each).
 __global__ void __launch_bounds__(256) common_pages_kernel(const __grid_constant__ SharedJob S) {
@@ -92,7 +93,7 @@ __global__ void __launch_bounds__(256) common_pages_kernel(const __grid_constant
   for (int e = rank * 32 + lane; e - lane < most; e += kCluster * 32) {
     if (e >= most) continue;
     const int32_t is = lead[e];
-    bool same = true;
+    bool same = is >= 0 && is < J.n_pages;
 #pragma unroll 8
     for (int b = first + 1 + warp; b < b1; b += 8)
       same &= J.off[b + 1] == J.off[b] || J.table[((size_t)b * J.Hkv + h) * J.max_pages + e] == is;
@@ -286,7 +287,7 @@ mmshift_status mmshift_cache_attention_shared(const mmshift_shape* s, const mmsh
     A[i].part_ml = P.ml[i];
     A[i].c.at = P.at[i];
     A[i].c.lens = P.lens[i];
-    const cudaError_t e = attend_parts(A[i], P.scratch[i], i ? kOwnRows : 0, &N.part[i]);
+    const cudaError_t e = attend_parts(A[i], P.scratch[i], i ? kOwnRows : 0, i == 0, &N.part[i]);
     if (e != cudaSuccess) return noalloc_cuda_fail(e);
     for (int b = 0; b < A[i].c.B; ++b) S.row[i][b] = attend_rows(N.part[i], b);
   }
