@@ -23,7 +23,7 @@ class Driver:
         P = self.P
         full = self.shape([P.page * P.max_pages] * P.B)
         self.n = M.mmshift_cache_pages_workspace_size(full, P.struct())
-        self.ws = torch.full((self.n,), 0xA5, dtype=torch.uint8, device="cuda")   # only the status word is zero
+        self.ws = torch.full((self.n + 512,), 0xA5, dtype=torch.uint8, device="cuda")   # only the status word is zero
         self.ws[:256].zero_()
 
     def shape(self, new, stride=0):
@@ -66,6 +66,7 @@ class Driver:
         P.compact(idx.tolist(), rows, counts)
 
     def poll(self):
+        assert (self.ws[self.n:] == 0xA5).all()
         return M.mmshift_poll_status(self.ws)
 
 
@@ -289,3 +290,34 @@ def test_the_class():
     for bad in (lambda: cache.fork([0], [0]), lambda: cache.fork([0, 0], [1, 1]), lambda: cache.fork([0, 1], [1, 0])):
         with pytest.raises(M.MMShiftError):
             bad()
+
+
+def test_compaction_without_free_pages():
+    """Rows whose shared pages nothing can replace are lost; the other holder keeps them."""
+    D = Driver(1, 2, 1, 64, "f32", 16, 5, 4, dtype="f32")
+    D.append([60, 0])
+    D.fork([0], [1])
+    D.compact([0, 40], rng=random.Random(4))       # three pages wanted, one free
+    assert D.P.exhausted
+    D.P.check("first page kept")
+    assert D.poll() == M._lib.MMSHIFT_ERR_DEVICE
+    D.free([0])
+    D.P.check("freed")
+    assert D.poll() == M._lib.MMSHIFT_OK
+
+
+def test_pages_past_four_gigabytes():
+    """Sequences whose pages are the pool's last."""
+    D = Driver(1, 2, 1, 128, "f32", 256, 36000, 4, dtype="f32")
+    P = D.P
+    assert (P.n_pages - 12) * 256 * 128 * 4 > 2 ** 32
+    P.refs[:P.n_pages - 12] = 1                    # held by others
+    P.m_refs[:P.n_pages - 12] = [1] * (P.n_pages - 12)
+    D.append([700, 0])
+    D.fork([0], [1])
+    D.append([3, 300])
+    D.compact([0, 450], rng=random.Random(6))
+    D.compact([333, 0], rng=random.Random(7))
+    assert P.table[P.table >= 0].min() >= P.n_pages - 12 and not P.exhausted
+    P.check("last pages")
+    assert D.poll() == M._lib.MMSHIFT_OK

@@ -69,11 +69,14 @@ def rows(cu, hq, hkv, d, dtype, seed=0, spread=1.0, strided=False):
 
 def run(q, k, v, cu, causal=True, scale=0.0, status=M._lib.MMSHIFT_OK):
     at = PromptAttention(q.shape[1], k.shape[1], q.shape[2], q.dtype, cu)
-    at._workspace[256:].fill_(0xA5)                # only the status word is zero
+    n = at._ws_bytes
+    at._workspace = torch.full((n + 512,), 0xA5, dtype=torch.uint8, device="cuda")   # only the status word is zero
+    at._workspace[:256].zero_()
     out = torch.full(q.shape, math.nan, dtype=q.dtype, device="cuda")
     lse = torch.full(q.shape[:2], math.nan, device="cuda")
     at(q, k, v, causal, scale, out=out, lse=lse)
     assert M.mmshift_poll_status(at._workspace) == status
+    assert (at._workspace[n:] == 0xA5).all()
     return out, lse
 
 
@@ -211,3 +214,25 @@ def test_repeated_calls_are_equal():
     for _ in range(3):
         b = run(*x, cu)
         assert R.same(a[0], b[0]) and R.same(a[1], b[1])
+
+
+def test_more_heads_than_a_block_has_rows():
+    """A token's query heads in several blocks."""
+    for hq, d, lens in ((130, 64, [3, 40]), (200, 128, [17])):
+        cu = R.cu_of(lens)
+        x = rows(cu, hq, 1, d, "bf16", seed=14)
+        R.check_attention(run(*x, cu), reference(*x, cu, True), (hq, d))
+
+
+def test_rows_past_four_gigabytes():
+    lens, hq, hkv, d, width = [33000, 130], 2, 1, 64, 70000
+    cu = R.cu_of(lens)
+    buf = torch.empty((cu[-1], width), dtype=torch.bfloat16, device="cuda")
+    assert buf[-130:].data_ptr() - buf.data_ptr() > 2 ** 32
+    gen = torch.Generator(device="cuda").manual_seed(15)
+    at = width - (hq + 2 * hkv) * d
+    buf[:, at:] = torch.randn((cu[-1], width - at), generator=gen, device="cuda").bfloat16()
+    q, k, v = (x.unflatten(-1, (-1, d)) for x in buf[:, at:].split([hq * d, hkv * d, hkv * d], -1))
+    out, lse = run(q, k, v, cu)
+    want = reference(q[-130:], k[-130:], v[-130:], [0, 130], True)
+    R.check_attention((out[-130:], lse[-130:]), want)

@@ -28,12 +28,13 @@ def attend(cache, q, new, groups, causal=True, scale=0.0, status=M._lib.MMSHIFT_
     struct, cu = cache.struct(0), R.cu_of(groups)
     shape = R.shape_of(cache, new, q.shape[1], "bf16" if q.dtype == torch.bfloat16 else "f32", layers=1)
     n = M.mmshift_cache_shared_workspace_size(shape, struct, cu)
-    ws = torch.full((n,), 0xA5, dtype=torch.uint8, device="cuda")
+    ws = torch.full((n + 512,), 0xA5, dtype=torch.uint8, device="cuda")
     ws[:256].zero_()
     out = torch.full(q.shape, math.nan, dtype=q.dtype, device="cuda")
     ls = torch.full(q.shape[:2], math.nan, device="cuda") if lse else None
     M.check(M.mmshift_cache_attention_shared(shape, struct, cu, q, stride, int(causal), scale, out, ls, ws, n), "attention_shared")
     assert M.mmshift_poll_status(ws) == status
+    assert (ws[n:] == 0xA5).all()
     return out, ls
 
 
@@ -177,3 +178,23 @@ def test_captured_and_replayed():
         if step == 0:
             cache.table[0, 1, :, 1] = cache.table[0, 2, :, 4]     # no longer the same page
     assert M.mmshift_poll_status(ws) == M._lib.MMSHIFT_OK
+
+
+def test_a_full_batch_and_strided_queries():
+    new = [1 + b % 3 for b in range(64)]
+    cache = R.Cache([[[150 + b, 140 + 2 * b] for b in range(64)]], 64, "bf16", 32).fill_random()
+    groups = [30, 1, 33]
+    share(cache, groups, [4, 0, [4, 3]])
+    wide = queries(new, 10, 64, "bf16")
+    q = wide[:, :6]
+    for causal in (True, False):
+        check(attend(cache, q, new, groups, causal, stride=wide.stride(0)), R.reference(cache, q, new, causal), causal)
+
+
+def test_scales_and_no_lse():
+    new = [2, 3, 1]
+    cache = R.Cache([[[200], [190], [170]]], 64, "bf16", 16).fill_random()
+    share(cache, [3], [9])
+    q = queries(new, 40, 64, "bf16")
+    check(attend(cache, q, new, [3], scale=0.3), R.reference(cache, q, new, scale=0.3))
+    assert R.same(attend(cache, q, new, [3], lse=False)[0], attend(cache, q, new, [3])[0])
