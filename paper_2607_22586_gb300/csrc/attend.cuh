@@ -166,8 +166,8 @@ __device__ __forceinline__ int attend_slot(int worker, int64_t begin, int64_t be
 }
 
 // Four values of an output row from its sums; a row without weights is zeros.
-// `row` counts the rows of the request's KV head.
-template <typename T, int D>
+// `row` counts the rows of the request's KV head. PART: by a kernel whose sums may be wanted as they are.
+template <typename T, int D, bool PART = false>
 __device__ __forceinline__ void attend_write(const AttendJob& A, int b, int h, int row, int d0, float4 v, float top,
                                              float z) {
   const CacheJob& J = A.c;
@@ -176,7 +176,7 @@ __device__ __forceinline__ void attend_write(const AttendJob& A, int b, int h, i
   const float f = z == 0.f ? 0.f : 1.f / z;
   T* out = reinterpret_cast<T*>(A.out) + at * D + d0;
   if (z == 0.f) v = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (A.part) {
+  if (PART && A.part) {
     *reinterpret_cast<float4*>(A.part + at * D + d0) = v;
     if (d0 == 0) A.part_ml[at] = make_float2(top, z);
     return;

@@ -64,11 +64,15 @@ __device__ __forceinline__ float4 codes4(uint32_t x) {
                      __uint_as_float(__byte_perm(x, 0x4b000000u, 0x7443)) - k);
 }
 
-template <int D, bool I8, int NT, int TR, bool PROMPT>
+// What the rows are: of a cache's pages, of a prompt, or of pages with sums as results.
+enum { CACHE = 0, PROMPT_ROWS = 1, PARTS = 2 };
+
+template <int D, bool I8, int NT, int TR, int MODE>
 __global__ void __launch_bounds__(NT, 1)
     attend_simt_kernel(const __grid_constant__ AttendJob A, const __grid_constant__ AttendPlan P) {
   using SM = Simt<D, NT, TR>;
   constexpr int BK = SM::BK, NK = SM::NK;
+  constexpr bool PROMPT = MODE == PROMPT_ROWS;
   extern __shared__ __align__(16) unsigned char smraw[];
   typename SM::Smem& sm = *reinterpret_cast<typename SM::Smem*>(smraw);
   cache_start();
@@ -315,7 +319,7 @@ __global__ void __launch_bounds__(NT, 1)
           upk2(o[i][c][0], a.x, a.y);
           upk2(o[i][c][1], a.z, a.w);
           if (whole) {
-            attend_write<float, D>(A, U.b, U.h, U.row0 + r, d0, a, m[i], z);
+            attend_write<float, D, MODE == PARTS>(A, U.b, U.h, U.row0 + r, d0, a, m[i], z);
           } else {
             *reinterpret_cast<float4*>(P.po + (slot + r) * D + d0) = a;
             if (d0 == 0) P.pml[slot + r] = make_float2(m[i], z);
@@ -332,31 +336,37 @@ __global__ void __launch_bounds__(NT, 1)
   }
 }
 
-template <int D, bool I8, int NT, int TR, bool PROMPT = false>
+template <int D, bool I8, int NT, int TR, int MODE>
 cudaError_t launch(const AttendJob& A, const AttendPlan& P, cudaStream_t st) {
   constexpr int bytes = (int)sizeof(typename Simt<D, NT, TR>::Smem);
-  const auto kernel = attend_simt_kernel<D, I8, NT, TR, PROMPT>;
+  const auto kernel = attend_simt_kernel<D, I8, NT, TR, MODE>;
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
   if (e != cudaSuccess) return e;
   return launch_kernel(kernel, dim3(P.workers), NT, bytes, st, true, 0, A, P);
 }
 
-template <int D, bool I8>
+template <int D, bool I8, int MODE>
 cudaError_t launch_rows(const AttendJob& A, const AttendPlan& P, cudaStream_t st) {
-  if (P.rows <= 8) return launch<D, I8, 64, 2>(A, P, st);
-  if (P.rows <= 16) return launch<D, I8, 128, 2>(A, P, st);
-  return launch<D, I8, 256, 8>(A, P, st);
+  if (P.rows <= 8) return launch<D, I8, 64, 2, MODE>(A, P, st);
+  if (P.rows <= 16) return launch<D, I8, 128, 2, MODE>(A, P, st);
+  return launch<D, I8, 256, 8, MODE>(A, P, st);
+}
+
+template <int MODE>
+cudaError_t launch_pages(const AttendJob& A, const AttendPlan& P, cudaStream_t st) {
+  if (A.c.d == 128) return A.c.i8 ? launch_rows<128, true, MODE>(A, P, st) : launch_rows<128, false, MODE>(A, P, st);
+  return A.c.i8 ? launch_rows<64, true, MODE>(A, P, st) : launch_rows<64, false, MODE>(A, P, st);
 }
 
 }  // namespace
 
 cudaError_t launch_prompt_simt(const AttendJob& A, const AttendPlan& P, cudaStream_t st) {
-  return A.c.d == 128 ? launch<128, false, 256, 8, true>(A, P, st) : launch<64, false, 256, 8, true>(A, P, st);
+  return A.c.d == 128 ? launch<128, false, 256, 8, PROMPT_ROWS>(A, P, st)
+                      : launch<64, false, 256, 8, PROMPT_ROWS>(A, P, st);
 }
 
 cudaError_t launch_attend_simt(const AttendJob& A, const AttendPlan& P, cudaStream_t st) {
-  if (A.c.d == 128) return A.c.i8 ? launch_rows<128, true>(A, P, st) : launch_rows<128, false>(A, P, st);
-  return A.c.i8 ? launch_rows<64, true>(A, P, st) : launch_rows<64, false>(A, P, st);
+  return A.part ? launch_pages<PARTS>(A, P, st) : launch_pages<CACHE>(A, P, st);
 }
 
 }  // namespace mmshift

@@ -547,7 +547,7 @@ __global__ void __launch_bounds__(NT, NQ == 1 ? 3 : 2) attend_token_kernel(const
         *reinterpret_cast<float4*>(&sm.o[0][r][d0]) = acc;   // read by this thread alone
         if (d0 == 0) sm.part[r] = make_float2(top, z);
       } else if (whole) {
-        attend_write<__nv_bfloat16, D>(A, U.b, U.h, U.row0 + r, d0, acc, top, z);
+        attend_write<__nv_bfloat16, D, true>(A, U.b, U.h, U.row0 + r, d0, acc, top, z);
       } else {
         *reinterpret_cast<float4*>(P.po + (slot + r) * D + d0) = acc;
         if (d0 == 0) P.pml[slot + r] = make_float2(top, z);
@@ -577,7 +577,7 @@ __global__ void __launch_bounds__(NT, NQ == 1 ? 3 : 2) attend_token_kernel(const
           acc.z += b.x * f;
           acc.w += b.y * f;
         }
-        attend_write<__nv_bfloat16, D>(A, U.b, U.h, U.row0 + r, d0, acc, top, z);
+        attend_write<__nv_bfloat16, D, true>(A, U.b, U.h, U.row0 + r, d0, acc, top, z);
       }
       umma::cluster_sync();                            // the others have read this CTA's part
       at = sp.end;

@@ -77,6 +77,7 @@ struct AttendJob {
   float2* part_ml;               // [T * Hq] maximum (base 2) and sum of weights, to be joined with others
   int64_t kv_stride;             // prompts: elements between two tokens' rows of K and V
   int32_t block_rows;            // prompts: rows of a block, whole tokens where a token's heads fit
+  int32_t qbox;                  // prompts: Q's rows come as TMA boxes
   int32_t causal;
   int32_t qvec, ovec;            // rows of q / out allow 16-byte accesses
   float alpha;                   // scale * log2(e)

@@ -594,7 +594,7 @@ __global__ void __launch_bounds__(PromptSmem<D>::NT, 1) attend_prompt_kernel(con
         const uint32_t phase = (uint32_t)(use / SM::QS) & 1u;
         if (!wait_all(&q_empty[place], phase ^ 1u, abort_)) { ok = false; break; }
         unsigned char* const to = sm + place * SM::TILE;
-        if (A.qvec && J.r <= BQ) {                       // the block begins with a token's first head
+        if (A.qbox) {                                    // the block begins with a token's first head
           if (lane == 0) {
             mbar_expect_tx(&q_full[place], A.block_rows * D * 2);
 #pragma unroll
@@ -735,7 +735,7 @@ __global__ void __launch_bounds__(PromptSmem<D>::NT, 1) attend_prompt_kernel(con
 }
 
 template <int D, bool PAGED>
-cudaError_t launch(const AttendJob& A, const AttendPlan& P, const PromptOrder& O, cudaStream_t st) {
+cudaError_t launch(AttendJob A, const AttendPlan& P, const PromptOrder& O, cudaStream_t st) {
   using SM = PromptSmem<D>;
   const CacheJob& J = A.c;
   CUtensorMap qmap, kmap, vmap;
@@ -749,7 +749,8 @@ cudaError_t launch(const AttendJob& A, const AttendPlan& P, const PromptOrder& O
   };
   if (!make(&kmap, J.kp) || !make(&vmap, J.vp)) return cudaErrorInvalidValue;
   qmap = kmap;                                           // not used where Q's rows are copied
-  if (A.qvec && J.r <= BQ &&
+  A.qbox = A.qvec && J.r <= BQ && J.stride < (int64_t)1 << 38;
+  if (A.qbox &&
       !make_tmap_bf16_box(&qmap, A.q, D, J.Hq, J.off[J.B], D * 2, J.stride * 2, J.r, A.block_rows / J.r))
     return cudaErrorInvalidValue;
   const cudaError_t e =
