@@ -236,3 +236,13 @@ def test_rows_past_four_gigabytes():
     out, lse = run(q, k, v, cu)
     want = reference(q[-130:], k[-130:], v[-130:], [0, 130], True)
     R.check_attention((out[-130:], lse[-130:]), want)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("causal", [True, False])
+def test_many_units_a_worker(d, causal):
+    """Units of one and of two blocks, of one key tile and of several, one after the other."""
+    lens = [17, 300, 1, 500, 64, 333, 129, 5, 260, 2, 350, 90, 0, 18]
+    cu = R.cu_of(lens)
+    x = rows(cu, 112, 16, d, "bf16", seed=16, spread=2.0)
+    R.check_attention(run(*x, cu, causal), reference(*x, cu, causal), (d, causal))
