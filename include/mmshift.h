@@ -473,7 +473,8 @@ mmshift_status mmshift_cache_attention(const mmshift_shape* s, const mmshift_cac
  * cu_groups[n_groups] = batch, each of at least one request). The pages that all sequences of a
  * group's KV head have in common from position 0 on, as their table entries say, are read and multiplied
  * once for all rows of the group; each row's two parts are joined in float32. Where a group's
- * sequences have nothing in common, its rows just attend to their own. Workspace:
+ * sequences have nothing in common, its rows just attend to their own. batch * n_kv_heads is
+ * below 2^28. Workspace:
  * mmshift_cache_shared_workspace_size() bytes for that shape. */
 mmshift_status mmshift_cache_shared_workspace_size(const mmshift_shape* s, const mmshift_cache* c,
                                                    int32_t n_groups, const int32_t* cu_groups,
@@ -589,7 +590,8 @@ mmshift_status mmshift_rope(const mmshift_shape* s, const mmshift_rotary* r, con
  * logits, roundings and `scale` as in mmshift_cache_attention; requests may be empty, T * Hq is
  * at most 2^30, window and budgets are not read. Q [T, Hq, d], K and V [T, Hkv, d], tokens
  * q_row_stride and kv_row_stride elements apart (0 = dense); K and V start at multiples of
- * 16 bytes, kv_row_stride is a multiple of 16 bytes. out [T, Hq, d] dense; lse (nullable)
+ * 16 bytes, kv_row_stride is a multiple of 16 bytes (below 2^38 elements). out [T, Hq, d] dense,
+ * apart from the inputs; lse (nullable)
  * [T, Hq] float32. Workspace: mmshift_prompt_workspace_size() bytes, 256-byte aligned, status
  * word zero at first; what it holds besides that need not outlive the call. */
 mmshift_status mmshift_prompt_workspace_size(const mmshift_shape* s, size_t* bytes);

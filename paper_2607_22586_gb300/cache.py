@@ -292,11 +292,12 @@ class PagedKVCache:
         cu, n = self._groups[key]
         capturing = torch.cuda.is_current_stream_capturing()
         if self._shared is None or self._shared.numel() < n:
+            if capturing:
+                raise RuntimeError("attention in groups of so many tokens has to run once before it is captured")
             grown = torch.zeros(n, dtype=torch.uint8, device=self.device)
             if self._shared is not None:               # what calls have reported
                 grown[:256].copy_(self._shared[:256])
-                if not capturing:
-                    self._shared.record_stream(torch.cuda.current_stream())
+                self._shared.record_stream(torch.cuda.current_stream())
             self._shared = grown
         if capturing and not any(t is self._shared for t in self._captured):
             self._captured.append(self._shared)        # used by every replay

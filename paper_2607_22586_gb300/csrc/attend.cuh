@@ -16,6 +16,8 @@
 
 namespace mmshift {
 
+static_assert(kPromptRequests == MMSHIFT_MAX_BATCH, "requests of a call");
+
 // Where a worker's share begins: the unit with its first piece, the costs before that.
 struct AttendStart {
   int64_t before;

@@ -64,7 +64,8 @@ __global__ void __launch_bounds__(256) common_pages_kernel(const __grid_constant
   __shared__ int32_t common, first_, keys, members;
   const CacheJob& J = S.c;
   shared_start();
-  const int rank = cluster_rank(), g = blockIdx.x / kCluster, h = blockIdx.y, b0 = S.group[g], b1 = S.group[g + 1];
+  const int rank = cluster_rank(), g = J.by_heads(blockIdx.x / kCluster), h = blockIdx.x / kCluster - g * J.Hkv;
+  const int b0 = S.group[g], b1 = S.group[g + 1];
   const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
   if (tid == 0) {
     first_ = keys = INT_MAX;
@@ -217,6 +218,7 @@ mmshift_status shared_job(const mmshift_shape* s, const mmshift_cache* c, int32_
   const mmshift_status st = rows_job(s, c, ws, J);
   if (st != MMSHIFT_OK) return st;
   if (J->L != 1) return MMSHIFT_ERR_UNSUPPORTED;
+  if ((int64_t)J->B * J->Hkv * kCluster >= (int64_t)1 << 31) return MMSHIFT_ERR_UNSUPPORTED;   // blocks
   if (!cu_groups || n_groups < 1 || n_groups > J->B || cu_groups[0] != 0 || cu_groups[n_groups] != J->B)
     return MMSHIFT_ERR_INVALID_ARG;
   for (int g = 0; g < n_groups; ++g)
@@ -292,7 +294,7 @@ mmshift_status mmshift_cache_attention_shared(const mmshift_shape* s, const mmsh
     for (int b = 0; b < A[i].c.B; ++b) S.row[i][b] = attend_rows(N.part[i], b);
   }
   const cudaStream_t cs = (cudaStream_t)stream;
-  cudaError_t e = launch_kernel(common_pages_kernel, dim3(n_groups * kCluster, J.Hkv), 256, 0, cs, true, kCluster, S);
+  cudaError_t e = launch_kernel(common_pages_kernel, dim3((unsigned)n_groups * J.Hkv * kCluster), 256, 0, cs, true, kCluster, S);
   for (int i = 0; e == cudaSuccess && i < 2; ++i) e = launch_attend(N.part[i], false, cs);
   if (e == cudaSuccess) e = launch_join(N, cs);
   return e == cudaSuccess ? MMSHIFT_OK : noalloc_cuda_fail(e);

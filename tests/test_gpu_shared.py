@@ -198,3 +198,16 @@ def test_scales_and_no_lse():
     q = queries(new, 40, 64, "bf16")
     check(attend(cache, q, new, [3], scale=0.3), R.reference(cache, q, new, scale=0.3))
     assert R.same(attend(cache, q, new, [3], lse=False)[0], attend(cache, q, new, [3])[0])
+
+
+def test_a_first_call_is_not_captured():
+    """The workspace of so many tokens would belong to the graph."""
+    cache = PagedKVCache(8, 2, 64, torch.bfloat16, 2, 100, page_size=16, pages=20)
+    q = queries([1, 1], 8, 64, "bf16")
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        with pytest.raises(RuntimeError):
+            cache.attend(q, [1, 1], groups=[2])
+    cache.attend(q, [1, 1], groups=[2])
+    cache.poll()

@@ -94,6 +94,14 @@ def test_bad_shared_arguments(bad, code):
                                             a["lse"], a["ws"], a["n"]) == code
 
 
+def test_more_sequences_than_blocks_count():
+    s = _shape(n_q_heads=2 ** 27, n_kv_heads=2 ** 27, cu_seqlens=[0, 1, 1, 2])
+    assert M.mmshift_cache_attention_shared(s, _cache(), [0, 3], FAKE, 0, 1, 0.0, FAKE, None, FAKE, BIG) == UNSUPPORTED
+    with pytest.raises(M.MMShiftError) as e:
+        M.mmshift_cache_shared_workspace_size(s, _cache(), [0, 3])
+    assert e.value.code == UNSUPPORTED
+
+
 def test_the_class_refuses():
     make = lambda **kw: PagedKVCache(**{**dict(n_q_heads=4, n_kv_heads=2, head_dim=64, dtype=torch.bfloat16, batch=3,  # noqa: E731
                                                rows=40, page_size=16, device="cpu"), **kw})
