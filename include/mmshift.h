@@ -541,8 +541,8 @@ mmshift_status mmshift_cache_compact(const mmshift_shape* s, const mmshift_cache
  * Pair j < rot_dims / 2 of a head turns by w = positions * inv_freq[j]:
  *   x' = amplitude (x cos w - y sin w),  y' = amplitude (y cos w + x sin w)
  * with (x, y) dimensions (j, j + rot_dims / 2), or (2j, 2j + 1) interleaved; dimensions from
- * rot_dims on stay. Angles are exact to 2^-29 turns and float32's rounding at any position;
- * sums are float32, rounded once. */
+ * rot_dims on stay. Angles keep their fraction of a turn at any position: they are off by at most
+ * 2^-25 turns (their float32) and |position| 2^-53 (the frequency's); sums are float32, rounded once. */
 enum { MMSHIFT_ROPE_HALF = 0, MMSHIFT_ROPE_INTERLEAVED = 1 };
 typedef struct {
   int32_t layout;           /* MMSHIFT_ROPE_HALF or MMSHIFT_ROPE_INTERLEAVED */

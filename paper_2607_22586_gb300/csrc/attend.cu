@@ -253,8 +253,8 @@ cudaError_t launch_prompt(AttendJob& A, void* scratch, cudaStream_t st) {
     return e == cudaSuccess ? launch_merge(A, P, st) : e;
   }
   // Whole units where the workers' last ones differ by less than the merge of shared ones takes, about
-  // as long as six key tiles: 16 ragged prompts of 28 heads, 8 units a worker, 94 us (112 with shares);
-  // images of 16 heads, 2 units a worker, 43 (56).
+  // as long as six key tiles: 16 ragged prompts of 28 heads, 8 units a worker, 95 us (112 with shares);
+  // images of 16 heads, 2 units a worker, 42 (56).
   PromptOrder O = prompt_order(A.c.B, A.c.off, A.c.r, P.rows, A.c.Hkv, A.causal);
   O.whole = prompt_whole(O, A.c.off, A.c.r, P.rows, A.c.Hkv, A.causal, P.workers, P.extra, 6);
   const cudaError_t e = launch_prompt_umma(A, P, O, st);

@@ -5,7 +5,7 @@
 // Nothing else is kept (no list of free pages), so the state cannot disagree with itself,
 // and which page a sequence gets follows from the counts alone: free pages go out by
 // number, lowest first, in the order of the sequences and of their positions. Counting
-// and taking is one cluster's work: eight CTAs add up what their sequences need and
+// and taking is one CTA's work, or a cluster's: eight CTAs add up what their sequences need and
 // which of their pages are free, and exchange sums through distributed shared memory.
 // The counts of 200,000 pages are 0.8 MB, which the cluster reads from the L2 twice, and only
 // where some sequence needs a page.
@@ -343,13 +343,13 @@ struct MoveShape {
 
 template <int ROWB, bool I8>
 __global__ void __launch_bounds__(kMoveThreads) move_rows_kernel(const __grid_constant__ PagesJob G,
-                                                                 const int32_t* idx, int clustered) {
+                                                                 const int32_t* idx, int ctas) {
   using S = MoveShape<ROWB, I8>;
   constexpr int PER = (S::ROWS + kMoveThreads - 1) / kMoveThreads;
   __shared__ int32_t from[3][S::ROWS], to[3][S::ROWS];
   const CacheJob& J = G.c;
   pages_start();
-  const int rank = clustered ? cluster_rank() : 0, ctas = clustered ? kCluster : 1;
+  const int rank = ctas > 1 ? cluster_rank() : 0;
   const int unit = blockIdx.x / ctas, l = blockIdx.z;
   // the requests that have rows, packed
   int b = 0, skip = J.by_heads(unit);
@@ -418,7 +418,7 @@ __global__ void __launch_bounds__(kMoveThreads) move_rows_kernel(const __grid_co
     }
   };
   auto sync = [&] {                                    // every read before it is done, every place looked up
-    if (clustered) cluster_sync();
+    if (ctas > 1) cluster_sync();
     else __syncthreads();
   };
   const int chunks = (kept + step - 1) / step;
@@ -495,9 +495,11 @@ mmshift_status pages_job(const mmshift_shape* s, const mmshift_cache* c, int32_t
 template <bool COMPACT>
 cudaError_t launch_take(const PagesJob& G, cudaStream_t st) {
   // One CTA where its threads see two sequences at most and a few pages: a cluster's barriers take
-  // 1 to 2 us each.
+  // 1 to 2 us each. A page for each of 112 sequences, lengths and copies of the state with it: of
+  // 8,000 pages 11.8 us by one CTA, 14.3 by a cluster; of 60,000 18.7 and 15.2; and for each of 12,288
+  // sequences of 150,000 pages 107 and 28.
   const int64_t U = (int64_t)G.c.L * G.c.B * G.c.Hkv;
-  if (U * G.group <= 2 * kTake && G.c.n_pages <= 64 * kTake)
+  if (U * G.group <= 2 * kTake && G.c.n_pages <= 32 * kTake)
     return launch_kernel(take_pages_kernel<COMPACT, 1>, dim3(1), kTake, 0, st, true, 0, G);
   return launch_kernel(take_pages_kernel<COMPACT, kCluster>, dim3(kCluster), kTake, 0, st, true, kCluster, G);
 }
@@ -512,10 +514,14 @@ cudaError_t launch_move(const PagesJob& G, const int32_t* idx, cudaStream_t st) 
     longest = std::max(longest, n);
   }
   const unsigned units = (unsigned)(requests * J.Hkv);
-  // Eight CTAs a sequence where they find places at once and have more than one chunk.
-  const bool clustered = (int64_t)units * J.L * 2 * kCluster <= 2 * 152 && longest > 2 * MoveShape<ROWB, I8>::ROWS;
-  return launch_kernel(move_rows_kernel<ROWB, I8>, dim3(units * (clustered ? kCluster : 1), 2, J.L), kMoveThreads, 0, st,
-                       true, clustered ? kCluster : 0, G, idx, clustered ? 1 : 0);
+  // As many CTAs a sequence as find places at once (three an SM) and have a chunk each: 16,000 of
+  // 32,000 rows of eight heads 53 us (a CTA a sequence 196), half of 4,100 rows of four heads and 28
+  // layers 37 (40).
+  int ctas = kCluster;
+  while (ctas > 1 && ((int64_t)units * J.L * 2 * ctas > 3 * 152 || longest <= ctas / 2 * MoveShape<ROWB, I8>::ROWS))
+    ctas /= 2;
+  return launch_kernel(move_rows_kernel<ROWB, I8>, dim3(units * ctas, 2, J.L), kMoveThreads, 0, st, true,
+                       ctas > 1 ? ctas : 0, G, idx, ctas);
 }
 
 // The pairs of a fork, or what is to be given back.

@@ -16,7 +16,7 @@
 // TMA box of their heads fills it; rows behind them are computed and dropped.
 // The issuer's loop has conditions and bounds that the compiler knows to be the same in all lanes, or
 // descriptors would go from vector to uniform registers one by one: the tensor cores would wait for
-// instructions (32,768 tokens of 28 heads: 6.33 instead of 4.8 to 5.0 ms). What all roles need of a run
+// instructions (32,768 tokens of 28 heads: 6.33 instead of 4.9 to 5.3 ms). What all roles need of a run
 // is in shared memory, and their code is kept short: it is fetched again and again.
 // K's and V's rows are tokens apart: a tile is one box of 128 rows. Rows behind a prompt's last
 // are the next prompt's: a zero weight times a NaN there would be a NaN, so in tiles that hold

@@ -111,6 +111,18 @@ def test_compaction_of_long_sequences(kind, d, rows, keep):
         assert D.poll() == M._lib.MMSHIFT_OK
 
 
+@pytest.mark.parametrize("kind,d", [("bf16", 128), ("i8", 128), ("f32", 64)])
+@pytest.mark.parametrize("L,B,H", [(1, 4, 7), (3, 3, 9), (2, 5, 5)])
+def test_compaction_by_few_blocks_a_sequence(kind, d, L, B, H):
+    """Four blocks a sequence, two, and four of layers; lengths that differ, one empty."""
+    D = Driver(L, B, H, d, kind, 16, L * B * H * 44, 44, hq=1, dtype="f32" if kind == "f32" else "bf16")
+    lens = [[643, 0, 300, 129, 64], [500, 431, 17, 1, 256]][B % 2][:B]
+    D.append(lens)
+    D.compact([n * 2 // 3 for n in lens], rng=random.Random(7))
+    D.P.check((L, B, H))
+    assert D.poll() == M._lib.MMSHIFT_OK
+
+
 def test_shared_pages_are_not_compacted_in_place():
     D = Driver(1, 3, 2, 64, "bf16", 16, 60, 9)
     D.append([100, 0, 0])
