@@ -32,6 +32,15 @@ def _token_stride(t: torch.Tensor) -> int:
     return t.stride(-3) if t.shape[-3] > 1 else heads * d
 
 
+def _layer_stride(t: torch.Tensor, layers: int) -> int:
+    """The elements between two layers of t [L, T, heads, d], 0 for a single one."""
+    if layers == 1 or not t.numel():
+        return 0
+    if t.stride(0) < (t.shape[-3] - 1) * _token_stride(t) + t.shape[-2] * t.shape[-1]:
+        raise ValueError("layers must not overlap")
+    return t.stride(0)
+
+
 class Rotary:
     """Rotation of heads of ``head_dim`` to positions: the first ``rot_dims`` of them (0 = all) in
     pairs (j, j + rot_dims / 2) or, ``interleaved``, (2j, 2j + 1). ``sections``: consecutive pairs
@@ -80,7 +89,7 @@ class Rotary:
     def _rotate(self, q, k, hq, hkv, layers, total, positions, in_place, inverse):
         rotary = L.make_rotary(self.inv_freq, positions, self.layout, self.sections, self.amplitude, inverse)
         shape = L.make_shape(hq, hkv, self.head_dim, 2, _DT[q.dtype], [0, total], [1], n_layers=layers)
-        strides = [(_token_stride(t), t.stride(0) if layers > 1 else 0) if t is not None else (0, 0) for t in (q, k)]
+        strides = [(_token_stride(t), _layer_stride(t, layers)) if t is not None else (0, 0) for t in (q, k)]
         with _on(q.device):
             outs = [t if t is None or in_place else torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k)]
             L.check(L.mmshift_rope(shape, rotary, q, *strides[0], k, *strides[1], *outs, torch.cuda.current_stream()),

@@ -160,3 +160,14 @@ def test_classes_refuse():
                     (rows(4), rows(2), rows(4)[:, ::2]), (rows(4), rows(4)[:, :2], rows(2))):
         with pytest.raises(ValueError):
             at(q, k, v)
+
+
+def test_layers_that_overlap_are_refused():
+    """A layer stride of 0, one tensor for all layers, is no dense one. (Rotary._rotate: behind
+    the check for rows of a GPU.)"""
+    r, p = Rotary(64), torch.zeros(3, dtype=torch.int32)
+    x = torch.zeros(5, 3, 2, 64)
+    for t in (x[0].expand(5, 3, 2, 64), x[:, :1].expand(5, 3, 2, 64), torch.zeros(2000).as_strided((5, 3, 2, 64), (380, 128, 64, 1))):
+        for q, k in ((t, None), (x, t)):
+            with pytest.raises(ValueError):
+                r._rotate(q, k, 2, 2, 5, 3, p, False, False)
