@@ -294,7 +294,8 @@ cudaError_t launch_attend(const AttendParts& S, bool merge, cudaStream_t st) {
     if (e == cudaSuccess && merge) e = launch_merge(A, S.c, st);
   }
   if (e == cudaSuccess && S.t.uoff[J.B]) {
-    e = J.bf16 ? launch_attend_token(A, S.t, S.whole, st) : launch_attend_simt(A, S.t, st);
+    const bool overlap = merge || !(S.behind || S.c.uoff[J.B]);
+    e = J.bf16 ? launch_attend_token(A, S.t, S.whole, overlap, st) : launch_attend_simt(A, S.t, st);
     if (e == cudaSuccess && merge && !S.whole) e = launch_merge(A, S.t, st);
   }
   return e;

@@ -260,6 +260,7 @@ struct AttendParts {
   int32_t few;         // rows of a request's KV head up to which it is in t
   int32_t whole;       // t's units are all in A.part
   int32_t common;      // c's keys are whole pages that all rows see
+  int32_t behind;      // the kernel in front has tiles of other parts
 };
 // The plans of a call (few: 0 for what attention itself takes; common: of pages that a group's sequences
 // share), and the call with or without its merges.
@@ -337,7 +338,7 @@ __device__ __forceinline__ void sum_of_row(const AttendParts& S, const AttendRow
   }
 }
 
-cudaError_t launch_attend_token(const AttendJob& A, const AttendPlan& P, bool cluster, cudaStream_t st);
+cudaError_t launch_attend_token(const AttendJob& A, const AttendPlan& P, bool cluster, bool overlap, cudaStream_t st);
 cudaError_t launch_attend_simt(const AttendJob& A, const AttendPlan& P, cudaStream_t st);
 cudaError_t launch_attend_chunk(const AttendJob& A, const AttendPlan& P, cudaStream_t st);
 cudaError_t launch_prompt_umma(const AttendJob& A, const AttendPlan& P, const PromptOrder& O, cudaStream_t st);

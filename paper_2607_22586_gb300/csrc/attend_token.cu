@@ -594,18 +594,17 @@ __global__ void __launch_bounds__(NT, NQ == 1 ? 3 : 2) attend_token_kernel(const
 
 }  // namespace
 
-cudaError_t launch_attend_token(const AttendJob& A, const AttendPlan& P, bool cluster, cudaStream_t st) {
+cudaError_t launch_attend_token(const AttendJob& A, const AttendPlan& P, bool cluster, bool overlap, cudaStream_t st) {
   const CacheJob& J = A.c;
-  // The balanced form is no programmatic dependent: behind a kernel that has all of an SM's shared
-  // memory (a matrix product, the chunks' and prompts' kernels) its CTAs would come to an SM that is never
-  // idle in between and seems to keep that split, with little L1 for loads in flight, whatever split the
-  // launch prefers. 64 requests of one token, 64/8 heads, bfloat16, after a library product: 25,265 rows
-  // 638 us (as a dependent 1,107), 1,329 rows 67 (91); alone 653 (653), 64.7 (64.6). A dependent
-  // saves up to 0.5 us of 40.
+  // Not as a programmatic dependent (`overlap`) behind a kernel that has all of an SM's shared memory: its
+  // CTAs would come to an SM that is never idle in between and seems to keep that split, with little L1
+  // for loads in flight, whatever split the launch prefers. 64 requests of one token over 1,265 rows,
+  // 64/8 heads, bfloat16, after the pages they share: 66 us (82); without such a kernel in front a
+  // dependent saves 2 us.
   auto go = [&](auto whole, auto parts) {
     if (cluster)
-      return launch_kernel(parts, dim3(P.uoff[J.B] * kCluster), NT, 0, st, true, kCluster, A, P);
-    return launch_kernel(whole, dim3(P.workers), NT, 0, st, false, 0, A, P);
+      return launch_kernel(parts, dim3(P.uoff[J.B] * kCluster), NT, 0, st, overlap, kCluster, A, P);
+    return launch_kernel(whole, dim3(P.workers), NT, 0, st, overlap, 0, A, P);
   };
 #define MMSHIFT_TOKEN(D, I8, NQ) go(attend_token_kernel<D, I8, NQ, false>, attend_token_kernel<D, I8, NQ, true>)
   if (P.rows <= 8) {

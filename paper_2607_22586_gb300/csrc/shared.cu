@@ -292,6 +292,7 @@ mmshift_status mmshift_cache_attention_shared(const mmshift_shape* s, const mmsh
     A[i].c.lens = P.lens[i];
     const cudaError_t e = attend_parts(A[i], P.scratch[i], i ? kOwnRows : 0, i == 0, &N.part[i]);
     if (e != cudaSuccess) return noalloc_cuda_fail(e);
+    if (i) N.part[1].behind = N.part[0].c.uoff[A[0].c.B] > 0 && N.part[0].t.uoff[A[0].c.B] == 0;
     for (int b = 0; b < A[i].c.B; ++b) S.row[i][b] = attend_rows(N.part[i], b);
   }
   const cudaStream_t cs = (cudaStream_t)stream;
