@@ -167,7 +167,7 @@ bool turns_of(const double* f, int n, uint64_t* turn) {
   for (int j = 0; j < n; ++j) {
     if (!std::isfinite(f[j])) return false;
     const double x = f[j] / kTurn, frac = x - std::floor(x);
-    turn[j] = frac < 1.0 ? (uint64_t)std::ldexp(frac, 64) : 0;
+    turn[j] = frac < 1.0 ? (uint64_t)(frac * 0x1p64) : 0;
   }
   return true;
 }
