@@ -21,11 +21,13 @@ mmshift_status noalloc_cuda_fail(cudaError_t e);
 
 namespace {
 
+using umma::cluster_arrive;
 using umma::cluster_rank;
 using umma::cluster_sync;
-using umma::ld_cluster_int;
+using umma::cluster_wait;
 using umma::mapa;
 using umma::smem_u32;
+using umma::st_cluster_int;
 
 constexpr int kCluster = 8;            // CTAs that compare a group's tables
 
@@ -35,6 +37,7 @@ struct SharedJob {
   int64_t* at[2];                      // of the groups' common pages, of the requests' own
   int32_t* lens[2];                    // [n_groups][Hkv], [batch][Hkv]
   int32_t group[MMSHIFT_MAX_BATCH + 1];   // first requests
+  int32_t lead[MMSHIFT_MAX_BATCH];     // of each group the first with rows, -1 where it is the only one
   AttendRows row[2][MMSHIFT_MAX_BATCH];   // of the groups, of the requests
   AttendRows* rows;                    // the same, in device memory
   int32_t* place;                      // [T] of each token: group << 16 | request
@@ -57,19 +60,37 @@ __device__ __forceinline__ void shared_start() {
 
 // A cluster a group and KV head: how many pages all its sequences with rows in the call have
 // in common, up to an entry that is no page. Only keys that every row attends to count, and requests
-// alone have none. Warps
-// compare 32 places of the table at a time, eight requests at once (64 requests of 375 pages, 8 heads:
-// 15 us by one CTA each).
+// alone have none. Warps compare 32 places of the table at a time, eight requests at once (64
+// requests of 375 pages, 8 heads: 15 us by one CTA each). It is a chain of loads that are not in the L2
+// after a pass over the cache, so the first places are asked for together with the lengths, which say
+// how many of them count (12.5 -> 6.4 us).
 __global__ void __launch_bounds__(256) common_pages_kernel(const __grid_constant__ SharedJob S) {
-  __shared__ int32_t common, first_, keys, members;
+  constexpr int AHEAD = 2, MOST = MMSHIFT_MAX_BATCH / 8;   // places of a lane at first; requests of a warp
+  __shared__ int32_t common, keys, found[kCluster];
   const CacheJob& J = S.c;
   shared_start();
   const int rank = cluster_rank(), g = J.by_heads(blockIdx.x / kCluster), h = blockIdx.x / kCluster - g * J.Hkv;
-  const int b0 = S.group[g], b1 = S.group[g + 1];
+  const int b0 = S.group[g], b1 = S.group[g + 1], lead = S.lead[g], first = max(lead, b0);
   const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
-  if (tid == 0) {
-    first_ = keys = INT_MAX;
-    members = 0;
+  if (tid == 0) common = keys = INT_MAX;
+  __syncwarp();
+  cluster_arrive();                                    // all CTAs are there before one writes to another
+  const int own = b0 + tid;
+  const bool mine = own < b1;
+  const int len = mine ? cache_len(J, (size_t)own * J.Hkv + h) : 0;
+  auto entry = [&](int b, int e) { return J.table[((size_t)b * J.Hkv + h) * J.max_pages + e]; };
+  auto rows_in = [&](int b) { return J.off[b + 1] > J.off[b]; };
+  int32_t is[AHEAD], other[AHEAD][MOST];
+#pragma unroll
+  for (int a = 0; a < AHEAD; ++a) {
+    const int e = (a * kCluster + rank) * 32 + lane;
+    const bool in = lead >= 0 && e < J.max_pages;
+    is[a] = in ? entry(first, e) : 0;
+#pragma unroll
+    for (int k = 0; k < MOST; ++k) {
+      const int b = first + 1 + warp + 8 * k;
+      other[a][k] = in && b < b1 && rows_in(b) ? entry(b, e) : is[a];
+    }
   }
   // what join_kernel would look up step by step
   if (h == 0) {
@@ -78,47 +99,44 @@ __global__ void __launch_bounds__(256) common_pages_kernel(const __grid_constant
       S.rows[tid] = S.row[tid / MMSHIFT_MAX_BATCH][tid % MMSHIFT_MAX_BATCH];
   }
   __syncthreads();
-  if (b0 + tid < b1) {
-    const int b = b0 + tid, n = J.off[b + 1] - J.off[b];
-    if (n) {
-      atomicMin(&first_, b);
-      atomicMin(&keys, keys_of(S.causal, cache_len(J, (size_t)b * J.Hkv + h), n, 0));
-      atomicAdd(&members, 1);
-    }
+  if (mine && rows_in(own)) atomicMin(&keys, keys_of(S.causal, len, J.off[own + 1] - J.off[own], 0));
+#pragma unroll
+  for (int a = 0; a < AHEAD; ++a) {
+    bool same = is[a] >= 0 && is[a] < J.n_pages;
+#pragma unroll
+    for (int k = 0; k < MOST; ++k) same &= other[a][k] == is[a];
+    if (!same) atomicMin(&common, (a * kCluster + rank) * 32 + lane);
   }
   __syncthreads();
-  const int first = members ? first_ : b0, most = members > 1 ? keys >> J.page_shift : 0;
-  if (tid == 0) common = most;
-  __syncthreads();
-  const int32_t* const lead = J.table + ((size_t)first * J.Hkv + h) * J.max_pages;
-  for (int e = rank * 32 + lane; e - lane < most; e += kCluster * 32) {
-    if (e >= most) continue;
-    const int32_t is = lead[e];
-    bool same = is >= 0 && is < J.n_pages;
+  const int most = lead >= 0 ? keys >> J.page_shift : 0;
+  for (int e = (AHEAD * kCluster + rank) * 32 + lane; e < most; e += kCluster * 32) {
+    const int32_t is_ = entry(first, e);
+    bool same = is_ >= 0 && is_ < J.n_pages;
 #pragma unroll 8
-    for (int b = first + 1 + warp; b < b1; b += 8)
-      same &= J.off[b + 1] == J.off[b] || J.table[((size_t)b * J.Hkv + h) * J.max_pages + e] == is;
+    for (int b = first + 1 + warp; b < b1; b += 8) same &= !rows_in(b) || entry(b, e) == is_;
     if (!same) {
       atomicMin(&common, e);
       break;                                           // what lies behind cannot be less
     }
   }
   __syncthreads();
+  cluster_wait();
+  if (tid == 0) st_cluster_int(mapa(smem_u32(&found[rank]), 0), common);
+  __syncwarp();
   cluster_sync();
-  int pages = common;
-#pragma unroll
-  for (int r = 0; r < kCluster; ++r) pages = min(pages, ld_cluster_int(mapa(smem_u32(&common), r)));
-  cluster_sync();                                      // no CTA leaves while its result is read
   if (rank) return;
+  int pages = most;
+#pragma unroll
+  for (int r = 0; r < kCluster; ++r) pages = min(pages, found[r]);
   if (tid == 0) {
     S.at[0][g * J.Hkv + h] = ((int64_t)first * J.Hkv + h) * J.max_pages;
     S.lens[0][g * J.Hkv + h] = pages << J.page_shift;
   }
-  for (int b = b0 + tid; b < b1; b += 256) {
-    const size_t u = (size_t)b * J.Hkv + h;
-    const bool rows = J.off[b + 1] > J.off[b];
-    S.at[1][u] = (int64_t)u * J.max_pages + (rows ? pages : 0);
-    S.lens[1][u] = cache_len(J, u) - (rows ? pages << J.page_shift : 0);
+  if (mine) {
+    const size_t u = (size_t)own * J.Hkv + h;
+    const int less = rows_in(own) ? pages : 0;
+    S.at[1][u] = (int64_t)u * J.max_pages + less;
+    S.lens[1][u] = len - (less << J.page_shift);
   }
 }
 
@@ -275,6 +293,15 @@ mmshift_status mmshift_cache_attention_shared(const mmshift_shape* s, const mmsh
   S.causal = causal;
   S.n_groups = n_groups;
   std::memcpy(S.group, cu_groups, (n_groups + 1) * sizeof(int32_t));
+  for (int g = 0; g < n_groups; ++g) {
+    int lead = -1, members = 0;
+    for (int b = cu_groups[g + 1] - 1; b >= cu_groups[g]; --b) {
+      if (J.off[b + 1] == J.off[b]) continue;
+      lead = b;
+      ++members;
+    }
+    S.lead[g] = members > 1 ? lead : -1;
+  }
   JoinJob N;
   std::memset(&N, 0, sizeof(N));
   N.out = static_cast<uint8_t*>(out);

@@ -265,6 +265,9 @@ __device__ __forceinline__ int ld_cluster_int(uint32_t caddr) {
   asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(caddr) : "memory");
   return v;
 }
+__device__ __forceinline__ void st_cluster_int(uint32_t caddr, int v) {
+  asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(caddr), "r"(v) : "memory");
+}
 // Relaxed arrival on an mbarrier of either CTA of the cluster: orders no
 // memory accesses, for releases whose data dependence is already complete
 // (e.g. tensor-memory reads finished by tcgen05.wait::ld).
