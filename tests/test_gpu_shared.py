@@ -102,6 +102,20 @@ def test_longer_prefix(kind):
     check(attend(cache, q, new, [5]), R.reference(cache, q, new), kind)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "i8"])
+def test_a_sequence_that_differs_somewhere(kind):
+    """720 pages in common but for one page of one request, at the ends of what is compared at a time; requests
+    without rows, and the first of a group among them."""
+    new = [0, 1, 1, 0, 1, 1, 1, 2, 1, 1, 1, 1]
+    for odd, at in ((1, 0), (2, 255), (4, 256), (11, 511), (10, 512), (9, 513), (5, 719), (3, 300), (0, 7)):
+        cache = R.Cache([[[11520 + 3 * b, 11536 - b] for b in range(12)]], 64, kind, 16).fill_random(seed=at)
+        share(cache, [12], [720])
+        cache.table[0, odd, :, at] = cache.table[0, odd, :, at ^ 1]
+        q = queries(new, 4, 64, "bf16", seed=at)
+        for groups in ([12], [1, 11]):
+            check(attend(cache, q, new, groups), R.reference(cache, q, new), (odd, at, groups))
+
+
 def test_shared_pages_that_are_none():
     """Entries outside the pool, shared ones and a request's own, are left out and reported."""
     new = [1, 1, 2]
