@@ -243,12 +243,26 @@ __global__ void __launch_bounds__(kTake) take_pages_kernel(const __grid_constant
         const int rows = min(max(w.start - (i << J.page_shift), 0), page);
         G.jobs[k] = PageJob{e, to, COMPACT || e < 0 || to < 0 ? 0 : rows, 0};
       }
-      G.table[(size_t)u * J.max_pages + i] = to;
+      // the page of an entry behind the last job is noted in the entry: -2 - e, below -1
+      G.table[(size_t)u * J.max_pages + i] = k < G.most || e < 0 ? to : -2 - e;
     });
     sync_all<C>();                                     // the counts are no longer asked for
     for (int k = tid; k < min(all, G.most); k += C * kTake) {
       const int32_t e = G.jobs[k].from;
       if (e >= 0) atomicSub(G.refs + e, 1);
+    }
+    // More wanted than the pool has pages: what had no job is given up by who noted it. Entries in what is
+    // written are pages, -1 or notes by now; lengths that other warps have set give the same range.
+    for (int k = 0; all > G.most && k < per && u0 + k < u1; ++k) {
+      const Written x = written<COMPACT>(G, u0 + k);
+      const int end = x.start < x.stop ? (x.stop + page - 1) >> J.page_shift : 0;
+      for (int i = (x.start >> J.page_shift) + part; i < end; i += G.group) {
+        int32_t* const at = G.table + (size_t)(u0 + k) * J.max_pages + i;
+        const int32_t e = *at;
+        if (e > -2) continue;
+        atomicSub(G.refs + (-2 - e), 1);
+        *at = -1;
+      }
     }
   }
   if (tid == 0) *G.taken = min(all, G.most);

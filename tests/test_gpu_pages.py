@@ -333,3 +333,104 @@ def test_pages_past_four_gigabytes():
     assert P.table[P.table >= 0].min() >= P.n_pages - 12 and not P.exhausted
     P.check("last pages")
     assert D.poll() == M._lib.MMSHIFT_OK
+
+
+def state(D, what=""):
+    """Tables, counts and lengths; rows of lost pages are not known, so none are compared."""
+    P = D.P
+    assert P.table.tolist() == P.m_table, (what, "table")
+    assert P.refs.tolist() == P.m_refs, (what, "refs")
+    assert P.lens.tolist() == [[[len(x) for x in y] for y in z] for z in P.held], (what, "lens")
+    # the counts are the entries that name a page, whatever was lost
+    named = P.table[P.table >= 0].long().flatten()
+    assert torch.equal(P.refs.long(), torch.bincount(named, minlength=P.n_pages)), (what, "entries")
+
+
+def emptied(D):
+    D.free(range(D.P.B))
+    state(D, "emptied")
+    assert not D.P.refs.any() and (D.P.table == -1).all()
+    D.poll()
+
+
+@pytest.mark.parametrize("n_pages", [2, 3, 4, 9])
+def test_more_pages_wanted_than_the_pool_has(n_pages):
+    """Every holder of a shared page writes to it, and the pool is smaller than their number."""
+    D = Driver(1, 8, 1, 64, "bf16", 16, n_pages, 4)
+    D.append([20] + [0] * 7)
+    D.fork([0] * 7, range(1, 8))
+    D.append([1] * 8)
+    assert D.P.exhausted
+    D.P.check("copies of the tail")
+    state(D, "copies of the tail")
+    assert D.poll() == M._lib.MMSHIFT_ERR_DEVICE
+    emptied(D)
+    D.append([0, 16 * min(n_pages, 4)] + [0] * 6)  # every page is there again
+    D.P.check("again")
+    assert D.poll() == M._lib.MMSHIFT_OK
+
+
+@pytest.mark.parametrize("L,B,H,rows,keep,max_pages,n_pages", [
+    (1, 3, 1, 60, 40, 4, 5),              # one block, a lane a sequence
+    (1, 2, 1, 2200, 2150, 140, 140),      # more pages of a sequence than its lanes hold at once
+    (3, 40, 20, 90, 50, 6, 1000),         # a cluster of blocks
+])
+def test_compaction_that_wants_more_pages_than_the_pool_has(L, B, H, rows, keep, max_pages, n_pages):
+    D = Driver(L, B, H, 64, "bf16", 16, n_pages, max_pages)
+    D.append([rows] + [0] * (B - 1))
+    assert not D.P.exhausted
+    D.fork([0] * (B - 1), range(1, B))
+    counts = None
+    if B == 3:
+        counts = [[[40], [17], [33]]]
+    idx = torch.arange(rows - keep, rows, dtype=torch.int32).repeat(B)[None, :, None].expand(L, B * keep, H).contiguous()
+    D.compact([keep] * B, idx=idx, counts=counts)
+    assert D.P.exhausted and sum(p < 0 for x in D.P.m_table for y in x for z in y for p in z[:1]) > 0
+    state(D, "compacted")
+    assert D.poll() == M._lib.MMSHIFT_ERR_DEVICE
+    emptied(D)
+
+
+def test_many_sequences_of_a_small_pool():
+    """More sequences than the cluster has threads, each of which wants a page of its own."""
+    D = Driver(17, 64, 8, 64, "i8", 16, 400, 3)
+    P = D.P
+    for new, copies in (([20] + [0] * 63, True), ([1] * 64, False), ([0, 30] * 32, False)):
+        lens = P.lens + torch.tensor(new, dtype=torch.int32, device="cuda")[None, :, None]
+        P.lens.copy_(lens)
+        M.check(M.mmshift_cache_reserve(D.shape(new), P.struct(), P.refs, D.ws, D.n), "reserve")
+        P.reserve(new, lens.tolist())
+        for l, b, h in P.units():
+            P.held[l][b][h] += [None] * new[b]
+        state(D, new[:2])
+        if copies:
+            D.fork([0] * 63, range(1, 64))
+    assert P.exhausted and D.poll() == M._lib.MMSHIFT_ERR_DEVICE
+    emptied(D)
+
+
+def test_random_lives_of_pools_that_are_too_small():
+    """As the lives above, on past every page that was not there."""
+    exhausted = 0
+    for seed in range(8):
+        rng = random.Random(100 + seed)
+        B, H, L = rng.choice([3, 8]), rng.choice([1, 2, 5]), rng.choice([1, 3])
+        n_pages = rng.choice([3, L * H, L * H * B])
+        D = Driver(L, B, H, 64, rng.choice(["bf16", "i8"]), 16, n_pages, 8, seed=seed)
+        for step in range(16):
+            kind = rng.choice(["append", "append", "fork", "fork", "compact", "free"])
+            lens = [max(len(D.P.held[l][b][h]) for l in range(L) for h in range(H)) for b in range(B)]
+            if kind == "append":
+                D.append([rng.choice([0, 1, 2, 16, 40]) if lens[b] < 8 * 16 - 40 else 0 for b in range(B)])
+            elif kind == "fork":
+                src = rng.randrange(B)
+                dst = rng.sample([b for b in range(B) if b != src], rng.randrange(1, B))
+                D.fork([src] * len(dst), dst)
+            elif kind == "compact":
+                D.compact([rng.choice([0, rng.randrange(lens[b] + 1)]) for b in range(B)], rng=rng)
+            else:
+                D.free(rng.sample(range(B), rng.randrange(2)))
+            state(D, (seed, step, kind))
+        exhausted += D.P.exhausted
+        emptied(D)
+    assert exhausted > 4
