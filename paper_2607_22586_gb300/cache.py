@@ -90,6 +90,7 @@ class PagedKVCache:
             self._ws_bytes = max(self._ws_bytes, L.mmshift_cache_pages_workspace_size(full, self._all))
         self._workspace = make(self._ws_bytes, dt=torch.uint8)
         self._shared = None                            # workspace of attention in groups
+        self._replayed = []                            # larger ones took their place, graphs still use them
 
     def _struct(self, table, lens):
         return L.make_cache(self.k_pages, self.v_pages, table, lens, self.k_scales, self.v_scales)
@@ -295,7 +296,9 @@ class PagedKVCache:
             if capturing:
                 raise RuntimeError("attention in groups of so many tokens has to run once before it is captured")
             grown = torch.zeros(n, dtype=torch.uint8, device=self.device)
-            if self._shared is not None:               # what calls have reported
+            if any(t is self._shared for t in self._captured):
+                self._replayed.append(self._shared)    # replays go on to report there
+            elif self._shared is not None:             # what calls have reported
                 grown[:256].copy_(self._shared[:256])
                 self._shared.record_stream(torch.cuda.current_stream())
             self._shared = grown
@@ -319,8 +322,10 @@ class PagedKVCache:
         return k, v
 
     def poll(self) -> None:
-        """Waits for the current stream and raises what a call on the cache reported."""
+        """Waits for the current stream and raises what a call on the cache, or a graph's replay of
+        one, reported."""
         with self._on_device():
-            stream, used = torch.cuda.current_stream(), [w for w in (self._workspace, self._shared) if w is not None]
+            stream = torch.cuda.current_stream()
+            used = [w for w in (self._workspace, self._shared, *self._replayed) if w is not None]
             for status in [L.mmshift_poll_status(w, stream) for w in used]:    # all are read and cleared
                 L.check(status, "mmshift_poll_status")

@@ -154,3 +154,51 @@ def test_a_captured_step_of_all():
         assert R.same(out, want), i
         assert torch.equal(cache.page_table, plain.page_table) and torch.equal(cache.refs, plain.refs)
     cache.poll()
+
+
+def test_replays_report_after_larger_calls():
+    """A graph's attention in groups goes on with the workspace it was captured with when a larger call
+    has taken another: what a replay reports there is raised, once."""
+    batch, new = 4, [1] * 4
+    cache = PagedKVCache(HQ, HKV, 64, torch.bfloat16, batch, 200, page_size=16, pages=80)
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    rnd = lambda *s: torch.randn(s, generator=gen, device="cuda").bfloat16()  # noqa: E731
+    cache.advance([60, 0, 0, 0])
+    cache.append(rnd(1, 60, HKV, 64), rnd(1, 60, HKV, 64), [60, 0, 0, 0])
+    cache.fork([0, 0, 0], [1, 2, 3])
+    q, out = rnd(batch, HQ, 64), torch.empty((batch, HQ, 64), dtype=torch.bfloat16, device="cuda")
+    graphs = []
+    for more in (1, 20, 45):
+        q_more = rnd(batch * more, HQ, 64)
+        cache.attend(q_more, [more] * batch, groups=[4])   # a larger workspace each time
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            cache.attend(q, new, groups=[4], out=out)
+    cache.poll()
+    table = cache.page_table.clone()
+    for g in graphs:
+        g.replay()
+        cache.poll()
+        cache.page_table[0, 2, 1, 0] = -1              # a page that is not there
+        g.replay()
+        with pytest.raises(M.MMShiftError):
+            cache.poll()
+        cache.page_table.copy_(table)
+        g.replay()
+        cache.poll()
+
+
+def test_what_was_reported_before_a_larger_call_is_raised():
+    cache = PagedKVCache(HQ, HKV, 64, torch.bfloat16, 2, 200, page_size=16, pages=40)
+    k = torch.zeros((1, 40, HKV, 64), dtype=torch.bfloat16, device="cuda")
+    cache.advance([20, 20])
+    cache.append(k, k, [20, 20])
+    cache.page_table[0, 1, 0, 0] = -1
+    for n in (1, 15):
+        cache.attend(torch.zeros((2 * n, HQ, 64), dtype=torch.bfloat16, device="cuda"), [n] * 2, groups=[2])
+    cache.page_table[0, 1, 0, 0] = cache.page_table[0, 1, 0, 1]
+    cache.attend(torch.zeros((80, HQ, 64), dtype=torch.bfloat16, device="cuda"), [40] * 2, groups=[2])
+    with pytest.raises(M.MMShiftError):
+        cache.poll()
+    cache.poll()
