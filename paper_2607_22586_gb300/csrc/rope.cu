@@ -269,7 +269,9 @@ mmshift_status mmshift_rope(const mmshift_shape* s, const mmshift_rotary* r, con
     if (!row) row = dense;
     if (row < dense || !aligned(in, esz) || !aligned(out, esz)) return false;
     if (L > 1 && !layer) layer = T * row;
-    if (L > 1 && T && layer < (T - 1) * row + dense) return false;
+    // layers one behind another, or side by side in a token's row
+    if (L > 1 && T && layer < dense) return false;
+    if (L > 1 && T > 1 && row > (layer - dense) / (T - 1) && (row - dense) / layer < L - 1) return false;
     S.in = static_cast<const uint8_t*>(in);
     S.out = static_cast<uint8_t*>(out);
     S.in_row = row * esz;

@@ -36,8 +36,11 @@ def _layer_stride(t: torch.Tensor, layers: int) -> int:
     """The elements between two layers of t [L, T, heads, d], 0 for a single one."""
     if layers == 1 or not t.numel():
         return 0
-    if t.stride(0) < (t.shape[-3] - 1) * _token_stride(t) + t.shape[-2] * t.shape[-1]:
-        raise ValueError("layers must not overlap")
+    tokens, row, dense = t.shape[-3], _token_stride(t), t.shape[-2] * t.shape[-1]
+    behind = t.stride(0) >= (tokens - 1) * row + dense
+    beside = t.stride(0) >= dense and row >= (layers - 1) * t.stride(0) + dense     # in a token's row
+    if not behind and not beside:
+        raise ValueError("layers must lie one behind another or side by side in a token's row, without overlap")
     return t.stride(0)
 
 

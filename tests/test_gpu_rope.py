@@ -164,3 +164,25 @@ def test_nothing_to_rotate():
     q, k = r(torch.empty((0, 4, 64), device="cuda"), torch.empty((0, 2, 64), device="cuda"),
              torch.empty(0, dtype=torch.int32, device="cuda"))
     assert q.shape == (0, 4, 64) and k.shape == (0, 2, 64)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("pad", [0, 3, 8])
+def test_layers_side_by_side_in_a_token(dtype, pad):
+    """[T, L, heads, d] buffers as [L, T, heads, d]: only their rows change in place."""
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    hq, hkv, d = 12, 4, 64
+    for T, L in ((37, 3), (1, 2), (2, 5), (300, 2)):
+        rows = torch.randn((T, L, (hq + hkv) * d + pad), generator=gen, device="cuda").to(R.DT[dtype])
+        before = rows.clone()
+        q, k = (x.unflatten(-1, (h, d)).transpose(0, 1) for x, h in ((rows[..., :hq * d], hq), (rows[..., hq * d:(hq + hkv) * d], hkv)))
+        pos = torch.randint(0, 40000, (T,), generator=gen, device="cuda", dtype=torch.int32)
+        rotary = Rotary(d)
+        args = (pos[None], rotary.inv_freq, "half", (d // 2,), 1.0)
+        q1, k1 = rotary(q, k, pos)
+        assert R.same(rows, before)
+        check(q1, q, *args)
+        check(k1, k, *args)
+        rotary(q, k, pos, in_place=True)
+        assert R.same(q.contiguous(), q1) and R.same(k.contiguous(), k1)
+        assert R.same(rows[..., (hq + hkv) * d:].contiguous(), before[..., (hq + hkv) * d:].contiguous())

@@ -171,3 +171,18 @@ def test_layers_that_overlap_are_refused():
         for q, k in ((t, None), (x, t)):
             with pytest.raises(ValueError):
                 r._rotate(q, k, 2, 2, 5, 3, p, False, False)
+
+
+def test_layers_side_by_side():
+    """Layers inside a token's row do not overlap; one element less between them or between tokens, and they do.
+    (Rotary._rotate: behind the check for rows of a GPU.)"""
+    from paper_2607_22586_gb300.prompt import _layer_stride
+
+    assert _layer_stride(torch.zeros(3, 5, 2, 64).transpose(0, 1), 5) == 128
+    assert _layer_stride(torch.zeros(5000).as_strided((5, 3, 2, 64), (130, 700, 64, 1)), 5) == 130
+    dense = 8 * 128
+    for layer, row in ((dense - 1, 3 * dense), (dense, 3 * dense - 1), (dense + 1, 3 * dense), (1 << 62, 1 << 62)):
+        if layer < 1 << 62:
+            with pytest.raises(ValueError):
+                _layer_stride(torch.zeros(40000).as_strided((3, 10, 8, 128), (layer, row, 128, 1)), 3)
+        assert _rope(_rotary(), _shape(n_layers=3), qs=row, ql=layer) == BAD
