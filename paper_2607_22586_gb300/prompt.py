@@ -23,6 +23,12 @@ def _on(device: torch.device):
     return nullcontext() if device.index == torch.cuda.current_device() else torch.cuda.device(device)
 
 
+def _no_gradient(*ts: Optional[torch.Tensor]) -> None:
+    """Results carry no gradient, so rows that one is wanted of are refused."""
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in ts):
+        raise ValueError("no gradient is taken here: call it under torch.no_grad(), or with detached rows")
+
+
 def _token_stride(t: torch.Tensor) -> int:
     """The elements between two tokens of t [..., T, heads, d], whose heads are dense."""
     heads, d = t.shape[-2:]
@@ -69,7 +75,9 @@ class Rotary:
                  in_place: bool = False, inverse: bool = False):
         """q [T, Hq, d] and k [T, Hkv, d], or [L, T, H, d] of layers at the same positions
         (either may be None); positions int32 [T], or [axes, T]. ``inverse`` turns the other
-        way, which is also the rotation's gradient."""
+        way, which is also the rotation's gradient; autograd does not take it (rows that require one
+        are refused where gradients are recorded)."""
+        _no_gradient(q, k)
         ts = [t for t in (q, k) if t is not None]
         if not ts:
             raise ValueError("nothing to rotate")
@@ -120,7 +128,9 @@ class PromptAttention:
     def __call__(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = True,
                  softmax_scale: float = 0.0, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None):
         """q [T, Hq, d], k and v [T, Hkv, d], tokens equally far apart (k and v alike):
-        [T, Hq, d]. ``lse`` [T, Hq] float32 receives the log-sum-exp where given."""
+        [T, Hq, d]. ``lse`` [T, Hq] float32 receives the log-sum-exp where given. There is no backward
+        pass: rows that require a gradient are refused where gradients are recorded."""
+        _no_gradient(q, k, v)
         for t, heads in ((q, self.n_q_heads), (k, self.n_kv_heads), (v, self.n_kv_heads)):
             if t.dtype != self.dtype or t.device != self.device or t.shape != (self.total_tokens, heads, self.head_dim):
                 raise ValueError(f"rows must be [{self.total_tokens}, {heads}, {self.head_dim}] of {self.dtype} "

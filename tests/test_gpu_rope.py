@@ -186,3 +186,15 @@ def test_layers_side_by_side_in_a_token(dtype, pad):
         rotary(q, k, pos, in_place=True)
         assert R.same(q.contiguous(), q1) and R.same(k.contiguous(), k1)
         assert R.same(rows[..., (hq + hkv) * d:].contiguous(), before[..., (hq + hkv) * d:].contiguous())
+
+
+def test_rows_that_require_a_gradient_where_none_is_recorded():
+    x = torch.randn((5, 2, 64), device="cuda", requires_grad=True)
+    pos = torch.arange(5, dtype=torch.int32, device="cuda")
+    r = Rotary(64)
+    with torch.no_grad():
+        a, _ = r(x, None, pos)
+    b, _ = r(x.detach(), None, pos)
+    assert R.same(a, b) and not a.requires_grad
+    with pytest.raises(ValueError, match="gradient"):
+        r(x, None, pos)

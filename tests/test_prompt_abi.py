@@ -186,3 +186,23 @@ def test_layers_side_by_side():
             with pytest.raises(ValueError):
                 _layer_stride(torch.zeros(40000).as_strided((3, 10, 8, 128), (layer, row, 128, 1)), 3)
         assert _rope(_rotary(), _shape(n_layers=3), qs=row, ql=layer) == BAD
+
+
+def test_no_gradient_is_lost_without_a_word():
+    """Rows that require a gradient are refused where gradients are recorded, before anything else."""
+    r, at = Rotary(64), PromptAttention(4, 2, 64, torch.bfloat16, [0, 3], device="cpu")
+    p = torch.zeros(3, dtype=torch.int32)
+    rows = lambda h, grad: torch.zeros(3, h, 64, dtype=torch.bfloat16, requires_grad=grad)  # noqa: E731
+    for i in range(3):
+        q, k, v = (rows(h, j == i) for j, h in enumerate((4, 2, 2)))
+        with pytest.raises(ValueError, match="gradient"):
+            at(q, k, v)
+        if i < 2:
+            with pytest.raises(ValueError, match="gradient"):
+                r(q, k, p)
+            with pytest.raises(ValueError, match="gradient"):
+                r(q if i == 0 else None, k if i == 1 else None, p)
+            with torch.no_grad(), pytest.raises(ValueError, match="one GPU"):   # the next check
+                r(q, k, p)
+            with pytest.raises(ValueError, match="one GPU"):
+                r(q.detach(), k.detach(), p)
