@@ -292,6 +292,19 @@ mmshift_status mmshift_rope(const mmshift_shape* s, const mmshift_rotary* r, con
   if (!side(J.side[0], Q, out_Q, s->n_q_heads, q_row_stride, q_layer_stride) ||
       !side(J.side[1], K, out_K, s->n_kv_heads, k_row_stride, k_layer_stride))
     return MMSHIFT_ERR_INVALID_ARG;
+  // Nor may a dense output lie where the other side is read or written: blocks run in any order.
+  auto apart = [&](const RopeSide& A, const RopeSide& B) {
+    if (!T || !A.heads || !B.heads || !A.copy) return true;
+    const uint8_t* const end = A.out + L * A.out_layer;
+    const int64_t row = (int64_t)B.heads * d * esz;
+    if (B.copy && A.out < B.out + L * B.out_layer && B.out < end) return false;
+    for (int l = 0; l < L; ++l) {
+      const uint8_t* const in = B.in + l * B.in_layer;
+      if (A.out < in + (T - 1) * B.in_row + row && in < end) return false;
+    }
+    return true;
+  };
+  if (!apart(J.side[0], J.side[1]) || !apart(J.side[1], J.side[0])) return MMSHIFT_ERR_INVALID_ARG;
   if (!T) return MMSHIFT_OK;
   J.pos = r->positions;
   J.T = T;

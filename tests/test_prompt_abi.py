@@ -206,3 +206,34 @@ def test_no_gradient_is_lost_without_a_word():
                 r(q, k, p)
             with pytest.raises(ValueError, match="one GPU"):
                 r(q.detach(), k.detach(), p)
+
+
+def test_an_output_where_the_other_side_lies():
+    """A dense output over the other side's rows, or over its output, would be read or written in any order."""
+    T, hq, hkv, esz = 10, 8 * 128, 2 * 128, 2
+    q, k = FAKE, FAKE + (1 << 36)
+    ends = T * hq * esz, T * hkv * esz
+    for oq, ok in ((k, None), (k + ends[1] - 2, None), (k - ends[0] + 2, None), (None, q), (None, q + ends[0] - 2),
+                   (None, q - ends[1] + 2), (FAKE + (2 << 36), FAKE + (2 << 36)),
+                   (FAKE + (2 << 36), FAKE + (2 << 36) + ends[0] - 2), (FAKE + (2 << 36), FAKE + (2 << 36) - ends[1] + 2),
+                   (k, q)):
+        assert _rope(_rotary(), oq=FAKE + (4 << 36) if oq is None else oq, ok=FAKE + (5 << 36) if ok is None else ok) == BAD
+    assert _rope(_rotary(), oq=k, ok=k) == BAD            # K in place, Q's output over it
+    assert _rope(_rotary(), oq=q, ok=q) == BAD            # Q in place, K's output over it
+    # K's second layer, and not what lies between its layers
+    s = _shape(n_layers=2)
+    assert _rope(_rotary(), s, kl=1 << 30, oq=k + (2 << 30) - 2) == BAD
+    assert _rope(_rotary(), s, kl=1 << 30, oq=k + (2 << 30) - 2 * ends[0] + 2) == BAD
+
+
+def test_outputs_next_to_the_other_side_are_no_error():
+    """What ends where the other begins passes the checks (there are no tokens to rotate, or there is no GPU)."""
+    T, hq, hkv, esz = 10, 8 * 128, 2 * 128, 2
+    q, k = FAKE, FAKE + (1 << 36)
+    if torch.cuda.is_available():
+        pytest.skip("the addresses are none")
+    for oq, ok in ((k + T * hkv * esz, FAKE + (3 << 36)), (k - T * hq * esz, FAKE + (3 << 36)),
+                   (FAKE + (2 << 36), FAKE + (2 << 36) + T * hq * esz), (q, k)):
+        assert _rope(_rotary(), oq=oq, ok=ok) not in (BAD, UNSUPPORTED)
+    assert _rope(_rotary(), _shape(cu_seqlens=[0, 0, 0, 0]), oq=k, ok=q) == L.MMSHIFT_OK
+    assert _rope(_rotary(), _shape(n_layers=2), kl=1 << 30, oq=k + (1 << 30)) not in (BAD, UNSUPPORTED)
