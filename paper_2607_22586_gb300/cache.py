@@ -150,9 +150,9 @@ class PagedKVCache:
             rows = [min(c, b - a) for c, a, b in zip(selector.budgets, selector.shape.cu_seqlens[:self.batch],
                                                      selector.shape.cu_seqlens[1:self.batch + 1])]
             most = self._row_counts(rows)
-            self.free(range(self.batch))
-            self.lens.copy_(most.expand(self.lens.shape) if counts is None
-                            else torch.minimum(counts.clamp(min=0), most))
+            lens = most.expand(self.lens.shape) if counts is None else torch.minimum(counts.clamp(min=0), most)
+            self.free(range(self.batch))               # behind them: counts may be the cache's lengths
+            self.lens.copy_(lens)
             self._reserve(rows)
         with self._on_device():
             L.check(L.mmshift_cache_fill(selector.shape, self._all, K, V, idx, counts, self._workspace, self._ws_bytes,

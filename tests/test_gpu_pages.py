@@ -434,3 +434,29 @@ def test_random_lives_of_pools_that_are_too_small():
         exhausted += D.P.exhausted
         emptied(D)
     assert exhausted > 4
+
+
+def test_a_fill_whose_counts_are_the_lengths():
+    """As many rows of another selection as the sequences hold already."""
+    from paper_2607_22586_gb300.selector import KVSelector
+
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    rnd = lambda *s: torch.randn(s, generator=gen, device="cuda").bfloat16()  # noqa: E731
+    sel = KVSelector(6, 2, 64, 8, torch.bfloat16, [0, 200, 290], [50, 30], n_layers=2,
+                     params=M.default_params(n_proxies=32, n_groups=2))
+    K, V, Q = rnd(2, 290, 2, 64), rnd(2, 290, 2, 64), rnd(2, 2, 8, 6, 64)
+    sel(K, V, Q)
+    counts = torch.tensor([[[50, 1], [0, 30]], [[17, 33], [29, 64]]], dtype=torch.int32, device="cuda")
+    held = counts.clamp(max=torch.tensor([50, 30], dtype=torch.int32, device="cuda")[None, :, None])
+    read = []
+    for pages in (60, None):
+        cache = PagedKVCache(6, 2, 64, torch.bfloat16, 2, 100, n_layers=2, page_size=16, pages=pages)
+        cache.lens.copy_(counts if pages is None else 0)
+        if pages is not None:
+            cache.fill(sel, K, V, counts=counts)
+        cache.fill(sel, K, V, counts=cache.lens)
+        assert cache.lens.tolist() == held.tolist()
+        read.append(cache.read([50, 30]))
+        cache.poll()
+    for x, y in zip(*read):
+        assert R.same(x, y)
