@@ -293,10 +293,12 @@ mmshift_status mmshift_rope(const mmshift_shape* s, const mmshift_rotary* r, con
       !side(J.side[1], K, out_K, s->n_kv_heads, k_row_stride, k_layer_stride))
     return MMSHIFT_ERR_INVALID_ARG;
   // Nor may a dense output lie where the other side is read or written: blocks run in any order.
+  // Rows that are turned in place are Q's or K's.
   auto apart = [&](const RopeSide& A, const RopeSide& B) {
-    if (!T || !A.heads || !B.heads || !A.copy) return true;
-    const uint8_t* const end = A.out + L * A.out_layer;
+    if (!T || !A.heads || !B.heads) return true;
     const int64_t row = (int64_t)B.heads * d * esz;
+    if (!A.copy) return B.copy || A.in >= B.in + row || B.in >= A.in + (int64_t)A.heads * d * esz;
+    const uint8_t* const end = A.out + L * A.out_layer;
     if (B.copy && A.out < B.out + L * B.out_layer && B.out < end) return false;
     for (int l = 0; l < L; ++l) {
       const uint8_t* const in = B.in + l * B.in_layer;

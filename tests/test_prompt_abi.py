@@ -237,3 +237,12 @@ def test_outputs_next_to_the_other_side_are_no_error():
         assert _rope(_rotary(), oq=oq, ok=ok) not in (BAD, UNSUPPORTED)
     assert _rope(_rotary(), _shape(cu_seqlens=[0, 0, 0, 0]), oq=k, ok=q) == L.MMSHIFT_OK
     assert _rope(_rotary(), _shape(n_layers=2), kl=1 << 30, oq=k + (1 << 30)) not in (BAD, UNSUPPORTED)
+
+
+def test_rows_of_both_sides_in_place():
+    """One token's rows turned as Q's and as K's would turn twice, or be written over."""
+    for k in (FAKE, FAKE + 8 * 128 * 2 - 2, FAKE - 2 * 128 * 2 + 2):
+        assert _rope(_rotary(), k=k, oq=FAKE, ok=k, qs=4096, ks=4096) == BAD
+    if not torch.cuda.is_available():                  # the addresses are none: side by side they pass the checks
+        for k in (FAKE + 8 * 128 * 2, FAKE - 2 * 128 * 2):
+            assert _rope(_rotary(), k=k, oq=FAKE, ok=k, qs=4096, ks=4096) != BAD
