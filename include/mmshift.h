@@ -573,9 +573,10 @@ mmshift_status mmshift_rope_frequencies(int32_t rot_dims, double theta,
 
 /* Q [L][T, Hq, d] and K [L][T, Hkv, d] (either nullable, with its output) rotated; all layers
  * at the same positions. Tokens row_stride elements apart (0 = dense), layers layer_stride
- * (0 = T * row_stride): one behind another, or side by side in a token's row. An output is its input (in place, with its strides; Q's and K's rows apart) or a dense [L][T, heads, d]
- * buffer that overlaps neither it nor the other side's input and output. T = cu_seqlens[batch], requests
- * may be empty, T * Hq at most 2^30; window and budgets are not read. */
+ * (0 = T * row_stride): one behind another, or side by side in a token's row. An output is its
+ * input (in place, with its strides; Q's and K's rows apart) or a dense [L][T, heads, d] buffer that
+ * overlaps neither it nor the other side's input and output. T = cu_seqlens[batch], requests may be
+ * empty, T * Hq at most 2^30; window and budgets are not read. */
 mmshift_status mmshift_rope(const mmshift_shape* s, const mmshift_rotary* r, const void* Q,
                             int64_t q_row_stride, int64_t q_layer_stride, const void* K,
                             int64_t k_row_stride, int64_t k_layer_stride, void* out_Q, void* out_K,

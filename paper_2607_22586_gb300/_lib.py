@@ -573,6 +573,8 @@ def make_rotary(inv_freq: Sequence[float], positions, layout: str = "half", sect
     sections = list(sections) if sections is not None else [len(inv_freq)]
     if len(sections) != axes or not 1 <= axes <= 3:
         raise ValueError(f"{len(sections)} sections for {axes} axes of positions")
+    if not amplitude > 0:                              # the C struct's 0 stands for 1
+        raise ValueError("amplitude must be positive")
     freq = (ctypes.c_double * max(len(inv_freq), 1))(*inv_freq)
     r = Rotary(layout=layouts[layout], rot_dims=2 * len(inv_freq), inverse=int(inverse), n_axes=axes,
                sections=(ctypes.c_int32 * 3)(*sections), amplitude=amplitude, inv_freq=freq, positions=_ptr(positions))

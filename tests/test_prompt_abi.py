@@ -246,3 +246,12 @@ def test_rows_of_both_sides_in_place():
     if not torch.cuda.is_available():                  # the addresses are none: side by side they pass the checks
         for k in (FAKE + 8 * 128 * 2, FAKE - 2 * 128 * 2):
             assert _rope(_rotary(), k=k, oq=FAKE, ok=k, qs=4096, ks=4096) != BAD
+
+
+def test_no_amplitude_stands_for_another():
+    """The C struct's 0 is 1, a caller's 0 would be rows of zeros."""
+    p = torch.zeros(3, dtype=torch.int32)
+    for a in (0.0, -1.0, math.nan):
+        with pytest.raises(ValueError):
+            M.make_rotary([1.0], p, amplitude=a)
+    assert M.make_rotary([1.0], p, amplitude=0.5).amplitude == 0.5 and M.make_rotary([1.0], p).amplitude == 1.0
