@@ -280,11 +280,6 @@ mmshift_status mmshift_rope(const mmshift_shape* s, const mmshift_rotary* r, con
     S.copy = in != out;
     S.out_row = (S.copy ? dense : row) * esz;
     S.out_layer = (S.copy ? T * dense : layer) * esz;
-    if (S.copy && T) {                                 // a row read after another was written there
-      const uint8_t *a = S.in + S.in_layer * (L > 1 ? L - 1 : 0) + (T - 1) * S.in_row + dense * esz;
-      const uint8_t *b = S.out + (int64_t)L * T * dense * esz;
-      if (S.in < b && S.out < a) return false;
-    }
     rows = rows && aligned(in, 16) && aligned(out, 16) && S.in_row % 16 == 0 && (L == 1 || S.in_layer % 16 == 0);
     return true;
   };
@@ -292,21 +287,26 @@ mmshift_status mmshift_rope(const mmshift_shape* s, const mmshift_rotary* r, con
   if (!side(J.side[0], Q, out_Q, s->n_q_heads, q_row_stride, q_layer_stride) ||
       !side(J.side[1], K, out_K, s->n_kv_heads, k_row_stride, k_layer_stride))
     return MMSHIFT_ERR_INVALID_ARG;
-  // Nor may a dense output lie where the other side is read or written: blocks run in any order.
-  // Rows that are turned in place are Q's or K's.
-  auto apart = [&](const RopeSide& A, const RopeSide& B) {
-    if (!T || !A.heads || !B.heads) return true;
-    const int64_t row = (int64_t)B.heads * d * esz;
-    if (!A.copy) return B.copy || A.in >= B.in + row || B.in >= A.in + (int64_t)A.heads * d * esz;
-    const uint8_t* const end = A.out + L * A.out_layer;
-    if (B.copy && A.out < B.out + L * B.out_layer && B.out < end) return false;
+  // Blocks run in any order: a dense output may not lie on rows that are read, of either side, nor on the other
+  // output; and rows that are turned in place are Q's or K's.
+  auto on_rows = [&](const RopeSide& A, const RopeSide& B) {
+    const int64_t out = (int64_t)A.out, end = out + L * A.out_layer, bytes = (int64_t)B.heads * d * esz;
     for (int l = 0; l < L; ++l) {
-      const uint8_t* const in = B.in + l * B.in_layer;
-      if (A.out < in + (T - 1) * B.in_row + row && in < end) return false;
+      const int64_t in = (int64_t)B.in + l * B.in_layer, before = out - in - bytes;
+      const int64_t t = before < 0 ? 0 : before / B.in_row + 1;   // the first row that ends behind the output's start
+      if (t < T && in + t * B.in_row < end) return true;
     }
-    return true;
+    return false;
   };
-  if (!apart(J.side[0], J.side[1]) || !apart(J.side[1], J.side[0])) return MMSHIFT_ERR_INVALID_ARG;
+  for (int i = 0; T && i < 2; ++i) {
+    const RopeSide &A = J.side[i], &B = J.side[1 - i];
+    if (A.heads && A.copy && on_rows(A, A)) return MMSHIFT_ERR_INVALID_ARG;
+    if (!A.heads || !B.heads) continue;
+    if (A.copy && on_rows(A, B)) return MMSHIFT_ERR_INVALID_ARG;
+    const int64_t gap = (int64_t)B.out - (int64_t)A.out;
+    if (A.copy == B.copy && gap >= 0 && gap < (A.copy ? L * A.out_layer : (int64_t)A.heads * d * esz))
+      return MMSHIFT_ERR_INVALID_ARG;
+  }
   if (!T) return MMSHIFT_OK;
   J.pos = r->positions;
   J.T = T;

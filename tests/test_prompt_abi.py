@@ -255,3 +255,17 @@ def test_no_amplitude_stands_for_another():
         with pytest.raises(ValueError):
             M.make_rotary([1.0], p, amplitude=a)
     assert M.make_rotary([1.0], p, amplitude=0.5).amplitude == 0.5 and M.make_rotary([1.0], p).amplitude == 1.0
+
+
+def test_outputs_between_rows_are_no_error():
+    """A dense output in the gap between two rows, or two layers, of what is read lies on none of them."""
+    if torch.cuda.is_available():
+        pytest.skip("the addresses are none")
+    s = _shape(cu_seqlens=[0, 1, 1, 2])
+    q, k, gap = FAKE, FAKE + (1 << 36), 1 << 20            # elements between tokens
+    dense = 2 * 8 * 128 * 2
+    for oq in (k + 2 * 128 * 2, k + gap * 2 - dense, q + 8 * 128 * 2, q + gap * 2 - dense):
+        assert _rope(_rotary(), s, qs=gap, ks=gap, oq=oq) not in (BAD, UNSUPPORTED)
+    for oq in (k + 2 * 128 * 2 - 2, k + gap * 2 - dense + 2, q + 8 * 128 * 2 - 2, q + gap * 2 - dense + 2, k + gap * 2):
+        assert _rope(_rotary(), s, qs=gap, ks=gap, oq=oq) == BAD
+    assert _rope(_rotary(), s, ks=gap, oq=k + gap * 2 + 2 * 128 * 2) not in (BAD, UNSUPPORTED)   # behind the last row
